@@ -13,7 +13,7 @@ LIB = os.path.join(PKG, "liblora_gfx950.so")
 LIB_CLOCKS = os.path.join(PKG, "liblora_gfx950_clocks.so")
 SOURCES = [os.path.join(CSRC, "lora_host.cpp"), os.path.join(CSRC, "lora_place.cpp"),
            os.path.join(CSRC, "lora_memory.cpp"), os.path.join(CSRC, "lora_kernels.hip")]
-HEADERS = [os.path.join(CSRC, "lora_internal.h"), os.path.join(ROOT, "include", "lora.h"),
+HEADERS = [os.path.join(CSRC, "lora_internal.h"), os.path.join(CSRC, "lora_device.h"), os.path.join(ROOT, "include", "lora.h"),
            os.path.join(ROOT, "include", "lora_placement.h")]
 
 
