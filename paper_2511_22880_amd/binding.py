@@ -1,4 +1,4 @@
-"""ctypes binding of include/lora.h: same names, argument marshalling only.
+"""ctypes binding of include/*.h: same names, argument marshalling only.
 
 Device buffers come from the caller (torch tensors, or raw integer addresses); every step of the
 path runs in the library's kernels.  A non-OK status raises ``LoraError`` carrying the status name
@@ -22,7 +22,12 @@ LORA_BF16 = 1
 STATUS = ("LORA_OK", "LORA_ERR_INVALID_ARG", "LORA_ERR_SHAPE", "LORA_ERR_OOM", "LORA_ERR_NOT_RESIDENT",
           "LORA_ERR_STALE_SEGMENTS", "LORA_ERR_WORKSPACE", "LORA_ERR_DEVICE")
 
-# every symbol include/lora.h declares
+# include/lora_experts.h.  Builds of the host source alone do not have these; a call then ends in an AttributeError.
+_EXPERTS = (
+    "lora_rows_quantize", "lora_experts_packed_bytes", "lora_experts_pack_weight", "lora_linear_scaled", "lora_experts_group_workspace_bytes",
+    "lora_experts_group", "lora_experts_linear", "lora_experts_linear_scaled", "lora_experts_combine",
+)
+# every symbol include/*.h declare
 EXPORTS = (
     "lora_pool_bytes", "lora_pool_create", "lora_pool_create_live", "lora_pool_load", "lora_pool_evict",
     "lora_pool_reserve", "lora_pool_mark_resident", "lora_pool_space", "lora_pool_compact", "lora_pool_adapter_info",
@@ -38,7 +43,7 @@ EXPORTS = (
     "lora_status_string",
     "lora_last_error",
     "lora_place_extrapolate", "lora_place_assign",
-)
+) + _EXPERTS
 
 
 class LoraError(RuntimeError):
@@ -104,6 +109,15 @@ _ARGTYPES = {
     "lora_apply_static": (_P, _P, _P, _I64, _P, _I64, _P),
     "lora_apply_multi": (_P, _I32, _P, _P, _I64, _P, _I64, _P, _SZ, _P),
     "lora_linear": (_P, _P, _P, _I64, _P, _P, _I64, _P, _SZ, _P),
+    "lora_rows_quantize": (_P, _I64, _I64, _I32, _P, _I64, _P, _I64, _P),
+    "lora_experts_packed_bytes": (_I32, _I32, _I32, _I32, _P),
+    "lora_experts_pack_weight": (_P, _I32, _I32, _I32, _I32, _P, _SZ, _P),
+    "lora_linear_scaled": (_P, _I64, _P, _I64, _I32, _I32, _P, _P, _I32, _P, _I64, _P),
+    "lora_experts_group_workspace_bytes": (_I64, _I32, _P),
+    "lora_experts_group": (_P, _I64, _I32, _I32, _I32, _P, _P, _P, _P, _SZ, _P),
+    "lora_experts_linear": (_P, _I64, _I32, _P, _P, _I32, _I32, _I32, _I32, _P, _I32, _P, _I64, _P),
+    "lora_experts_linear_scaled": (_P, _I64, _P, _I64, _I32, _P, _P, _I32, _I32, _I32, _I32, _P, _P, _I32, _P, _I64, _P),
+    "lora_experts_combine": (_P, _I64, _I32, _P, _P, _I32, _I32, _I32, _P, _I64, _P),
 }
 
 
@@ -115,6 +129,8 @@ def lib() -> ctypes.CDLL:
                               "(there is no fallback path)")
         L = ctypes.CDLL(LIB_PATH)
         for name in EXPORTS:
+            if name in _EXPERTS and not hasattr(L, name):
+                continue
             fn = getattr(L, name)
             fn.restype = ctypes.c_char_p if name in ("lora_status_string", "lora_last_error") else ctypes.c_int
             if name in _ARGTYPES:
@@ -633,3 +649,140 @@ def lora_place_assign(n_servers: int, ranks, demand_tps, operating_points: dict,
                                    ctypes.byref(target)))
     return {"phi": phi, "server_util": util, "server_max_rank": maxr,
             "budget": {int(r): int(b) for r, b in zip(op_r, budget)}, "target": float(target.value)}
+
+
+# ---- frozen layers beside an adapter, in block-scaled 8 bits and grouped by expert (include/lora_experts.h) ----------------
+# The arguments are torch device tensors, whose shapes and strides say what the C calls are told; a tensor that cannot hold what a
+# call writes or reads there is refused here, since the library sees addresses only.
+def _blocks(n: int) -> int:
+    return (n + 127) >> 7
+
+
+def _rows(name: str, t, columns: Optional[int] = None, rows: Optional[int] = None, itemsize: Optional[int] = None):
+    """(address, row stride) of a tensor of rows, whose elements lie side by side."""
+    shape = t.shape
+    if len(shape) != 2 or (shape[1] > 1 and t.stride(1) != 1) or (columns is not None and shape[1] < columns) or (rows is not None and shape[0] < rows) \
+            or (itemsize is not None and t.element_size() != itemsize):
+        raise ValueError(f"{name}: {tuple(shape)} of {t.dtype} with strides {tuple(t.stride())} does not do: {'any' if rows is None else rows} rows of "
+                         f"{'any' if columns is None else columns} elements" + ("" if itemsize is None else f" of {itemsize} bytes") + " are meant")
+    # (of a single row torch states any stride)
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(shape[1], t.stride(0))
+
+
+def _whole(name: str, t, dtype_size: int, n: int):
+    """Address of a contiguous tensor of at least n elements."""
+    if t.element_size() != dtype_size or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} does not do: {n} contiguous elements of {dtype_size} bytes are meant")
+    return t.data_ptr()
+
+
+def lora_rows_quantize(x, q, scales, stream=None) -> None:
+    """x: bf16 [rows][in]; q: 8-bit [rows][128 * blocks]; scales: fp32 [rows][blocks]."""
+    rows, in_f = x.shape
+    px, ldx = _rows("x", x, itemsize=2)
+    pq, ldq = _rows("q", q, _blocks(in_f) * 128, rows, 1)
+    ps, lds = _rows("scales", scales, _blocks(in_f), rows, 4)
+    status = (_lib or lib()).lora_rows_quantize(px, ldx, rows, in_f, pq, ldq, ps, lds, None if stream is None else _queue(stream))
+    if status:
+        _check(status)
+
+
+def lora_experts_packed_bytes(n_experts: int, in_features: int, out_features: int, bits: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().lora_experts_packed_bytes(n_experts, in_features, out_features, bits, ctypes.addressof(n)))
+    return int(n.value)
+
+
+def lora_experts_pack_weight(w, dev_packed, stream=None, in_features: Optional[int] = None) -> None:
+    """w: [experts][out][in] bf16, or 8-bit with rows of 128 * blocks; dev_packed: lora_experts_packed_bytes long."""
+    e, out_f, row = w.shape
+    bits = 8 * w.element_size()
+    in_f = row if in_features is None else int(in_features)
+    if row != (in_f if bits == 16 else 128 * _blocks(in_f)):
+        raise ValueError(f"w: rows of {row} elements are not those of {in_f} input features")
+    _check(lib().lora_experts_pack_weight(_whole("w", w, w.element_size(), 0), e, in_f, out_f, bits, dev_packed.data_ptr(), _nbytes(dev_packed), _queue(stream)))
+
+
+def _packed(w_packed, n_experts: int, in_features: int, out_features: int, bits: int):
+    row = 2 * in_features if bits == 16 else 128 * _blocks(in_features)
+    return _whole("w_packed", w_packed, 1, n_experts * out_features * row)
+
+
+def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
+    """q, scales: of lora_rows_quantize; w_packed: uint8; w_scales: fp32 [out / 128][blocks]; y: bf16 [rows][out]."""
+    rows, in_f = q.shape
+    out_f, blocks = y.shape[1], _blocks(in_f)
+    pq, ldq = _rows("q", q, itemsize=1)
+    ps, lds = _rows("scales", scales, blocks, rows, 4)
+    py, ldy = _rows("y", y, out_f, rows, 2)
+    status = (_lib or lib()).lora_linear_scaled(pq, ldq, ps, lds, rows, in_f, _packed(w_packed, 1, in_f, out_f, 8),
+                                                _whole("w_scales", w_scales, 4, (out_f >> 7) * blocks), out_f, py, ldy,
+                                                None if stream is None else _queue(stream))
+    if status:
+        _check(status)
+
+
+def lora_experts_group_workspace_bytes(n_picks: int, n_experts: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().lora_experts_group_workspace_bytes(n_picks, n_experts, ctypes.addressof(n)))
+    return int(n.value)
+
+
+def lora_experts_group(ids, starts, order, place, workspace=None, stream=None) -> None:
+    """ids: int32 [tokens][picks]; written: starts [experts + 1], order and place [tokens * picks], int32."""
+    tokens, picks = ids.shape
+    n_experts, n = starts.numel() - 1, tokens * picks
+    pi, ldi = _rows("ids", ids, itemsize=4)
+    status = (_lib or lib()).lora_experts_group(pi, ldi, tokens, picks, n_experts, _whole("starts", starts, 4, 1), _whole("order", order, 4, n),
+                                                _whole("place", place, 4, n), None if workspace is None else workspace.data_ptr(), _nbytes(workspace),
+                                                None if stream is None else _queue(stream))
+    if status:
+        _check(status)
+
+
+def _places(rows: int, order, picks: int):
+    if order is None:
+        return None, rows
+    return _whole("order", order, 4, rows * picks), rows * picks
+
+
+def lora_experts_linear(x, starts, order, picks: int, w_packed, y, stream=None) -> None:
+    """x: bf16 [tokens][in]; starts, order: of lora_experts_group (order None: x is in expert order); y: bf16 [tokens * picks][out]."""
+    tokens, in_f = x.shape
+    n_experts, out_f = starts.numel() - 1, y.shape[1]
+    po, n_rows = _places(tokens, order, picks)
+    px, ldx = _rows("x", x, itemsize=2)
+    py, ldy = _rows("y", y, out_f, n_rows, 2)
+    status = (_lib or lib()).lora_experts_linear(px, ldx, tokens, _whole("starts", starts, 4, 1), po, picks, n_rows, n_experts, in_f,
+                                                 _packed(w_packed, n_experts, in_f, out_f, 16), out_f, py, ldy,
+                                                 None if stream is None else _queue(stream))
+    if status:
+        _check(status)
+
+
+def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w_scales, y, stream=None) -> None:
+    """The same in 8 bits: q, scales of lora_rows_quantize, w_scales fp32 [experts][out / 128][blocks]."""
+    tokens, in_f = q.shape
+    n_experts, out_f, blocks = starts.numel() - 1, y.shape[1], _blocks(in_f)
+    po, n_rows = _places(tokens, order, picks)
+    pq, ldq = _rows("q", q, itemsize=1)
+    ps, lds = _rows("scales", scales, blocks, tokens, 4)
+    py, ldy = _rows("y", y, out_f, n_rows, 2)
+    status = (_lib or lib()).lora_experts_linear_scaled(pq, ldq, ps, lds, tokens, _whole("starts", starts, 4, 1), po, picks, n_rows, n_experts, in_f,
+                                                        _packed(w_packed, n_experts, in_f, out_f, 8),
+                                                        _whole("w_scales", w_scales, 4, n_experts * (out_f >> 7) * blocks), out_f, py, ldy,
+                                                        None if stream is None else _queue(stream))
+    if status:
+        _check(status)
+
+
+def lora_experts_combine(y, place, weights, z, stream=None) -> None:
+    """y: bf16 [rows][out]; place, weights: int32 and fp32 [tokens][picks]; z: bf16 [tokens][out]."""
+    tokens, picks = weights.shape
+    out_f = z.shape[1]
+    py, ldy = _rows("y", y, out_f, itemsize=2)
+    pz, ldz = _rows("z", z, out_f, tokens, 2)
+    status = (_lib or lib()).lora_experts_combine(py, ldy, y.shape[0], _whole("place", place, 4, tokens * picks), _whole("weights", weights, 4, tokens * picks),
+                                                  tokens, picks, out_f, pz, ldz, None if stream is None else _queue(stream))
+    if status:
+        _check(status)

@@ -1,0 +1,55 @@
+// Launch entry points of the operators in include/lora_experts.h (lora_experts.hip), which their host side (lora_experts.cpp) calls.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace lora {
+
+constexpr int kScaleBlock = 128;     // values of a row, or of a row and a column of a weight, that share a scale
+constexpr int kPieceBytes = 128;     // of a row: what the products walk k in (64 bf16 or 128 8-bit values)
+constexpr int kMaxExperts = 512;     // (a work group that groups picks has a count of each for 16 wavefronts in LDS)
+constexpr int kGroupChunk = 2048;    // picks of a work group that groups them, at least
+constexpr int kGroupMaxChunks = 256; // and so many work groups at most
+
+inline int64_t group_chunk(int64_t n_picks)
+{
+    const int64_t least = (n_picks + kGroupMaxChunks - 1) / kGroupMaxChunks;
+    return least <= kGroupChunk ? kGroupChunk : (least + kGroupChunk - 1) / kGroupChunk * kGroupChunk;
+}
+inline int group_chunks(int64_t n_picks) { const int64_t c = group_chunk(n_picks); return (int)((n_picks + c - 1) / c); }
+
+// Rows of x, by expert, times the experts' weights (see include/lora_experts.h).  starts == NULL: one expert that has all rows.
+struct ExpertsArgs {
+    const char *x;           // rows of `pieces` pieces of 128 bytes, row stride ldx_bytes
+    int64_t ldx_bytes;
+    const float *x_scales;   // 8 bits: [tokens][pieces], row stride ld_scales
+    int64_t ld_scales;
+    int tokens;              // rows of x
+    const int32_t *starts;   // [experts + 1]
+    const int32_t *order;    // place -> pick, or NULL: place -> row of x
+    int picks;               // per token
+    int n_rows;              // places
+    int n_experts;
+    const char *w;           // packed
+    const float *w_scales;   // 8 bits: [experts][out / 128][pieces]
+    int pieces, out;
+    uint16_t *y;
+    int64_t ldy;
+};
+hipError_t launch_experts_linear(const ExpertsArgs &a, bool bits8, hipStream_t stream);
+
+// W [experts][out][row_bytes] -> operand order (see the kernels).  row_bytes: whole pieces, of which the bytes behind used_bytes become zero.
+hipError_t launch_experts_pack(const char *w, int64_t n_experts, int row_bytes, int used_bytes, int out, char *dst, hipStream_t stream);
+
+hipError_t launch_rows_quantize(const uint16_t *x, int64_t ldx, int64_t rows, int in, uint8_t *q, int64_t ldq, float *scales,
+                                int64_t ld_scales, hipStream_t stream);
+
+// workspace: group_chunks(n) * n_experts ints where there is more than one chunk
+hipError_t launch_experts_group(const int32_t *ids, int64_t ld_ids, int64_t tokens, int picks, int n_experts, int32_t *starts,
+                                int32_t *order, int32_t *place, int32_t *workspace, hipStream_t stream);
+
+hipError_t launch_experts_combine(const uint16_t *y, int64_t ldy, int n_rows, const int32_t *place, const float *weights, int64_t tokens, int picks,
+                                  int out, uint16_t *z, int64_t ldz, hipStream_t stream);
+
+}  // namespace lora

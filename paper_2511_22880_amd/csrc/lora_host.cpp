@@ -36,6 +36,9 @@ static lora_status_t fail(lora_status_t st, const char *fmt, ...)
     return st;
 }
 
+// the same for the library's other host sources (declared in lora_internal.h)
+int lora::report(int status, const char *detail) { return fail((lora_status_t)status, "%s", detail); }
+
 static lora_status_t hip_fail(hipError_t e, const char *what)
 {
     return fail(LORA_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));

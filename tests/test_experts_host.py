@@ -1,0 +1,115 @@
+"""include/lora_experts.h without a GPU: what the calls refuse, before the device is touched, and the sizes they state."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2511_22880_amd import binding as L
+
+P = 0x7F0000000000  # a 256-byte aligned address that is never dereferenced
+
+
+def status(name, *args):
+    return L.STATUS[getattr(L.lib(), name)(*args)]
+
+
+QUANTIZE = dict(x=P, ldx=256, rows=3, in_f=256, q=P, ldq=256, scales=P, lds=2)
+LINEAR = dict(q=P, ldq=256, scales=P, lds=2, rows=3, in_f=256, w=P, ws=P, out=128, y=P, ldy=128)
+GROUP = dict(ids=P, ld=2, tokens=5, picks=2, experts=8, starts=P, order=P, place=P, work=None, nwork=0)
+EXPERTS = dict(x=P, ldx=256, tokens=5, starts=P, order=P, picks=2, rows=10, experts=8, in_f=256, w=P, out=128, y=P, ldy=128)
+SCALED = dict(q=P, ldq=256, scales=P, lds=2, tokens=5, starts=P, order=P, picks=2, rows=10, experts=8, in_f=256, w=P, ws=P, out=128, y=P, ldy=128)
+COMBINE = dict(y=P, ldy=128, rows=10, place=P, weights=P, tokens=5, picks=2, out=128, z=P, ldz=128)
+PACK = dict(w=P, experts=2, in_f=256, out=128, bits=8, packed=P, n=2 * 128 * 256)
+
+CASES = [("lora_rows_quantize", QUANTIZE, c, s) for c, s in [
+    (dict(x=None), "INVALID_ARG"), (dict(x=P + 8), "INVALID_ARG"), (dict(ldx=248), "INVALID_ARG"), (dict(ldx=260), "INVALID_ARG"),
+    (dict(rows=-1), "INVALID_ARG"), (dict(in_f=0), "SHAPE"), (dict(in_f=96), "SHAPE"), (dict(q=None), "INVALID_ARG"), (dict(q=P + 4), "INVALID_ARG"),
+    (dict(ldq=240), "INVALID_ARG"), (dict(ldq=264), "INVALID_ARG"), (dict(scales=None), "INVALID_ARG"), (dict(scales=P + 2), "INVALID_ARG"),
+    (dict(lds=1), "INVALID_ARG"), (dict(in_f=192, ldx=192, ldq=192), "INVALID_ARG")]]
+CASES += [("lora_linear_scaled", LINEAR, c, s) for c, s in [
+    (dict(q=None), "INVALID_ARG"), (dict(ldq=128), "INVALID_ARG"), (dict(scales=None), "INVALID_ARG"), (dict(lds=1), "INVALID_ARG"),
+    (dict(rows=-1), "INVALID_ARG"), (dict(in_f=100), "SHAPE"), (dict(out=192), "SHAPE"), (dict(out=0), "SHAPE"), (dict(w=None), "INVALID_ARG"),
+    (dict(w=P + 128), "INVALID_ARG"), (dict(ws=None), "INVALID_ARG"), (dict(y=None), "INVALID_ARG"), (dict(ldy=120), "INVALID_ARG"),
+    (dict(ldy=132), "INVALID_ARG"), (dict(y=P + 8), "INVALID_ARG"), (dict(ldq=1 << 62), "INVALID_ARG")]]
+CASES += [("lora_experts_group", GROUP, c, s) for c, s in [
+    (dict(ids=None), "INVALID_ARG"), (dict(ld=1), "INVALID_ARG"), (dict(tokens=-1), "INVALID_ARG"), (dict(picks=0), "SHAPE"), (dict(picks=65), "SHAPE"),
+    (dict(tokens=1 << 30, picks=2), "SHAPE"), (dict(experts=0), "SHAPE"), (dict(experts=513), "SHAPE"), (dict(starts=None), "INVALID_ARG"),
+    (dict(order=None), "INVALID_ARG"), (dict(place=None), "INVALID_ARG"), (dict(tokens=5000), "WORKSPACE"),
+    (dict(tokens=5000, work=P, nwork=8), "WORKSPACE"), (dict(tokens=5000, work=P + 4, nwork=1 << 20), "WORKSPACE")]]
+for name, base in (("lora_experts_linear", EXPERTS), ("lora_experts_linear_scaled", SCALED)):
+    CASES += [(name, base, c, s) for c, s in [
+        ({next(iter(base)): None}, "INVALID_ARG"), (dict(starts=None), "INVALID_ARG"), (dict(starts=P + 1), "INVALID_ARG"),
+        (dict(order=P + 2), "INVALID_ARG"), (dict(rows=9), "INVALID_ARG"), (dict(order=None), "INVALID_ARG"), (dict(picks=0), "SHAPE"),
+        (dict(experts=0), "SHAPE"), (dict(experts=600), "SHAPE"), (dict(tokens=-5, rows=-10), "INVALID_ARG"), (dict(w=P + 16), "INVALID_ARG"),
+        (dict(out=100), "SHAPE"), (dict(in_f=32), "SHAPE"), (dict(y=None), "INVALID_ARG"), (dict(ldy=64), "INVALID_ARG")]]
+CASES += [("lora_experts_linear_scaled", SCALED, c, s) for c, s in [
+    (dict(scales=None), "INVALID_ARG"), (dict(lds=1), "INVALID_ARG"), (dict(ws=None), "INVALID_ARG"), (dict(ldq=264), "INVALID_ARG")]]
+CASES += [("lora_experts_combine", COMBINE, c, s) for c, s in [
+    (dict(y=None), "INVALID_ARG"), (dict(ldy=64), "INVALID_ARG"), (dict(rows=-1), "INVALID_ARG"), (dict(place=None), "INVALID_ARG"),
+    (dict(weights=None), "INVALID_ARG"), (dict(tokens=-1), "INVALID_ARG"), (dict(picks=0), "SHAPE"), (dict(out=64), "SHAPE"),
+    (dict(z=None), "INVALID_ARG"), (dict(z=P + 2), "INVALID_ARG"), (dict(ldz=100), "INVALID_ARG")]]
+CASES += [("lora_experts_pack_weight", PACK, c, s) for c, s in [
+    (dict(w=None), "INVALID_ARG"), (dict(w=P + 4), "INVALID_ARG"), (dict(experts=0), "SHAPE"), (dict(bits=4), "INVALID_ARG"), (dict(in_f=63), "SHAPE"),
+    (dict(out=130), "SHAPE"), (dict(packed=None), "INVALID_ARG"), (dict(packed=P + 64), "INVALID_ARG"), (dict(n=100), "OOM")]]
+
+
+@pytest.mark.parametrize("name, base, change, expected", CASES, ids=lambda v: str(v) if isinstance(v, str) else "")
+def test_refusals(name, base, change, expected):
+    assert status(name, *dict(base, **change).values(), None) == "LORA_ERR_" + expected
+    assert len(L.lora_last_error()) > 5
+
+
+@pytest.mark.parametrize("name, base, change", [
+    ("lora_rows_quantize", QUANTIZE, dict(rows=0, x=None, q=None, scales=None)),
+    ("lora_linear_scaled", LINEAR, dict(rows=0, q=None, y=None)),
+    ("lora_experts_linear", EXPERTS, dict(tokens=0, rows=0, x=None, y=None)),
+    ("lora_experts_linear_scaled", SCALED, dict(tokens=0, rows=0, q=None, order=None)),
+    ("lora_experts_combine", COMBINE, dict(tokens=0, y=None, z=None)),
+])
+def test_nothing_to_do_is_no_error(name, base, change):
+    assert status(name, *dict(base, **change).values(), None) == "LORA_OK"
+
+
+def test_sizes():
+    assert L.lora_experts_packed_bytes(1, 4096, 4096, 8) == 4096 * 4096
+    assert L.lora_experts_packed_bytes(3, 192, 256, 8) == 3 * 256 * 256  # 8-bit rows are filled up to whole blocks of 128
+    assert L.lora_experts_packed_bytes(3, 192, 256, 16) == 3 * 192 * 256 * 2
+    assert L.lora_experts_packed_bytes(512, 16384, 16384, 16) == 512 << 29  # past 32 bits
+    assert L.lora_experts_group_workspace_bytes(0, 8) == 0
+    assert L.lora_experts_group_workspace_bytes(2048, 512) == 0
+    assert L.lora_experts_group_workspace_bytes(2049, 512) == 2 * 512 * 4
+    assert L.lora_experts_group_workspace_bytes(2 ** 31 - 1, 512) <= 256 * 512 * 4
+    for args in ((-1, 8), (2 ** 31, 8), (5, 0), (5, 513)):
+        with pytest.raises(L.LoraError):
+            L.lora_experts_group_workspace_bytes(*args)
+    n = ctypes.c_size_t(0)
+    assert status("lora_experts_packed_bytes", 1, 64, 128, 8, None) == "LORA_ERR_INVALID_ARG"
+    assert status("lora_experts_packed_bytes", 1, 64, 128, 32, ctypes.addressof(n)) == "LORA_ERR_INVALID_ARG"
+
+
+def test_the_binding_refuses_tensors_that_are_too_small_or_of_another_type():
+    bf, f8 = torch.bfloat16, torch.float8_e4m3fn
+    e = torch.empty
+    x, q, s, y = e(4, 256, dtype=bf), e(4, 256, dtype=f8), e(4, 2), e(4, 128, dtype=bf)
+    w, ws = e(128 * 256, dtype=torch.uint8), e(1, 2)
+    ids, st, od, pl, wt = e(2, 2, dtype=torch.int32), e(9, dtype=torch.int32), e(4, dtype=torch.int32), e(2, 2, dtype=torch.int32), e(2, 2)
+    wide = e(8 * 128 * 512, dtype=torch.uint8)
+    bad = [
+        lambda: L.lora_rows_quantize(x.float(), q, s), lambda: L.lora_rows_quantize(x, q[:, :128], s), lambda: L.lora_rows_quantize(x, q[:3], s),
+        lambda: L.lora_rows_quantize(x, q, s[:, :1]), lambda: L.lora_rows_quantize(x.t(), q, s), lambda: L.lora_rows_quantize(x, q, s.double()),
+        lambda: L.lora_linear_scaled(q, s, w[:-1], ws, y), lambda: L.lora_linear_scaled(q, s, w, ws[:, :1], y), lambda: L.lora_linear_scaled(q, s[:3], w, ws, y),
+        lambda: L.lora_linear_scaled(q, s, w, ws, y[:3]), lambda: L.lora_linear_scaled(x, s, w, ws, y), lambda: L.lora_linear_scaled(q, s, w, ws, y.float()),
+        lambda: L.lora_experts_group(ids.long(), st, od, pl), lambda: L.lora_experts_group(ids, st, od[:3], pl), lambda: L.lora_experts_group(ids, st, od, pl[:1]),
+        lambda: L.lora_experts_group(ids, st.float().double(), od, pl), lambda: L.lora_experts_group(ids.t(), st, od, pl),
+        lambda: L.lora_experts_linear(x[:2], st, od[:3], 2, wide, y), lambda: L.lora_experts_linear(x[:2], st, od, 2, wide[:-1], y),
+        lambda: L.lora_experts_linear(x[:2], st, od, 2, wide, y[:3]), lambda: L.lora_experts_linear(q[:2], st, od, 2, wide, y),
+        lambda: L.lora_experts_linear_scaled(q[:2], s[:1], st, od, 2, wide, e(8, 1, 2), y), lambda: L.lora_experts_linear_scaled(q[:2], s, st, od, 2, wide, ws, y),
+        lambda: L.lora_experts_combine(y, pl[:1], wt, y[:2]), lambda: L.lora_experts_combine(y, pl, wt.double(), y[:2]),
+        lambda: L.lora_experts_combine(y[:, :64], pl, wt, y[:2]), lambda: L.lora_experts_combine(y, pl, wt, y[:1]),
+        lambda: L.lora_experts_pack_weight(e(1, 128, 192, dtype=f8), w, in_features=256),
+        lambda: L.lora_experts_pack_weight(e(1, 256, 128, dtype=f8).transpose(1, 2), w),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises((ValueError, L.LoraError)):
+            call()
+            pytest.fail(f"call {i} went through")
