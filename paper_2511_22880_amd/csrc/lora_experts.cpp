@@ -123,8 +123,8 @@ extern "C" lora_status_t lora_experts_pack_weight(const void *w, int32_t n_exper
     TRY(check_packed(dev_packed));
     if (packed < need) return fail(LORA_ERR_OOM, "the packed weights need %zu bytes, %zu are there", need, packed);
     const int row_bytes = bits == 16 ? 2 * in_features : blocks_of(in_features) * lora::kScaleBlock;
-    return of_hip(lora::launch_experts_pack((const char *)w, n_experts, row_bytes, bits == 16 ? row_bytes : in_features, out_features, (char *)dev_packed,
-                                            (hipStream_t)stream),
+    return of_hip(lora::launch_experts_pack((const char *)w, n_experts, row_bytes, bits == 16 ? row_bytes : in_features, out_features, bits == 8,
+                                            (char *)dev_packed, (hipStream_t)stream),
                   "lora_experts_pack_weight");
 }
 
@@ -144,6 +144,9 @@ static lora_status_t check_product(lora::ExpertsArgs &a, int bits, const void *x
         TRY(check_scales(scales, ld_scales, a.pieces));
         TRY(check_values(w_scales, "w_scales"));
     }
+    // (the kernels take rows of x by 32-bit numbers of 16 bytes, and their scales by 32-bit indices)
+    if ((a.tokens - 1) * (bits == 16 ? ldx / 8 : ldx / 16) > UINT32_MAX - 8 || (bits == 8 && (a.tokens - 1) * ld_scales > UINT32_MAX))
+        return fail(LORA_ERR_SHAPE, "%d rows with a stride of %lld take more than 64 GiB, or their scales more than 16", a.tokens, (long long)ldx);
     TRY(check_packed(w_packed));
     TRY(check_rows(y, ldy, out, 8, "y"));
     a.x = (const char *)x;

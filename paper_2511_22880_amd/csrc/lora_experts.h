@@ -40,7 +40,8 @@ struct ExpertsArgs {
 hipError_t launch_experts_linear(const ExpertsArgs &a, bool bits8, hipStream_t stream);
 
 // W [experts][out][row_bytes] -> operand order (see the kernels).  row_bytes: whole pieces, of which the bytes behind used_bytes become zero.
-hipError_t launch_experts_pack(const char *w, int64_t n_experts, int row_bytes, int used_bytes, int out, char *dst, hipStream_t stream);
+hipError_t launch_experts_pack(const char *w, int64_t n_experts, int row_bytes, int used_bytes, int out, bool bits8, char *dst,
+                               hipStream_t stream);
 
 hipError_t launch_rows_quantize(const uint16_t *x, int64_t ldx, int64_t rows, int in, uint8_t *q, int64_t ldq, float *scales,
                                 int64_t ld_scales, hipStream_t stream);

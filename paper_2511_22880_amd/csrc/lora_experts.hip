@@ -4,11 +4,12 @@
 // Both element types walk k in pieces of 128 bytes: 64 bf16 or 128 8-bit values.  A weight tile of 16 columns x one piece is, for either type,
 // two operands of 16 bytes a lane (halves of the piece): two 16x16x32 bf16 MFMAs, or one 16x16x128 f8f6f4 MFMA that takes both.  So
 // the weights are packed alike:
-//   expert e, 128-column strip, piece P, half h, sub-block b, lane slot (kq, n): 16 bytes
+//   expert e, 128-column strip, piece P, half h, sub-block b of 8, lane slot (kq, n): 16 bytes
 //     128 P + 64 h + 16 kq .. of column 128 strip + 64 (b / 4) + 4 n + b mod 4
-//   at  e * out * 128 pieces + ((strip * pieces + P) * 2 + h) * 8192 + b * 1024 + (16 kq + n) * 16
+//   at  ((e * strips + strip) * pieces + P) * 16384 + operand_at(h, b) + (16 kq + n) * 16
 // A wavefront's load of an operand is 1 KB of consecutive bytes, and of four sub-blocks lane n ends up with four consecutive columns.
-// The token operand uses the same mapping of lanes to k.
+// Half of a piece of a strip is what a large tile multiplies by at a time: in bf16 the first half of k for all columns, in 8 bits all of k
+// for the first 64 columns.  The token operand uses the same mapping of lanes to k.
 #include "lora_device.h"
 #include "lora_experts.h"
 
@@ -23,6 +24,12 @@ static __device__ __forceinline__ uint4 ldb16(const char *p) { return *reinterpr
 static __device__ __forceinline__ i32x8 as_i32x8(uint4 lo, uint4 hi)
 {
     return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+}
+
+template <bool F8>
+static __device__ __forceinline__ constexpr int operand_at(int h, int b)
+{
+    return F8 ? (b >> 2) * 8192 + h * 4096 + (b & 3) * 1024 : h * 8192 + b * 1024;
 }
 
 // LDS operations of a wavefront complete in order; the compiler keeps them so
@@ -139,6 +146,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
     constexpr int kRegion = kSlab + (F8 ? 64 * RB : 0);  // .. and the rows' scales
     constexpr int kTiles = RB * CB, R = 16 * RB;
     static_assert(RB <= 4, "a lane for the scale of every row");
+    static_assert(CB <= 4, "sub-blocks of one half of a strip");
     __shared__ __attribute__((aligned(16))) char lds[kThinLds<F8, RB, CB, WAVES>];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kq = lane >> 4;
@@ -171,7 +179,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
             const int tok = token_at(a, t.row0 + (r < t.rows ? r : 0));
             xrow[q] = a.x + (int64_t)max(tok, 0) * a.ldx_bytes + kPieceBytes * wave + 16 * lc;
         }
-        const char *wbase = a.w + ((int64_t)t.expert * (a.out >> 7) + strip) * np * 16384 + (int64_t)wave * 16384 + b0 * 1024 + lane * 16;
+        const char *wbase = a.w + ((int64_t)t.expert * (a.out >> 7) + strip) * np * 16384 + (int64_t)wave * 16384 + operand_at<F8>(0, b0) + lane * 16;
         const float *xs_at = nullptr, *ws_at = nullptr;
         if constexpr (F8) {
             const int tok = token_at(a, t.row0 + (lane < t.rows ? lane : 0));
@@ -197,7 +205,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int b = 0; b < CB; ++b) wq[d][h][b] = ldb16(wbase + at * (16384 * WAVES) + h * 8192 + b * 1024);
+                for (int b = 0; b < CB; ++b) wq[d][h][b] = ldb16(wbase + at * (16384 * WAVES) + operand_at<F8>(h, b));
         };
         auto stage = [&](int d) __attribute__((always_inline)) {
 #pragma unroll
@@ -289,13 +297,282 @@ static hipError_t launch_thin(const ExpertsArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
+// ------------------------------------------------------------------------------------------------
+// Tiles of many rows: 64 WR rows (256, or 128 where an expert's last tile has no more) x 256 columns, 8 wavefronts.  Wavefronts 0 .. 3 have the first
+// strip of 128 columns, 4 .. 7 the second; of a strip a wavefront has 64 rows x 128 columns (WR = 4), or 64 x 64 (WR = 2).
+//   * x and W come by loads that write LDS directly, x in slots of one piece (128 bytes of k), W in slots of a step: half a piece, the half that
+//     the packed order says (WR = 4), or a piece (WR = 2).  Three slots each: a step requests W of the step after the next, and the first step of a
+//     piece x of the piece after the next.  x is gathered by the copy itself, whole cache lines of 8 rows; inside a 1 KB block of 8 rows chunk p of row r
+//     sits in slot 8 r + (p XOR r), so that the lanes that read one chunk of 8 rows meet 8 bank groups.
+//   * A step is a phase that requests copies and reads the step's operands from LDS, and a phase that multiplies (512 cycles of the matrix unit), with a
+//     barrier behind each and the second strip's wavefronts one phase behind: of the two wavefronts of a SIMD one multiplies while the other reads.
+//     No request passes through registers the compiler tracks, so the waits count exactly what is under way.
+//   * In 8 bits a product spans a whole block of 128: its sum starts at zero, and 4 fp32 FMAs with x's scale times W's add it to the accumulators
+//     while the next ones run (half as long as the matrix unit takes).  A wavefront copies the scales of its own 64 rows beside x.
+// ------------------------------------------------------------------------------------------------
+constexpr int kWideThreads8 = 512;
+constexpr int kRing = 3;
+template <bool F8, int WR>
+constexpr int kWideLds = kRing * (64 * WR * kPieceBytes + (WR == 4 ? 16384 : 32768) + (F8 ? 2048 : 0));
+
+// One dword a lane straight to LDS: lane l's at `to` + 4 l.
+static __device__ __forceinline__ void dma4_to_lds(const void *g, uint32_t to)
+{
+    uint32_t saved_m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved_m0)
+                 : "v"(g), "s"(to)
+                 : "memory");
+}
+
+// N KB (2 or 4) from consecutive addresses, base (of the wavefront) + 16 lane, to consecutive LDS addresses.
+template <int N>
+static __device__ __forceinline__ void dma_kb_to_lds(const char *base, uint32_t lane16, uint32_t to)
+{
+    uint32_t saved_m0;
+    if constexpr (N == 4)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+                     "global_load_lds_dwordx4 %1, %2 offset:1024\n\tglobal_load_lds_dwordx4 %1, %2 offset:2048\n\t"
+                     "global_load_lds_dwordx4 %1, %2 offset:3072\n\ts_mov_b32 m0, %0"
+                     : "=&s"(saved_m0)
+                     : "v"(lane16), "s"(base), "s"(to)
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+                     "global_load_lds_dwordx4 %1, %2 offset:1024\n\ts_mov_b32 m0, %0"
+                     : "=&s"(saved_m0)
+                     : "v"(lane16), "s"(base), "s"(to)
+                     : "memory");
+}
+
+// Sixteen tiles' values are computed by here: the compiler moves them neither up nor down.
+static __device__ __forceinline__ void here(f32x4 (&v)[16])
+{
+    asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]), "+v"(v[8]), "+v"(v[9]),
+                      "+v"(v[10]), "+v"(v[11]), "+v"(v[12]), "+v"(v[13]), "+v"(v[14]), "+v"(v[15]));
+}
+
+template <bool F8, int WR>
+static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Tile &t, char *lds)
+{
+    constexpr int NB = 2 * WR;                     // sub-blocks of a wavefront
+    constexpr int SP = WR == 4 ? 2 : 1;            // steps of a piece
+    constexpr int XBUF = 64 * WR * kPieceBytes, WHALF = 16384 / SP, WBUF = 2 * WHALF;
+    constexpr int XC = WR + (F8 ? 1 : 0), WC = 4 / SP;  // copies of a wavefront: x (and scales) of a piece, W of a step
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, kq = lane >> 4;
+    const int rw = WR == 4 ? wave & 3 : wave & 1;  // rows 64 rw .. of the tile
+    const int half = WR == 4 ? 0 : (wave >> 1) & 1;
+    const int strip = 2 * t.ct + (wave >> 2);
+    // The last tile of a row of y may hold one strip: the wavefronts without one take part in everything up to the epilogue, so that
+    // copies and barriers count alike, and multiply strip 0's W for nothing.
+    const bool has_strip = strip * 128 < a.out;
+    const int np = a.pieces, steps = np * SP;
+
+    char *const xring = lds, *const wring = lds + kRing * XBUF, *const sring = wring + kRing * WBUF;
+    // rows of x by 32-bit offsets in 16 bytes (the host sees to it that they fit), which take half of the registers of addresses
+    uint32_t xoff[WR];
+#pragma unroll
+    for (int j = 0; j < WR; ++j) {
+        const int r = lane >> 3, row = 8 * (WR * wave + j) + r;
+        const int tok = token_at(a, t.row0 + (row < t.rows ? row : 0));
+        xoff[j] = (uint32_t)((uint64_t)max(tok, 0) * (uint64_t)a.ldx_bytes >> 4) + ((lane & 7) ^ r);
+    }
+    const int my_row = 64 * rw + lane;
+    const int my_tok = token_at(a, t.row0 + (my_row < t.rows ? my_row : 0));
+    const uint64_t there = __ballot(my_row < t.rows && my_tok >= 0);  // rows of this wavefront that are written
+    [[maybe_unused]] const uint32_t soff = F8 ? (uint32_t)((uint64_t)max(my_tok, 0) * (uint64_t)a.ld_scales) : 0u;
+    const int64_t es = (int64_t)t.expert * (a.out >> 7) + (has_strip ? strip : 0);
+    const char *wsrc = a.w + es * np * 16384 + (wave & 3) * (WC * 1024);
+    const char *xp = a.x;            // the next piece of every row
+    [[maybe_unused]] const float *sp = a.x_scales;
+    const uint32_t lane16 = lane * 16;
+    // (the scalar cache's path: a vector load would be counted among the copies)
+    const __attribute__((address_space(4))) float *wscale =
+        (const __attribute__((address_space(4))) float *)(uintptr_t)(F8 ? a.w_scales + es * np : nullptr);
+
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)lds);
+    const uint32_t x_end = lds0 + kRing * XBUF, w_end = x_end + kRing * WBUF, s_end = w_end + kRing * 2048;
+    uint32_t x_to = lds0 + WR * wave * 1024, w_to = x_end + (wave >> 2) * WHALF + (wave & 3) * (WC * 1024), s_to = w_end + wave * 256;
+    auto issue_x = [&]() __attribute__((always_inline)) {
+        auto at = [&](int j) { return xp + (uint64_t)xoff[j] * 16 - 1024 * j; };  // as the copies take it
+        if constexpr (WR == 4)
+            dma16x4_to_lds(at(0), at(1), at(2), at(3), x_to);
+        else
+            dma16x2_to_lds(at(0), at(1), x_to);
+        xp += kPieceBytes;
+        x_to = x_to + XBUF >= x_end ? x_to - (kRing - 1) * XBUF : x_to + XBUF;
+        if constexpr (F8) {
+            dma4_to_lds(sp + soff, s_to);
+            ++sp;
+            s_to = s_to + 2048 >= s_end ? s_to - (kRing - 1) * 2048 : s_to + 2048;
+        }
+    };
+    auto issue_w = [&]() __attribute__((always_inline)) {
+        dma_kb_to_lds<WC>(wsrc, lane16, w_to);
+        wsrc += WHALF;
+        w_to = w_to + WBUF >= w_end ? w_to - (kRing - 1) * WBUF : w_to + WBUF;
+    };
+
+    f32x4 acc[NB / 4][16];  // of 64 columns: sub-block b, 16 rows i at 4 b + i
+#pragma unroll
+    for (int g = 0; g < NB / 4; ++g)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[g][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    issue_x();
+    issue_w();
+    if (steps > 1) issue_w();
+    if (np > 1) issue_x();
+    if (np > 1)
+        wait_vm<XC + WC>();
+    else if (steps > 1)
+        wait_vm<WC>();
+    else
+        wait_vm<0>();
+
+    // the end of a phase: every wavefront has come this far
+    auto phase_end = [&]() __attribute__((always_inline)) {
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    };
+    phase_end();
+    if (wave >= 4) phase_end();  // the second strip's wavefronts run one phase behind the first's
+
+    constexpr int XH = WR == 4 && !F8 ? 1 : 2;  // halves of x's rows in registers at a time
+    constexpr int WB = WR == 4 && !F8 ? 8 : 4, WH = WR == 4 && !F8 ? 1 : 2;  // .. sub-blocks and halves of W
+    uint4 xo[XH][4], wo[WH][WB];
+    [[maybe_unused]] f32x4 sc[4];
+    int xget = 0, wget = 0, sget = 0;
+    const int xlane = (8 * rw + (n >> 3)) * 1024 + (n & 7) * 128;
+    const int wlane = (wave >> 2) * WHALF + lane * 16;
+    // step q of piece P, behind which come two pieces or more (AFTER = 2), one or none
+    auto step = [&](int P, auto qc, auto afterc) __attribute__((always_inline)) {
+        constexpr int q = decltype(qc)::value, AFTER = decltype(afterc)::value;
+        constexpr bool kMoreW = SP == 2 ? AFTER >= 1 : AFTER == 2;  // there is a step after the next
+        if constexpr (kMoreW) issue_w();
+        if constexpr (q == 0 && AFTER == 2) issue_x();
+        if constexpr (XH == 1 || q == 0)
+#pragma unroll
+            for (int h = 0; h < XH; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    // row 16 i + n of this wavefront's: block 8 rw + 2 i + n / 8, row n mod 8 of it
+                    xo[h][i] = *reinterpret_cast<const uint4 *>(xring + xget + xlane + 2048 * i + (((4 * (XH == 1 ? q : h) + kq) ^ (n & 7)) * 16));
+#pragma unroll
+        for (int h = 0; h < WH; ++h)
+#pragma unroll
+            for (int b = 0; b < WB; ++b) {
+                const int at = WR == 4 ? (F8 ? h * 4096 : 0) + b * 1024 : operand_at<F8>(h, 4 * half + b);
+                wo[h][b] = *reinterpret_cast<const uint4 *>(wring + wget + wlane + at);
+            }
+        if constexpr (F8 && q == 0) {
+            const float w = wscale[P];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[i] = *reinterpret_cast<const f32x4 *>(sring + sget + wave * 256 + (16 * i + 4 * kq) * 4) * w;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // W of the next step and, where that begins one, x of the next piece have landed: behind them were requested
+        // W of the step after and x of the piece after
+        wait_vm<AFTER == 2 ? XC + WC : kMoreW ? WC : 0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what was read is in registers: the slots may be written
+        phase_end();
+        if constexpr (F8) {
+            // the product k, and the sum of the one two before it
+            f32x4 part[3];
+#pragma unroll
+            for (int k = 0; k < 18; ++k) {
+                if (k < 16) part[k % 3] = mfma_e4m3(as_i32x8(xo[0][k & 3], xo[XH - 1][k & 3]), as_i32x8(wo[0][k >> 2], wo[WH - 1][k >> 2]), f32x4{0.f, 0.f, 0.f, 0.f});
+                __builtin_amdgcn_sched_barrier(0);
+                if (k >= 2) {
+                    const int j = k - 2;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[q][j][e] = fmaf(sc[j & 3][e], part[j % 3][e], acc[q][j][e]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            here(acc[q]);
+        } else {
+#pragma unroll
+            for (int h = 0; h < XH; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+                        acc[b >> 2][4 * (b & 3) + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(xo[h][i]), as_bf16x8(wo[h][b]), acc[b >> 2][4 * (b & 3) + i], 0, 0, 0);
+#pragma unroll
+            for (int g = 0; g < NB / 4; ++g) here(acc[g]);
+        }
+        phase_end();
+        wget = wget == (kRing - 1) * WBUF ? 0 : wget + WBUF;
+        if constexpr (q == SP - 1) {
+            xget = xget == (kRing - 1) * XBUF ? 0 : xget + XBUF;
+            if (F8) sget = sget == (kRing - 1) * 2048 ? 0 : sget + 2048;
+        }
+    };
+    auto piece = [&](int P, auto after) __attribute__((always_inline)) {
+        step(P, std::integral_constant<int, 0>{}, after);
+        if constexpr (SP == 2) step(P, std::integral_constant<int, 1>{}, after);
+    };
+    for (int P = 0; P + 2 < np; ++P) piece(P, std::integral_constant<int, 2>{});
+    if (np > 1) piece(np - 2, std::integral_constant<int, 1>{});
+    piece(np - 1, std::integral_constant<int, 0>{});
+    if (wave < 4) phase_end();
+    if (!has_strip) return;
+
+    uint16_t *const y0 = a.y + (int64_t)(t.row0 + 64 * rw) * a.ldy + strip * 128 + 64 * half + 4 * n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = 16 * i + 4 * kq + e;
+            if ((there >> r) & 1)
+#pragma unroll
+                for (int g = 0; g < NB / 4; ++g)
+                    *reinterpret_cast<uint2 *>(y0 + (int64_t)r * a.ldy + 64 * g) =
+                        uint2{pack_bf16_rne(acc[g][i][e], acc[g][4 + i][e]), pack_bf16_rne(acc[g][8 + i][e], acc[g][12 + i][e])};
+        }
+}
+
+template <bool F8>
+__global__ __launch_bounds__(kWideThreads8, 1) void k_experts_wide(ExpertsArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char lds[kWideLds<F8, 4> > kWideLds<F8, 2> ? kWideLds<F8, 4> : kWideLds<F8, 2>];
+    const int n_ct = (a.out + 255) >> 8;
+    Tile t;
+    // Every XCD a run of the tiles.
+    if (!find_tile<256>(a.starts, a.n_experts, a.n_rows, n_ct, threadIdx.x & 63, [&](int total) {
+            const int per_xcd = (total + 7) >> 3, idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+            return (int)(blockIdx.x >> 3) >= per_xcd || idx >= total ? -1 : idx;
+        }, t))
+        return;
+    if (t.rows > 128)
+        wide_body<F8, 4>(a, t, lds);
+    else
+        wide_body<F8, 2>(a, t, lds);
+}
+
+template <bool F8>
+static hipError_t launch_wide(const ExpertsArgs &a, hipStream_t stream)
+{
+    const int64_t row_tiles = (int64_t)(a.n_rows + 255) / 256 + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
+    const int64_t grid = (row_tiles * ((a.out + 255) / 256) + 7) / 8 * 8;
+    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k_experts_wide<F8>, dim3((unsigned)grid), dim3(kWideThreads8), 0, stream, a);
+    return hipGetLastError();
+}
+
 template <bool F8>
 static hipError_t launch_by_rows(const ExpertsArgs &a, hipStream_t stream)
 {
     const int per = a.n_rows / a.n_experts;
     if (per <= 16) return launch_thin<F8, 1, 4, 2, 8>(a, stream);
     if (per <= 32) return launch_thin<F8, 2, 4, 2, 8>(a, stream);
-    return launch_thin<F8, 4, 4, 2, 8>(a, stream);
+    if (per <= 64) return launch_thin<F8, 4, 4, 2, 8>(a, stream);
+    return launch_wide<F8>(a, stream);
 }
 
 hipError_t launch_experts_linear(const ExpertsArgs &a, bool bits8, hipStream_t stream)
@@ -306,11 +583,13 @@ hipError_t launch_experts_linear(const ExpertsArgs &a, bool bits8, hipStream_t s
 // ------------------------------------------------------------------------------------------------
 // Weights into operand order: a thread per 16 bytes of the destination.
 // ------------------------------------------------------------------------------------------------
+template <bool F8>
 __global__ __launch_bounds__(256) void k_experts_pack(const char *__restrict__ w, int64_t pieces_of_16, int row_bytes, int used_bytes,
                                                       int pieces, char *__restrict__ dst)
 {
     for (int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x; d < pieces_of_16; d += (int64_t)gridDim.x * 256) {
-        const int slot = (int)(d & 63), b = (int)(d >> 6) & 7, h = (int)(d >> 9) & 1;
+        const int slot = (int)(d & 63), at_b = (int)(d >> 6) & 15;
+        const int b = F8 ? (at_b & 3) + 4 * (at_b >> 3) : at_b & 7, h = F8 ? (at_b >> 2) & 1 : at_b >> 3;  // operand_at
         const int64_t rest = d >> 10;  // (expert * strips + strip) * pieces + piece
         const int64_t es = rest / pieces;
         const int64_t col = 128 * es + 64 * (b >> 2) + 4 * (slot & 15) + (b & 3);  // (strips of all experts are consecutive columns)
@@ -321,12 +600,13 @@ __global__ __launch_bounds__(256) void k_experts_pack(const char *__restrict__ w
     }
 }
 
-hipError_t launch_experts_pack(const char *w, int64_t n_experts, int row_bytes, int used_bytes, int out, char *dst, hipStream_t stream)
+hipError_t launch_experts_pack(const char *w, int64_t n_experts, int row_bytes, int used_bytes, int out, bool bits8, char *dst, hipStream_t stream)
 {
     const int pieces = row_bytes / kPieceBytes;
     const int64_t n = n_experts * out * pieces * (kPieceBytes / 16);
     const int64_t grid = (n + 255) / 256;
-    hipLaunchKernelGGL(k_experts_pack, dim3((unsigned)(grid < (1 << 20) ? grid : (1 << 20))), dim3(256), 0, stream, w, n, row_bytes, used_bytes, pieces, dst);
+    hipLaunchKernelGGL(bits8 ? k_experts_pack<true> : k_experts_pack<false>, dim3((unsigned)(grid < (1 << 20) ? grid : (1 << 20))), dim3(256), 0, stream, w, n,
+                       row_bytes, used_bytes, pieces, dst);
     return hipGetLastError();
 }
 

@@ -113,3 +113,10 @@ def test_the_binding_refuses_tensors_that_are_too_small_or_of_another_type():
         with pytest.raises((ValueError, L.LoraError)):
             call()
             pytest.fail(f"call {i} went through")
+
+
+@pytest.mark.parametrize("name, base, change", [
+    ("lora_linear_scaled", LINEAR, dict(rows=1 << 16, ldq=(1 << 20) + 1024, lds=2)), ("lora_linear_scaled", LINEAR, dict(rows=1 << 16, lds=1 << 17)),
+    ("lora_experts_linear", EXPERTS, dict(tokens=1 << 20, order=None, rows=1 << 20, ldx=1 << 16))])
+def test_rows_beyond_what_the_kernels_reach_are_refused(name, base, change):
+    assert status(name, *dict(base, **change).values(), None) == "LORA_ERR_SHAPE"
