@@ -658,30 +658,33 @@ def _blocks(n: int) -> int:
     return (n + 127) >> 7
 
 
-def _rows(name: str, t, columns: Optional[int] = None, rows: Optional[int] = None, itemsize: Optional[int] = None):
+# (These run several times in every call of a serving loop: what a tensor is asked for costs 0.1 us each.)
+def _rows(name: str, t, rows: int, columns: int, itemsize: int):
     """(address, row stride) of a tensor of rows, whose elements lie side by side."""
-    shape = t.shape
-    if len(shape) != 2 or (shape[1] > 1 and t.stride(1) != 1) or (columns is not None and shape[1] < columns) or (rows is not None and shape[0] < rows) \
-            or (itemsize is not None and t.element_size() != itemsize):
-        raise ValueError(f"{name}: {tuple(shape)} of {t.dtype} with strides {tuple(t.stride())} does not do: {'any' if rows is None else rows} rows of "
-                         f"{'any' if columns is None else columns} elements" + ("" if itemsize is None else f" of {itemsize} bytes") + " are meant")
-    # (of a single row torch states any stride)
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(shape[1], t.stride(0))
+    try:
+        (r, c), (ld, step) = t.shape, t.stride()
+    except ValueError:
+        r = c = ld = step = -1
+    if r < rows or c < columns or (step != 1 and c > 1) or t.itemsize != itemsize:
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} with strides {t.stride()} does not do: {rows} rows of {columns} elements of {itemsize} "
+                         "bytes side by side are meant")
+    return t.data_ptr(), ld if r > 1 else c  # (of a single row torch states any stride)
 
 
-def _whole(name: str, t, dtype_size: int, n: int):
+def _whole(name: str, t, n: int, itemsize: int):
     """Address of a contiguous tensor of at least n elements."""
-    if t.element_size() != dtype_size or not t.is_contiguous() or t.numel() < n:
-        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} does not do: {n} contiguous elements of {dtype_size} bytes are meant")
+    if t.numel() < n or t.itemsize != itemsize or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} does not do: {n} contiguous elements of {itemsize} bytes are meant")
     return t.data_ptr()
 
 
 def lora_rows_quantize(x, q, scales, stream=None) -> None:
     """x: bf16 [rows][in]; q: 8-bit [rows][128 * blocks]; scales: fp32 [rows][blocks]."""
     rows, in_f = x.shape
-    px, ldx = _rows("x", x, itemsize=2)
-    pq, ldq = _rows("q", q, _blocks(in_f) * 128, rows, 1)
-    ps, lds = _rows("scales", scales, _blocks(in_f), rows, 4)
+    blocks = (in_f + 127) >> 7
+    px, ldx = _rows("x", x, 0, 0, 2)
+    pq, ldq = _rows("q", q, rows, blocks << 7, 1)
+    ps, lds = _rows("scales", scales, rows, blocks, 4)
     status = (_lib or lib()).lora_rows_quantize(px, ldx, rows, in_f, pq, ldq, ps, lds, None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -696,27 +699,22 @@ def lora_experts_packed_bytes(n_experts: int, in_features: int, out_features: in
 def lora_experts_pack_weight(w, dev_packed, stream=None, in_features: Optional[int] = None) -> None:
     """w: [experts][out][in] bf16, or 8-bit with rows of 128 * blocks; dev_packed: lora_experts_packed_bytes long."""
     e, out_f, row = w.shape
-    bits = 8 * w.element_size()
+    bits = 8 * w.itemsize
     in_f = row if in_features is None else int(in_features)
-    if row != (in_f if bits == 16 else 128 * _blocks(in_f)):
+    if row != (in_f if bits == 16 else _blocks(in_f) << 7):
         raise ValueError(f"w: rows of {row} elements are not those of {in_f} input features")
-    _check(lib().lora_experts_pack_weight(_whole("w", w, w.element_size(), 0), e, in_f, out_f, bits, dev_packed.data_ptr(), _nbytes(dev_packed), _queue(stream)))
-
-
-def _packed(w_packed, n_experts: int, in_features: int, out_features: int, bits: int):
-    row = 2 * in_features if bits == 16 else 128 * _blocks(in_features)
-    return _whole("w_packed", w_packed, 1, n_experts * out_features * row)
+    _check(lib().lora_experts_pack_weight(_whole("w", w, 0, w.itemsize), e, in_f, out_f, bits, dev_packed.data_ptr(), _nbytes(dev_packed), _queue(stream)))
 
 
 def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
     """q, scales: of lora_rows_quantize; w_packed: uint8; w_scales: fp32 [out / 128][blocks]; y: bf16 [rows][out]."""
     rows, in_f = q.shape
-    out_f, blocks = y.shape[1], _blocks(in_f)
-    pq, ldq = _rows("q", q, itemsize=1)
-    ps, lds = _rows("scales", scales, blocks, rows, 4)
-    py, ldy = _rows("y", y, out_f, rows, 2)
-    status = (_lib or lib()).lora_linear_scaled(pq, ldq, ps, lds, rows, in_f, _packed(w_packed, 1, in_f, out_f, 8),
-                                                _whole("w_scales", w_scales, 4, (out_f >> 7) * blocks), out_f, py, ldy,
+    out_f, blocks = y.shape[1], (in_f + 127) >> 7
+    pq, ldq = _rows("q", q, 0, 0, 1)
+    ps, lds = _rows("scales", scales, rows, blocks, 4)
+    py, ldy = _rows("y", y, rows, out_f, 2)
+    status = (_lib or lib()).lora_linear_scaled(pq, ldq, ps, lds, rows, in_f, _whole("w_packed", w_packed, out_f * blocks << 7, 1),
+                                                _whole("w_scales", w_scales, (out_f >> 7) * blocks, 4), out_f, py, ldy,
                                                 None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -732,30 +730,24 @@ def lora_experts_group(ids, starts, order, place, workspace=None, stream=None) -
     """ids: int32 [tokens][picks]; written: starts [experts + 1], order and place [tokens * picks], int32."""
     tokens, picks = ids.shape
     n_experts, n = starts.numel() - 1, tokens * picks
-    pi, ldi = _rows("ids", ids, itemsize=4)
-    status = (_lib or lib()).lora_experts_group(pi, ldi, tokens, picks, n_experts, _whole("starts", starts, 4, 1), _whole("order", order, 4, n),
-                                                _whole("place", place, 4, n), None if workspace is None else workspace.data_ptr(), _nbytes(workspace),
-                                                None if stream is None else _queue(stream))
+    pi, ldi = _rows("ids", ids, 0, 0, 4)
+    pw, nw = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    status = (_lib or lib()).lora_experts_group(pi, ldi, tokens, picks, n_experts, _whole("starts", starts, 1, 4), _whole("order", order, n, 4),
+                                                _whole("place", place, n, 4), pw, nw, None if stream is None else _queue(stream))
     if status:
         _check(status)
-
-
-def _places(rows: int, order, picks: int):
-    if order is None:
-        return None, rows
-    return _whole("order", order, 4, rows * picks), rows * picks
 
 
 def lora_experts_linear(x, starts, order, picks: int, w_packed, y, stream=None) -> None:
     """x: bf16 [tokens][in]; starts, order: of lora_experts_group (order None: x is in expert order); y: bf16 [tokens * picks][out]."""
     tokens, in_f = x.shape
     n_experts, out_f = starts.numel() - 1, y.shape[1]
-    po, n_rows = _places(tokens, order, picks)
-    px, ldx = _rows("x", x, itemsize=2)
-    py, ldy = _rows("y", y, out_f, n_rows, 2)
-    status = (_lib or lib()).lora_experts_linear(px, ldx, tokens, _whole("starts", starts, 4, 1), po, picks, n_rows, n_experts, in_f,
-                                                 _packed(w_packed, n_experts, in_f, out_f, 16), out_f, py, ldy,
-                                                 None if stream is None else _queue(stream))
+    n_rows = tokens if order is None else tokens * picks
+    px, ldx = _rows("x", x, 0, 0, 2)
+    py, ldy = _rows("y", y, n_rows, out_f, 2)
+    status = (_lib or lib()).lora_experts_linear(px, ldx, tokens, _whole("starts", starts, 1, 4), None if order is None else _whole("order", order, n_rows, 4),
+                                                 picks, n_rows, n_experts, in_f, _whole("w_packed", w_packed, n_experts * out_f * in_f << 1, 1), out_f,
+                                                 py, ldy, None if stream is None else _queue(stream))
     if status:
         _check(status)
 
@@ -763,14 +755,15 @@ def lora_experts_linear(x, starts, order, picks: int, w_packed, y, stream=None) 
 def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w_scales, y, stream=None) -> None:
     """The same in 8 bits: q, scales of lora_rows_quantize, w_scales fp32 [experts][out / 128][blocks]."""
     tokens, in_f = q.shape
-    n_experts, out_f, blocks = starts.numel() - 1, y.shape[1], _blocks(in_f)
-    po, n_rows = _places(tokens, order, picks)
-    pq, ldq = _rows("q", q, itemsize=1)
-    ps, lds = _rows("scales", scales, blocks, tokens, 4)
-    py, ldy = _rows("y", y, out_f, n_rows, 2)
-    status = (_lib or lib()).lora_experts_linear_scaled(pq, ldq, ps, lds, tokens, _whole("starts", starts, 4, 1), po, picks, n_rows, n_experts, in_f,
-                                                        _packed(w_packed, n_experts, in_f, out_f, 8),
-                                                        _whole("w_scales", w_scales, 4, n_experts * (out_f >> 7) * blocks), out_f, py, ldy,
+    n_experts, out_f, blocks = starts.numel() - 1, y.shape[1], (in_f + 127) >> 7
+    n_rows = tokens if order is None else tokens * picks
+    pq, ldq = _rows("q", q, 0, 0, 1)
+    ps, lds = _rows("scales", scales, tokens, blocks, 4)
+    py, ldy = _rows("y", y, n_rows, out_f, 2)
+    status = (_lib or lib()).lora_experts_linear_scaled(pq, ldq, ps, lds, tokens, _whole("starts", starts, 1, 4),
+                                                        None if order is None else _whole("order", order, n_rows, 4), picks, n_rows, n_experts, in_f,
+                                                        _whole("w_packed", w_packed, n_experts * out_f * blocks << 7, 1),
+                                                        _whole("w_scales", w_scales, n_experts * (out_f >> 7) * blocks, 4), out_f, py, ldy,
                                                         None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -779,10 +772,10 @@ def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w
 def lora_experts_combine(y, place, weights, z, stream=None) -> None:
     """y: bf16 [rows][out]; place, weights: int32 and fp32 [tokens][picks]; z: bf16 [tokens][out]."""
     tokens, picks = weights.shape
-    out_f = z.shape[1]
-    py, ldy = _rows("y", y, out_f, itemsize=2)
-    pz, ldz = _rows("z", z, out_f, tokens, 2)
-    status = (_lib or lib()).lora_experts_combine(py, ldy, y.shape[0], _whole("place", place, 4, tokens * picks), _whole("weights", weights, 4, tokens * picks),
-                                                  tokens, picks, out_f, pz, ldz, None if stream is None else _queue(stream))
+    out_f, n = z.shape[1], tokens * picks
+    py, ldy = _rows("y", y, 0, out_f, 2)
+    pz, ldz = _rows("z", z, tokens, out_f, 2)
+    status = (_lib or lib()).lora_experts_combine(py, ldy, y.shape[0], _whole("place", place, n, 4), _whole("weights", weights, n, 4), tokens, picks, out_f,
+                                                  pz, ldz, None if stream is None else _queue(stream))
     if status:
         _check(status)

@@ -74,17 +74,27 @@ static __device__ __forceinline__ int expert_rows(const int32_t *__restrict__ st
     return max(b - a, 0);
 }
 
+// Tile `in_e` of an expert's mt row tiles x n_ct column tiles: column tiles in groups of CG, in a group row tile by row tile.
+template <int CG>
+static __device__ __forceinline__ void tile_of(int in_e, int mt, int n_ct, int &ct, int &m)
+{
+    const int grp = in_e / (mt * CG), rest = in_e - grp * (mt * CG), wide = min(CG, n_ct - grp * CG);
+    m = rest / wide;
+    ct = grp * CG + rest - m * wide;
+}
+
 // tile `at(total)` of all; false if there is none
-template <int R, class At>
+template <int R, int CG, class At>
 static __device__ __forceinline__ bool find_tile(const int32_t *__restrict__ starts, int n_experts, int n_rows, int n_ct, int lane, At at,
                                                  Tile &t)
 {
     if (!starts) {
         const int mt = (n_rows + R - 1) / R, idx = at(mt * n_ct);
         if (idx < 0) return false;
+        int m;
+        tile_of<CG>(idx, mt, n_ct, t.ct, m);
         t.expert = 0;
-        t.ct = idx / mt;
-        t.row0 = (idx - t.ct * mt) * R;
+        t.row0 = m * R;
         t.rows = min(R, n_rows - t.row0);
         return true;
     }
@@ -105,7 +115,9 @@ static __device__ __forceinline__ bool find_tile(const int32_t *__restrict__ sta
             const int l = __builtin_ctzll(hit);
             const int e_mt = __shfl(mt, l, 64), e_first = __shfl(first, l, 64), e_rows = __shfl(rows, l, 64);
             const int in_e = idx - (__shfl(upto, l, 64) - e_mt) * n_ct;
-            const int ct = in_e / e_mt, row = (in_e - ct * e_mt) * R;
+            int ct, m;
+            tile_of<CG>(in_e, e_mt, n_ct, ct, m);
+            const int row = m * R;
             t.expert = __builtin_amdgcn_readfirstlane(base + l);
             t.ct = __builtin_amdgcn_readfirstlane(ct);
             t.row0 = __builtin_amdgcn_readfirstlane(e_first + row);
@@ -152,7 +164,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
     const int n = lane & 15, kq = lane >> 4;
     Tile t;
     // work group b runs on XCD b mod 8: every XCD an eighth of the tiles, in one run
-    if (!find_tile<R>(a.starts, a.n_experts, a.n_rows, a.out / (16 * CB), lane, [&](int total) {
+    if (!find_tile<R, 1>(a.starts, a.n_experts, a.n_rows, a.out / (16 * CB), lane, [&](int total) {
             const int per_xcd = (total + 7) >> 3, idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
             return (int)(blockIdx.x >> 3) >= per_xcd || idx >= total ? -1 : idx;
         }, t))
@@ -308,18 +320,31 @@ static hipError_t launch_thin(const ExpertsArgs &a, hipStream_t stream)
 //     barrier behind each and the second strip's wavefronts one phase behind: of the two wavefronts of a SIMD one multiplies while the other reads.
 //     No request passes through registers the compiler tracks, so the waits count exactly what is under way.
 //   * In 8 bits a product spans a whole block of 128: its sum starts at zero, and 4 fp32 FMAs with x's scale times W's add it to the accumulators
-//     while the next ones run (half as long as the matrix unit takes).  A wavefront copies the scales of its own 64 rows beside x.
+//     while the next ones run (half as long as the matrix unit takes).  A wavefront copies the scales of its own 64 rows, of four pieces at a
+//     time: every row's lie in cache lines of their own, and one copy a piece took as long as half of the others together (8192 tokens
+//     8192 -> 8192: copies alone 418 us with one a piece, 304 without any).  Rows of x enter registers while the piece before is multiplied
+//     (WR = 4): a piece's first reading phase had 20 of its 28 operands, and lasted longer than the products beside it.
 // ------------------------------------------------------------------------------------------------
 constexpr int kWideThreads8 = 512;
 constexpr int kRing = 3;
 template <bool F8, int WR>
-constexpr int kWideLds = kRing * (64 * WR * kPieceBytes + (WR == 4 ? 16384 : 32768) + (F8 ? 2048 : 0));
+constexpr int kWideLds = kRing * (64 * WR * kPieceBytes + (WR == 4 ? 16384 : 32768)) + (F8 ? 8 * 2048 : 0);
 
 // One dword a lane straight to LDS: lane l's at `to` + 4 l.
 static __device__ __forceinline__ void dma4_to_lds(const void *g, uint32_t to)
 {
     uint32_t saved_m0;
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved_m0)
+                 : "v"(g), "s"(to)
+                 : "memory");
+}
+
+// 16 bytes a lane straight to LDS: lane l's at `to` + 16 l.
+static __device__ __forceinline__ void dma16x1_to_lds(const void *g, uint32_t to)
+{
+    uint32_t saved_m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
                  : "=&s"(saved_m0)
                  : "v"(g), "s"(to)
                  : "memory");
@@ -358,7 +383,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     constexpr int NB = 2 * WR;                     // sub-blocks of a wavefront
     constexpr int SP = WR == 4 ? 2 : 1;            // steps of a piece
     constexpr int XBUF = 64 * WR * kPieceBytes, WHALF = 16384 / SP, WBUF = 2 * WHALF;
-    constexpr int XC = WR + (F8 ? 1 : 0), WC = 4 / SP;  // copies of a wavefront: x (and scales) of a piece, W of a step
+    constexpr int XC = WR, WC = 4 / SP;            // copies of a wavefront: x of a piece, W of a step
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kq = lane >> 4;
     const int rw = WR == 4 ? wave & 3 : wave & 1;  // rows 64 rw .. of the tile
@@ -369,7 +394,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     const bool has_strip = strip * 128 < a.out;
     const int np = a.pieces, steps = np * SP;
 
-    char *const xring = lds, *const wring = lds + kRing * XBUF, *const sring = wring + kRing * WBUF;
+    char *const xring = lds, *const wring = lds + kRing * XBUF;
     // rows of x by 32-bit offsets in 16 bytes (the host sees to it that they fit), which take half of the registers of addresses
     uint32_t xoff[WR];
 #pragma unroll
@@ -385,15 +410,14 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     const int64_t es = (int64_t)t.expert * (a.out >> 7) + (has_strip ? strip : 0);
     const char *wsrc = a.w + es * np * 16384 + (wave & 3) * (WC * 1024);
     const char *xp = a.x;            // the next piece of every row
-    [[maybe_unused]] const float *sp = a.x_scales;
     const uint32_t lane16 = lane * 16;
     // (the scalar cache's path: a vector load would be counted among the copies)
     const __attribute__((address_space(4))) float *wscale =
         (const __attribute__((address_space(4))) float *)(uintptr_t)(F8 ? a.w_scales + es * np : nullptr);
 
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)lds);
-    const uint32_t x_end = lds0 + kRing * XBUF, w_end = x_end + kRing * WBUF, s_end = w_end + kRing * 2048;
-    uint32_t x_to = lds0 + WR * wave * 1024, w_to = x_end + (wave >> 2) * WHALF + (wave & 3) * (WC * 1024), s_to = w_end + wave * 256;
+    const uint32_t x_end = lds0 + kRing * XBUF, w_end = x_end + kRing * WBUF;
+    uint32_t x_to = lds0 + WR * wave * 1024, w_to = x_end + (wave >> 2) * WHALF + (wave & 3) * (WC * 1024);
     auto issue_x = [&]() __attribute__((always_inline)) {
         auto at = [&](int j) { return xp + (uint64_t)xoff[j] * 16 - 1024 * j; };  // as the copies take it
         if constexpr (WR == 4)
@@ -402,11 +426,28 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
             dma16x2_to_lds(at(0), at(1), x_to);
         xp += kPieceBytes;
         x_to = x_to + XBUF >= x_end ? x_to - (kRing - 1) * XBUF : x_to + XBUF;
-        if constexpr (F8) {
-            dma4_to_lds(sp + soff, s_to);
-            ++sp;
-            s_to = s_to + 2048 >= s_end ? s_to - (kRing - 1) * 2048 : s_to + 2048;
-        }
+    };
+    // The scales of this wavefront's rows, [piece of four][row], in 2 KB of its own.  Where rows of scales are whole numbers of 16 bytes: one copy of four
+    // pieces of every row into the second KB, put in order in the first one when its turn comes.  Else four copies, into one KB and the other in turn.
+    [[maybe_unused]] char *const sbuf = lds + kRing * (XBUF + WBUF) + wave * 2048;
+    [[maybe_unused]] const uint32_t s_to = w_end + wave * 2048;
+    [[maybe_unused]] const bool by16 = ((uintptr_t)a.x_scales % 16 | a.ld_scales % 4 | np % 4) == 0;
+    [[maybe_unused]] int fours = 0;  // of pieces requested
+    auto issue_scales = [&]() __attribute__((always_inline)) {
+        if (4 * fours >= np) return;
+        const float *sp = a.x_scales + soff;
+        if (by16)
+            dma16x1_to_lds(sp + 4 * fours, s_to + 1024);
+        else
+#pragma unroll
+            for (int c = 0; c < 4; ++c) dma4_to_lds(sp + min(4 * fours + c, np - 1), s_to + (fours & 1) * 1024 + 256 * c);
+        ++fours;
+    };
+    auto order_scales = [&]() __attribute__((always_inline)) {
+        if (!by16) return;
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(sbuf + 1024 + 16 * lane);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *reinterpret_cast<float *>(sbuf + 256 * c + 4 * lane) = v[c];
     };
     auto issue_w = [&]() __attribute__((always_inline)) {
         dma_kb_to_lds<WC>(wsrc, lane16, w_to);
@@ -420,6 +461,10 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
 #pragma unroll
         for (int k = 0; k < 16; ++k) acc[g][k] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+    if constexpr (F8) {
+        issue_scales();
+        if (!by16) issue_scales();
+    }
     issue_x();
     issue_w();
     if (steps > 1) issue_w();
@@ -439,29 +484,44 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         __builtin_amdgcn_sched_barrier(0);
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
     };
+    if constexpr (F8) {
+        order_scales();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (by16) issue_scales();
+    }
     phase_end();
-    if (wave >= 4) phase_end();  // the second strip's wavefronts run one phase behind the first's
 
     constexpr int XH = WR == 4 && !F8 ? 1 : 2;  // halves of x's rows in registers at a time
     constexpr int WB = WR == 4 && !F8 ? 8 : 4, WH = WR == 4 && !F8 ? 1 : 2;  // .. sub-blocks and halves of W
     uint4 xo[XH][4], wo[WH][WB];
     [[maybe_unused]] f32x4 sc[4];
-    int xget = 0, wget = 0, sget = 0;
+    int xget = 0, wget = 0;
+    [[maybe_unused]] int sget = 0;
     const int xlane = (8 * rw + (n >> 3)) * 1024 + (n & 7) * 128;
     const int wlane = (wave >> 2) * WHALF + lane * 16;
+    // row 16 i + n of this wavefront's: block 8 rw + 2 i + n / 8, row n mod 8 of it
+    auto x_at = [&](int i, int h) __attribute__((always_inline)) {
+        return *reinterpret_cast<const uint4 *>(xring + xget + xlane + 2048 * i + (((4 * h + kq) ^ (n & 7)) * 16));
+    };
+    constexpr bool kEarlyX = F8 && WR == 4;  // rows of x are read while the piece before is multiplied
+    if constexpr (kEarlyX) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) xo[h][i] = x_at(i, h);
+    }
+    if (wave >= 4) phase_end();  // the second strip's wavefronts run one phase behind the first's
     // step q of piece P, behind which come two pieces or more (AFTER = 2), one or none
     auto step = [&](int P, auto qc, auto afterc) __attribute__((always_inline)) {
         constexpr int q = decltype(qc)::value, AFTER = decltype(afterc)::value;
         constexpr bool kMoreW = SP == 2 ? AFTER >= 1 : AFTER == 2;  // there is a step after the next
         if constexpr (kMoreW) issue_w();
         if constexpr (q == 0 && AFTER == 2) issue_x();
-        if constexpr (XH == 1 || q == 0)
+        if constexpr (!kEarlyX && (XH == 1 || q == 0))
 #pragma unroll
             for (int h = 0; h < XH; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    // row 16 i + n of this wavefront's: block 8 rw + 2 i + n / 8, row n mod 8 of it
-                    xo[h][i] = *reinterpret_cast<const uint4 *>(xring + xget + xlane + 2048 * i + (((4 * (XH == 1 ? q : h) + kq) ^ (n & 7)) * 16));
+                for (int i = 0; i < 4; ++i) xo[h][i] = x_at(i, XH == 1 ? q : h);
 #pragma unroll
         for (int h = 0; h < WH; ++h)
 #pragma unroll
@@ -472,26 +532,40 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         if constexpr (F8 && q == 0) {
             const float w = wscale[P];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sc[i] = *reinterpret_cast<const f32x4 *>(sring + sget + wave * 256 + (16 * i + 4 * kq) * 4) * w;
+            for (int i = 0; i < 4; ++i) sc[i] = *reinterpret_cast<const f32x4 *>(sbuf + sget + (16 * i + 4 * kq) * 4) * w;
+            sget = (sget + 256) & (by16 ? 1023 : 2047);
         }
+        if constexpr (F8 && q == SP - 1)
+            if ((P & 3) == 3 && P + 1 < np) order_scales();
         __builtin_amdgcn_sched_barrier(0);
         // W of the next step and, where that begins one, x of the next piece have landed: behind them were requested
         // W of the step after and x of the piece after
         wait_vm<AFTER == 2 ? XC + WC : kMoreW ? WC : 0>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what was read is in registers: the slots may be written
+        // (requested four pieces before their use: long landed by the time that the waits above let a wavefront come there)
+        if constexpr (F8 && q == SP - 1)
+            if ((P & 3) == 3) issue_scales();
         phase_end();
+        if constexpr (q == SP - 1) xget = xget == (kRing - 1) * XBUF ? 0 : xget + XBUF;
         if constexpr (F8) {
             // the product k, and the sum of the one two before it
             f32x4 part[3];
 #pragma unroll
             for (int k = 0; k < 18; ++k) {
-                if (k < 16) part[k % 3] = mfma_e4m3(as_i32x8(xo[0][k & 3], xo[XH - 1][k & 3]), as_i32x8(wo[0][k >> 2], wo[WH - 1][k >> 2]), f32x4{0.f, 0.f, 0.f, 0.f});
+                if (k < 16) part[k % 3] = mfma_e4m3(as_i32x8(xo[0][k >> 2], xo[XH - 1][k >> 2]), as_i32x8(wo[0][k & 3], wo[WH - 1][k & 3]), f32x4{0.f, 0.f, 0.f, 0.f});
                 __builtin_amdgcn_sched_barrier(0);
                 if (k >= 2) {
                     const int j = k - 2;
+                    f32x4 &to = acc[q][4 * (j & 3) + (j >> 2)];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[q][j][e] = fmaf(sc[j & 3][e], part[j % 3][e], acc[q][j][e]);
+                    for (int e = 0; e < 4; ++e) to[e] = fmaf(sc[j >> 2][e], part[j % 3][e], to[e]);
                 }
+                // these rows of x have been multiplied: the next piece's.  All of it has landed: W of this step, requested behind it, has been waited
+                // for by every wavefront.
+                if constexpr (kEarlyX && q == SP - 1 && AFTER >= 1)
+                    if (k < 16 && (k & 3) == 3)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) xo[h][k >> 2] = x_at(k >> 2, h);
                 __builtin_amdgcn_sched_barrier(0);
             }
             here(acc[q]);
@@ -508,10 +582,6 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         }
         phase_end();
         wget = wget == (kRing - 1) * WBUF ? 0 : wget + WBUF;
-        if constexpr (q == SP - 1) {
-            xget = xget == (kRing - 1) * XBUF ? 0 : xget + XBUF;
-            if (F8) sget = sget == (kRing - 1) * 2048 ? 0 : sget + 2048;
-        }
     };
     auto piece = [&](int P, auto after) __attribute__((always_inline)) {
         step(P, std::integral_constant<int, 0>{}, after);
@@ -543,8 +613,9 @@ __global__ __launch_bounds__(kWideThreads8, 1) void k_experts_wide(ExpertsArgs a
     __shared__ __attribute__((aligned(16))) char lds[kWideLds<F8, 4> > kWideLds<F8, 2> ? kWideLds<F8, 4> : kWideLds<F8, 2>];
     const int n_ct = (a.out + 255) >> 8;
     Tile t;
-    // Every XCD a run of the tiles.
-    if (!find_tile<256>(a.starts, a.n_experts, a.n_rows, n_ct, threadIdx.x & 63, [&](int total) {
+    // Every XCD a run of the tiles: of 32, one on each of its compute units, 8 row tiles x 4 column tiles walk k together, and every chunk of x
+    // and W that one of them brings into the XCD's L2 serves four or eight of them.
+    if (!find_tile<256, 4>(a.starts, a.n_experts, a.n_rows, n_ct, threadIdx.x & 63, [&](int total) {
             const int per_xcd = (total + 7) >> 3, idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
             return (int)(blockIdx.x >> 3) >= per_xcd || idx >= total ? -1 : idx;
         }, t))
@@ -562,6 +633,174 @@ static hipError_t launch_wide(const ExpertsArgs &a, hipStream_t stream)
     const int64_t grid = (row_tiles * ((a.out + 255) / 256) + 7) / 8 * 8;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL(k_experts_wide<F8>, dim3((unsigned)grid), dim3(kWideThreads8), 0, stream, a);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------
+// Tiles of up to 64 rows whose columns the wavefronts share out: 16 RB rows x 64 CB columns, four wavefronts of 16 CB columns each.  A wavefront's
+// weights come straight from memory in operand order, D pieces ahead, and no other wavefront wants them; x, which all four want, passes through
+// LDS, two slots of a piece, a barrier per piece.
+// ------------------------------------------------------------------------------------------------
+constexpr int kMidWaves = 4;
+
+template <bool F8, int RB, int CB, int D>
+__global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a)
+{
+    constexpr int R = 16 * RB, XBUF = R * kPieceBytes;
+    constexpr int NX = RB > 2 ? RB / 2 : 1;  // x loads of a wavefront per piece
+    constexpr int NS = (R + 63) / 64;        // .. of scales
+    static_assert(D % 2 == 0, "slots of x by the place in the unrolled loop");
+    __shared__ __attribute__((aligned(16))) char lds[2 * XBUF + (F8 ? kMidWaves * R * 4 : 0)];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, kq = lane >> 4;
+    Tile t;
+    if (!find_tile<R, 1>(a.starts, a.n_experts, a.n_rows, a.out / (64 * CB), lane, [&](int total) {
+            const int per_xcd = (total + 7) >> 3, idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+            return (int)(blockIdx.x >> 3) >= per_xcd || idx >= total ? -1 : idx;
+        }, t))
+        return;
+    // this wavefront's sub-blocks, of all in the row
+    const int b_all = (t.ct * kMidWaves + wave) * CB, strip = b_all >> 3, b0 = b_all & 7;
+    const int np = a.pieces;
+
+    f32x4 acc[RB][CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int b = 0; b < CB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // x: 16 bytes a lane (8 where the tile has 16 rows), the tile's rows in order over the wavefronts; chunk c of row r goes to slot c XOR (r mod 8)
+    typedef __attribute__((ext_vector_type(RB == 1 ? 2 : 4))) unsigned XLoad;
+    constexpr int LPR = kPieceBytes / (int)sizeof(XLoad);  // lanes per row
+    const char *xrow[NX];
+    int xput[NX];
+#pragma unroll
+    for (int q = 0; q < NX; ++q) {
+        const int l = q * 64 * kMidWaves + tid, r = l / LPR, at = l % LPR * (int)sizeof(XLoad);
+        const int tok = token_at(a, t.row0 + (r < t.rows ? r : 0));
+        xrow[q] = a.x + (int64_t)max(tok, 0) * a.ldx_bytes + at;
+        xput[q] = r * kPieceBytes + (((at >> 4) ^ (r & 7)) << 4) + (at & 15);
+    }
+    const char *wbase = a.w + ((int64_t)t.expert * (a.out >> 7) + strip) * np * 16384 + operand_at<F8>(0, b0);
+    const unsigned lane16 = lane * 16;
+    [[maybe_unused]] const float *xs_at[NS], *ws_at = nullptr;
+    [[maybe_unused]] float *const sc = reinterpret_cast<float *>(lds + 2 * XBUF) + wave * R;
+    if constexpr (F8) {
+#pragma unroll
+        for (int q = 0; q < NS; ++q) {
+            const int tok = token_at(a, t.row0 + (64 * q + lane < t.rows ? 64 * q + lane : 0));
+            xs_at[q] = a.x_scales + (int64_t)max(tok, 0) * a.ld_scales;
+        }
+        int zero = 0;
+        asm("" : "+v"(zero));  // (a vector load, counted in order with the others)
+        ws_at = a.w_scales + ((int64_t)t.expert * (a.out >> 7) + strip) * np + zero;
+    }
+    XLoad xq[D][NX];
+    uint4 wq[D][2][CB];
+    [[maybe_unused]] float sx[D][NS], sw[D];
+    // Loads without branches (around one the compiler would wait for everything in flight): past the last piece, the last one again.
+    auto load_x = [&](int s, int d) __attribute__((always_inline)) {
+        const int at = min(s, np - 1);
+#pragma unroll
+        for (int q = 0; q < NX; ++q) xq[d][q] = *reinterpret_cast<const XLoad *>(xrow[q] + (int64_t)at * kPieceBytes);
+        if constexpr (F8) {
+#pragma unroll
+            for (int q = 0; q < NS; ++q) sx[d][q] = xs_at[q][at];
+            sw[d] = ws_at[at];
+        }
+    };
+    auto load_w = [&](int s, int d) __attribute__((always_inline)) {
+        const char *p = wbase + (int64_t)min(s, np - 1) * 16384;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < CB; ++b) wq[d][h][b] = ldb16(p + operand_at<F8>(h, b) + lane16);
+    };
+    auto put_x = [&](int d, int slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < NX; ++q) *reinterpret_cast<XLoad *>(lds + slot * XBUF + xput[q]) = xq[d][q];
+    };
+    auto barrier = [&]() __attribute__((always_inline)) {
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+        load_x(d, d);
+        __builtin_amdgcn_sched_barrier(0);
+        load_w(d, d);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    for (int s0 = 0; s0 < np; s0 += D) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int slot = d & 1;
+            put_x(d, slot);
+            if constexpr (F8)
+#pragma unroll
+                for (int q = 0; q < NS; ++q)
+                    if (64 * q + lane < R) sc[64 * q + lane] = sx[d][q] * sw[d];
+            load_x(s0 + d + D, d);
+            // what a slot held two pieces ago has been read by everyone: each came to the barrier of the piece between behind its reads
+            barrier();
+            if (s0 + d < np) {
+                const char *xs = lds + slot * XBUF;
+                uint4 xo[2][RB];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < RB; ++i)
+                        xo[h][i] = *reinterpret_cast<const uint4 *>(xs + (16 * i + n) * kPieceBytes + (((4 * h + kq) ^ (n & 7)) << 4));
+                if constexpr (F8) {
+#pragma unroll
+                    for (int i = 0; i < RB; ++i) {
+                        const f32x4 f = *reinterpret_cast<const f32x4 *>(sc + 16 * i + 4 * kq);
+#pragma unroll
+                        for (int b = 0; b < CB; ++b)
+                            acc[i][b] += f * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), f32x4{0.f, 0.f, 0.f, 0.f});
+                    }
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < RB; ++i)
+#pragma unroll
+                            for (int b = 0; b < CB; ++b)
+                                acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(xo[h][i]), as_bf16x8(wq[d][h][b]), acc[i][b], 0, 0, 0);
+                }
+            }
+            load_w(s0 + d + D, d);
+            in_order();  // (the scales' region is this wavefront's own)
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    uint16_t *const y0 = a.y + (int64_t)t.row0 * a.ldy + strip * 128 + 64 * (b0 >> 2) + 4 * n + (b0 & 3);
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = 16 * i + 4 * kq + e;
+            if (r >= t.rows || token_at(a, t.row0 + r) < 0) continue;
+            [[maybe_unused]] uint32_t *const dst = reinterpret_cast<uint32_t *>(y0 + (int64_t)r * a.ldy);
+            if constexpr (CB == 4)
+                *reinterpret_cast<uint2 *>(dst) = uint2{pack_bf16_rne(acc[i][0][e], acc[i][1][e]), pack_bf16_rne(acc[i][2][e], acc[i][3][e])};
+            else if constexpr (CB == 2)
+                *dst = pack_bf16_rne(acc[i][0][e], acc[i][1][e]);
+            else
+                y0[(int64_t)r * a.ldy] = (uint16_t)pack_bf16_rne(acc[i][0][e], 0.f);
+        }
+}
+
+template <bool F8, int RB, int CB, int D>
+static hipError_t launch_mid(const ExpertsArgs &a, hipStream_t stream)
+{
+    const int64_t row_tiles = (int64_t)(a.n_rows + 16 * RB - 1) / (16 * RB) + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
+    const int64_t grid = (row_tiles * (a.out / (64 * CB)) + 7) / 8 * 8;
+    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_experts_mid<F8, RB, CB, D>), dim3((unsigned)grid), dim3(64 * kMidWaves), 0, stream, a);
     return hipGetLastError();
 }
 
