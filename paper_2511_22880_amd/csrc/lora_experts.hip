@@ -12,6 +12,7 @@
 // for the first 64 columns.  The token operand uses the same mapping of lanes to k.
 #include "lora_device.h"
 #include "lora_experts.h"
+#include "lora_internal.h"
 
 #include <type_traits>
 
@@ -804,14 +805,28 @@ static hipError_t launch_mid(const ExpertsArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
+// The tiles of a launch: the largest that still make a work group per compute unit, no higher than an expert's rows in the mean ask for.  Row tiles are
+// counted as if every expert's last one came on top (the host does not know who picked what).  us, 8 bits, 256 x 256 / 64 x 256 / 64 x 128 / 32 x 128 /
+// 32 x 64 / 16 x 64 / 16 x 32, the one taken in brackets: one layer of 4096 -> 4096, 32 rows 32 / 32 / 20 / 12.4 / 8.4 / 6.8 / (6.3), 64 rows 32 / 32 / 20 / 12.3 /
+// 8.7 / (7.1) / 9.2, 128 rows 32 / 32 / 20 / 12.5 / (9.2) / 11.2 / 14.8, 256 rows 51 / 32 / 20 / (12.7) / 14.4 / 18.8 / 25.6, 512 rows 51 / 32 / (20.6) / 20.6 / 24.0 /
+// 31.9 / 52, 1024 rows 52 / (32.4) / 30.1 / 38 / 49 / - / 107, 2048 rows 54 / (48) / 59 / 78 / 97 / - / 215; 16384 -> 16384, 128 rows 170 / 129 / (85) / 105 / 107 / 140
+// / 193; 8192 -> 1024, 512 rows 97 / 60 / 36 / 22 / (15.0) / - / 26.8; 64 experts 2048 -> 1536, 8 rows each 49 / - / 47 / (39) / 44 / 41 / 54, 64 rows each (56) / 64 / 70 /
+// 66 / 81 / 91 / 169; in bf16 there 8 rows 81 / - / 77 / (76) / 73 / 74 / 76, 32 rows 85 / 84 / (79) / 88 / 91 / 105 / 130, 64 rows (90) / 98 / 102 / 109 / 115 / 153 / 200.
 template <bool F8>
 static hipError_t launch_by_rows(const ExpertsArgs &a, hipStream_t stream)
 {
-    const int per = a.n_rows / a.n_experts;
-    if (per <= 16) return launch_thin<F8, 1, 4, 2, 8>(a, stream);
-    if (per <= 32) return launch_thin<F8, 2, 4, 2, 8>(a, stream);
-    if (per <= 64) return launch_thin<F8, 4, 4, 2, 8>(a, stream);
-    return launch_wide<F8>(a, stream);
+    const int met = a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0;
+    const int per = met ? a.n_rows / met : a.n_rows;
+    auto fills = [&](int rows, int columns) {
+        return ((int64_t)(a.n_rows + rows - 1) / rows + met) * ((a.out + columns - 1) / columns) >= kComputeUnits;
+    };
+    if (per > 48 && fills(256, 256)) return launch_wide<F8>(a, stream);
+    if (per > 32 && a.out % 256 == 0 && fills(64, 256)) return launch_mid<F8, 4, 4, 2>(a, stream);
+    if (per > 24 && fills(64, 128)) return launch_mid<F8, 4, 2, 2>(a, stream);
+    if (per > 6 && fills(32, 128)) return launch_mid<F8, 2, 2, 2>(a, stream);
+    if (per > 16 && fills(32, 64)) return launch_thin<F8, 2, 4, 2, 4>(a, stream);
+    if (fills(16, 64)) return launch_thin<F8, 1, 4, 2, 4>(a, stream);
+    return launch_thin<F8, 1, 2, 2, 8>(a, stream);
 }
 
 hipError_t launch_experts_linear(const ExpertsArgs &a, bool bits8, hipStream_t stream)
