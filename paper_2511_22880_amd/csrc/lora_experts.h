@@ -9,13 +9,19 @@ namespace lora {
 constexpr int kScaleBlock = 128;     // values of a row, or of a row and a column of a weight, that share a scale
 constexpr int kPieceBytes = 128;     // of a row: what the products walk k in (64 bf16 or 128 8-bit values)
 constexpr int kMaxExperts = 512;     // (a work group that groups picks has a count of each for 16 wavefronts in LDS)
-constexpr int kGroupChunk = 2048;    // picks of a work group that groups them, at least
-constexpr int kGroupMaxChunks = 256; // and so many work groups at most
+constexpr int kGroupUnit = 1024;      // picks of a work group that groups them: 1, 2, 4, 8 or a multiple of 16 times as many
+constexpr int kGroupAlone = 8;        // .. times as many are one work group's at most ...
+constexpr int kGroupMaxChunks = 256;  // ... beyond which there are up to so many work groups
 
+// picks of a work group
 inline int64_t group_chunk(int64_t n_picks)
 {
-    const int64_t least = (n_picks + kGroupMaxChunks - 1) / kGroupMaxChunks;
-    return least <= kGroupChunk ? kGroupChunk : (least + kGroupChunk - 1) / kGroupChunk * kGroupChunk;
+    for (int m = 1; m <= kGroupAlone; m *= 2)
+        if (n_picks <= m * kGroupUnit) return m * kGroupUnit;
+    for (int m = 2; m <= 8; m *= 2)
+        if (n_picks <= (int64_t)m * kGroupUnit * kGroupMaxChunks) return m * kGroupUnit;
+    const int64_t unit = 16 * kGroupUnit, least = (n_picks + kGroupMaxChunks - 1) / kGroupMaxChunks;
+    return (least + unit - 1) / unit * unit;
 }
 inline int group_chunks(int64_t n_picks) { const int64_t c = group_chunk(n_picks); return (int)((n_picks + c - 1) / c); }
 

@@ -76,8 +76,8 @@ def test_sizes():
     assert L.lora_experts_packed_bytes(3, 192, 256, 16) == 3 * 192 * 256 * 2
     assert L.lora_experts_packed_bytes(512, 16384, 16384, 16) == 512 << 29  # past 32 bits
     assert L.lora_experts_group_workspace_bytes(0, 8) == 0
-    assert L.lora_experts_group_workspace_bytes(2048, 512) == 0
-    assert L.lora_experts_group_workspace_bytes(2049, 512) == 2 * 512 * 4
+    assert L.lora_experts_group_workspace_bytes(8192, 512) == 0
+    assert L.lora_experts_group_workspace_bytes(8193, 512) == 5 * 512 * 4
     assert L.lora_experts_group_workspace_bytes(2 ** 31 - 1, 512) <= 256 * 512 * 4
     for args in ((-1, 8), (2 ** 31, 8), (5, 0), (5, 513)):
         with pytest.raises(L.LoraError):

@@ -230,7 +230,8 @@ def group(ids, experts):
 
 @pytest.mark.parametrize("tokens, picks, experts", [
     (0, 1, 4), (1, 1, 1), (1, 8, 8), (3, 2, 512), (63, 1, 5), (64, 8, 128), (255, 8, 64), (256, 8, 256), (257, 8, 255), (2049, 1, 7), (3000, 6, 512),
-    (19675, 8, 256), (70001, 8, 33), (100, 64, 200)])
+    (19675, 8, 256), (70001, 8, 33), (100, 64, 200), (1024, 1, 100), (1025, 1, 100), (511, 4, 9), (2047, 2, 64), (4097, 1, 12), (8191, 1, 511), (8192, 1, 60), (8193, 1, 60),
+    (90000, 6, 17), (140001, 8, 130), (262144, 9, 40)])
 @pytest.mark.parametrize("kind", ["any", "one", "none", "wild"])
 def test_group(tokens, picks, experts, kind):
     g = gen(tokens + experts)
