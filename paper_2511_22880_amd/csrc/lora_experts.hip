@@ -874,65 +874,81 @@ hipError_t launch_experts_pack(const char *w, int64_t n_experts, int row_bytes, 
 static __device__ __forceinline__ float value_lo(uint32_t u) { return __uint_as_float(u << 16); }
 static __device__ __forceinline__ float value_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
 
-__global__ __launch_bounds__(256) void k_rows_quantize(const uint16_t *__restrict__ x, int64_t ldx, int64_t rows, int in, int blocks,
+constexpr int kQuantizeBlocks = 2;  // of 128 a thread has a part of
+
+__global__ __launch_bounds__(256) void k_rows_quantize(const uint16_t *__restrict__ x, int64_t ldx, unsigned total, int in, unsigned blocks,
                                                        uint8_t *__restrict__ q, int64_t ldq, float *__restrict__ scales, int64_t ld_scales)
 {
-    const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);  // block of 128
-    if (at >= rows * blocks) return;
     const int l = threadIdx.x & 15;
-    const int64_t row = at / blocks;
-    const int blk = (int)(at - row * blocks), k = blk * kScaleBlock + 8 * l;
-    uint4 v = {0u, 0u, 0u, 0u};
-    if (k < in) v = ld16(x + row * ldx + k);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t top = 0;
+    const unsigned at0 = blockIdx.x * (16 * kQuantizeBlocks) + (threadIdx.x >> 4);
+    uint4 v[kQuantizeBlocks];
+    unsigned row[kQuantizeBlocks], blk[kQuantizeBlocks];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-    const float largest = __uint_as_float(top << 16);
-    uint32_t o[2] = {0u, 0u};
-    float scale = largest;
-    if (top < 0x7F80u) {
-        const float d = fmaxf(largest, 448.f * 0x1p-126f);
-        scale = d / 448.f;
-        const uint32_t bits = __float_as_uint(d), e = bits >> 23;       // d = m 2^(e - 127), e >= 9
-        const float m = __uint_as_float((bits & 0x007FFFFFu) | 0x3F800000u);
-        const float f = 1.75f * __uint_as_float((262u - e) << 23);  // 448 2^(127 - e)
-        const float r = __builtin_amdgcn_rcpf(m);
-        float c[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float n0 = value_lo(w[i]) * f, n1 = value_hi(w[i]) * f;
-            const float t0 = n0 * r, t1 = n1 * r;
-            c[2 * i] = fmaf(fmaf(-t0, m, n0), r, t0);
-            c[2 * i + 1] = fmaf(fmaf(-t1, m, n1), r, t1);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            int p = __builtin_amdgcn_cvt_pk_fp8_f32(c[4 * i], c[4 * i + 1], 0, false);
-            o[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[4 * i + 2], c[4 * i + 3], p, true);
-        }
-    } else {
-        // an infinity, or a NaN: no scale has a meaning, and the values say so
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t mag = (w[i >> 1] >> (16 * (i & 1))) & 0x7FFFu;
-            o[i >> 2] |= (top > 0x7F80u || mag >= 0x7F80u ? 0x7Fu : 0u) << (8 * (i & 3));
-        }
+    for (int j = 0; j < kQuantizeBlocks; ++j) {
+        const unsigned at = min(at0 + 16 * j, total - 1);
+        row[j] = at / blocks;
+        blk[j] = at - row[j] * blocks;
+        const int k = (int)blk[j] * kScaleBlock + 8 * l;
+        v[j] = ld16_stream(x + (int64_t)row[j] * ldx + (k < in ? k : 0));
+        if (k >= in) v[j] = uint4{0u, 0u, 0u, 0u};
     }
-    *reinterpret_cast<uint2 *>(q + row * ldq + k) = uint2{o[0], o[1]};
-    if (l == 0) scales[row * ld_scales + blk] = scale;
+#pragma unroll
+    for (int j = 0; j < kQuantizeBlocks; ++j) {
+        if (at0 + 16 * j >= total) return;
+        const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+        const float largest = __uint_as_float(top << 16);
+        uint32_t o[2] = {0u, 0u};
+        float scale = largest;
+        if (top < 0x7F80u) {
+            const float d = fmaxf(largest, 448.f * 0x1p-126f);
+            scale = d / 448.f;
+            const uint32_t bits = __float_as_uint(d), e = bits >> 23;  // d = m 2^(e - 127), e >= 9
+            const float m = __uint_as_float((bits & 0x007FFFFFu) | 0x3F800000u);
+            const float f = 1.75f * __uint_as_float((262u - e) << 23);  // 448 2^(127 - e)
+            const float r = __builtin_amdgcn_rcpf(m);
+            float c[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float n0 = value_lo(w[i]) * f, n1 = value_hi(w[i]) * f;
+                const float t0 = n0 * r, t1 = n1 * r;
+                c[2 * i] = fmaf(fmaf(-t0, m, n0), r, t0);
+                c[2 * i + 1] = fmaf(fmaf(-t1, m, n1), r, t1);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int p = __builtin_amdgcn_cvt_pk_fp8_f32(c[4 * i], c[4 * i + 1], 0, false);
+                o[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[4 * i + 2], c[4 * i + 3], p, true);
+            }
+        } else {
+            // an infinity, or a NaN: no scale has a meaning, and the values say so
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t mag = (w[i >> 1] >> (16 * (i & 1))) & 0x7FFFu;
+                o[i >> 2] |= (top > 0x7F80u || mag >= 0x7F80u ? 0x7Fu : 0u) << (8 * (i & 3));
+            }
+        }
+        *reinterpret_cast<uint2 *>(q + (int64_t)row[j] * ldq + (int)blk[j] * kScaleBlock + 8 * l) = uint2{o[0], o[1]};
+        if (l == 0) scales[(int64_t)row[j] * ld_scales + blk[j]] = scale;
+    }
 }
 
 hipError_t launch_rows_quantize(const uint16_t *x, int64_t ldx, int64_t rows, int in, uint8_t *q, int64_t ldq, float *scales,
                                 int64_t ld_scales, hipStream_t stream)
 {
     const int blocks = (in + kScaleBlock - 1) / kScaleBlock;
-    const int64_t grid = (rows * blocks + 15) / 16;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k_rows_quantize, dim3((unsigned)grid), dim3(256), 0, stream, x, ldx, rows, in, blocks, q, ldq, scales, ld_scales);
-    return hipGetLastError();
+    const int64_t most = ((int64_t)1 << 31) / blocks;  // rows of a launch, whose blocks are counted in 32 bits
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t total = (rows - r < most ? rows - r : most) * blocks;
+        hipLaunchKernelGGL(k_rows_quantize, dim3((unsigned)((total + 16 * kQuantizeBlocks - 1) / (16 * kQuantizeBlocks))), dim3(256), 0, stream,
+                           x + r * ldx, ldx, (unsigned)total, in, (unsigned)blocks, q + r * ldq, ldq, scales + r * ld_scales, ld_scales);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1141,39 +1157,64 @@ hipError_t launch_experts_group(const int32_t *ids, int64_t ld_ids, int64_t toke
 }
 
 // ------------------------------------------------------------------------------------------------
-// The weighted sum of a token's rows: a thread has 8 columns of one token.
+// The weighted sum of a token's rows: a thread has 8 columns of one token, and requests PB of its rows before it adds the first.  Rows are read once
+// and past the caches; a pick without one reads the first row, which lies in the caches, and counts nothing.
 // ------------------------------------------------------------------------------------------------
+template <int PB>
 __global__ __launch_bounds__(256) void k_experts_combine(const uint16_t *__restrict__ y, int64_t ldy, int n_rows, const int32_t *__restrict__ place,
-                                                         const float *__restrict__ weights, int64_t tokens, int picks, int eighths,
+                                                         const float *__restrict__ weights, unsigned pieces, int picks, unsigned eighths,
                                                          uint16_t *__restrict__ z, int64_t ldz)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= tokens * eighths) return;
-    const int64_t t = i / eighths;
-    const int c = (int)(i - t * eighths) * 8;
+    const unsigned i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= pieces) return;
+    const unsigned t = i / eighths, c = (i - t * eighths) * 8;
+    const int32_t *const at = place + (int64_t)t * picks;
+    const float *const of = weights + (int64_t)t * picks;
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < picks; ++j) {
-        const int p = place[t * picks + j];
-        if ((unsigned)p >= (unsigned)n_rows) continue;
-        const float w = weights[t * picks + j];
-        const uint4 v = ld16(y + (int64_t)p * ldy + c);
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    for (int j = 0; j < picks; j += PB) {
+        uint4 v[PB];
+        float w[PB];
+        bool there[PB];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            s[2 * k] += w * value_lo(u[k]);
-            s[2 * k + 1] += w * value_hi(u[k]);
+        for (int q = 0; q < PB; ++q) {
+            const int p = at[j + q];
+            there[q] = (unsigned)p < (unsigned)n_rows;
+            w[q] = of[j + q];
+            v[q] = ld16_stream(y + (int64_t)(there[q] ? p : 0) * ldy + c);
+        }
+#pragma unroll
+        for (int q = 0; q < PB; ++q) {
+            const uint32_t u[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float lo = fmaf(w[q], value_lo(u[k]), s[2 * k]), hi = fmaf(w[q], value_hi(u[k]), s[2 * k + 1]);
+                s[2 * k] = there[q] ? lo : s[2 * k];
+                s[2 * k + 1] = there[q] ? hi : s[2 * k + 1];
+            }
         }
     }
-    st16_stream(z + t * ldz + c, uint4{pack_bf16_rne(s[0], s[1]), pack_bf16_rne(s[2], s[3]), pack_bf16_rne(s[4], s[5]), pack_bf16_rne(s[6], s[7])});
+    st16_stream(z + (int64_t)t * ldz + c, uint4{pack_bf16_rne(s[0], s[1]), pack_bf16_rne(s[2], s[3]), pack_bf16_rne(s[4], s[5]), pack_bf16_rne(s[6], s[7])});
 }
 
 hipError_t launch_experts_combine(const uint16_t *y, int64_t ldy, int n_rows, const int32_t *place, const float *weights, int64_t tokens, int picks,
                                   int out, uint16_t *z, int64_t ldz, hipStream_t stream)
 {
-    const int64_t grid = (tokens * (out / 8) + 255) / 256;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k_experts_combine, dim3((unsigned)grid), dim3(256), 0, stream, y, ldy, n_rows, place, weights, tokens, picks, out / 8, z, ldz);
-    return hipGetLastError();
+    const int64_t most = ((int64_t)1 << 31) / (out / 8);  // tokens of a launch, whose pieces are counted in 32 bits
+    for (int64_t t = 0; t < tokens; t += most) {
+        const int64_t pieces = (tokens - t < most ? tokens - t : most) * (out / 8);
+        auto go = [&](auto pb) {
+            hipLaunchKernelGGL(k_experts_combine<decltype(pb)::value>, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, stream, y, ldy, n_rows,
+                               place + t * picks, weights + t * picks, (unsigned)pieces, n_rows > 0 ? picks : 0, (unsigned)(out / 8), z + t * ldz, ldz);
+        };
+        if (picks % 4 == 0)
+            go(std::integral_constant<int, 4>{});
+        else if (picks % 2 == 0)
+            go(std::integral_constant<int, 2>{});
+        else
+            go(std::integral_constant<int, 1>{});
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace lora
