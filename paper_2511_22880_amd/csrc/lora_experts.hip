@@ -75,59 +75,94 @@ static __device__ __forceinline__ int expert_rows(const int32_t *__restrict__ st
     return max(b - a, 0);
 }
 
-// Tile `in_e` of an expert's mt row tiles x n_ct column tiles: column tiles in groups of CG, in a group row tile by row tile.
-template <int CG>
-static __device__ __forceinline__ void tile_of(int in_e, int mt, int n_ct, int &ct, int &m)
+static __device__ __forceinline__ int wave_sum(int v)
 {
-    const int grp = in_e / (mt * CG), rest = in_e - grp * (mt * CG), wide = min(CG, n_ct - grp * CG);
-    m = rest / wide;
-    ct = grp * CG + rest - m * wide;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+    return __builtin_amdgcn_readfirstlane(v);
 }
 
-// tile `at(total)` of all; false if there is none
-template <int R, int CG, class At>
-static __device__ __forceinline__ bool find_tile(const int32_t *__restrict__ starts, int n_experts, int n_rows, int n_ct, int lane, At at,
-                                                 Tile &t)
+// Row tile q of all, experts in their order, tiles(rows) of them for an expert: its expert, which of the expert's it is, how many those are, and the
+// expert's places.  q is one of them.
+struct RowTile {
+    int expert, m, of, first, rows;
+};
+template <class Tiles>
+static __device__ __forceinline__ RowTile find_row_tile(const int32_t *__restrict__ starts, int n_experts, int n_rows, int lane, int q, Tiles tiles)
 {
-    if (!starts) {
-        const int mt = (n_rows + R - 1) / R, idx = at(mt * n_ct);
-        if (idx < 0) return false;
-        int m;
-        tile_of<CG>(idx, mt, n_ct, t.ct, m);
-        t.expert = 0;
-        t.row0 = m * R;
-        t.rows = min(R, n_rows - t.row0);
-        return true;
-    }
-    int mine = 0, first;
-    for (int e = lane; e < n_experts; e += 64) mine += (expert_rows(starts, e, n_rows, first) + R - 1) / R;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d, 64);
-    const int idx = at(__builtin_amdgcn_readfirstlane(mine) * n_ct);
-    if (idx < 0) return false;
-    const int q = idx / n_ct;  // row tile, expert by expert: which expert's
     int before = 0;
     for (int base = 0; base < n_experts; base += 64) {
         const int e = base + lane;
+        int first = 0;
         const int rows = e < n_experts ? expert_rows(starts, e, n_rows, first) : 0;
-        const int mt = (rows + R - 1) / R, upto = before + wave_scan(mt, lane);
+        const int mt = tiles(rows), upto = before + wave_scan(mt, lane);
         const uint64_t hit = __ballot(q < upto);
         if (hit) {
-            const int l = __builtin_ctzll(hit);
-            const int e_mt = __shfl(mt, l, 64), e_first = __shfl(first, l, 64), e_rows = __shfl(rows, l, 64);
-            const int in_e = idx - (__shfl(upto, l, 64) - e_mt) * n_ct;
-            int ct, m;
-            tile_of<CG>(in_e, e_mt, n_ct, ct, m);
-            const int row = m * R;
-            t.expert = __builtin_amdgcn_readfirstlane(base + l);
-            t.ct = __builtin_amdgcn_readfirstlane(ct);
-            t.row0 = __builtin_amdgcn_readfirstlane(e_first + row);
-            t.rows = __builtin_amdgcn_readfirstlane(min(R, e_rows - row));
-            return true;
+            const int l = __builtin_ctzll(hit), e_mt = __shfl(mt, l, 64);
+            return RowTile{__builtin_amdgcn_readfirstlane(base + l), __builtin_amdgcn_readfirstlane(q - (__shfl(upto, l, 64) - e_mt)),
+                           __builtin_amdgcn_readfirstlane(e_mt), __builtin_amdgcn_readfirstlane(__shfl(first, l, 64)),
+                           __builtin_amdgcn_readfirstlane(__shfl(rows, l, 64))};
         }
         before = __shfl(upto, 63, 64);
     }
-    return false;
+    return RowTile{0, 0, 1, 0, 0};
+}
+
+// The tile of R rows that work group `blk` has, of all; false if none.  Work group b runs on XCD b mod 8: every XCD an eighth of the tiles, in one run.
+template <int R>
+static __device__ __forceinline__ bool find_tile(const int32_t *__restrict__ starts, int n_experts, int n_rows, int n_ct, int lane, int blk, Tile &t)
+{
+    auto tiles = [](int rows) { return (rows + R - 1) / R; };
+    int mine = 0, first;
+    if (starts)
+        for (int e = lane; e < n_experts; e += 64) mine += tiles(expert_rows(starts, e, n_rows, first));
+    const int total = (starts ? wave_sum(mine) : tiles(n_rows)) * n_ct, per_xcd = (total + 7) >> 3, idx = (blk & 7) * per_xcd + (blk >> 3);
+    if ((blk >> 3) >= per_xcd || idx >= total) return false;
+    const RowTile r = starts ? find_row_tile(starts, n_experts, n_rows, lane, idx / n_ct, tiles) : RowTile{0, 0, tiles(n_rows), 0, n_rows};
+    // inside an expert column tile by column tile, so that neighbours share W: which it is
+    const int in_e = starts ? idx - (idx / n_ct - r.m) * n_ct : idx;
+    t.ct = in_e / r.of;
+    const int row = (in_e - t.ct * r.of) * R;
+    t.expert = r.expert;
+    t.row0 = r.first + row;
+    t.rows = min(R, r.rows - row);
+    return true;
+}
+
+// The same for tiles of 256 rows x 256 columns, an expert's last one of up to 128 rows apart: the whole ones come first, and the others, which take about
+// half as long, fill the compute units that the last round of those leaves idle.  Inside an expert column tiles in groups of four, in a group row tile by row tile:
+// of 32 tiles in a run, one on each of an XCD's compute units, 8 row tiles x 4 column tiles walk k together, and every chunk of x and W that
+// one of them brings into the XCD's L2 serves four or eight of them (8192 tokens 8192 -> 8192 in 8 bits 567 us column by column, 502 so).
+static __device__ __forceinline__ bool find_wide_tile(const int32_t *__restrict__ starts, int n_experts, int n_rows, int n_ct, int lane, int blk, Tile &t)
+{
+    auto whole = [](int rows) { return (rows + 127) >> 8; };
+    auto rest = [](int rows) { return ((rows + 255) >> 8) - ((rows + 127) >> 8); };
+    int n_whole = whole(n_rows), n_rest = rest(n_rows);
+    if (starts) {
+        int a = 0, b = 0, first;
+        for (int e = lane; e < n_experts; e += 64) {
+            const int rows = expert_rows(starts, e, n_rows, first);
+            a += whole(rows);
+            b += rest(rows);
+        }
+        n_whole = wave_sum(a);
+        n_rest = wave_sum(b);
+    }
+    const int xcd = blk & 7, per_whole = (n_whole * n_ct + 7) >> 3, per_rest = (n_rest * n_ct + 7) >> 3;
+    const bool is_rest = (blk >> 3) >= per_whole;
+    const int j = (blk >> 3) - (is_rest ? per_whole : 0), per = is_rest ? per_rest : per_whole, idx = xcd * per + j;
+    if (j >= per || idx >= (is_rest ? n_rest : n_whole) * n_ct) return false;
+    const int q = idx / n_ct;
+    const RowTile r = !starts   ? RowTile{0, is_rest ? 0 : q, is_rest ? n_rest : n_whole, 0, n_rows}
+                      : is_rest ? find_row_tile(starts, n_experts, n_rows, lane, q, rest)
+                                : find_row_tile(starts, n_experts, n_rows, lane, q, whole);
+    const int in_e = idx - (q - r.m) * n_ct, grp = in_e / (r.of * 4), left = in_e - grp * (r.of * 4), wide = min(4, n_ct - grp * 4);
+    const int m = left / wide, row = (is_rest ? whole(r.rows) : m) * 256;
+    t.expert = r.expert;
+    t.ct = grp * 4 + left - m * wide;
+    t.row0 = r.first + row;
+    t.rows = min(256, r.rows - row);
+    return true;
 }
 
 // row of x at a place, -1 if the order names none
@@ -164,12 +199,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kq = lane >> 4;
     Tile t;
-    // work group b runs on XCD b mod 8: every XCD an eighth of the tiles, in one run
-    if (!find_tile<R, 1>(a.starts, a.n_experts, a.n_rows, a.out / (16 * CB), lane, [&](int total) {
-            const int per_xcd = (total + 7) >> 3, idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-            return (int)(blockIdx.x >> 3) >= per_xcd || idx >= total ? -1 : idx;
-        }, t))
-        return;
+    if (!find_tile<R>(a.starts, a.n_experts, a.n_rows, a.out / (16 * CB), lane, (int)blockIdx.x, t)) return;
     const int strip = t.ct / (8 / CB), b0 = t.ct % (8 / CB) * CB;
 
     f32x4 acc[RB][CB];
@@ -291,12 +321,14 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
         for (int w = 1; w < WAVES; ++w)
 #pragma unroll
             for (int b = 0; b < CB; ++b) f[b] += reinterpret_cast<const float *>(&red[w][i * CB + b][l])[e];
-        uint32_t *dst = reinterpret_cast<uint32_t *>(a.y + (int64_t)(t.row0 + r) * a.ldy + strip * 128 + (b0 >> 2) * 64 + 4 * (l & 15) + (b0 & 3));
+        uint16_t *const to = a.y + (int64_t)(t.row0 + r) * a.ldy + strip * 128 + (b0 >> 2) * 64 + 4 * (l & 15) + (b0 & 3);
+        [[maybe_unused]] uint32_t *const dst = reinterpret_cast<uint32_t *>(to);
         if constexpr (CB == 4)
             *reinterpret_cast<uint2 *>(dst) = uint2{pack_bf16_rne(f[0], f[1]), pack_bf16_rne(f[2], f[3])};
+        else if constexpr (CB == 2)
+            *dst = pack_bf16_rne(f[0], f[1]);
         else
-#pragma unroll
-            for (int b = 0; b < CB; b += 2) dst[b >> 1] = pack_bf16_rne(f[b], f[b + 1]);
+            *to = (uint16_t)pack_bf16_rne(f[0], 0.f);
     }
 }
 
@@ -614,13 +646,7 @@ __global__ __launch_bounds__(kWideThreads8, 1) void k_experts_wide(ExpertsArgs a
     __shared__ __attribute__((aligned(16))) char lds[kWideLds<F8, 4> > kWideLds<F8, 2> ? kWideLds<F8, 4> : kWideLds<F8, 2>];
     const int n_ct = (a.out + 255) >> 8;
     Tile t;
-    // Every XCD a run of the tiles: of 32, one on each of its compute units, 8 row tiles x 4 column tiles walk k together, and every chunk of x
-    // and W that one of them brings into the XCD's L2 serves four or eight of them.
-    if (!find_tile<256, 4>(a.starts, a.n_experts, a.n_rows, n_ct, threadIdx.x & 63, [&](int total) {
-            const int per_xcd = (total + 7) >> 3, idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-            return (int)(blockIdx.x >> 3) >= per_xcd || idx >= total ? -1 : idx;
-        }, t))
-        return;
+    if (!find_wide_tile(a.starts, a.n_experts, a.n_rows, n_ct, threadIdx.x & 63, (int)blockIdx.x, t)) return;
     if (t.rows > 128)
         wide_body<F8, 4>(a, t, lds);
     else
@@ -631,7 +657,7 @@ template <bool F8>
 static hipError_t launch_wide(const ExpertsArgs &a, hipStream_t stream)
 {
     const int64_t row_tiles = (int64_t)(a.n_rows + 255) / 256 + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
-    const int64_t grid = (row_tiles * ((a.out + 255) / 256) + 7) / 8 * 8;
+    const int64_t grid = (row_tiles * ((a.out + 255) / 256) + 7) / 8 * 8 + 8;  // (an eighth of either kind is rounded up)
     if (grid > INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL(k_experts_wide<F8>, dim3((unsigned)grid), dim3(kWideThreads8), 0, stream, a);
     return hipGetLastError();
@@ -655,11 +681,7 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kq = lane >> 4;
     Tile t;
-    if (!find_tile<R, 1>(a.starts, a.n_experts, a.n_rows, a.out / (64 * CB), lane, [&](int total) {
-            const int per_xcd = (total + 7) >> 3, idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-            return (int)(blockIdx.x >> 3) >= per_xcd || idx >= total ? -1 : idx;
-        }, t))
-        return;
+    if (!find_tile<R>(a.starts, a.n_experts, a.n_rows, a.out / (64 * CB), lane, (int)blockIdx.x, t)) return;
     // this wavefront's sub-blocks, of all in the row
     const int b_all = (t.ct * kMidWaves + wave) * CB, strip = b_all >> 3, b0 = b_all & 7;
     const int np = a.pieces;
@@ -817,8 +839,8 @@ static hipError_t launch_by_rows(const ExpertsArgs &a, hipStream_t stream)
 {
     const int met = a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0;
     const int per = met ? a.n_rows / met : a.n_rows;
-    auto fills = [&](int rows, int columns) {
-        return ((int64_t)(a.n_rows + rows - 1) / rows + met) * ((a.out + columns - 1) / columns) >= kComputeUnits;
+    auto fills = [&](int rows, int columns, int least = kComputeUnits) {
+        return ((int64_t)(a.n_rows + rows - 1) / rows + met) * ((a.out + columns - 1) / columns) >= least;
     };
     if (per > 48 && fills(256, 256)) return launch_wide<F8>(a, stream);
     if (per > 32 && a.out % 256 == 0 && fills(64, 256)) return launch_mid<F8, 4, 4, 2>(a, stream);
@@ -826,7 +848,10 @@ static hipError_t launch_by_rows(const ExpertsArgs &a, hipStream_t stream)
     if (per > 6 && fills(32, 128)) return launch_mid<F8, 2, 2, 2>(a, stream);
     if (per > 16 && fills(32, 64)) return launch_thin<F8, 2, 4, 2, 4>(a, stream);
     if (fills(16, 64)) return launch_thin<F8, 1, 4, 2, 4>(a, stream);
-    return launch_thin<F8, 1, 2, 2, 8>(a, stream);
+    // Less than a work group per compute unit: us of one row 4096 -> 4096 16 x 32 / 16 x 16 5.6 / 5.3, 8192 -> 1024 6.2 / 5.1, 16 rows 16384 -> 512 12.2 / 9.2;
+    // but 57 rows 3008 -> 1920, 240 tiles of 16 x 32, 5.4 / 6.4.
+    if (fills(16, 32, kComputeUnits * 3 / 4)) return launch_thin<F8, 1, 2, 2, 8>(a, stream);
+    return launch_thin<F8, 1, 1, 2, 8>(a, stream);
 }
 
 hipError_t launch_experts_linear(const ExpertsArgs &a, bool bits8, hipStream_t stream)
