@@ -21,6 +21,12 @@ namespace lora {
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
 static __device__ __forceinline__ uint4 ldb16(const char *p) { return *reinterpret_cast<const uint4 *>(p); }
+// past the caches, where ONCE says that nobody else wants it
+template <bool ONCE>
+static __device__ __forceinline__ uint4 ldw16(const char *p)
+{
+    return ONCE ? ld16_stream(reinterpret_cast<const uint16_t *>(p)) : ldb16(p);
+}
 
 static __device__ __forceinline__ i32x8 as_i32x8(uint4 lo, uint4 hi)
 {
@@ -186,7 +192,7 @@ constexpr int kThinSlab = WAVES * (16 * RB * 128 + (F8 ? 16 * RB * 4 : 0));
 template <bool F8, int RB, int CB, int WAVES>
 constexpr int kThinLds = kThinSlab<F8, RB, WAVES> > WAVES * RB * CB * 1024 ? kThinSlab<F8, RB, WAVES> : WAVES *RB *CB * 1024;
 
-template <bool F8, int RB, int CB, int D, int WAVES>
+template <bool F8, int RB, int CB, int D, int WAVES, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
 {
     constexpr int NX = 2 * RB;                        // x loads of a wavefront per piece: 8 rows each
@@ -248,7 +254,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int b = 0; b < CB; ++b) wq[d][h][b] = ldb16(wbase + at * (16384 * WAVES) + operand_at<F8>(h, b));
+                for (int b = 0; b < CB; ++b) wq[d][h][b] = ldw16<ONCE>(wbase + at * (16384 * WAVES) + operand_at<F8>(h, b));
         };
         auto stage = [&](int d) __attribute__((always_inline)) {
 #pragma unroll
@@ -332,13 +338,13 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
     }
 }
 
-template <bool F8, int RB, int CB, int D, int WAVES>
+template <bool F8, int RB, int CB, int D, int WAVES, bool ONCE = false>
 static hipError_t launch_thin(const ExpertsArgs &a, hipStream_t stream)
 {
     const int64_t row_tiles = (int64_t)(a.n_rows + 16 * RB - 1) / (16 * RB) + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
     const int64_t grid = (row_tiles * (a.out / (16 * CB)) + 7) / 8 * 8;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_experts_thin<F8, RB, CB, D, WAVES>), dim3((unsigned)grid), dim3(64 * WAVES), 0, stream, a);
+    hipLaunchKernelGGL((k_experts_thin<F8, RB, CB, D, WAVES, ONCE>), dim3((unsigned)grid), dim3(64 * WAVES), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -670,7 +676,7 @@ static hipError_t launch_wide(const ExpertsArgs &a, hipStream_t stream)
 // ------------------------------------------------------------------------------------------------
 constexpr int kMidWaves = 4;
 
-template <bool F8, int RB, int CB, int D>
+template <bool F8, int RB, int CB, int D, bool ONCE>
 __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a)
 {
     constexpr int R = 16 * RB, XBUF = R * kPieceBytes;
@@ -737,7 +743,7 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int b = 0; b < CB; ++b) wq[d][h][b] = ldb16(p + operand_at<F8>(h, b) + lane16);
+            for (int b = 0; b < CB; ++b) wq[d][h][b] = ldw16<ONCE>(p + operand_at<F8>(h, b) + lane16);
     };
     auto put_x = [&](int d, int slot) __attribute__((always_inline)) {
 #pragma unroll
@@ -817,13 +823,13 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
         }
 }
 
-template <bool F8, int RB, int CB, int D>
+template <bool F8, int RB, int CB, int D, bool ONCE = false>
 static hipError_t launch_mid(const ExpertsArgs &a, hipStream_t stream)
 {
     const int64_t row_tiles = (int64_t)(a.n_rows + 16 * RB - 1) / (16 * RB) + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
     const int64_t grid = (row_tiles * (a.out / (64 * CB)) + 7) / 8 * 8;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_experts_mid<F8, RB, CB, D>), dim3((unsigned)grid), dim3(64 * kMidWaves), 0, stream, a);
+    hipLaunchKernelGGL((k_experts_mid<F8, RB, CB, D, ONCE>), dim3((unsigned)grid), dim3(64 * kMidWaves), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -842,12 +848,19 @@ static hipError_t launch_by_rows(const ExpertsArgs &a, hipStream_t stream)
     auto fills = [&](int rows, int columns, int least = kComputeUnits) {
         return ((int64_t)(a.n_rows + rows - 1) / rows + met) * ((a.out + columns - 1) / columns) >= least;
     };
+    // Weights of more than half of what the chip's last cache holds are read past the caches where an expert has one tile of rows: they would leave
+    // there whatever else a layer keeps, and another pass would hardly find them.  us, through the caches / past them: 512 rows of 64 experts
+    // 2048 -> 1536 in bf16 72 / 64 (6.4 TB/s), 1024 78 / 69, 2048 81 / 72, in 8 bits 512 rows 40 / 36; 16 rows 16384 -> 16384 in 8 bits 50 / 44.  Smaller ones: one row
+    // 8192 -> 8192 (three such layers in turn, 201 MB) 11.9 / 15.5.
+    const bool large = (int64_t)(met ? met : 1) * a.out * a.pieces * kPieceBytes > ((int64_t)128 << 20);
+    auto once = [&](int rows) { return large && (met ? per <= rows * 3 / 4 : per <= rows); };
     if (per > 48 && fills(256, 256)) return launch_wide<F8>(a, stream);
     if (per > 32 && a.out % 256 == 0 && fills(64, 256)) return launch_mid<F8, 4, 4, 2>(a, stream);
-    if (per > 24 && fills(64, 128)) return launch_mid<F8, 4, 2, 2>(a, stream);
-    if (per > 6 && fills(32, 128)) return launch_mid<F8, 2, 2, 2>(a, stream);
-    if (per > 16 && fills(32, 64)) return launch_thin<F8, 2, 4, 2, 4>(a, stream);
-    if (fills(16, 64)) return launch_thin<F8, 1, 4, 2, 4>(a, stream);
+    if (per > 24 && fills(64, 128)) return once(64) ? launch_mid<F8, 4, 2, 2, true>(a, stream) : launch_mid<F8, 4, 2, 2>(a, stream);
+    if ((per > 6 || (large && met)) && fills(32, 128))
+        return once(32) ? launch_mid<F8, 2, 2, 2, true>(a, stream) : launch_mid<F8, 2, 2, 2>(a, stream);
+    if (per > 16 && fills(32, 64)) return once(32) ? launch_thin<F8, 2, 4, 2, 4, true>(a, stream) : launch_thin<F8, 2, 4, 2, 4>(a, stream);
+    if (fills(16, 64)) return once(16) ? launch_thin<F8, 1, 4, 2, 4, true>(a, stream) : launch_thin<F8, 1, 4, 2, 4>(a, stream);
     // Less than a work group per compute unit: us of one row 4096 -> 4096 16 x 32 / 16 x 16 5.6 / 5.3, 8192 -> 1024 6.2 / 5.1, 16 rows 16384 -> 512 12.2 / 9.2;
     // but 57 rows 3008 -> 1920, 240 tiles of 16 x 32, 5.4 / 6.4.
     if (fills(16, 32, kComputeUnits * 3 / 4)) return launch_thin<F8, 1, 2, 2, 8>(a, stream);
