@@ -40,6 +40,7 @@ struct ExpertsArgs {
     const char *w;           // packed
     const float *w_scales;   // 8 bits: [experts][out / 128][pieces]
     int pieces, out;
+    bool large;              // the weights that are met do not fit half of the chip's last cache (set by the launcher)
     uint16_t *y;
     int64_t ldy;
 };

@@ -61,6 +61,7 @@ static __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c)
 struct Tile {
     int expert, ct;
     int row0, rows;  // first place, places
+    bool only;       // the expert has no other rows (of wide tiles)
 };
 
 static __device__ __forceinline__ int wave_scan(int v, int lane)
@@ -168,6 +169,7 @@ static __device__ __forceinline__ bool find_wide_tile(const int32_t *__restrict_
     t.ct = grp * 4 + left - m * wide;
     t.row0 = r.first + row;
     t.rows = min(256, r.rows - row);
+    t.only = r.rows <= 256;
     return true;
 }
 
@@ -389,24 +391,31 @@ static __device__ __forceinline__ void dma16x1_to_lds(const void *g, uint32_t to
                  : "memory");
 }
 
-// N KB (2 or 4) from consecutive addresses, base (of the wavefront) + 16 lane, to consecutive LDS addresses.
-template <int N>
+// N KB (2 or 4) from consecutive addresses, base (of the wavefront) + 16 lane, to consecutive LDS addresses; ONCE: past the caches.
+template <int N, bool ONCE>
 static __device__ __forceinline__ void dma_kb_to_lds(const char *base, uint32_t lane16, uint32_t to)
 {
     uint32_t saved_m0;
-    if constexpr (N == 4)
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
-                     "global_load_lds_dwordx4 %1, %2 offset:1024\n\tglobal_load_lds_dwordx4 %1, %2 offset:2048\n\t"
-                     "global_load_lds_dwordx4 %1, %2 offset:3072\n\ts_mov_b32 m0, %0"
-                     : "=&s"(saved_m0)
-                     : "v"(lane16), "s"(base), "s"(to)
-                     : "memory");
+#define LORA_COPY(offset, how) "global_load_lds_dwordx4 %1, %2 offset:" #offset how "\n\t"
+#define LORA_COPIES_2(how) LORA_COPY(0, how) LORA_COPY(1024, how)
+#define LORA_COPIES_4(how) LORA_COPIES_2(how) LORA_COPY(2048, how) LORA_COPY(3072, how)
+#define LORA_COPY_ASM(copies)                                                                                                               \
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t" copies "s_mov_b32 m0, %0"                                          \
+                 : "=&s"(saved_m0)                                                                                                          \
+                 : "v"(lane16), "s"(base), "s"(to)                                                                                          \
+                 : "memory")
+    if constexpr (N == 4 && ONCE)
+        LORA_COPY_ASM(LORA_COPIES_4(" nt"));
+    else if constexpr (N == 4)
+        LORA_COPY_ASM(LORA_COPIES_4(""));
+    else if constexpr (ONCE)
+        LORA_COPY_ASM(LORA_COPIES_2(" nt"));
     else
-        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
-                     "global_load_lds_dwordx4 %1, %2 offset:1024\n\ts_mov_b32 m0, %0"
-                     : "=&s"(saved_m0)
-                     : "v"(lane16), "s"(base), "s"(to)
-                     : "memory");
+        LORA_COPY_ASM(LORA_COPIES_2(""));
+#undef LORA_COPY_ASM
+#undef LORA_COPIES_4
+#undef LORA_COPIES_2
+#undef LORA_COPY
 }
 
 // Sixteen tiles' values are computed by here: the compiler moves them neither up nor down.
@@ -416,7 +425,7 @@ static __device__ __forceinline__ void here(f32x4 (&v)[16])
                       "+v"(v[10]), "+v"(v[11]), "+v"(v[12]), "+v"(v[13]), "+v"(v[14]), "+v"(v[15]));
 }
 
-template <bool F8, int WR>
+template <bool F8, int WR, bool ONCE>
 static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Tile &t, char *lds)
 {
     constexpr int NB = 2 * WR;                     // sub-blocks of a wavefront
@@ -489,7 +498,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         for (int c = 0; c < 4; ++c) *reinterpret_cast<float *>(sbuf + 256 * c + 4 * lane) = v[c];
     };
     auto issue_w = [&]() __attribute__((always_inline)) {
-        dma_kb_to_lds<WC>(wsrc, lane16, w_to);
+        dma_kb_to_lds<WC, ONCE>(wsrc, lane16, w_to);
         wsrc += WHALF;
         w_to = w_to + WBUF >= w_end ? w_to - (kRing - 1) * WBUF : w_to + WBUF;
     };
@@ -653,10 +662,12 @@ __global__ __launch_bounds__(kWideThreads8, 1) void k_experts_wide(ExpertsArgs a
     const int n_ct = (a.out + 255) >> 8;
     Tile t;
     if (!find_wide_tile(a.starts, a.n_experts, a.n_rows, n_ct, threadIdx.x & 63, (int)blockIdx.x, t)) return;
+    // W past the caches where an expert has this one tile of rows and the weights are many (see launch_by_rows): us, 64 experts of 64 rows each,
+    // 2048 -> 1536, in bf16 90 / 83, in 8 bits 54.6 / 50.5
     if (t.rows > 128)
-        wide_body<F8, 4>(a, t, lds);
+        t.only && a.large ? wide_body<F8, 4, true>(a, t, lds) : wide_body<F8, 4, false>(a, t, lds);
     else
-        wide_body<F8, 2>(a, t, lds);
+        t.only && a.large ? wide_body<F8, 2, true>(a, t, lds) : wide_body<F8, 2, false>(a, t, lds);
 }
 
 template <bool F8>
@@ -841,7 +852,7 @@ static hipError_t launch_mid(const ExpertsArgs &a, hipStream_t stream)
 // / 193; 8192 -> 1024, 512 rows 97 / 60 / 36 / 22 / (15.0) / - / 26.8; 64 experts 2048 -> 1536, 8 rows each 49 / - / 47 / (39) / 44 / 41 / 54, 64 rows each (56) / 64 / 70 /
 // 66 / 81 / 91 / 169; in bf16 there 8 rows 81 / - / 77 / (76) / 73 / 74 / 76, 32 rows 85 / 84 / (79) / 88 / 91 / 105 / 130, 64 rows (90) / 98 / 102 / 109 / 115 / 153 / 200.
 template <bool F8>
-static hipError_t launch_by_rows(const ExpertsArgs &a, hipStream_t stream)
+static hipError_t launch_by_rows(ExpertsArgs a, hipStream_t stream)
 {
     const int met = a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0;
     const int per = met ? a.n_rows / met : a.n_rows;
@@ -852,7 +863,7 @@ static hipError_t launch_by_rows(const ExpertsArgs &a, hipStream_t stream)
     // there whatever else a layer keeps, and another pass would hardly find them.  us, through the caches / past them: 512 rows of 64 experts
     // 2048 -> 1536 in bf16 72 / 64 (6.4 TB/s), 1024 78 / 69, 2048 81 / 72, in 8 bits 512 rows 40 / 36; 16 rows 16384 -> 16384 in 8 bits 50 / 44.  Smaller ones: one row
     // 8192 -> 8192 (three such layers in turn, 201 MB) 11.9 / 15.5.
-    const bool large = (int64_t)(met ? met : 1) * a.out * a.pieces * kPieceBytes > ((int64_t)128 << 20);
+    const bool large = a.large = (int64_t)(met ? met : 1) * a.out * a.pieces * kPieceBytes > ((int64_t)128 << 20);
     auto once = [&](int rows) { return large && (met ? per <= rows * 3 / 4 : per <= rows); };
     if (per > 48 && fills(256, 256)) return launch_wide<F8>(a, stream);
     if (per > 32 && a.out % 256 == 0 && fills(64, 256)) return launch_mid<F8, 4, 4, 2>(a, stream);
