@@ -5,7 +5,7 @@
 names.  There is no fallback: if the library is missing or the GPU is absent, calls fail.
 ``workloads`` (seeded synthetic inputs) imports nothing from the binding.
 """
-__all__ = ["binding", "workloads", "build"]
+__all__ = ["binding", "workloads", "build", "expert_layer"]
 
 
 def __getattr__(name):

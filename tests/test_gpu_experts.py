@@ -497,3 +497,34 @@ def test_in_a_graph(tokens):
         layer.run()
         torch.cuda.synchronize()
         assert torch.equal(got, layer.z) and got.abs().sum() > 0
+
+
+# ---- the block of expert_layer.py ---------------------------------------------------------------------------
+def test_adapted_projection_and_layer_of_experts_together(capsys):
+    """Every step of both paths on 200 tokens.  What an 8-bit quantiser with a scale per 128 leaves of a normal value, 2^-4 / sqrt(12) of it or less in
+    the mean (half of a step of 2^-3 of the power of two below, uniform), is what separates them from 64 bits: once in the projection, twice in the
+    experts, whose product of two such rows counts it once more."""
+    from paper_2511_22880_amd import expert_layer
+    expert_layer.main()
+    errors = [float(line.rsplit(" ", 1)[1]) for line in capsys.readouterr().out.splitlines() if "relative error" in line]
+    step = 2.0 ** -3 / 12 ** 0.5  # rms of a rounding to 4 bits, of the value at worst
+    assert len(errors) == 2 and errors[0] < step and errors[1] < 2 * step
+
+
+def test_layer_of_experts_on_fewer_tokens_than_it_has_room_for():
+    from paper_2511_22880_amd import expert_layer as m
+    g = gen(31)
+    gate_up, gs = m.weights_to_8_bits(torch.randn(6, 512, 256, generator=g, device="cuda") * 0.05)
+    down, ds = m.weights_to_8_bits(torch.randn(6, 256, 256, generator=g, device="cuda") * 0.05)
+    layer = m.ExpertLayer(m.Packed(gate_up, gs), m.Packed(down, ds), 2, 64)
+    whole = []
+    for tokens in (64, 1, 17):
+        x = torch.randn(64, 256, generator=gen(5), device="cuda").to(BF)[:tokens]
+        ids = torch.randint(-1, 6, (64, 2), generator=gen(6), device="cuda", dtype=torch.int32)[:tokens]
+        w = torch.rand(64, 2, generator=gen(7), device="cuda")[:tokens]
+        z = torch.empty(tokens, 256, dtype=BF, device="cuda")
+        layer(x, ids, w, z)
+        ref = m.reference(x, ids, w, m._values(gate_up, gs), m._values(down, ds))
+        assert (z.double() - ref).norm() <= 2 * 2.0 ** -3 / 12 ** 0.5 * ref.norm()
+        whole.append(z)
+    assert torch.isfinite(whole[2]).all() and torch.isfinite(whole[1]).all()
