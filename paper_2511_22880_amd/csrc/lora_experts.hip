@@ -683,19 +683,27 @@ static hipError_t launch_wide(const ExpertsArgs &a, hipStream_t stream)
 // ------------------------------------------------------------------------------------------------
 // Tiles of up to 64 rows whose columns the wavefronts share out: 16 RB rows x 64 CB columns, four wavefronts of 16 CB columns each.  A wavefront's
 // weights come straight from memory in operand order, D pieces ahead, and no other wavefront wants them; x, which all four want, passes through
-// LDS, two slots of a piece, a barrier per piece.
+// LDS, two slots of a piece, a barrier per piece.  A compute unit with one such tile has a wavefront per SIMD, whose loads, LDS reads, products and sums
+// wait for each other, deeper prefetch or not; there KS = 2 such groups of wavefronts take the pieces in turn, and their sums meet in LDS.
 // ------------------------------------------------------------------------------------------------
 constexpr int kMidWaves = 4;
 
-template <bool F8, int RB, int CB, int D, bool ONCE>
-__global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a)
+template <bool F8, int RB, int CB, int D, int KS>
+constexpr int kMidLoopLds = KS * (2 * 16 * RB * kPieceBytes + (F8 ? kMidWaves * 16 * RB * 4 : 0));
+template <bool F8, int RB, int CB, int D, int KS>
+constexpr int kMidLds = KS == 2 && RB * CB * kMidWaves * 1024 > kMidLoopLds<F8, RB, CB, D, KS> ? RB *CB *kMidWaves * 1024 : kMidLoopLds<F8, RB, CB, D, KS>;
+
+template <bool F8, int RB, int CB, int D, int KS, bool ONCE>
+__global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsArgs a)
 {
     constexpr int R = 16 * RB, XBUF = R * kPieceBytes;
     constexpr int NX = RB > 2 ? RB / 2 : 1;  // x loads of a wavefront per piece
     constexpr int NS = (R + 63) / 64;        // .. of scales
     static_assert(D % 2 == 0, "slots of x by the place in the unrolled loop");
-    __shared__ __attribute__((aligned(16))) char lds[2 * XBUF + (F8 ? kMidWaves * R * 4 : 0)];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ __attribute__((aligned(16))) char all_lds[kMidLds<F8, RB, CB, D, KS>];
+    const int tid = threadIdx.x % (64 * kMidWaves), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ks = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / (64 * kMidWaves));  // pieces ks, ks + KS, ..
+    char *const lds = all_lds + ks * (kMidLoopLds<F8, RB, CB, D, KS> / KS);
     const int n = lane & 15, kq = lane >> 4;
     Tile t;
     if (!find_tile<R>(a.starts, a.n_experts, a.n_rows, a.out / (64 * CB), lane, (int)blockIdx.x, t)) return;
@@ -740,7 +748,7 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
     [[maybe_unused]] float sx[D][NS], sw[D];
     // Loads without branches (around one the compiler would wait for everything in flight): past the last piece, the last one again.
     auto load_x = [&](int s, int d) __attribute__((always_inline)) {
-        const int at = min(s, np - 1);
+        const int at = min(s * KS + ks, np - 1);
 #pragma unroll
         for (int q = 0; q < NX; ++q) xq[d][q] = *reinterpret_cast<const XLoad *>(xrow[q] + (int64_t)at * kPieceBytes);
         if constexpr (F8) {
@@ -750,7 +758,7 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
         }
     };
     auto load_w = [&](int s, int d) __attribute__((always_inline)) {
-        const char *p = wbase + (int64_t)min(s, np - 1) * 16384;
+        const char *p = wbase + (int64_t)min(s * KS + ks, np - 1) * 16384;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -773,7 +781,7 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
         load_w(d, d);
         __builtin_amdgcn_sched_barrier(0);
     }
-    for (int s0 = 0; s0 < np; s0 += D) {
+    for (int s0 = 0; s0 * KS < np; s0 += D) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
             const int slot = d & 1;
@@ -785,7 +793,7 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
             load_x(s0 + d + D, d);
             // what a slot held two pieces ago has been read by everyone: each came to the barrier of the piece between behind its reads
             barrier();
-            if (s0 + d < np) {
+            if ((s0 + d) * KS + ks < np) {
                 const char *xs = lds + slot * XBUF;
                 uint4 xo[2][RB];
 #pragma unroll
@@ -817,6 +825,22 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
         }
     }
 
+    if constexpr (KS == 2) {
+        __syncthreads();  // everyone has left the slots
+        f32x4(*const other)[64 * kMidWaves] = reinterpret_cast<f32x4(*)[64 * kMidWaves]>(all_lds);
+        if (ks == 1)
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int b = 0; b < CB; ++b) other[i * CB + b][tid] = acc[i][b];
+        __syncthreads();
+        if (ks == 1) return;
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int b = 0; b < CB; ++b) acc[i][b] += other[i * CB + b][tid];
+    }
+
     uint16_t *const y0 = a.y + (int64_t)t.row0 * a.ldy + strip * 128 + 64 * (b0 >> 2) + 4 * n + (b0 & 3);
 #pragma unroll
     for (int i = 0; i < RB; ++i)
@@ -834,47 +858,72 @@ __global__ __launch_bounds__(64 * kMidWaves, 1) void k_experts_mid(ExpertsArgs a
         }
 }
 
-template <bool F8, int RB, int CB, int D, bool ONCE = false>
+template <bool F8, int RB, int CB, int D, int KS = 1, bool ONCE = false>
 static hipError_t launch_mid(const ExpertsArgs &a, hipStream_t stream)
 {
     const int64_t row_tiles = (int64_t)(a.n_rows + 16 * RB - 1) / (16 * RB) + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
     const int64_t grid = (row_tiles * (a.out / (64 * CB)) + 7) / 8 * 8;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_experts_mid<F8, RB, CB, D, ONCE>), dim3((unsigned)grid), dim3(64 * kMidWaves), 0, stream, a);
+    hipLaunchKernelGGL((k_experts_mid<F8, RB, CB, D, KS, ONCE>), dim3((unsigned)grid), dim3(64 * kMidWaves * KS), 0, stream, a);
     return hipGetLastError();
 }
 
-// The tiles of a launch: the largest that still make a work group per compute unit, no higher than an expert's rows in the mean ask for.  Row tiles are
-// counted as if every expert's last one came on top (the host does not know who picked what).  us, 8 bits, 256 x 256 / 64 x 256 / 64 x 128 / 32 x 128 /
-// 32 x 64 / 16 x 64 / 16 x 32, the one taken in brackets: one layer of 4096 -> 4096, 32 rows 32 / 32 / 20 / 12.4 / 8.4 / 6.8 / (6.3), 64 rows 32 / 32 / 20 / 12.3 /
-// 8.7 / (7.1) / 9.2, 128 rows 32 / 32 / 20 / 12.5 / (9.2) / 11.2 / 14.8, 256 rows 51 / 32 / 20 / (12.7) / 14.4 / 18.8 / 25.6, 512 rows 51 / 32 / (20.6) / 20.6 / 24.0 /
-// 31.9 / 52, 1024 rows 52 / (32.4) / 30.1 / 38 / 49 / - / 107, 2048 rows 54 / (48) / 59 / 78 / 97 / - / 215; 16384 -> 16384, 128 rows 170 / 129 / (85) / 105 / 107 / 140
-// / 193; 8192 -> 1024, 512 rows 97 / 60 / 36 / 22 / (15.0) / - / 26.8; 64 experts 2048 -> 1536, 8 rows each 49 / - / 47 / (39) / 44 / 41 / 54, 64 rows each (56) / 64 / 70 /
-// 66 / 81 / 91 / 169; in bf16 there 8 rows 81 / - / 77 / (76) / 73 / 74 / 76, 32 rows 85 / 84 / (79) / 88 / 91 / 105 / 130, 64 rows (90) / 98 / 102 / 109 / 115 / 153 / 200.
+// The tiles of a launch: the largest of which there are enough to occupy most compute units, no higher than an expert's rows in the mean ask for.  Row
+// tiles are counted as if every expert's last one were half there (the host does not know who picked what).  With one tile of 64 x 256, 64 x 128 or 32 x 128 on a
+// compute unit two groups of wavefronts share its pieces (two), unless k is short; with more of them the tiles' own wavefronts are enough (one).
+// Device time in us, one layer in 8 bits:
+//   rows, layer        256 x 256   64 x 256, one / two   64 x 128, one / two   32 x 128, one / two   32 x 64   16 x 64   16 x 32   16 x 16
+//   1     4096 4096                                                                                            6.3       5.6       5.3
+//   64    4096 4096    36          32 / 25               21 / 17               12.6 / 12.5           8.9       7.3       9.2
+//   128   4096 4096    36          32 / 25               21 / 17               12.7 / 12.6           9.4       11.3      14.8
+//   256   4096 4096    52          33 / 25               21 / 17               13.4 / 13.1           15.0      19.1      26
+//   512   4096 4096    52          33 / 26               22 / 17.5             22 / 21               25        32        52
+//   1024  4096 4096    52          35 / 27               32 / 32               39 / 40               49        69        107
+//   2048  4096 4096    53          49 / 53               60 / 64               78 / 79               98        136       215
+//   64    16384 16384  131         132 / 122             90 / 86               75 / 66               70        90        117
+//   256   16384 16384  198         131 / 118             134 / 144             181 / 175             179       252       372
+//   115   5568 3584    48          42 / 32               27 / 21               16.3 / 15.5           11.6      13.8      17.4
+//   373   5440 640     68                                26 / 21               15.8 / 15.1           11.3      9.1       11.4
+//   1149  7232 512     93          54 / 41               33 / 27               20.3 / 19.4           24        24        33
+//   689   8128 14848   114         150 / 152             156 / 160             201 / 195             218       316       472
+//   10081 704 512      16.4        15.1 / 18.8           15.9 / 18.4           14.6 / 18.2           28        33        59
+//   7     3008 4352                                                                                            5.5       4.9       5.8
+// and of 64 experts 2048 -> 1536, rows each, in 8 bits: 8 49, - , 47, 39.9, 44, 41, 54; 64 54, 64, 71, 66, 82, 91, 170; in bf16: 8 81, - , 75, 75, 71, 73, 76;
+// 32 85, 86, 78, 90, 91, 104, 130; 64 90, 98, 102, 109, 115, 153, 200 (in the same order, one group of wavefronts, through the caches).
+// Over 60 random sizes of one layer the choice was 2.2 % from the best of all of these in the mean, over 60 of experts 5 % (where most picks have no
+// expert here, which the host does not know, up to twice the best).
 template <bool F8>
 static hipError_t launch_by_rows(ExpertsArgs a, hipStream_t stream)
 {
     const int met = a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0;
     const int per = met ? a.n_rows / met : a.n_rows;
-    auto fills = [&](int rows, int columns, int least = kComputeUnits) {
-        return ((int64_t)(a.n_rows + rows - 1) / rows + met) * ((a.out + columns - 1) / columns) >= least;
+    auto fills = [&](int rows, int columns, int least) {
+        const int64_t row_tiles = (int64_t)(a.n_rows + rows - 1) / rows + met / 2;
+        return (row_tiles > met ? row_tiles : met) * ((a.out + columns - 1) / columns) >= least;
     };
+    constexpr int kMost = kComputeUnits * 9 / 16;
     // Weights of more than half of what the chip's last cache holds are read past the caches where an expert has one tile of rows: they would leave
     // there whatever else a layer keeps, and another pass would hardly find them.  us, through the caches / past them: 512 rows of 64 experts
     // 2048 -> 1536 in bf16 72 / 64 (6.4 TB/s), 1024 78 / 69, 2048 81 / 72, in 8 bits 512 rows 40 / 36; 16 rows 16384 -> 16384 in 8 bits 50 / 44.  Smaller ones: one row
     // 8192 -> 8192 (three such layers in turn, 201 MB) 11.9 / 15.5.
     const bool large = a.large = (int64_t)(met ? met : 1) * a.out * a.pieces * kPieceBytes > ((int64_t)128 << 20);
     auto once = [&](int rows) { return large && (met ? per <= rows * 3 / 4 : per <= rows); };
-    if (per > 48 && fills(256, 256)) return launch_wide<F8>(a, stream);
-    if (per > 32 && a.out % 256 == 0 && fills(64, 256)) return launch_mid<F8, 4, 4, 2>(a, stream);
-    if (per > 24 && fills(64, 128)) return once(64) ? launch_mid<F8, 4, 2, 2, true>(a, stream) : launch_mid<F8, 4, 2, 2>(a, stream);
-    if ((per > 6 || (large && met)) && fills(32, 128))
-        return once(32) ? launch_mid<F8, 2, 2, 2, true>(a, stream) : launch_mid<F8, 2, 2, 2>(a, stream);
-    if (per > 16 && fills(32, 64)) return once(32) ? launch_thin<F8, 2, 4, 2, 4, true>(a, stream) : launch_thin<F8, 2, 4, 2, 4>(a, stream);
-    if (fills(16, 64)) return once(16) ? launch_thin<F8, 1, 4, 2, 4, true>(a, stream) : launch_thin<F8, 1, 4, 2, 4>(a, stream);
-    // Less than a work group per compute unit: us of one row 4096 -> 4096 16 x 32 / 16 x 16 5.6 / 5.3, 8192 -> 1024 6.2 / 5.1, 16 rows 16384 -> 512 12.2 / 9.2;
-    // but 57 rows 3008 -> 1920, 240 tiles of 16 x 32, 5.4 / 6.4.
-    if (fills(16, 32, kComputeUnits * 3 / 4)) return launch_thin<F8, 1, 2, 2, 8>(a, stream);
+    auto middle = [&](auto rb, auto cb) {
+        constexpr int RB = decltype(rb)::value, CB = decltype(cb)::value;
+        const bool two = a.pieces >= 16 && !fills(16 * RB, 64 * CB, 2 * kComputeUnits);
+        if constexpr (CB == 2)
+            if (once(16 * RB)) return two ? launch_mid<F8, RB, CB, 2, 2, true>(a, stream) : launch_mid<F8, RB, CB, 2, 1, true>(a, stream);
+        return two ? launch_mid<F8, RB, CB, 2, 2>(a, stream) : launch_mid<F8, RB, CB, 2, 1>(a, stream);
+    };
+    constexpr std::integral_constant<int, 2> two;
+    constexpr std::integral_constant<int, 4> four;
+    if (per > 48 && fills(256, 256, kMost)) return launch_wide<F8>(a, stream);
+    if (per > 32 && a.out % 256 == 0 && fills(64, 256, kMost)) return middle(four, four);
+    if (per > 24 && fills(64, 128, kMost)) return middle(four, two);
+    if ((per > 6 || (large && met)) && fills(32, 128, kMost)) return middle(two, two);
+    if (per > 16 && fills(32, 64, kMost)) return once(32) ? launch_thin<F8, 2, 4, 2, 4, true>(a, stream) : launch_thin<F8, 2, 4, 2, 4>(a, stream);
+    if (fills(16, 64, kMost)) return once(16) ? launch_thin<F8, 1, 4, 2, 4, true>(a, stream) : launch_thin<F8, 1, 4, 2, 4>(a, stream);
+    if (fills(16, 32, kMost)) return launch_thin<F8, 1, 2, 2, 8>(a, stream);
     return launch_thin<F8, 1, 1, 2, 8>(a, stream);
 }
 
