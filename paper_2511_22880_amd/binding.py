@@ -658,17 +658,13 @@ def _blocks(n: int) -> int:
     return (n + 127) >> 7
 
 
-# (These run several times in every call of a serving loop: what a tensor is asked for costs 0.1 us each.)
-def _rows(name: str, t, rows: int, columns: int, itemsize: int):
-    """(address, row stride) of a tensor of rows, whose elements lie side by side."""
-    try:
-        (r, c), (ld, step) = t.shape, t.stride()
-    except ValueError:
-        r = c = ld = step = -1
-    if r < rows or c < columns or (step != 1 and c > 1) or t.itemsize != itemsize:
+# What a tensor is asked for costs 0.1 us each time, and so does a call of Python's: the calls below, which a decode step waits for, ask for shape and
+# strides once, in line, and compare; where anything is unusual _usable looks closer.
+def _usable(name: str, t, rows: int, columns: int, itemsize: int) -> None:
+    """Refuses a tensor that does not hold so many rows of so many elements, side by side within a row."""
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < columns or t.itemsize != itemsize or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} with strides {t.stride()} does not do: {rows} rows of {columns} elements of {itemsize} "
                          "bytes side by side are meant")
-    return t.data_ptr(), ld if r > 1 else c  # (of a single row torch states any stride)
 
 
 def _whole(name: str, t, n: int, itemsize: int):
@@ -678,14 +674,36 @@ def _whole(name: str, t, n: int, itemsize: int):
     return t.data_ptr()
 
 
+def _two(t, name: str):
+    """Shape and strides of a tensor of rows."""
+    if t.dim() != 2:
+        raise ValueError(f"{name}: {tuple(t.shape)} does not do: rows are meant")
+    return t.shape, t.stride()
+
+
 def lora_rows_quantize(x, q, scales, stream=None) -> None:
     """x: bf16 [rows][in]; q: 8-bit [rows][128 * blocks]; scales: fp32 [rows][blocks]."""
-    rows, in_f = x.shape
+    try:
+        (rows, in_f), (ldx, x1) = x.shape, x.stride()
+        (qr, qc), (ldq, q1) = q.shape, q.stride()
+        (sr, sc), (lds, s1) = scales.shape, scales.stride()
+    except ValueError:
+        (rows, in_f), (ldx, x1), (qr, qc), (ldq, q1), (sr, sc), (lds, s1) = _two(x, "x") + _two(q, "q") + _two(scales, "scales")
     blocks = (in_f + 127) >> 7
-    px, ldx = _rows("x", x, 0, 0, 2)
-    pq, ldq = _rows("q", q, rows, blocks << 7, 1)
-    ps, lds = _rows("scales", scales, rows, blocks, 4)
-    status = (_lib or lib()).lora_rows_quantize(px, ldx, rows, in_f, pq, ldq, ps, lds, None if stream is None else _queue(stream))
+    if x1 != 1 or x.itemsize != 2:
+        _usable("x", x, rows, in_f, 2)
+    if qr < rows or qc < blocks << 7 or q1 != 1 or q.itemsize != 1:
+        _usable("q", q, rows, blocks << 7, 1)
+    if sr < rows or sc < blocks or s1 != 1 or scales.itemsize != 4:
+        _usable("scales", scales, rows, blocks, 4)
+    if rows == 1:  # (of a single row torch states any stride)
+        ldx = in_f
+    if qr == 1:
+        ldq = qc
+    if sr == 1:
+        lds = sc
+    status = (_lib or lib()).lora_rows_quantize(x.data_ptr(), ldx, rows, in_f, q.data_ptr(), ldq, scales.data_ptr(), lds,
+                                                None if stream is None else _queue(stream))
     if status:
         _check(status)
 
@@ -708,13 +726,27 @@ def lora_experts_pack_weight(w, dev_packed, stream=None, in_features: Optional[i
 
 def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
     """q, scales: of lora_rows_quantize; w_packed: uint8; w_scales: fp32 [out / 128][blocks]; y: bf16 [rows][out]."""
-    rows, in_f = q.shape
-    out_f, blocks = y.shape[1], (in_f + 127) >> 7
-    pq, ldq = _rows("q", q, 0, 0, 1)
-    ps, lds = _rows("scales", scales, rows, blocks, 4)
-    py, ldy = _rows("y", y, rows, out_f, 2)
-    status = (_lib or lib()).lora_linear_scaled(pq, ldq, ps, lds, rows, in_f, _whole("w_packed", w_packed, out_f * blocks << 7, 1),
-                                                _whole("w_scales", w_scales, (out_f >> 7) * blocks, 4), out_f, py, ldy,
+    try:
+        (rows, in_f), (ldq, q1) = q.shape, q.stride()
+        (sr, sc), (lds, s1) = scales.shape, scales.stride()
+        (yr, out_f), (ldy, y1) = y.shape, y.stride()
+    except ValueError:
+        (rows, in_f), (ldq, q1), (sr, sc), (lds, s1), (yr, out_f), (ldy, y1) = _two(q, "q") + _two(scales, "scales") + _two(y, "y")
+    blocks = (in_f + 127) >> 7
+    if q1 != 1 or q.itemsize != 1:
+        _usable("q", q, rows, in_f, 1)
+    if sr < rows or sc < blocks or s1 != 1 or scales.itemsize != 4:
+        _usable("scales", scales, rows, blocks, 4)
+    if yr < rows or y1 != 1 or y.itemsize != 2:
+        _usable("y", y, rows, out_f, 2)
+    if rows == 1:
+        ldq = in_f
+    if sr == 1:
+        lds = sc
+    if yr == 1:
+        ldy = out_f
+    status = (_lib or lib()).lora_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, rows, in_f, _whole("w_packed", w_packed, out_f * blocks << 7, 1),
+                                                _whole("w_scales", w_scales, (out_f >> 7) * blocks, 4), out_f, y.data_ptr(), ldy,
                                                 None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -728,42 +760,70 @@ def lora_experts_group_workspace_bytes(n_picks: int, n_experts: int) -> int:
 
 def lora_experts_group(ids, starts, order, place, workspace=None, stream=None) -> None:
     """ids: int32 [tokens][picks]; written: starts [experts + 1], order and place [tokens * picks], int32."""
-    tokens, picks = ids.shape
+    try:
+        (tokens, picks), (ldi, i1) = ids.shape, ids.stride()
+    except ValueError:
+        (tokens, picks), (ldi, i1) = _two(ids, "ids")
     n_experts, n = starts.numel() - 1, tokens * picks
-    pi, ldi = _rows("ids", ids, 0, 0, 4)
+    if i1 != 1 or ids.itemsize != 4:
+        _usable("ids", ids, tokens, picks, 4)
     pw, nw = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
-    status = (_lib or lib()).lora_experts_group(pi, ldi, tokens, picks, n_experts, _whole("starts", starts, 1, 4), _whole("order", order, n, 4),
-                                                _whole("place", place, n, 4), pw, nw, None if stream is None else _queue(stream))
+    status = (_lib or lib()).lora_experts_group(ids.data_ptr(), ldi if tokens > 1 else picks, tokens, picks, n_experts, _whole("starts", starts, 1, 4),
+                                                _whole("order", order, n, 4), _whole("place", place, n, 4), pw, nw,
+                                                None if stream is None else _queue(stream))
     if status:
         _check(status)
 
 
 def lora_experts_linear(x, starts, order, picks: int, w_packed, y, stream=None) -> None:
     """x: bf16 [tokens][in]; starts, order: of lora_experts_group (order None: x is in expert order); y: bf16 [tokens * picks][out]."""
-    tokens, in_f = x.shape
-    n_experts, out_f = starts.numel() - 1, y.shape[1]
-    n_rows = tokens if order is None else tokens * picks
-    px, ldx = _rows("x", x, 0, 0, 2)
-    py, ldy = _rows("y", y, n_rows, out_f, 2)
-    status = (_lib or lib()).lora_experts_linear(px, ldx, tokens, _whole("starts", starts, 1, 4), None if order is None else _whole("order", order, n_rows, 4),
-                                                 picks, n_rows, n_experts, in_f, _whole("w_packed", w_packed, n_experts * out_f * in_f << 1, 1), out_f,
-                                                 py, ldy, None if stream is None else _queue(stream))
+    try:
+        (tokens, in_f), (ldx, x1) = x.shape, x.stride()
+        (yr, out_f), (ldy, y1) = y.shape, y.stride()
+    except ValueError:
+        (tokens, in_f), (ldx, x1), (yr, out_f), (ldy, y1) = _two(x, "x") + _two(y, "y")
+    n_experts, n_rows = starts.numel() - 1, tokens if order is None else tokens * picks
+    if x1 != 1 or x.itemsize != 2:
+        _usable("x", x, tokens, in_f, 2)
+    if yr < n_rows or y1 != 1 or y.itemsize != 2:
+        _usable("y", y, n_rows, out_f, 2)
+    if tokens == 1:
+        ldx = in_f
+    if yr == 1:
+        ldy = out_f
+    status = (_lib or lib()).lora_experts_linear(x.data_ptr(), ldx, tokens, _whole("starts", starts, 1, 4),
+                                                 None if order is None else _whole("order", order, n_rows, 4), picks, n_rows, n_experts, in_f,
+                                                 _whole("w_packed", w_packed, n_experts * out_f * in_f << 1, 1), out_f, y.data_ptr(), ldy,
+                                                 None if stream is None else _queue(stream))
     if status:
         _check(status)
 
 
 def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w_scales, y, stream=None) -> None:
     """The same in 8 bits: q, scales of lora_rows_quantize, w_scales fp32 [experts][out / 128][blocks]."""
-    tokens, in_f = q.shape
-    n_experts, out_f, blocks = starts.numel() - 1, y.shape[1], (in_f + 127) >> 7
-    n_rows = tokens if order is None else tokens * picks
-    pq, ldq = _rows("q", q, 0, 0, 1)
-    ps, lds = _rows("scales", scales, tokens, blocks, 4)
-    py, ldy = _rows("y", y, n_rows, out_f, 2)
-    status = (_lib or lib()).lora_experts_linear_scaled(pq, ldq, ps, lds, tokens, _whole("starts", starts, 1, 4),
+    try:
+        (tokens, in_f), (ldq, q1) = q.shape, q.stride()
+        (sr, sc), (lds, s1) = scales.shape, scales.stride()
+        (yr, out_f), (ldy, y1) = y.shape, y.stride()
+    except ValueError:
+        (tokens, in_f), (ldq, q1), (sr, sc), (lds, s1), (yr, out_f), (ldy, y1) = _two(q, "q") + _two(scales, "scales") + _two(y, "y")
+    n_experts, n_rows, blocks = starts.numel() - 1, tokens if order is None else tokens * picks, (in_f + 127) >> 7
+    if q1 != 1 or q.itemsize != 1:
+        _usable("q", q, tokens, in_f, 1)
+    if sr < tokens or sc < blocks or s1 != 1 or scales.itemsize != 4:
+        _usable("scales", scales, tokens, blocks, 4)
+    if yr < n_rows or y1 != 1 or y.itemsize != 2:
+        _usable("y", y, n_rows, out_f, 2)
+    if tokens == 1:
+        ldq = in_f
+    if sr == 1:
+        lds = sc
+    if yr == 1:
+        ldy = out_f
+    status = (_lib or lib()).lora_experts_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, tokens, _whole("starts", starts, 1, 4),
                                                         None if order is None else _whole("order", order, n_rows, 4), picks, n_rows, n_experts, in_f,
                                                         _whole("w_packed", w_packed, n_experts * out_f * blocks << 7, 1),
-                                                        _whole("w_scales", w_scales, n_experts * (out_f >> 7) * blocks, 4), out_f, py, ldy,
+                                                        _whole("w_scales", w_scales, n_experts * (out_f >> 7) * blocks, 4), out_f, y.data_ptr(), ldy,
                                                         None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -771,11 +831,22 @@ def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w
 
 def lora_experts_combine(y, place, weights, z, stream=None) -> None:
     """y: bf16 [rows][out]; place, weights: int32 and fp32 [tokens][picks]; z: bf16 [tokens][out]."""
-    tokens, picks = weights.shape
-    out_f, n = z.shape[1], tokens * picks
-    py, ldy = _rows("y", y, 0, out_f, 2)
-    pz, ldz = _rows("z", z, tokens, out_f, 2)
-    status = (_lib or lib()).lora_experts_combine(py, ldy, y.shape[0], _whole("place", place, n, 4), _whole("weights", weights, n, 4), tokens, picks, out_f,
-                                                  pz, ldz, None if stream is None else _queue(stream))
+    try:
+        (yr, yc), (ldy, y1) = y.shape, y.stride()
+        (zr, out_f), (ldz, z1) = z.shape, z.stride()
+        tokens, picks = weights.shape
+    except ValueError:
+        (yr, yc), (ldy, y1), (zr, out_f), (ldz, z1), (tokens, picks), _ = _two(y, "y") + _two(z, "z") + _two(weights, "weights")
+    n = tokens * picks
+    if yc < out_f or y1 != 1 or y.itemsize != 2:
+        _usable("y", y, 0, out_f, 2)
+    if zr < tokens or z1 != 1 or z.itemsize != 2:
+        _usable("z", z, tokens, out_f, 2)
+    if yr == 1:
+        ldy = yc
+    if zr == 1:
+        ldz = out_f
+    status = (_lib or lib()).lora_experts_combine(y.data_ptr(), ldy, yr, _whole("place", place, n, 4), _whole("weights", weights, n, 4), tokens, picks, out_f,
+                                                  z.data_ptr(), ldz, None if stream is None else _queue(stream))
     if status:
         _check(status)
