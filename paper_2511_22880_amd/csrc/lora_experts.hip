@@ -368,6 +368,9 @@ static hipError_t launch_thin(const ExpertsArgs &a, hipStream_t stream)
 // ------------------------------------------------------------------------------------------------
 constexpr int kWideThreads8 = 512;
 constexpr int kRing = 3;
+// Products between one and its sum.  A phase's last ones leave theirs to the reading phase behind it, where the other wavefront multiplies: us with all of them
+// in the phase itself / 1, 2, 3, 4 behind it, 8192 tokens 8192 -> 8192 496 / 488, 491, 500, 488, 32 of 256 x 256 tiles 96.6 / 92.9, 95.8, 97, 94.
+constexpr int kLag = 1;
 template <bool F8, int WR>
 constexpr int kWideLds = kRing * (64 * WR * kPieceBytes + (WR == 4 ? 16384 : 32768)) + (F8 ? 8 * 2048 : 0);
 
@@ -418,13 +421,13 @@ static __device__ __forceinline__ void dma_kb_to_lds(const char *base, uint32_t 
 #undef LORA_COPY
 }
 
-// Sixteen tiles' values are computed by here: the compiler moves them neither up nor down.
-static __device__ __forceinline__ void here(f32x4 (&v)[16])
+// The tiles' values are computed by here: the compiler moves them neither up nor down.
+template <int N>
+static __device__ __forceinline__ void here(f32x4 (&v)[N])
 {
-    asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]), "+v"(v[8]), "+v"(v[9]),
-                      "+v"(v[10]), "+v"(v[11]), "+v"(v[12]), "+v"(v[13]), "+v"(v[14]), "+v"(v[15]));
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
-
 template <bool F8, int WR, bool ONCE>
 static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Tile &t, char *lds)
 {
@@ -559,6 +562,19 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
             for (int h = 0; h < 2; ++h) xo[h][i] = x_at(i, h);
     }
     if (wave >= 4) phase_end();  // the second strip's wavefronts run one phase behind the first's
+    // 8 bits: product k of a step (rows k / 4, sub-block k mod 4 of it) and the sums kLag products behind it
+    [[maybe_unused]] f32x4 part[kLag + 1];
+    if constexpr (F8) {
+#pragma unroll
+        for (int k = 0; k <= kLag; ++k) part[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto add = [&](int q, int k) __attribute__((always_inline)) {
+        f32x4 &to = acc[q][4 * (k & 3) + (k >> 2)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[e] = fmaf(sc[k >> 2][e], part[k % (kLag + 1)][e], to[e]);
+    };
     // step q of piece P, behind which come two pieces or more (AFTER = 2), one or none
     auto step = [&](int P, auto qc, auto afterc) __attribute__((always_inline)) {
         constexpr int q = decltype(qc)::value, AFTER = decltype(afterc)::value;
@@ -577,6 +593,14 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
                 const int at = WR == 4 ? (F8 ? h * 4096 : 0) + b * 1024 : operand_at<F8>(h, 4 * half + b);
                 wo[h][b] = *reinterpret_cast<const uint4 *>(wring + wget + wlane + at);
             }
+        if constexpr (F8) {  // the sums that the products before did not wait for
+            __builtin_amdgcn_sched_barrier(0);
+            constexpr int before = (q + SP - 1) % SP;
+#pragma unroll
+            for (int k = 16 - kLag; k < 16; ++k) add(before, k);
+            here(acc[before]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         if constexpr (F8 && q == 0) {
             const float w = wscale[P];
 #pragma unroll
@@ -596,26 +620,20 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         phase_end();
         if constexpr (q == SP - 1) xget = xget == (kRing - 1) * XBUF ? 0 : xget + XBUF;
         if constexpr (F8) {
-            // the product k, and the sum of the one two before it
-            f32x4 part[3];
 #pragma unroll
-            for (int k = 0; k < 18; ++k) {
-                if (k < 16) part[k % 3] = mfma_e4m3(as_i32x8(xo[0][k >> 2], xo[XH - 1][k >> 2]), as_i32x8(wo[0][k & 3], wo[WH - 1][k & 3]), f32x4{0.f, 0.f, 0.f, 0.f});
+            for (int k = 0; k < 16; ++k) {
+                part[k % (kLag + 1)] = mfma_e4m3(as_i32x8(xo[0][k >> 2], xo[XH - 1][k >> 2]), as_i32x8(wo[0][k & 3], wo[WH - 1][k & 3]), f32x4{0.f, 0.f, 0.f, 0.f});
                 __builtin_amdgcn_sched_barrier(0);
-                if (k >= 2) {
-                    const int j = k - 2;
-                    f32x4 &to = acc[q][4 * (j & 3) + (j >> 2)];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) to[e] = fmaf(sc[j >> 2][e], part[j % 3][e], to[e]);
-                }
+                if (k >= kLag) add(q, k - kLag);
                 // these rows of x have been multiplied: the next piece's.  All of it has landed: W of this step, requested behind it, has been waited
                 // for by every wavefront.
                 if constexpr (kEarlyX && q == SP - 1 && AFTER >= 1)
-                    if (k < 16 && (k & 3) == 3)
+                    if ((k & 3) == 3)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) xo[h][k >> 2] = x_at(k >> 2, h);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            here(part);
             here(acc[q]);
         } else {
 #pragma unroll
@@ -638,6 +656,9 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     for (int P = 0; P + 2 < np; ++P) piece(P, std::integral_constant<int, 2>{});
     if (np > 1) piece(np - 2, std::integral_constant<int, 1>{});
     piece(np - 1, std::integral_constant<int, 0>{});
+    if constexpr (F8)
+#pragma unroll
+        for (int k = 16 - kLag; k < 16; ++k) add(SP - 1, k);
     if (wave < 4) phase_end();
     if (!has_strip) return;
 
