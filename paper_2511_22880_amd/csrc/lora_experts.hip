@@ -440,8 +440,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     const int rw = WR == 4 ? wave & 3 : wave & 1;  // rows 64 rw .. of the tile
     const int half = WR == 4 ? 0 : (wave >> 1) & 1;
     const int strip = 2 * t.ct + (wave >> 2);
-    // The last tile of a row of y may hold one strip: the wavefronts without one take part in everything up to the epilogue, so that
-    // copies and barriers count alike, and multiply strip 0's W for nothing.
+    // The last tile of a row of y may hold one strip: the wavefronts without one copy strip 0's W for nothing.
     const bool has_strip = strip * 128 < a.out;
     const int np = a.pieces, steps = np * SP;
 
@@ -542,6 +541,39 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     }
     phase_end();
 
+    // The copies of step q of a piece behind which come two pieces or more (AFTER = 2), one or none, and the wait for W of the next step and, where that
+    // begins a piece, x of it: behind them were requested W of the step after and x of the piece after.
+    auto request = [&](auto qc, auto afterc) __attribute__((always_inline)) {
+        constexpr int q = decltype(qc)::value, AFTER = decltype(afterc)::value;
+        if constexpr (SP == 2 ? AFTER >= 1 : AFTER == 2) issue_w();
+        if constexpr (q == 0 && AFTER == 2) issue_x();
+    };
+    auto await = [&](auto afterc) __attribute__((always_inline)) {
+        constexpr int AFTER = decltype(afterc)::value;
+        wait_vm<AFTER == 2 ? XC + WC : SP == 2 && AFTER == 1 ? WC : 0>();
+    };
+    auto pieces = [&](auto step) __attribute__((always_inline)) {
+        auto piece = [&](int P, auto after) __attribute__((always_inline)) {
+            step(P, std::integral_constant<int, 0>{}, after);
+            if constexpr (SP == 2) step(P, std::integral_constant<int, 1>{}, after);
+        };
+        for (int P = 0; P + 2 < np; ++P) piece(P, std::integral_constant<int, 2>{});
+        if (np > 1) piece(np - 2, std::integral_constant<int, 1>{});
+        piece(np - 1, std::integral_constant<int, 0>{});
+    };
+    // a wavefront without rows or columns: its part of the copies, and the others' phases
+    if (t.rows <= 64 * rw || !has_strip) {
+        if (wave >= 4) phase_end();
+        pieces([&](int, auto q, auto after) __attribute__((always_inline)) {
+            request(q, after);
+            await(after);
+            phase_end();
+            phase_end();
+        });
+        if (wave < 4) phase_end();
+        return;
+    }
+
     constexpr int XH = WR == 4 && !F8 ? 1 : 2;  // halves of x's rows in registers at a time
     constexpr int WB = WR == 4 && !F8 ? 8 : 4, WH = WR == 4 && !F8 ? 1 : 2;  // .. sub-blocks and halves of W
     uint4 xo[XH][4], wo[WH][WB];
@@ -575,12 +607,9 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[e] = fmaf(sc[k >> 2][e], part[k % (kLag + 1)][e], to[e]);
     };
-    // step q of piece P, behind which come two pieces or more (AFTER = 2), one or none
-    auto step = [&](int P, auto qc, auto afterc) __attribute__((always_inline)) {
+    pieces([&](int P, auto qc, auto afterc) __attribute__((always_inline)) {
         constexpr int q = decltype(qc)::value, AFTER = decltype(afterc)::value;
-        constexpr bool kMoreW = SP == 2 ? AFTER >= 1 : AFTER == 2;  // there is a step after the next
-        if constexpr (kMoreW) issue_w();
-        if constexpr (q == 0 && AFTER == 2) issue_x();
+        request(qc, afterc);
         if constexpr (!kEarlyX && (XH == 1 || q == 0))
 #pragma unroll
             for (int h = 0; h < XH; ++h)
@@ -610,9 +639,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         if constexpr (F8 && q == SP - 1)
             if ((P & 3) == 3 && P + 1 < np) order_scales();
         __builtin_amdgcn_sched_barrier(0);
-        // W of the next step and, where that begins one, x of the next piece have landed: behind them were requested
-        // W of the step after and x of the piece after
-        wait_vm<AFTER == 2 ? XC + WC : kMoreW ? WC : 0>();
+        await(afterc);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what was read is in registers: the slots may be written
         // (requested four pieces before their use: long landed by the time that the waits above let a wavefront come there)
         if constexpr (F8 && q == SP - 1)
@@ -648,19 +675,11 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         }
         phase_end();
         wget = wget == (kRing - 1) * WBUF ? 0 : wget + WBUF;
-    };
-    auto piece = [&](int P, auto after) __attribute__((always_inline)) {
-        step(P, std::integral_constant<int, 0>{}, after);
-        if constexpr (SP == 2) step(P, std::integral_constant<int, 1>{}, after);
-    };
-    for (int P = 0; P + 2 < np; ++P) piece(P, std::integral_constant<int, 2>{});
-    if (np > 1) piece(np - 2, std::integral_constant<int, 1>{});
-    piece(np - 1, std::integral_constant<int, 0>{});
+    });
     if constexpr (F8)
 #pragma unroll
         for (int k = 16 - kLag; k < 16; ++k) add(SP - 1, k);
     if (wave < 4) phase_end();
-    if (!has_strip) return;
 
     uint16_t *const y0 = a.y + (int64_t)(t.row0 + 64 * rw) * a.ldy + strip * 128 + 64 * half + 4 * n;
 #pragma unroll
