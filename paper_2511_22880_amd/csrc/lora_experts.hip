@@ -47,7 +47,9 @@ static __device__ __forceinline__ void in_order()
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
-// 16 x 16 products over 128 8-bit values of k (both operands E4M3, the instruction's own scales at 1)
+// 16 x 16 products over 128 8-bit values of k (both operands E4M3, the instruction's own scales at 1).  The instruction drops what lies 2^-17 below the
+// largest of an element's 128 products (all in all up to 2^-10 of that product was seen), and the ones for 32 values of k do the same: there is none more exact.
+// A block's sum is fp32 from there on.
 static __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c)
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
@@ -61,7 +63,8 @@ static __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c)
 struct Tile {
     int expert, ct;
     int row0, rows;  // first place, places
-    bool only;       // the expert has no other rows (of wide tiles)
+    bool only;       // of wide tiles: the expert has no other rows
+    bool four;       // .. those of up to 128 rows have four strips of columns, not two
 };
 
 static __device__ __forceinline__ int wave_scan(int v, int lane)
@@ -136,6 +139,20 @@ static __device__ __forceinline__ bool find_tile(const int32_t *__restrict__ sta
     return true;
 }
 
+// A tile of up to 128 rows has two strips of 128 columns, or four.  With two it takes 5/8 as long as a whole one (8 bits, k 4096: 37 - 43 us and 65; its
+// wavefronts have 64 x 64 of it and wait for LDS), with four, where they have 64 x 128, little longer than that (63 - 71).  So: four where all tiles
+// are then through earlier, in eighths of a whole one, by the count of tiles; where the compute units that whole ones leave have room for all of two strips, two.
+// us, always two / always four / so: 6000 rows of 64 experts 4096 -> 2048 in 8 bits 131 / - / 106, 32 experts' 6000 of uneven numbers 100 / - / 89;
+// 2560 rows of 32 3456 -> 1664 40.6 / 55.1 / 41.8, 2688 of 32 4352 -> 6272 207 / 172 / 178; over 36 random sizes of experts 4 %, 3 % and 2 % from the
+// better of the first two.
+static __device__ __forceinline__ bool four_strips(int whole, int n_rest, int n_ct)
+{
+    const int rest = n_rest * n_ct, rest4 = n_rest * ((n_ct + 1) >> 1), rounds = whole / kComputeUnits, left = whole - rounds * kComputeUnits;
+    const int room = kComputeUnits - left;
+    if (rest <= room) return false;
+    return 8 * ((whole + rest4 + kComputeUnits - 1) / kComputeUnits) < max(8 * rounds + 10, (8 * whole + 5 * rest) / kComputeUnits + 3);
+}
+
 // The same for tiles of 256 rows x 256 columns, an expert's last one of up to 128 rows apart: the whole ones come first, and the others, which take about
 // half as long, fill the compute units that the last round of those leaves idle.  Inside an expert column tiles in groups of four, in a group row tile by row tile:
 // of 32 tiles in a run, one on each of an XCD's compute units, 8 row tiles x 4 column tiles walk k together, and every chunk of x and W that
@@ -155,9 +172,11 @@ static __device__ __forceinline__ bool find_wide_tile(const int32_t *__restrict_
         n_whole = wave_sum(a);
         n_rest = wave_sum(b);
     }
-    const int xcd = blk & 7, per_whole = (n_whole * n_ct + 7) >> 3, per_rest = (n_rest * n_ct + 7) >> 3;
+    t.four = four_strips(n_whole * n_ct, n_rest, n_ct);
+    const int xcd = blk & 7, per_whole = (n_whole * n_ct + 7) >> 3;
     const bool is_rest = (blk >> 3) >= per_whole;
-    const int j = (blk >> 3) - (is_rest ? per_whole : 0), per = is_rest ? per_rest : per_whole, idx = xcd * per + j;
+    if (is_rest && t.four) n_ct = (n_ct + 1) >> 1;
+    const int j = (blk >> 3) - (is_rest ? per_whole : 0), per = is_rest ? (n_rest * n_ct + 7) >> 3 : per_whole, idx = xcd * per + j;
     if (j >= per || idx >= (is_rest ? n_rest : n_whole) * n_ct) return false;
     const int q = idx / n_ct;
     const RowTile r = !starts   ? RowTile{0, is_rest ? 0 : q, is_rest ? n_rest : n_whole, 0, n_rows}
@@ -351,28 +370,32 @@ static hipError_t launch_thin(const ExpertsArgs &a, hipStream_t stream)
 }
 
 // ------------------------------------------------------------------------------------------------
-// Tiles of many rows: 64 WR rows (256, or 128 where an expert's last tile has no more) x 256 columns, 8 wavefronts.  Wavefronts 0 .. 3 have the first
-// strip of 128 columns, 4 .. 7 the second; of a strip a wavefront has 64 rows x 128 columns (WR = 4), or 64 x 64 (WR = 2).
+// Tiles of many rows: 64 WR rows (256, or 128 where an expert's last tile has no more) x NS strips of 128 columns (2; 4 of few rows: see four_strips),
+// 8 wavefronts.  Wavefronts 0 .. 3 have the first half of the strips, 4 .. 7 the second; a wavefront has 64 rows x 128 columns of one, or, where
+// 128 rows x 2 strips leave it no more, 64 x 64.
 //   * x and W come by loads that write LDS directly, x in slots of one piece (128 bytes of k), W in slots of a step: half a piece, the half that
-//     the packed order says (WR = 4), or a piece (WR = 2).  Three slots each: a step requests W of the step after the next, and the first step of a
+//     the packed order says, or a piece (64 x 64).  Three slots each: a step requests W of the step after the next, and the first step of a
 //     piece x of the piece after the next.  x is gathered by the copy itself, whole cache lines of 8 rows; inside a 1 KB block of 8 rows chunk p of row r
 //     sits in slot 8 r + (p XOR r), so that the lanes that read one chunk of 8 rows meet 8 bank groups.
 //   * A step is a phase that requests copies and reads the step's operands from LDS, and a phase that multiplies (512 cycles of the matrix unit), with a
-//     barrier behind each and the second strip's wavefronts one phase behind: of the two wavefronts of a SIMD one multiplies while the other reads.
+//     barrier behind each and the second half's wavefronts one phase behind: of the two wavefronts of a SIMD one multiplies while the other reads.
 //     No request passes through registers the compiler tracks, so the waits count exactly what is under way.
 //   * In 8 bits a product spans a whole block of 128: its sum starts at zero, and 4 fp32 FMAs with x's scale times W's add it to the accumulators
 //     while the next ones run (half as long as the matrix unit takes).  A wavefront copies the scales of its own 64 rows, of four pieces at a
 //     time: every row's lie in cache lines of their own, and one copy a piece took as long as half of the others together (8192 tokens
 //     8192 -> 8192: copies alone 418 us with one a piece, 304 without any).  Rows of x enter registers while the piece before is multiplied
-//     (WR = 4): a piece's first reading phase had 20 of its 28 operands, and lasted longer than the products beside it.
+//     (64 x 128): a piece's first reading phase had 20 of its 28 operands, and lasted longer than the products beside it.
+//   * What bounds it is the chip's power: 8192 tokens 8192 -> 8192 in 8 bits take 474 us (2.32 PFLOP/s) at 1.95 of 2.4 GHz, and the parts add up like
+//     energies, not like times: products and LDS reads alone 278 (products from registers alone run at 4.05 PFLOP/s, 271 us), copies 105 more, the fp32
+//     sums 110 more, in phases or without, copies requested two steps ahead or four.  In bf16 8002 rows of 8 experts 4096 -> 14336 take 755 us
+//     (1.25 PFLOP/s; a library's product of their size 750, products from registers alone 1.90 PFLOP/s).
 // ------------------------------------------------------------------------------------------------
 constexpr int kWideThreads8 = 512;
 constexpr int kRing = 3;
 // Products between one and its sum.  A phase's last ones leave theirs to the reading phase behind it, where the other wavefront multiplies: us with all of them
 // in the phase itself / 1, 2, 3, 4 behind it, 8192 tokens 8192 -> 8192 496 / 488, 491, 500, 488, 32 of 256 x 256 tiles 96.6 / 92.9, 95.8, 97, 94.
 constexpr int kLag = 1;
-template <bool F8, int WR>
-constexpr int kWideLds = kRing * (64 * WR * kPieceBytes + (WR == 4 ? 16384 : 32768)) + (F8 ? 8 * 2048 : 0);
+constexpr int kWideLds = kRing * 49152 + 8 * 2048;  // (of whichever form, in 8 bits)
 
 // One dword a lane straight to LDS: lane l's at `to` + 4 l.
 static __device__ __forceinline__ void dma4_to_lds(const void *g, uint32_t to)
@@ -428,18 +451,20 @@ static __device__ __forceinline__ void here(f32x4 (&v)[N])
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
-template <bool F8, int WR, bool ONCE>
+template <bool F8, int WR, int NS, bool ONCE>
 static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Tile &t, char *lds)
 {
-    constexpr int NB = 2 * WR;                     // sub-blocks of a wavefront
-    constexpr int SP = WR == 4 ? 2 : 1;            // steps of a piece
-    constexpr int XBUF = 64 * WR * kPieceBytes, WHALF = 16384 / SP, WBUF = 2 * WHALF;
-    constexpr int XC = WR, WC = 4 / SP;            // copies of a wavefront: x of a piece, W of a step
+    constexpr int WS = 8 / NS;                     // wavefronts of a strip
+    constexpr bool FULL = WS == WR;                // .. which have all of its columns, or half of them
+    constexpr int NB = FULL ? 8 : 4;               // sub-blocks of a wavefront
+    constexpr int SP = FULL ? 2 : 1;               // steps of a piece
+    constexpr int XBUF = 64 * WR * kPieceBytes, WPART = 16384 / SP, WBUF = NS * WPART;
+    constexpr int XC = WR, WC = WPART / 1024 / WS; // copies of a wavefront: x of a piece, W of a step
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, kq = lane >> 4;
-    const int rw = WR == 4 ? wave & 3 : wave & 1;  // rows 64 rw .. of the tile
-    const int half = WR == 4 ? 0 : (wave >> 1) & 1;
-    const int strip = 2 * t.ct + (wave >> 2);
+    const int rw = wave % WR;                      // rows 64 rw .. of the tile
+    const int half = FULL ? 0 : (wave >> 1) & 1;
+    const int strip = NS * t.ct + wave / WS;
     // The last tile of a row of y may hold one strip: the wavefronts without one copy strip 0's W for nothing.
     const bool has_strip = strip * 128 < a.out;
     const int np = a.pieces, steps = np * SP;
@@ -458,7 +483,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     const uint64_t there = __ballot(my_row < t.rows && my_tok >= 0);  // rows of this wavefront that are written
     [[maybe_unused]] const uint32_t soff = F8 ? (uint32_t)((uint64_t)max(my_tok, 0) * (uint64_t)a.ld_scales) : 0u;
     const int64_t es = (int64_t)t.expert * (a.out >> 7) + (has_strip ? strip : 0);
-    const char *wsrc = a.w + es * np * 16384 + (wave & 3) * (WC * 1024);
+    const char *wsrc = a.w + es * np * 16384 + (wave % WS) * (WC * 1024);
     const char *xp = a.x;            // the next piece of every row
     const uint32_t lane16 = lane * 16;
     // (the scalar cache's path: a vector load would be counted among the copies)
@@ -467,7 +492,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
 
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)lds);
     const uint32_t x_end = lds0 + kRing * XBUF, w_end = x_end + kRing * WBUF;
-    uint32_t x_to = lds0 + WR * wave * 1024, w_to = x_end + (wave >> 2) * WHALF + (wave & 3) * (WC * 1024);
+    uint32_t x_to = lds0 + WR * wave * 1024, w_to = x_end + wave / WS * WPART + wave % WS * (WC * 1024);
     auto issue_x = [&]() __attribute__((always_inline)) {
         auto at = [&](int j) { return xp + (uint64_t)xoff[j] * 16 - 1024 * j; };  // as the copies take it
         if constexpr (WR == 4)
@@ -501,7 +526,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     };
     auto issue_w = [&]() __attribute__((always_inline)) {
         dma_kb_to_lds<WC, ONCE>(wsrc, lane16, w_to);
-        wsrc += WHALF;
+        wsrc += WPART;
         w_to = w_to + WBUF >= w_end ? w_to - (kRing - 1) * WBUF : w_to + WBUF;
     };
 
@@ -574,26 +599,26 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         return;
     }
 
-    constexpr int XH = WR == 4 && !F8 ? 1 : 2;  // halves of x's rows in registers at a time
-    constexpr int WB = WR == 4 && !F8 ? 8 : 4, WH = WR == 4 && !F8 ? 1 : 2;  // .. sub-blocks and halves of W
+    constexpr int XH = FULL && !F8 ? 1 : 2;  // halves of x's rows in registers at a time
+    constexpr int WB = FULL && !F8 ? 8 : 4, WH = FULL && !F8 ? 1 : 2;  // .. sub-blocks and halves of W
     uint4 xo[XH][4], wo[WH][WB];
     [[maybe_unused]] f32x4 sc[4];
     int xget = 0, wget = 0;
     [[maybe_unused]] int sget = 0;
     const int xlane = (8 * rw + (n >> 3)) * 1024 + (n & 7) * 128;
-    const int wlane = (wave >> 2) * WHALF + lane * 16;
+    const int wlane = wave / WS * WPART + lane * 16;
     // row 16 i + n of this wavefront's: block 8 rw + 2 i + n / 8, row n mod 8 of it
     auto x_at = [&](int i, int h) __attribute__((always_inline)) {
         return *reinterpret_cast<const uint4 *>(xring + xget + xlane + 2048 * i + (((4 * h + kq) ^ (n & 7)) * 16));
     };
-    constexpr bool kEarlyX = F8 && WR == 4;  // rows of x are read while the piece before is multiplied
+    constexpr bool kEarlyX = F8 && FULL;  // rows of x are read while the piece before is multiplied
     if constexpr (kEarlyX) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) xo[h][i] = x_at(i, h);
     }
-    if (wave >= 4) phase_end();  // the second strip's wavefronts run one phase behind the first's
+    if (wave >= 4) phase_end();  // the second half's wavefronts run one phase behind the first's
     // 8 bits: product k of a step (rows k / 4, sub-block k mod 4 of it) and the sums kLag products behind it
     [[maybe_unused]] f32x4 part[kLag + 1];
     if constexpr (F8) {
@@ -619,7 +644,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         for (int h = 0; h < WH; ++h)
 #pragma unroll
             for (int b = 0; b < WB; ++b) {
-                const int at = WR == 4 ? (F8 ? h * 4096 : 0) + b * 1024 : operand_at<F8>(h, 4 * half + b);
+                const int at = FULL ? (F8 ? h * 4096 : 0) + b * 1024 : operand_at<F8>(h, 4 * half + b);
                 wo[h][b] = *reinterpret_cast<const uint4 *>(wring + wget + wlane + at);
             }
         if constexpr (F8) {  // the sums that the products before did not wait for
@@ -698,16 +723,18 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
 template <bool F8>
 __global__ __launch_bounds__(kWideThreads8, 1) void k_experts_wide(ExpertsArgs a)
 {
-    __shared__ __attribute__((aligned(16))) char lds[kWideLds<F8, 4> > kWideLds<F8, 2> ? kWideLds<F8, 4> : kWideLds<F8, 2>];
+    __shared__ __attribute__((aligned(16))) char lds[F8 ? kWideLds : kWideLds - 8 * 2048];
     const int n_ct = (a.out + 255) >> 8;
     Tile t;
     if (!find_wide_tile(a.starts, a.n_experts, a.n_rows, n_ct, threadIdx.x & 63, (int)blockIdx.x, t)) return;
     // W past the caches where an expert has this one tile of rows and the weights are many (see launch_by_rows): us, 64 experts of 64 rows each,
     // 2048 -> 1536, in bf16 90 / 83, in 8 bits 54.6 / 50.5
     if (t.rows > 128)
-        t.only && a.large ? wide_body<F8, 4, true>(a, t, lds) : wide_body<F8, 4, false>(a, t, lds);
+        t.only && a.large ? wide_body<F8, 4, 2, true>(a, t, lds) : wide_body<F8, 4, 2, false>(a, t, lds);
+    else if (t.four)
+        t.only && a.large ? wide_body<F8, 2, 4, true>(a, t, lds) : wide_body<F8, 2, 4, false>(a, t, lds);
     else
-        t.only && a.large ? wide_body<F8, 2, true>(a, t, lds) : wide_body<F8, 2, false>(a, t, lds);
+        t.only && a.large ? wide_body<F8, 2, 2, true>(a, t, lds) : wide_body<F8, 2, 2, false>(a, t, lds);
 }
 
 template <bool F8>

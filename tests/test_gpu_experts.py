@@ -311,6 +311,18 @@ def test_experts(sizes, picks, in_f, out_f, idle, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("sizes, in_f, out_f", [
+    ([65, 128, 90, 1] * 12, 64, 1792),                           # as many tiles of up to 128 rows as give each four strips of columns,
+    ([65, 128, 90, 127] * 10, 192, 1920),                        # the last of them two or three
+    ([100] * 36 + [0, 20, 64], 448, 2048),
+    ([300] * 30 + [90] * 10, 704, 1024),                         # beside whole ones
+    ([77, 128, 64, 100] * 10, 2048, 1792),                       # weights that are read past the caches
+])
+def test_experts_with_many_tiles_of_few_rows(sizes, in_f, out_f, bits):
+    run_experts(sizes, 2, in_f, out_f, bits, idle=3)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("sizes", [[7, 0, 30], [400, 3, 0, 290]])
 def test_experts_rows_in_expert_order(sizes, bits):
     run_experts(sizes, 1, 384, 256, bits, idle=9, ordered=False)

@@ -48,6 +48,14 @@ def test_spilled_registers(kernel, most):
     assert hits[0][".vgpr_spill_count"] <= most, hits[0][".vgpr_spill_count"]
 
 
+@pytest.mark.parametrize("kernel", ["k_experts_wideILb0E", "k_experts_wideILb1E"])  # 232 and 246 of 256 registers
+def test_wide_products_spill_nothing(kernel):
+    """Their waits count memory operations, and a spill's, like any other use of private memory, are among them."""
+    hits = [k for name, k in _kernels().items() if "4lora" in name and kernel in name]
+    assert len(hits) == 1
+    assert hits[0][".vgpr_spill_count"] == 0 and hits[0][".private_segment_fixed_size"] == 0
+
+
 def _dynamic_symbols():
     """(offset of the code object, its sections' headers, symbol's entry, name) of every dynamic symbol of the library's AMDGPU code."""
     data, at = open(build.LIB, "rb").read(), 0
