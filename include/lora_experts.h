@@ -90,7 +90,7 @@ lora_status_t lora_experts_linear_scaled(const void *q, int64_t ldq, const float
                                          int64_t ldy, void *stream);
 
 /* z[t, :] = bf16(sum over j of weights[t][j] * y[place[t][j], :]), the products and the sum in fp32, in the order of j; picks whose place is
- * outside 0 .. n_rows - 1 are left out (their rows and weights are not read), and a token without any is a row of zeros.  y: device, bf16, [n_rows][out],
+ * outside 0 .. n_rows - 1 are left out (whatever their weights hold), and a token without any is a row of zeros.  y: device, bf16, [n_rows][out],
  * row stride ldy; place, weights: device, int32 and fp32, [tokens][picks]; z: device, bf16, [tokens][out], row stride ldz as above.
  * z must not overlap y. */
 lora_status_t lora_experts_combine(const void *y, int64_t ldy, int32_t n_rows, const int32_t *place, const float *weights, int32_t tokens,
