@@ -14,7 +14,8 @@
  *
  * One adapted layer on an 8-bit base is lora_rows_quantize, lora_linear_scaled, then lora_apply on the same y.
  *
- * Shapes: in_features a multiple of 64 and out_features of 128, as everywhere in this library; up to LORA_MAX_EXPERTS experts.
+ * Shapes: in_features a multiple of 64 and out_features of 128, as everywhere in this library, neither beyond
+ * LORA_EXPERTS_MAX_FEATURES; up to LORA_MAX_EXPERTS experts.  x of a product spans up to 64 GiB, its scales up to 16.
  * "blocks" is in_features / 128 rounded up: the last block of 128 may be half there.
  *
  * 8-bit format: OCP E4M3 (largest value 448, no infinities), fp32 scales.  value(q[t][k]) = q[t][k] * x_scales[t][k / 128],
@@ -36,6 +37,7 @@ extern "C" {
 
 #define LORA_MAX_EXPERTS 512
 #define LORA_MAX_PICKS 64
+#define LORA_EXPERTS_MAX_FEATURES (1 << 24)
 
 /* Rows of bf16 to 8 bits: for every row t and block b of 128 (what lies behind in_features counts as zero)
  *     d = max(largest |x| of the block, 448 * 2^-126),   scales[t][b] = d / 448,   q[t][k] = nearest E4M3 of x[t][k] * 448 / d

@@ -34,6 +34,9 @@ static lora_status_t check_sizes(int32_t in, int32_t out)
 {
     if (in <= 0 || in % 64 || out <= 0 || out % 128)
         return fail(LORA_ERR_SHAPE, "in_features (%d) must be a positive multiple of 64 and out_features (%d) of 128", in, out);
+    // (bytes of a row then fit 32 bits, those of all experts 63)
+    if (in > LORA_EXPERTS_MAX_FEATURES || out > LORA_EXPERTS_MAX_FEATURES)
+        return fail(LORA_ERR_SHAPE, "in_features (%d) or out_features (%d) beyond %d", in, out, LORA_EXPERTS_MAX_FEATURES);
     return LORA_OK;
 }
 

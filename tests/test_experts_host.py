@@ -53,6 +53,18 @@ CASES += [("lora_experts_pack_weight", PACK, c, s) for c, s in [
     (dict(out=130), "SHAPE"), (dict(packed=None), "INVALID_ARG"), (dict(packed=P + 64), "INVALID_ARG"), (dict(n=100), "OOM")]]
 
 
+@pytest.mark.parametrize("name, base, change", [
+    ("lora_rows_quantize", QUANTIZE, dict(in_f=1 << 30, ldx=1 << 30, ldq=1 << 30, lds=1 << 23)),
+    ("lora_experts_pack_weight", PACK, dict(experts=512, in_f=(1 << 31) - 64, out=(1 << 31) - 128)),  # (bytes that are few in 64 bits)
+    ("lora_experts_pack_weight", PACK, dict(experts=1, in_f=(1 << 30) + 64, bits=16, n=1 << 62)),
+    ("lora_experts_linear", EXPERTS, dict(out=(1 << 24) + 128, ldy=1 << 25)),
+    ("lora_linear_scaled", LINEAR, dict(in_f=1 << 25, ldq=1 << 25, lds=1 << 18)),
+    ("lora_experts_combine", COMBINE, dict(out=1 << 25, ldy=1 << 25, ldz=1 << 25)),
+])
+def test_features_whose_bytes_would_not_fit_are_refused(name, base, change):
+    assert status(name, *dict(base, **change).values(), None) == "LORA_ERR_SHAPE"
+
+
 @pytest.mark.parametrize("name, base, change, expected", CASES, ids=lambda v: str(v) if isinstance(v, str) else "")
 def test_refusals(name, base, change, expected):
     assert status(name, *dict(base, **change).values(), None) == "LORA_ERR_" + expected
