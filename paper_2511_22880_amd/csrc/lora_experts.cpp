@@ -220,8 +220,7 @@ extern "C" lora_status_t lora_experts_group_workspace_bytes(int64_t n_picks, int
     if (!bytes) return fail(LORA_ERR_INVALID_ARG, "bytes is NULL");
     if (n_picks < 0 || n_picks > INT32_MAX) return fail(LORA_ERR_INVALID_ARG, "n_picks = %lld", (long long)n_picks);
     TRY(check_experts(n_experts));
-    const int chunks = lora::group_chunks(n_picks);
-    *bytes = chunks > 1 ? (size_t)chunks * n_experts * sizeof(int32_t) : 0;
+    *bytes = lora::group_counts(n_picks) ? (size_t)lora::group_chunks(n_picks) * n_experts * sizeof(int32_t) : 0;
     return LORA_OK;
 }
 

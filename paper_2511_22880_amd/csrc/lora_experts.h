@@ -10,20 +10,20 @@ constexpr int kScaleBlock = 128;     // values of a row, or of a row and a colum
 constexpr int kPieceBytes = 128;     // of a row: what the products walk k in (64 bf16 or 128 8-bit values)
 constexpr int kMaxExperts = 512;     // (a work group that groups picks has a count of each for 16 wavefronts in LDS)
 constexpr int kGroupUnit = 1024;      // picks of a work group that groups them: 1, 2, 4, 8 or a multiple of 16 times as many
-constexpr int kGroupAlone = 8;        // .. times as many are one work group's at most ...
-constexpr int kGroupMaxChunks = 256;  // ... beyond which there are up to so many work groups
+constexpr int kGroupAlone = 8;        // up to so many work groups each look at all picks; with more a launch counts ahead
+constexpr int kGroupMaxChunks = 256;  // of either launch then
 
 // picks of a work group
 inline int64_t group_chunk(int64_t n_picks)
 {
-    for (int m = 1; m <= kGroupAlone; m *= 2)
-        if (n_picks <= m * kGroupUnit) return m * kGroupUnit;
+    if (n_picks <= kGroupAlone * kGroupUnit) return kGroupUnit;
     for (int m = 2; m <= 8; m *= 2)
         if (n_picks <= (int64_t)m * kGroupUnit * kGroupMaxChunks) return m * kGroupUnit;
     const int64_t unit = 16 * kGroupUnit, least = (n_picks + kGroupMaxChunks - 1) / kGroupMaxChunks;
     return (least + unit - 1) / unit * unit;
 }
 inline int group_chunks(int64_t n_picks) { const int64_t c = group_chunk(n_picks); return (int)((n_picks + c - 1) / c); }
+inline bool group_counts(int64_t n_picks) { return n_picks > kGroupAlone * kGroupUnit; }
 
 // Rows of x, by expert, times the experts' weights (see include/lora_experts.h).  starts == NULL: one expert that has all rows.
 struct ExpertsArgs {
@@ -53,7 +53,7 @@ hipError_t launch_experts_pack(const char *w, int64_t n_experts, int row_bytes, 
 hipError_t launch_rows_quantize(const uint16_t *x, int64_t ldx, int64_t rows, int in, uint8_t *q, int64_t ldq, float *scales,
                                 int64_t ld_scales, hipStream_t stream);
 
-// workspace: group_chunks(n) * n_experts ints where there is more than one chunk
+// workspace: group_chunks(n) * n_experts ints where group_counts(n)
 hipError_t launch_experts_group(const int32_t *ids, int64_t ld_ids, int64_t tokens, int picks, int n_experts, int32_t *starts,
                                 int32_t *order, int32_t *place, int32_t *workspace, hipStream_t stream);
 

@@ -1125,11 +1125,12 @@ hipError_t launch_rows_quantize(const uint16_t *x, int64_t ldx, int64_t rows, in
 // Picks by expert: a counting sort that keeps the picks' order.  The picks are cut into chunks, one work group each, a chunk into 16 runs, one
 // wavefront each.  A wavefront counts 64 picks at a time: lanes with the same expert find each other by ballots over the id's bits, and
 // their first lane adds their number to the wavefront's own count of that expert.  The first place of (expert, chunk, wavefront) is then a sum
-// over the experts before, the chunks before and the wavefronts before; a second walk over the picks hands the places out.  No atomics.
-// Up to kGroupAlone picks are one chunk and one launch, else a launch counts and a second one, each of whose work groups adds up all chunks' counts,
-// hands out.  A wavefront's S x 64 picks stay in registers between its two walks; S = 0 (beyond 2 M picks) reads them twice.
+// over the experts before, the chunks before and the wavefronts before; a second walk over the picks hands the places out.  No atomics whose order shows.
+// Up to kGroupAlone chunks of a pick a thread are one launch, each of whose work groups counts all picks by itself, by atomic adds in LDS; else a launch counts and
+// a second one, each of whose work groups adds up all chunks' counts, hands out.  A wavefront's S x 64 picks stay in registers between its two walks; S = 0 (beyond 2 M picks) reads them twice.
 // What bounds it is the way through memory and LDS, not bytes: device time 3.5 us for 512 picks, 13 for 157400
-// (counts 4.2, places 8.8; the chunks' counts all requested at once, 32 a thread: 10).
+// (counts 4.2, places 8.8; the chunks' counts all requested at once, 32 a thread: 10).  Up to 8192 picks by one work group instead of up to eight: 4148 of 72
+// experts 9.0 / 6.2 us a call, 8192 of 256 14.2 / 7.7, all of one 7.3 / 6.6, mostly of one of 8 9.4 / 9.5.
 // ------------------------------------------------------------------------------------------------
 constexpr int kGroupWaves = 16;
 
@@ -1224,7 +1225,25 @@ __global__ __launch_bounds__(64 * kGroupWaves) void k_experts_place(const int32_
     in_order();
     // the chunks' counts: as many threads an expert as there are
     const int share = 64 * kGroupWaves / n_experts;
-    if (counts) {
+    const bool several = S == 1 && gridDim.x > 1;  // and none were taken: a chunk is a pick of every thread, and every work group looks at all
+    if (several) {
+        some_all[tid] = 0;
+        some_before[tid] = 0;
+        int id[kGroupAlone];
+#pragma unroll
+        for (int c = 0; c < kGroupAlone; ++c) id[c] = id_at(ids, ld_ids, picks, (int64_t)c * kGroupUnit + tid, n, n_experts);
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < kGroupAlone; ++c) {
+            // the picks of the first lane's expert at once, as adds to one address wait for each other
+            const int e = id[c], first = __builtin_amdgcn_readfirstlane(e), of_first = (int)__popcll(__ballot(e == first));
+            const int m = lane == 0 ? of_first : 1;
+            if (e < n_experts && (lane == 0 || e != first)) {
+                atomicAdd(&some_all[e], m);  // (sums of whole numbers: their order does not show)
+                if (c < (int)blockIdx.x) atomicAdd(&some_before[e], m);
+            }
+        }
+    } else if (counts) {
         int all = 0, before = 0;
         const int e = tid % n_experts, q = tid / n_experts;
         if (q < share)
@@ -1243,7 +1262,10 @@ __global__ __launch_bounds__(64 * kGroupWaves) void k_experts_place(const int32_
     // thread e: expert e (at most 512 of them)
     int total = 0, before = 0;
     if (tid < n_experts) {
-        if (counts)
+        if (several) {
+            total = some_all[tid];
+            before = some_before[tid];
+        } else if (counts)
             for (int q = 0; q < share; ++q) {
                 total += some_all[q * n_experts + tid];
                 before += some_before[q * n_experts + tid];
@@ -1305,11 +1327,11 @@ static hipError_t launch_group(const int32_t *ids, int64_t ld_ids, int64_t n, in
     int bits = 0;
     while ((n_experts >> bits) != 0) ++bits;  // of the ids and of n_experts, which stands for none
     const size_t lds = (size_t)kGroupWaves * n_experts * 4;
-    if (chunks > 1)
+    if constexpr (S != 1)
         hipLaunchKernelGGL(k_experts_count<S>, dim3((unsigned)chunks), dim3(64 * kGroupWaves), lds, stream, ids, ld_ids, picks, n, chunk, n_experts, bits,
                            workspace);
     hipLaunchKernelGGL(k_experts_place<S>, dim3((unsigned)chunks), dim3(64 * kGroupWaves), lds + (kGroupWaves + (chunks > 1 ? 2 * 64 * kGroupWaves : 0)) * 4,
-                       stream, ids, ld_ids, picks, n, chunk, n_experts, bits, chunks > 1 ? workspace : nullptr, chunks, starts, order, place);
+                       stream, ids, ld_ids, picks, n, chunk, n_experts, bits, S != 1 ? workspace : nullptr, chunks, starts, order, place);
     return hipGetLastError();
 }
 

@@ -249,6 +249,15 @@ def test_group(tokens, picks, experts, kind):
         assert np.array_equal(a.cpu().numpy(), b)
 
 
+@pytest.mark.parametrize("n, experts", [(1025, 3), (3000, 512), (8191, 8), (8192, 300)])
+def test_group_of_picks_that_are_mostly_one_experts(n, experts):
+    g = gen(n)
+    ids = torch.randint(-1, experts, (n, 1), generator=g, device="cuda", dtype=torch.int32)
+    ids = torch.where(torch.rand(n, 1, generator=g, device="cuda") < 0.8, experts // 2, ids)
+    for a, b in zip(group(ids, experts), grouped(ids, experts)):
+        assert np.array_equal(a.cpu().numpy(), b)
+
+
 def test_group_reads_rows_of_any_stride():
     ids = torch.randint(0, 9, (300, 12), generator=gen(1), device="cuda", dtype=torch.int32)
     for a, b in zip(group(ids[:, 3:7], 9), grouped(ids[:, 3:7], 9)):
