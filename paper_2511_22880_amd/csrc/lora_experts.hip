@@ -153,6 +153,15 @@ static __device__ __forceinline__ bool four_strips(int whole, int n_rest, int n_
     return 8 * ((whole + rest4 + kComputeUnits - 1) / kComputeUnits) < max(8 * rounds + 10, (8 * whole + 5 * rest) / kComputeUnits + 3);
 }
 
+// How many whole tiles, the last ones, are cut into two of 128 rows: those of the last round of compute units, where all of them and the tiles of up to 128
+// rows are through in one round that way.  8 bits, us, whole / cut: 1665 rows 1088 -> 11520 (315 tiles) 42.6 / 37.1, 2500 rows 4096 -> 7680 (300) 110 / 97,
+// 3000 rows of 15 experts 4096 -> 2048 (120) 62.4 / 46.
+static __host__ __device__ __forceinline__ int cut_tiles(int whole, int rest)
+{
+    const int left = whole % kComputeUnits;
+    return 2 * left + rest <= kComputeUnits ? left : 0;
+}
+
 // The same for tiles of 256 rows x 256 columns, an expert's last one of up to 128 rows apart: the whole ones come first, and the others, which take about
 // half as long, fill the compute units that the last round of those leaves idle.  Inside an expert column tiles in groups of four, in a group row tile by row tile:
 // of 32 tiles in a run, one on each of an XCD's compute units, 8 row tiles x 4 column tiles walk k together, and every chunk of x and W that
@@ -172,23 +181,38 @@ static __device__ __forceinline__ bool find_wide_tile(const int32_t *__restrict_
         n_whole = wave_sum(a);
         n_rest = wave_sum(b);
     }
-    t.four = four_strips(n_whole * n_ct, n_rest, n_ct);
-    const int xcd = blk & 7, per_whole = (n_whole * n_ct + 7) >> 3;
-    const bool is_rest = (blk >> 3) >= per_whole;
-    if (is_rest && t.four) n_ct = (n_ct + 1) >> 1;
-    const int j = (blk >> 3) - (is_rest ? per_whole : 0), per = is_rest ? (n_rest * n_ct + 7) >> 3 : per_whole, idx = xcd * per + j;
-    if (j >= per || idx >= (is_rest ? n_rest : n_whole) * n_ct) return false;
+    const int cut = cut_tiles(n_whole * n_ct, n_rest * n_ct), uncut = n_whole * n_ct - cut;
+    t.four = cut == 0 && four_strips(n_whole * n_ct, n_rest, n_ct);
+    const int xcd = blk & 7, per_uncut = (uncut + 7) >> 3, per_cut = (2 * cut + 7) >> 3;
+    int j = blk >> 3, half = -1, idx;  // half of a tile cut in two
+    bool is_rest = false;
+    if (j < per_uncut) {
+        idx = xcd * per_uncut + j;
+        if (idx >= uncut) return false;
+    } else if ((j -= per_uncut) < per_cut) {
+        idx = xcd * per_cut + j;
+        if (idx >= 2 * cut) return false;
+        half = idx & 1;
+        idx = uncut + (idx >> 1);
+    } else {
+        j -= per_cut;
+        is_rest = true;
+        if (t.four) n_ct = (n_ct + 1) >> 1;
+        const int per_rest = (n_rest * n_ct + 7) >> 3;
+        idx = xcd * per_rest + j;
+        if (j >= per_rest || idx >= n_rest * n_ct) return false;
+    }
     const int q = idx / n_ct;
     const RowTile r = !starts   ? RowTile{0, is_rest ? 0 : q, is_rest ? n_rest : n_whole, 0, n_rows}
                       : is_rest ? find_row_tile(starts, n_experts, n_rows, lane, q, rest)
                                 : find_row_tile(starts, n_experts, n_rows, lane, q, whole);
     const int in_e = idx - (q - r.m) * n_ct, grp = in_e / (r.of * 4), left = in_e - grp * (r.of * 4), wide = min(4, n_ct - grp * 4);
-    const int m = left / wide, row = (is_rest ? whole(r.rows) : m) * 256;
+    const int m = left / wide, row = (is_rest ? whole(r.rows) : m) * 256 + (half > 0 ? 128 : 0);
     t.expert = r.expert;
     t.ct = grp * 4 + left - m * wide;
     t.row0 = r.first + row;
-    t.rows = min(256, r.rows - row);
-    t.only = r.rows <= 256;
+    t.rows = min(half < 0 ? 256 : 128, r.rows - row);
+    t.only = half < 0 && r.rows <= 256;
     return true;
 }
 
@@ -741,9 +765,14 @@ __global__ __launch_bounds__(kWideThreads8, 1) void k_experts_wide(ExpertsArgs a
 template <bool F8>
 static hipError_t launch_wide(const ExpertsArgs &a, hipStream_t stream)
 {
-    const int64_t row_tiles = (int64_t)(a.n_rows + 255) / 256 + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
-    const int64_t grid = (row_tiles * ((a.out + 255) / 256) + 7) / 8 * 8 + 8;  // (an eighth of either kind is rounded up)
+    const int64_t row_tiles = ((int64_t)a.n_rows + 255) / 256 + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0), n_ct = (a.out + 255) / 256;
+    // an eighth of each kind is rounded up, and up to half a round of tiles cut in two
+    int64_t grid = (row_tiles * n_ct + 7) / 8 * 8 + 16 + kComputeUnits / 2;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
+    if (!a.starts) {  // known here (150 work groups without a tile take about 1 us)
+        const int whole = (int)(((int64_t)a.n_rows + 127) / 256 * n_ct), rest = (int)(row_tiles * n_ct) - whole;
+        grid = (int64_t)(whole + 7) / 8 * 8 + (cut_tiles(whole, rest) + 7) / 8 * 8 + (rest + 7) / 8 * 8;
+    }
     hipLaunchKernelGGL(k_experts_wide<F8>, dim3((unsigned)grid), dim3(kWideThreads8), 0, stream, a);
     return hipGetLastError();
 }

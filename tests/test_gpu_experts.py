@@ -326,6 +326,9 @@ def test_experts(sizes, picks, in_f, out_f, idle, bits):
     ([100] * 36 + [0, 20, 64], 448, 2048),
     ([300] * 30 + [90] * 10, 704, 1024),                         # beside whole ones
     ([77, 128, 64, 100] * 10, 2048, 1792),                       # weights that are read past the caches
+    ([200] * 15, 320, 2048),                                     # whole tiles cut in two, all of them
+    ([256, 129, 255, 200] * 9 + [60] * 10, 192, 2048),           # .. those of the second round, beside some of few rows
+    ([2500], 448, 7680),
 ])
 def test_experts_with_many_tiles_of_few_rows(sizes, in_f, out_f, bits):
     run_experts(sizes, 2, in_f, out_f, bits, idle=3)
