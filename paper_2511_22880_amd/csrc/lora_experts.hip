@@ -1014,7 +1014,10 @@ static hipError_t launch_by_rows(ExpertsArgs a, hipStream_t stream)
     };
     constexpr std::integral_constant<int, 2> two;
     constexpr std::integral_constant<int, 4> four;
-    if (per > 48 && fills(256, 256, kMost)) return launch_wide<F8>(a, stream);
+    // (more tiles of 64 x 256 than one round: half as many of 128 x 256 or 256 x 256, in one, are earlier.  us, 64 x 256 / wide: 1024 rows 4096 -> 4096 in 8 bits 27 / 33,
+    // 1152 49 / 33, 2048 49 / 40, 1100 9152 -> 4480 92 / 67, 2000 of 8 experts 4096 -> 2048 in bf16 77 / 62, 1600 of them 58 / 60.  Few rows an expert, 64 experts
+    // 2048 -> 1536, what was taken else / wide: in 8 bits 20 rows 40 / 44, 30 51 / 45, 40 57 / 45, in bf16 30 72 / 78, 40 87 / 79)
+    if (per > (F8 ? 25 : 35) && (fills(256, 256, kMost) || fills(64, 256, kComputeUnits + 1))) return launch_wide<F8>(a, stream);
     if (per > 32 && a.out % 256 == 0 && fills(64, 256, kMost)) return middle(four, four);
     if (per > 24 && fills(64, 128, kMost)) return middle(four, two);
     // (a row an expert, of large weights: 16 x 64 tiles cost up to a tenth more where all picks have an expert here, but where one in ten has, as with experts on
