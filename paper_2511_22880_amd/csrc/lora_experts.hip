@@ -968,27 +968,27 @@ static hipError_t launch_mid(const ExpertsArgs &a, hipStream_t stream)
 // The tiles of a launch: the largest of which there are enough to occupy most compute units, no higher than an expert's rows in the mean ask for.  Row
 // tiles are counted as if every expert's last one were half there (the host does not know who picked what).  With one tile of 64 x 256, 64 x 128 or 32 x 128 on a
 // compute unit two groups of wavefronts share its pieces (two), unless k is short; with more of them the tiles' own wavefronts are enough (one).
-// Device time in us, one layer in 8 bits:
-//   rows, layer        256 x 256   64 x 256, one / two   64 x 128, one / two   32 x 128, one / two   32 x 64   16 x 64   16 x 32   16 x 16
+// Device time in us, one layer in 8 bits (wide: k_experts_wide, whose tiles are 256 x 256 or 128 x 256):
+//   rows, layer        wide        64 x 256, one / two   64 x 128, one / two   32 x 128, one / two   32 x 64   16 x 64   16 x 32   16 x 16
 //   1     4096 4096                                                                                            6.3       5.6       5.3
 //   64    4096 4096    36          32 / 25               21 / 17               12.6 / 12.5           8.9       7.3       9.2
 //   128   4096 4096    36          32 / 25               21 / 17               12.7 / 12.6           9.4       11.3      14.8
-//   256   4096 4096    52          33 / 25               21 / 17               13.4 / 13.1           15.0      19.1      26
-//   512   4096 4096    52          33 / 26               22 / 17.5             22 / 21               25        32        52
-//   1024  4096 4096    52          35 / 27               32 / 32               39 / 40               49        69        107
-//   2048  4096 4096    53          49 / 53               60 / 64               78 / 79               98        136       215
+//   256   4096 4096    33          33 / 25               21 / 17               13.4 / 13.1           15.0      19.1      26
+//   512   4096 4096    34          33 / 26               22 / 17.5             22 / 21               25        32        52
+//   1024  4096 4096    36          35 / 27               32 / 32               39 / 40               49        69        107
+//   2048  4096 4096    42          49 / 53               60 / 64               78 / 79               98        136       215
 //   64    16384 16384  131         132 / 122             90 / 86               75 / 66               70        90        117
-//   256   16384 16384  198         131 / 118             134 / 144             181 / 175             179       252       372
-//   115   5568 3584    48          42 / 32               27 / 21               16.3 / 15.5           11.6      13.8      17.4
-//   373   5440 640     68                                26 / 21               15.8 / 15.1           11.3      9.1       11.4
-//   1149  7232 512     93          54 / 41               33 / 27               20.3 / 19.4           24        24        33
-//   689   8128 14848   114         150 / 152             156 / 160             201 / 195             218       316       472
-//   10081 704 512      16.4        15.1 / 18.8           15.9 / 18.4           14.6 / 18.2           28        33        59
+//   256   16384 16384  132         131 / 118             134 / 144             181 / 175             179       252       372
+//   115   5568 3584    43          42 / 32               27 / 21               16.3 / 15.5           11.6      13.8      17.4
+//   373   5440 640     41                                26 / 21               15.8 / 15.1           11.3      9.1       11.4
+//   1149  7232 512     54          54 / 41               33 / 27               20.3 / 19.4           24        24        33
+//   689   8128 14848   111         150 / 152             156 / 160             201 / 195             218       316       472
+//   10081 704 512      12.1        15.1 / 18.8           15.9 / 18.4           14.6 / 18.2           28        33        59
 //   7     3008 4352                                                                                            5.5       4.9       5.8
 // and of 64 experts 2048 -> 1536, rows each, in 8 bits: 8 49, - , 47, 39.9, 44, 41, 54; 64 54, 64, 71, 66, 82, 91, 170; in bf16: 8 81, - , 75, 75, 71, 73, 76;
 // 32 85, 86, 78, 90, 91, 104, 130; 64 90, 98, 102, 109, 115, 153, 200 (in the same order, one group of wavefronts, through the caches).
-// Over 60 random sizes of one layer the choice was 2.2 % from the best of all of these in the mean, over 60 of experts 5 % (where most picks have no
-// expert here, which the host does not know, up to twice the best).
+// Over 50 random sizes of one layer the choice was 1.7 % from the best of all of these in the mean, over 50 of experts 7 % (a quarter of them with one pick in
+// ten here, which the host does not know: up to twice the best).
 template <bool F8>
 static hipError_t launch_by_rows(ExpertsArgs a, hipStream_t stream)
 {
