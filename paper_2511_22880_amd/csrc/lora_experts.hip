@@ -47,12 +47,27 @@ static __device__ __forceinline__ void in_order()
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
-// 16 x 16 products over 128 8-bit values of k (both operands E4M3, the instruction's own scales at 1).  The instruction drops what lies 2^-17 below the
-// largest of an element's 128 products (all in all up to 2^-10 of that product was seen), and the ones for 32 values of k do the same: there is none more exact.
-// A block's sum is fp32 from there on.
-static __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c)
+// A weight's scale as 2^(power - 127), which the matrix instruction applies to its sum for nothing, times the factor left over: half to one, unless the scale
+// is beyond 2^100 or 2^-100.  x's scale times the whole one can be far below 2^-126, where it would lose bits (x's alone goes down to that) though y does not:
+// a sum of 128 products of up to 448^2 lies up to 2^25 above it.  x's scale times the factor loses none to speak of, and never overflows where x's scale does not; a
+// sum times 2^-100 to 2^100 is still exact.  Zero, infinities and NaN stay in the factor.
+struct WeightScale {
+    float factor;
+    int power;
+};
+static __device__ __forceinline__ WeightScale weight_scale(float w)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
+    const int e = min(max((int)((__float_as_uint(w) >> 23) & 0xFFu) - 126, -100), 100);
+    return WeightScale{w * __uint_as_float((uint32_t)(127 - e) << 23), e + 127};
+}
+
+// 16 x 16 products over 128 8-bit values of k (both operands E4M3, b's times 2^(power - 127)).  The instruction drops what lies 2^-17 below the
+// largest of an element's 128 products (all in all up to 2^-10 of that product was seen), and the ones for 32 values of k do the same: of those that take 8 bits there is
+// none more exact.  (E4M3 is exact in bf16, whose instruction adds in fp32: that would take twice as long at the matrix units and a conversion of
+// every operand.)  A block's sum is fp32 from there on.
+static __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, int power)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 127, 0, power);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -302,11 +317,15 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
 #pragma unroll
                 for (int b = 0; b < CB; ++b) wq[d][h][b] = ldw16<ONCE>(wbase + at * (16384 * WAVES) + operand_at<F8>(h, b));
         };
+        [[maybe_unused]] int power = 127;  // of the staged piece's scale of W
         auto stage = [&](int d) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < NX; ++q) *reinterpret_cast<uint4 *>(slab + (8 * q + lr) * 128 + ((lc ^ lr) << 4)) = xq[d][q];
-            if constexpr (F8)
-                if (lane < R) reinterpret_cast<float *>(slab + kSlab)[lane] = sx[d] * sw[d];
+            if constexpr (F8) {
+                const WeightScale s = weight_scale(sw[d]);
+                power = s.power;
+                if (lane < R) reinterpret_cast<float *>(slab + kSlab)[lane] = sx[d] * s.factor;
+            }
         };
         auto compute = [&](int d) __attribute__((always_inline)) {
             uint4 xo[2][RB];
@@ -321,7 +340,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
                     const f32x4 s = *reinterpret_cast<const f32x4 *>(slab + kSlab + (16 * i + 4 * kq) * 4);
 #pragma unroll
                     for (int b = 0; b < CB; ++b)
-                        acc[i][b] += s * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), f32x4{0.f, 0.f, 0.f, 0.f});
+                        acc[i][b] += s * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), power);
                 }
             } else {
 #pragma unroll
@@ -629,7 +648,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     uint4 xo[XH][4], wo[WH][WB];
     [[maybe_unused]] f32x4 sc[4];
     int xget = 0, wget = 0;
-    [[maybe_unused]] int sget = 0;
+    [[maybe_unused]] int sget = 0, power = 127;
     const int xlane = (8 * rw + (n >> 3)) * 1024 + (n & 7) * 128;
     const int wlane = wave / WS * WPART + lane * 16;
     // row 16 i + n of this wavefront's: block 8 rw + 2 i + n / 8, row n mod 8 of it
@@ -681,9 +700,10 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (F8 && q == 0) {
-            const float w = wscale[P];
+            const WeightScale w = weight_scale(wscale[P]);
+            power = w.power;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sc[i] = *reinterpret_cast<const f32x4 *>(sbuf + sget + (16 * i + 4 * kq) * 4) * w;
+            for (int i = 0; i < 4; ++i) sc[i] = *reinterpret_cast<const f32x4 *>(sbuf + sget + (16 * i + 4 * kq) * 4) * w.factor;
             sget = (sget + 256) & (by16 ? 1023 : 2047);
         }
         if constexpr (F8 && q == SP - 1)
@@ -699,7 +719,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         if constexpr (F8) {
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-                part[k % (kLag + 1)] = mfma_e4m3(as_i32x8(xo[0][k >> 2], xo[XH - 1][k >> 2]), as_i32x8(wo[0][k & 3], wo[WH - 1][k & 3]), f32x4{0.f, 0.f, 0.f, 0.f});
+                part[k % (kLag + 1)] = mfma_e4m3(as_i32x8(xo[0][k >> 2], xo[XH - 1][k >> 2]), as_i32x8(wo[0][k & 3], wo[WH - 1][k & 3]), power);
                 __builtin_amdgcn_sched_barrier(0);
                 if (k >= kLag) add(q, k - kLag);
                 // these rows of x have been multiplied: the next piece's.  All of it has landed: W of this step, requested behind it, has been waited
@@ -883,10 +903,14 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
         for (int d = 0; d < D; ++d) {
             const int slot = d & 1;
             put_x(d, slot);
-            if constexpr (F8)
+            [[maybe_unused]] int power = 127;
+            if constexpr (F8) {
+                const WeightScale s = weight_scale(sw[d]);
+                power = s.power;
 #pragma unroll
                 for (int q = 0; q < NS; ++q)
-                    if (64 * q + lane < R) sc[64 * q + lane] = sx[d][q] * sw[d];
+                    if (64 * q + lane < R) sc[64 * q + lane] = sx[d][q] * s.factor;
+            }
             load_x(s0 + d + D, d);
             // what a slot held two pieces ago has been read by everyone: each came to the barrier of the piece between behind its reads
             barrier();
@@ -904,7 +928,7 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
                         const f32x4 f = *reinterpret_cast<const f32x4 *>(sc + 16 * i + 4 * kq);
 #pragma unroll
                         for (int b = 0; b < CB; ++b)
-                            acc[i][b] += f * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), f32x4{0.f, 0.f, 0.f, 0.f});
+                            acc[i][b] += f * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), power);
                     }
                 } else {
 #pragma unroll

@@ -552,3 +552,25 @@ def test_layer_of_experts_on_fewer_tokens_than_it_has_room_for():
         assert (z.double() - ref).norm() <= 2 * 2.0 ** -3 / 12 ** 0.5 * ref.norm()
         whole.append(z)
     assert torch.isfinite(whole[2]).all() and torch.isfinite(whole[1]).all()
+
+
+# ---- scales at the ends of their range ----------------------------------------------------------------------
+@pytest.mark.parametrize("rows, in_f, out_f", [(3, 512, 256), (300, 256, 2048), (515, 256, 1408), (2200, 256, 4096)])
+@pytest.mark.parametrize("x_power, w_power, small", [
+    (-126, -10, False), (-126, -19, False), (-100, -45, False), (-73, -73, False), (-20, -126, False),  # scales whose product has few bits left
+    (119, 12, True), (12, 119, True),                                                                   # .. or does not fit
+    (119, -126, False), (-126, 119, False), (0, 0, False),
+])
+def test_linear_scaled_where_the_scales_product_is_no_normal_number(rows, in_f, out_f, x_power, w_power, small):
+    """y is one: a block's sum lies 2^23 above the scales' product, or 2^-11.  A scale times 1/2 to 1, at 2^-126, has one bit less, so one more
+    rounding's worth: still (blocks + 3) 2^-24 in all."""
+    g = gen(rows - x_power)
+    blocks = in_f // 128
+    draw = (lambda *s: torch.randint(1, 4, s, generator=g, device="cuda") * 2.0 ** -9) if small else (  # noqa: E731
+        lambda *s: torch.randint(8, 15, s, generator=g, device="cuda") * 32.0)
+    q, w = draw(rows, in_f).to(F8), draw(1, out_f, in_f).to(F8)
+    scales = lambda power, *s: (torch.rand(*s, generator=g, device="cuda") * 0.9 + 1) * 2.0 ** power  # noqa: E731
+    s, ws = scales(x_power, rows, blocks), scales(w_power, 1, out_f // 128, blocks)
+    y = torch.full((rows, out_f), float("nan"), dtype=BF, device="cuda")
+    L.lora_linear_scaled(q, s, packed(w), ws, y)
+    close(y, *product8(q, s, w[0], ws[0]))
