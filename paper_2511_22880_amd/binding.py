@@ -652,25 +652,56 @@ def lora_place_assign(n_servers: int, ranks, demand_tps, operating_points: dict,
 
 
 # ---- frozen layers beside an adapter, in block-scaled 8 bits and grouped by expert (include/lora_experts.h) ----------------
-# The arguments are torch device tensors, whose shapes and strides say what the C calls are told; a tensor that cannot hold what a
-# call writes or reads there is refused here, since the library sees addresses only.
+# The arguments are torch device tensors, whose shapes and strides say what the C calls are told; a tensor of another type, or one that cannot hold what
+# a call writes or reads there, is refused here, since the library sees addresses only.
+# Element types, filled in when the first tensor comes (this module does not import torch).  bf16 and 8-bit values may also come as their bits.
+_BF16, _F32, _INT32, _E4M3 = set(), set(), set(), set()
+
+
+def _know_types() -> None:
+    import torch
+    _BF16.update((torch.bfloat16, torch.uint16))
+    _F32.add(torch.float32)
+    _INT32.add(torch.int32)
+    _E4M3.update((torch.float8_e4m3fn, torch.uint8))
+
+
 def _blocks(n: int) -> int:
     return (n + 127) >> 7
 
 
 # What a tensor is asked for costs 0.1 us each time, and so does a call of Python's: the calls below, which a decode step waits for, ask for shape and
 # strides once, in line, and compare; where anything is unusual _usable looks closer.
-def _usable(name: str, t, rows: int, columns: int, itemsize: int) -> None:
-    """Refuses a tensor that does not hold so many rows of so many elements, side by side within a row."""
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < columns or t.itemsize != itemsize or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} with strides {t.stride()} does not do: {rows} rows of {columns} elements of {itemsize} "
-                         "bytes side by side are meant")
+def _names(types) -> str:
+    return " or ".join(sorted(str(t).replace("torch.", "") for t in types))
 
 
-def _whole(name: str, t, n: int, itemsize: int):
-    """Address of a contiguous tensor of at least n elements."""
-    if t.numel() < n or t.itemsize != itemsize or not t.is_contiguous():
-        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} does not do: {n} contiguous elements of {itemsize} bytes are meant")
+def _usable(name: str, t, rows: int, columns: int, types: set) -> None:
+    """Refuses a tensor that does not hold so many rows of so many elements of one of these types, side by side within a row."""
+    if not types:
+        _know_types()
+    if t.dtype not in types:
+        raise ValueError(f"{name}: {t.dtype} does not do: {_names(types)} is meant")
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < columns or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()} does not do: {rows} rows of {columns} elements side by side are meant")
+
+
+def _whole(name: str, t, n: int, types: set):
+    """Address of a contiguous tensor of at least n elements of one of these types."""
+    if t.dtype not in types:
+        if not types:
+            _know_types()
+        if t.dtype not in types:
+            raise ValueError(f"{name}: {t.dtype} does not do: {_names(types)} is meant")
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()} does not do: {n} contiguous elements are meant")
+    return t.data_ptr()
+
+
+def _packed(t, n: int):
+    """Address of packed weights, n bytes of whatever type."""
+    if t.itemsize != 1 or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"w_packed: {tuple(t.shape)} of {t.dtype} does not do: {n} contiguous bytes are meant")
     return t.data_ptr()
 
 
@@ -690,12 +721,12 @@ def lora_rows_quantize(x, q, scales, stream=None) -> None:
     except ValueError:
         (rows, in_f), (ldx, x1), (qr, qc), (ldq, q1), (sr, sc), (lds, s1) = _two(x, "x") + _two(q, "q") + _two(scales, "scales")
     blocks = (in_f + 127) >> 7
-    if x1 != 1 or x.itemsize != 2:
-        _usable("x", x, rows, in_f, 2)
-    if qr < rows or qc < blocks << 7 or q1 != 1 or q.itemsize != 1:
-        _usable("q", q, rows, blocks << 7, 1)
-    if sr < rows or sc < blocks or s1 != 1 or scales.itemsize != 4:
-        _usable("scales", scales, rows, blocks, 4)
+    if x1 != 1 or x.dtype not in _BF16:
+        _usable("x", x, rows, in_f, _BF16)
+    if qr < rows or qc < blocks << 7 or q1 != 1 or q.dtype not in _E4M3:
+        _usable("q", q, rows, blocks << 7, _E4M3)
+    if sr < rows or sc < blocks or s1 != 1 or scales.dtype not in _F32:
+        _usable("scales", scales, rows, blocks, _F32)
     if rows == 1:  # (of a single row torch states any stride)
         ldx = in_f
     if qr == 1:
@@ -721,7 +752,7 @@ def lora_experts_pack_weight(w, dev_packed, stream=None, in_features: Optional[i
     in_f = row if in_features is None else int(in_features)
     if row != (in_f if bits == 16 else _blocks(in_f) << 7):
         raise ValueError(f"w: rows of {row} elements are not those of {in_f} input features")
-    _check(lib().lora_experts_pack_weight(_whole("w", w, 0, w.itemsize), e, in_f, out_f, bits, dev_packed.data_ptr(), _nbytes(dev_packed), _queue(stream)))
+    _check(lib().lora_experts_pack_weight(_whole("w", w, 0, _BF16 if bits == 16 else _E4M3), e, in_f, out_f, bits, dev_packed.data_ptr(), _nbytes(dev_packed), _queue(stream)))
 
 
 def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
@@ -733,20 +764,20 @@ def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
     except ValueError:
         (rows, in_f), (ldq, q1), (sr, sc), (lds, s1), (yr, out_f), (ldy, y1) = _two(q, "q") + _two(scales, "scales") + _two(y, "y")
     blocks = (in_f + 127) >> 7
-    if q1 != 1 or q.itemsize != 1:
-        _usable("q", q, rows, in_f, 1)
-    if sr < rows or sc < blocks or s1 != 1 or scales.itemsize != 4:
-        _usable("scales", scales, rows, blocks, 4)
-    if yr < rows or y1 != 1 or y.itemsize != 2:
-        _usable("y", y, rows, out_f, 2)
+    if q1 != 1 or q.dtype not in _E4M3:
+        _usable("q", q, rows, in_f, _E4M3)
+    if sr < rows or sc < blocks or s1 != 1 or scales.dtype not in _F32:
+        _usable("scales", scales, rows, blocks, _F32)
+    if yr < rows or y1 != 1 or y.dtype not in _BF16:
+        _usable("y", y, rows, out_f, _BF16)
     if rows == 1:
         ldq = in_f
     if sr == 1:
         lds = sc
     if yr == 1:
         ldy = out_f
-    status = (_lib or lib()).lora_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, rows, in_f, _whole("w_packed", w_packed, out_f * blocks << 7, 1),
-                                                _whole("w_scales", w_scales, (out_f >> 7) * blocks, 4), out_f, y.data_ptr(), ldy,
+    status = (_lib or lib()).lora_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, rows, in_f, _packed(w_packed, out_f * blocks << 7),
+                                                _whole("w_scales", w_scales, (out_f >> 7) * blocks, _F32), out_f, y.data_ptr(), ldy,
                                                 None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -765,11 +796,11 @@ def lora_experts_group(ids, starts, order, place, workspace=None, stream=None) -
     except ValueError:
         (tokens, picks), (ldi, i1) = _two(ids, "ids")
     n_experts, n = starts.numel() - 1, tokens * picks
-    if i1 != 1 or ids.itemsize != 4:
-        _usable("ids", ids, tokens, picks, 4)
+    if i1 != 1 or ids.dtype not in _INT32:
+        _usable("ids", ids, tokens, picks, _INT32)
     pw, nw = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
-    status = (_lib or lib()).lora_experts_group(ids.data_ptr(), ldi if tokens > 1 else picks, tokens, picks, n_experts, _whole("starts", starts, 1, 4),
-                                                _whole("order", order, n, 4), _whole("place", place, n, 4), pw, nw,
+    status = (_lib or lib()).lora_experts_group(ids.data_ptr(), ldi if tokens > 1 else picks, tokens, picks, n_experts, _whole("starts", starts, 1, _INT32),
+                                                _whole("order", order, n, _INT32), _whole("place", place, n, _INT32), pw, nw,
                                                 None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -783,17 +814,17 @@ def lora_experts_linear(x, starts, order, picks: int, w_packed, y, stream=None) 
     except ValueError:
         (tokens, in_f), (ldx, x1), (yr, out_f), (ldy, y1) = _two(x, "x") + _two(y, "y")
     n_experts, n_rows = starts.numel() - 1, tokens if order is None else tokens * picks
-    if x1 != 1 or x.itemsize != 2:
-        _usable("x", x, tokens, in_f, 2)
-    if yr < n_rows or y1 != 1 or y.itemsize != 2:
-        _usable("y", y, n_rows, out_f, 2)
+    if x1 != 1 or x.dtype not in _BF16:
+        _usable("x", x, tokens, in_f, _BF16)
+    if yr < n_rows or y1 != 1 or y.dtype not in _BF16:
+        _usable("y", y, n_rows, out_f, _BF16)
     if tokens == 1:
         ldx = in_f
     if yr == 1:
         ldy = out_f
-    status = (_lib or lib()).lora_experts_linear(x.data_ptr(), ldx, tokens, _whole("starts", starts, 1, 4),
-                                                 None if order is None else _whole("order", order, n_rows, 4), picks, n_rows, n_experts, in_f,
-                                                 _whole("w_packed", w_packed, n_experts * out_f * in_f << 1, 1), out_f, y.data_ptr(), ldy,
+    status = (_lib or lib()).lora_experts_linear(x.data_ptr(), ldx, tokens, _whole("starts", starts, 1, _INT32),
+                                                 None if order is None else _whole("order", order, n_rows, _INT32), picks, n_rows, n_experts, in_f,
+                                                 _packed(w_packed, n_experts * out_f * in_f << 1), out_f, y.data_ptr(), ldy,
                                                  None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -808,22 +839,22 @@ def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w
     except ValueError:
         (tokens, in_f), (ldq, q1), (sr, sc), (lds, s1), (yr, out_f), (ldy, y1) = _two(q, "q") + _two(scales, "scales") + _two(y, "y")
     n_experts, n_rows, blocks = starts.numel() - 1, tokens if order is None else tokens * picks, (in_f + 127) >> 7
-    if q1 != 1 or q.itemsize != 1:
-        _usable("q", q, tokens, in_f, 1)
-    if sr < tokens or sc < blocks or s1 != 1 or scales.itemsize != 4:
-        _usable("scales", scales, tokens, blocks, 4)
-    if yr < n_rows or y1 != 1 or y.itemsize != 2:
-        _usable("y", y, n_rows, out_f, 2)
+    if q1 != 1 or q.dtype not in _E4M3:
+        _usable("q", q, tokens, in_f, _E4M3)
+    if sr < tokens or sc < blocks or s1 != 1 or scales.dtype not in _F32:
+        _usable("scales", scales, tokens, blocks, _F32)
+    if yr < n_rows or y1 != 1 or y.dtype not in _BF16:
+        _usable("y", y, n_rows, out_f, _BF16)
     if tokens == 1:
         ldq = in_f
     if sr == 1:
         lds = sc
     if yr == 1:
         ldy = out_f
-    status = (_lib or lib()).lora_experts_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, tokens, _whole("starts", starts, 1, 4),
-                                                        None if order is None else _whole("order", order, n_rows, 4), picks, n_rows, n_experts, in_f,
-                                                        _whole("w_packed", w_packed, n_experts * out_f * blocks << 7, 1),
-                                                        _whole("w_scales", w_scales, n_experts * (out_f >> 7) * blocks, 4), out_f, y.data_ptr(), ldy,
+    status = (_lib or lib()).lora_experts_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, tokens, _whole("starts", starts, 1, _INT32),
+                                                        None if order is None else _whole("order", order, n_rows, _INT32), picks, n_rows, n_experts, in_f,
+                                                        _packed(w_packed, n_experts * out_f * blocks << 7),
+                                                        _whole("w_scales", w_scales, n_experts * (out_f >> 7) * blocks, _F32), out_f, y.data_ptr(), ldy,
                                                         None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -838,15 +869,15 @@ def lora_experts_combine(y, place, weights, z, stream=None) -> None:
     except ValueError:
         (yr, yc), (ldy, y1), (zr, out_f), (ldz, z1), (tokens, picks), _ = _two(y, "y") + _two(z, "z") + _two(weights, "weights")
     n = tokens * picks
-    if yc < out_f or y1 != 1 or y.itemsize != 2:
-        _usable("y", y, 0, out_f, 2)
-    if zr < tokens or z1 != 1 or z.itemsize != 2:
-        _usable("z", z, tokens, out_f, 2)
+    if yc < out_f or y1 != 1 or y.dtype not in _BF16:
+        _usable("y", y, 0, out_f, _BF16)
+    if zr < tokens or z1 != 1 or z.dtype not in _BF16:
+        _usable("z", z, tokens, out_f, _BF16)
     if yr == 1:
         ldy = yc
     if zr == 1:
         ldz = out_f
-    status = (_lib or lib()).lora_experts_combine(y.data_ptr(), ldy, yr, _whole("place", place, n, 4), _whole("weights", weights, n, 4), tokens, picks, out_f,
+    status = (_lib or lib()).lora_experts_combine(y.data_ptr(), ldy, yr, _whole("place", place, n, _INT32), _whole("weights", weights, n, _F32), tokens, picks, out_f,
                                                   z.data_ptr(), ldz, None if stream is None else _queue(stream))
     if status:
         _check(status)

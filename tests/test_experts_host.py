@@ -132,3 +132,35 @@ def test_the_binding_refuses_tensors_that_are_too_small_or_of_another_type():
     ("lora_experts_linear", EXPERTS, dict(tokens=1 << 20, order=None, rows=1 << 20, ldx=1 << 16))])
 def test_rows_beyond_what_the_kernels_reach_are_refused(name, base, change):
     assert status(name, *dict(base, **change).values(), None) == "LORA_ERR_SHAPE"
+
+
+# ---- the binding, on tensors that would do but for one thing ------------------------------------------------
+def good(device="cpu"):
+    """{call: its tensors by name, in order}: 4 rows, 256 -> 128 features, 8 experts, 2 tokens of 2 picks"""
+    bf, f8, i32 = torch.bfloat16, torch.float8_e4m3fn, torch.int32
+    e = lambda *shape, dtype=torch.float32: torch.zeros(*shape, device=device).to(dtype)  # noqa: E731
+    x, q, s, y = e(4, 256, dtype=bf), e(4, 256, dtype=f8), e(4, 2), e(4, 128, dtype=bf)
+    starts, order, place, ids = e(9, dtype=i32), e(4, dtype=i32), e(2, 2, dtype=i32), e(2, 2, dtype=i32)
+    raw = lambda n: e(n, dtype=torch.uint8)  # noqa: E731
+    return {
+        "lora_rows_quantize": dict(x=x, q=q, scales=s),
+        "lora_linear_scaled": dict(q=q, scales=s, w_packed=raw(128 * 256), w_scales=e(1, 2), y=y),
+        "lora_experts_group": dict(ids=ids, starts=starts, order=order, place=place),
+        "lora_experts_linear": dict(x=x[:2], starts=starts, order=order, picks=2, w_packed=raw(8 * 128 * 512), y=y),
+        "lora_experts_linear_scaled": dict(q=q[:2], scales=s[:2], starts=starts, order=order, picks=2, w_packed=raw(8 * 128 * 256), w_scales=e(8, 1, 2), y=y),
+        "lora_experts_combine": dict(y=y, place=place, weights=e(2, 2), z=y[:2]),
+        "lora_experts_pack_weight": dict(w=e(1, 128, 256, dtype=f8), dev_packed=raw(128 * 256)),
+    }
+
+
+SAME_SIZE = {torch.bfloat16: (torch.float16, torch.int16), torch.float8_e4m3fn: (torch.float8_e5m2, torch.float8_e4m3fnuz, torch.int8, torch.bool),
+             torch.float32: (torch.int32,), torch.int32: (torch.float32, torch.uint32)}
+
+
+@pytest.mark.parametrize("call, name, dtype", [(c, n, d) for c, given in good().items() for n, t in given.items() if isinstance(t, torch.Tensor)
+                                               for d in SAME_SIZE.get(t.dtype, ())])
+def test_the_binding_refuses_types_of_the_same_size(call, name, dtype):
+    given = good()[call]
+    given[name] = given[name].to(torch.float32).to(dtype)
+    with pytest.raises(ValueError, match=f"^{name}: {dtype} does not do"):
+        getattr(L, call)(**given)
