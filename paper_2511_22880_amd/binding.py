@@ -652,8 +652,8 @@ def lora_place_assign(n_servers: int, ranks, demand_tps, operating_points: dict,
 
 
 # ---- frozen layers beside an adapter, in block-scaled 8 bits and grouped by expert (include/lora_experts.h) ----------------
-# The arguments are torch device tensors, whose shapes and strides say what the C calls are told; a tensor of another type, or one that cannot hold what
-# a call writes or reads there, is refused here, since the library sees addresses only.
+# The arguments are torch device tensors, whose shapes and strides say what the C calls are told; a tensor of another type, one that is not on a GPU, or one that
+# cannot hold what a call writes or reads there, is refused here, since the library sees addresses only.
 # Element types, filled in when the first tensor comes (this module does not import torch).  bf16 and 8-bit values may also come as their bits.
 _BF16, _F32, _INT32, _E4M3 = set(), set(), set(), set()
 
@@ -676,6 +676,11 @@ def _names(types) -> str:
     return " or ".join(sorted(str(t).replace("torch.", "") for t in types))
 
 
+def _on_gpu(name: str, t) -> None:
+    if not t.is_cuda:
+        raise ValueError(f"{name}: a tensor on {t.device} does not do: one on the GPU is meant")
+
+
 def _usable(name: str, t, rows: int, columns: int, types: set) -> None:
     """Refuses a tensor that does not hold so many rows of so many elements of one of these types, side by side within a row."""
     if not types:
@@ -684,6 +689,7 @@ def _usable(name: str, t, rows: int, columns: int, types: set) -> None:
         raise ValueError(f"{name}: {t.dtype} does not do: {_names(types)} is meant")
     if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < columns or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()} does not do: {rows} rows of {columns} elements side by side are meant")
+    _on_gpu(name, t)
 
 
 def _whole(name: str, t, n: int, types: set):
@@ -695,6 +701,8 @@ def _whole(name: str, t, n: int, types: set):
             raise ValueError(f"{name}: {t.dtype} does not do: {_names(types)} is meant")
     if t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()} does not do: {n} contiguous elements are meant")
+    if not t.is_cuda:
+        _on_gpu(name, t)
     return t.data_ptr()
 
 
@@ -702,6 +710,8 @@ def _packed(t, n: int):
     """Address of packed weights, n bytes of whatever type."""
     if t.itemsize != 1 or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"w_packed: {tuple(t.shape)} of {t.dtype} does not do: {n} contiguous bytes are meant")
+    if not t.is_cuda:
+        _on_gpu("w_packed", t)
     return t.data_ptr()
 
 
@@ -721,11 +731,11 @@ def lora_rows_quantize(x, q, scales, stream=None) -> None:
     except ValueError:
         (rows, in_f), (ldx, x1), (qr, qc), (ldq, q1), (sr, sc), (lds, s1) = _two(x, "x") + _two(q, "q") + _two(scales, "scales")
     blocks = (in_f + 127) >> 7
-    if x1 != 1 or x.dtype not in _BF16:
+    if x1 != 1 or x.dtype not in _BF16 or not x.is_cuda:
         _usable("x", x, rows, in_f, _BF16)
-    if qr < rows or qc < blocks << 7 or q1 != 1 or q.dtype not in _E4M3:
+    if qr < rows or qc < blocks << 7 or q1 != 1 or q.dtype not in _E4M3 or not q.is_cuda:
         _usable("q", q, rows, blocks << 7, _E4M3)
-    if sr < rows or sc < blocks or s1 != 1 or scales.dtype not in _F32:
+    if sr < rows or sc < blocks or s1 != 1 or scales.dtype not in _F32 or not scales.is_cuda:
         _usable("scales", scales, rows, blocks, _F32)
     if rows == 1:  # (of a single row torch states any stride)
         ldx = in_f
@@ -752,6 +762,7 @@ def lora_experts_pack_weight(w, dev_packed, stream=None, in_features: Optional[i
     in_f = row if in_features is None else int(in_features)
     if row != (in_f if bits == 16 else _blocks(in_f) << 7):
         raise ValueError(f"w: rows of {row} elements are not those of {in_f} input features")
+    _on_gpu("dev_packed", dev_packed)
     _check(lib().lora_experts_pack_weight(_whole("w", w, 0, _BF16 if bits == 16 else _E4M3), e, in_f, out_f, bits, dev_packed.data_ptr(), _nbytes(dev_packed), _queue(stream)))
 
 
@@ -764,11 +775,11 @@ def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
     except ValueError:
         (rows, in_f), (ldq, q1), (sr, sc), (lds, s1), (yr, out_f), (ldy, y1) = _two(q, "q") + _two(scales, "scales") + _two(y, "y")
     blocks = (in_f + 127) >> 7
-    if q1 != 1 or q.dtype not in _E4M3:
+    if q1 != 1 or q.dtype not in _E4M3 or not q.is_cuda:
         _usable("q", q, rows, in_f, _E4M3)
-    if sr < rows or sc < blocks or s1 != 1 or scales.dtype not in _F32:
+    if sr < rows or sc < blocks or s1 != 1 or scales.dtype not in _F32 or not scales.is_cuda:
         _usable("scales", scales, rows, blocks, _F32)
-    if yr < rows or y1 != 1 or y.dtype not in _BF16:
+    if yr < rows or y1 != 1 or y.dtype not in _BF16 or not y.is_cuda:
         _usable("y", y, rows, out_f, _BF16)
     if rows == 1:
         ldq = in_f
@@ -796,9 +807,15 @@ def lora_experts_group(ids, starts, order, place, workspace=None, stream=None) -
     except ValueError:
         (tokens, picks), (ldi, i1) = _two(ids, "ids")
     n_experts, n = starts.numel() - 1, tokens * picks
-    if i1 != 1 or ids.dtype not in _INT32:
+    if i1 != 1 or ids.dtype not in _INT32 or not ids.is_cuda:
         _usable("ids", ids, tokens, picks, _INT32)
-    pw, nw = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    if workspace is None:
+        pw, nw = None, 0
+    else:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            _on_gpu("workspace", workspace)
+            raise ValueError(f"workspace: strides {workspace.stride()} do not do: contiguous bytes are meant")
+        pw, nw = workspace.data_ptr(), workspace.nbytes
     status = (_lib or lib()).lora_experts_group(ids.data_ptr(), ldi if tokens > 1 else picks, tokens, picks, n_experts, _whole("starts", starts, 1, _INT32),
                                                 _whole("order", order, n, _INT32), _whole("place", place, n, _INT32), pw, nw,
                                                 None if stream is None else _queue(stream))
@@ -814,9 +831,9 @@ def lora_experts_linear(x, starts, order, picks: int, w_packed, y, stream=None) 
     except ValueError:
         (tokens, in_f), (ldx, x1), (yr, out_f), (ldy, y1) = _two(x, "x") + _two(y, "y")
     n_experts, n_rows = starts.numel() - 1, tokens if order is None else tokens * picks
-    if x1 != 1 or x.dtype not in _BF16:
+    if x1 != 1 or x.dtype not in _BF16 or not x.is_cuda:
         _usable("x", x, tokens, in_f, _BF16)
-    if yr < n_rows or y1 != 1 or y.dtype not in _BF16:
+    if yr < n_rows or y1 != 1 or y.dtype not in _BF16 or not y.is_cuda:
         _usable("y", y, n_rows, out_f, _BF16)
     if tokens == 1:
         ldx = in_f
@@ -839,11 +856,11 @@ def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w
     except ValueError:
         (tokens, in_f), (ldq, q1), (sr, sc), (lds, s1), (yr, out_f), (ldy, y1) = _two(q, "q") + _two(scales, "scales") + _two(y, "y")
     n_experts, n_rows, blocks = starts.numel() - 1, tokens if order is None else tokens * picks, (in_f + 127) >> 7
-    if q1 != 1 or q.dtype not in _E4M3:
+    if q1 != 1 or q.dtype not in _E4M3 or not q.is_cuda:
         _usable("q", q, tokens, in_f, _E4M3)
-    if sr < tokens or sc < blocks or s1 != 1 or scales.dtype not in _F32:
+    if sr < tokens or sc < blocks or s1 != 1 or scales.dtype not in _F32 or not scales.is_cuda:
         _usable("scales", scales, tokens, blocks, _F32)
-    if yr < n_rows or y1 != 1 or y.dtype not in _BF16:
+    if yr < n_rows or y1 != 1 or y.dtype not in _BF16 or not y.is_cuda:
         _usable("y", y, n_rows, out_f, _BF16)
     if tokens == 1:
         ldq = in_f
@@ -869,9 +886,9 @@ def lora_experts_combine(y, place, weights, z, stream=None) -> None:
     except ValueError:
         (yr, yc), (ldy, y1), (zr, out_f), (ldz, z1), (tokens, picks), _ = _two(y, "y") + _two(z, "z") + _two(weights, "weights")
     n = tokens * picks
-    if yc < out_f or y1 != 1 or y.dtype not in _BF16:
+    if yc < out_f or y1 != 1 or y.dtype not in _BF16 or not y.is_cuda:
         _usable("y", y, 0, out_f, _BF16)
-    if zr < tokens or z1 != 1 or z.dtype not in _BF16:
+    if zr < tokens or z1 != 1 or z.dtype not in _BF16 or not z.is_cuda:
         _usable("z", z, tokens, out_f, _BF16)
     if yr == 1:
         ldy = yc

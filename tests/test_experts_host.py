@@ -135,10 +135,15 @@ def test_rows_beyond_what_the_kernels_reach_are_refused(name, base, change):
 
 
 # ---- the binding, on tensors that would do but for one thing ------------------------------------------------
-def good(device="cpu"):
+class OnGpu(torch.Tensor):
+    """A tensor that stands on the GPU as far as the binding can tell."""
+    is_cuda = True
+
+
+def good():
     """{call: its tensors by name, in order}: 4 rows, 256 -> 128 features, 8 experts, 2 tokens of 2 picks"""
     bf, f8, i32 = torch.bfloat16, torch.float8_e4m3fn, torch.int32
-    e = lambda *shape, dtype=torch.float32: torch.zeros(*shape, device=device).to(dtype)  # noqa: E731
+    e = lambda *shape, dtype=torch.float32: torch.zeros(*shape).to(dtype).as_subclass(OnGpu)  # noqa: E731
     x, q, s, y = e(4, 256, dtype=bf), e(4, 256, dtype=f8), e(4, 2), e(4, 128, dtype=bf)
     starts, order, place, ids = e(9, dtype=i32), e(4, dtype=i32), e(2, 2, dtype=i32), e(2, 2, dtype=i32)
     raw = lambda n: e(n, dtype=torch.uint8)  # noqa: E731
@@ -163,4 +168,13 @@ def test_the_binding_refuses_types_of_the_same_size(call, name, dtype):
     given = good()[call]
     given[name] = given[name].to(torch.float32).to(dtype)
     with pytest.raises(ValueError, match=f"^{name}: {dtype} does not do"):
+        getattr(L, call)(**given)
+
+
+@pytest.mark.parametrize("call, name", [(c, n) for c, given in good().items() for n, t in given.items() if isinstance(t, torch.Tensor)]
+                         + [("lora_experts_group", "workspace")])
+def test_the_binding_refuses_tensors_of_the_host(call, name):
+    given = good()[call]
+    given[name] = given[name].as_subclass(torch.Tensor) if name in given else torch.zeros(64, dtype=torch.uint8)
+    with pytest.raises(ValueError, match=f"^{name}: a tensor on cpu does not do"):
         getattr(L, call)(**given)
