@@ -722,6 +722,12 @@ def _two(t, name: str):
     return t.shape, t.stride()
 
 
+def _last_block(q, rows: int, ldq: int, row: int) -> None:
+    """The products read a row's last block of 128 whole, so memory goes on that far behind columns that end inside it."""
+    if q.storage_offset() + (rows - 1) * ldq + row > q.untyped_storage().nbytes():
+        raise ValueError(f"q: the last row's block of 128 that column {q.shape[1]} ends in is not all there")
+
+
 def lora_rows_quantize(x, q, scales, stream=None) -> None:
     """x: bf16 [rows][in]; q: 8-bit [rows][128 * blocks]; scales: fp32 [rows][blocks]."""
     try:
@@ -767,7 +773,7 @@ def lora_experts_pack_weight(w, dev_packed, stream=None, in_features: Optional[i
 
 
 def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
-    """q, scales: of lora_rows_quantize; w_packed: uint8; w_scales: fp32 [out / 128][blocks]; y: bf16 [rows][out]."""
+    """q, scales: of lora_rows_quantize, q's columns all or the first in_features; w_packed: uint8; w_scales: fp32 [out / 128][blocks]; y: bf16 [rows][out]."""
     try:
         (rows, in_f), (ldq, q1) = q.shape, q.stride()
         (sr, sc), (lds, s1) = scales.shape, scales.stride()
@@ -782,7 +788,9 @@ def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
     if yr < rows or y1 != 1 or y.dtype not in _BF16 or not y.is_cuda:
         _usable("y", y, rows, out_f, _BF16)
     if rows == 1:
-        ldq = in_f
+        ldq = blocks << 7
+    if in_f & 127:
+        _last_block(q, rows, ldq, blocks << 7)
     if sr == 1:
         lds = sc
     if yr == 1:
@@ -863,7 +871,9 @@ def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w
     if yr < n_rows or y1 != 1 or y.dtype not in _BF16 or not y.is_cuda:
         _usable("y", y, n_rows, out_f, _BF16)
     if tokens == 1:
-        ldq = in_f
+        ldq = blocks << 7
+    if in_f & 127:
+        _last_block(q, tokens, ldq, blocks << 7)
     if sr == 1:
         lds = sc
     if yr == 1:

@@ -178,3 +178,35 @@ def test_the_binding_refuses_tensors_of_the_host(call, name):
     given[name] = given[name].as_subclass(torch.Tensor) if name in given else torch.zeros(64, dtype=torch.uint8)
     with pytest.raises(ValueError, match=f"^{name}: a tensor on cpu does not do"):
         getattr(L, call)(**given)
+
+
+def eights(q, scales, call):
+    """the tensors of a product in 8 bits, 192 -> 128 features, of one layer or of one expert"""
+    e = lambda *shape, dtype=torch.float32: torch.zeros(*shape).to(dtype).as_subclass(OnGpu)  # noqa: E731
+    w, ws, y = e(128 * 256, dtype=torch.uint8), e(1, 1, 2), e(q.shape[0], 128, dtype=torch.bfloat16)
+    if call == "lora_linear_scaled":
+        return q, scales, w, ws[0], y
+    return q, scales, e(2, dtype=torch.int32), None, 1, w, ws, y
+
+
+@pytest.mark.parametrize("call", ["lora_linear_scaled", "lora_experts_linear_scaled"])
+@pytest.mark.parametrize("rows", [1, 3])
+def test_the_binding_refuses_rows_whose_last_block_is_not_in_memory(call, rows):
+    q = torch.zeros(rows, 256, dtype=torch.float8_e4m3fn).as_subclass(OnGpu)[:, 64:]  # 192 columns: the last row has 64 too few
+    with pytest.raises(ValueError, match="^q: the last row's block of 128"):
+        getattr(L, call)(*eights(q, torch.zeros(rows, 2).as_subclass(OnGpu), call))
+
+
+@pytest.mark.parametrize("call", ["lora_linear_scaled", "lora_experts_linear_scaled"])
+@pytest.mark.parametrize("rows", [1, 3])
+def test_the_binding_takes_the_columns_that_are_there_of_rows_of_whole_blocks(call, rows, monkeypatch):
+    told = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: told.append((name, *args)) or 0
+    monkeypatch.setattr(L, "_lib", Library())
+    q = torch.zeros(rows, 256, dtype=torch.float8_e4m3fn).as_subclass(OnGpu)[:, :192]
+    getattr(L, call)(*eights(q, torch.zeros(rows, 2).as_subclass(OnGpu), call))
+    name, address, ldq, _, _, n = told[0][:6]
+    assert (name, address, ldq, n) == (call, q.data_ptr(), 256, rows) and 192 in told[0]

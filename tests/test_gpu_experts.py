@@ -574,3 +574,14 @@ def test_linear_scaled_where_the_scales_product_is_no_normal_number(rows, in_f, 
     y = torch.full((rows, out_f), float("nan"), dtype=BF, device="cuda")
     L.lora_linear_scaled(q, s, packed(w), ws, y)
     close(y, *product8(q, s, w[0], ws[0]))
+
+
+@pytest.mark.parametrize("rows", [1, 5])
+def test_linear_scaled_on_the_columns_that_are_there_of_rows_of_whole_blocks(rows):
+    g = gen(rows)
+    q, s = rows8(g, rows, 192)
+    w, ws = weights8(g, 1, 128, 192)
+    y = torch.empty(rows, 128, dtype=BF, device="cuda")
+    L.lora_linear_scaled(q[:, :192], s, packed(w, 192), ws, y)
+    w[:, :, 192:] = 0.0
+    close(y, *product8(q, s, w[0], ws[0]))
