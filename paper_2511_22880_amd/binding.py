@@ -815,6 +815,8 @@ def lora_experts_group(ids, starts, order, place, workspace=None, stream=None) -
     except ValueError:
         (tokens, picks), (ldi, i1) = _two(ids, "ids")
     n_experts, n = starts.numel() - 1, tokens * picks
+    if n > 0x7FFFFFFF:  # (ctypes passes on the low 32 bits of the tokens)
+        raise ValueError(f"ids: {tokens} tokens x {picks} picks do not fit 32 bits")
     if i1 != 1 or ids.dtype not in _INT32 or not ids.is_cuda:
         _usable("ids", ids, tokens, picks, _INT32)
     if workspace is None:

@@ -210,3 +210,19 @@ def test_the_binding_takes_the_columns_that_are_there_of_rows_of_whole_blocks(ca
     getattr(L, call)(*eights(q, torch.zeros(rows, 2).as_subclass(OnGpu), call))
     name, address, ldq, _, _, n = told[0][:6]
     assert (name, address, ldq, n) == (call, q.data_ptr(), 256, rows) and 192 in told[0]
+
+
+def test_the_binding_refuses_more_picks_than_32_bits_count(monkeypatch):
+    told = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: told.append(args) or 0
+    monkeypatch.setattr(L, "_lib", Library())
+    e = lambda *shape: torch.empty(*shape, dtype=torch.int32, device="meta").as_subclass(OnGpu)  # noqa: E731
+    n = 2 ** 32 + 5
+    with pytest.raises(ValueError, match="^ids: 4294967301 tokens x 1 picks"):
+        L.lora_experts_group(e(n, 1), e(9), e(n), e(n))
+    assert not told
+    L.lora_experts_group(e(5, 1), e(9), e(5), e(5))
+    assert told[0][2] == 5
