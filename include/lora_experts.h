@@ -71,7 +71,8 @@ lora_status_t lora_linear_scaled(const void *q, int64_t ldq, const float *scales
  *   order[p]: the pick at place p, the picks of an expert in their own order, -1 from starts[n_experts] on;
  *   place[i]: the place of pick i, or -1.
  * No atomics whose order could show: the same ids give the same bits.  workspace: device, 16-byte aligned, as many bytes as
- * lora_experts_group_workspace_bytes says (0 is possible); its contents are of no account. */
+ * lora_experts_group_workspace_bytes says (0 is possible); its contents are of no account.  What that says for a number of picks and of experts is enough for
+ * any smaller ones. */
 lora_status_t lora_experts_group_workspace_bytes(int64_t n_picks, int32_t n_experts, size_t *bytes);
 lora_status_t lora_experts_group(const int32_t *ids, int64_t ld_ids, int32_t tokens, int32_t picks, int32_t n_experts, int32_t *starts,
                                  int32_t *order, int32_t *place, void *workspace, size_t ws_bytes, void *stream);

@@ -220,7 +220,7 @@ extern "C" lora_status_t lora_experts_group_workspace_bytes(int64_t n_picks, int
     if (!bytes) return fail(LORA_ERR_INVALID_ARG, "bytes is NULL");
     if (n_picks < 0 || n_picks > INT32_MAX) return fail(LORA_ERR_INVALID_ARG, "n_picks = %lld", (long long)n_picks);
     TRY(check_experts(n_experts));
-    *bytes = lora::group_counts(n_picks) ? (size_t)lora::group_chunks(n_picks) * n_experts * sizeof(int32_t) : 0;
+    *bytes = lora::group_counts(n_picks) ? (size_t)lora::group_most_chunks(n_picks) * n_experts * sizeof(int32_t) : 0;
     return LORA_OK;
 }
 
@@ -228,8 +228,9 @@ extern "C" lora_status_t lora_experts_group(const int32_t *ids, int64_t ld_ids, 
                                             int32_t *order, int32_t *place, void *workspace, size_t ws_bytes, void *stream)
 {
     TRY(check_picks(tokens, picks));
-    size_t need = 0;
-    TRY(lora_experts_group_workspace_bytes((int64_t)tokens * picks, n_experts, &need));
+    TRY(check_experts(n_experts));
+    const int64_t n = (int64_t)tokens * picks;
+    const size_t need = lora::group_counts(n) ? (size_t)lora::group_chunks(n) * n_experts * sizeof(int32_t) : 0;
     TRY(check_values(starts, "starts"));
     if (tokens > 0) {
         TRY(check_values(ids, "ids"));

@@ -24,6 +24,8 @@ inline int64_t group_chunk(int64_t n_picks)
 }
 inline int group_chunks(int64_t n_picks) { const int64_t c = group_chunk(n_picks); return (int)((n_picks + c - 1) / c); }
 inline bool group_counts(int64_t n_picks) { return n_picks > kGroupAlone * kGroupUnit; }
+// as many work groups as any number of picks up to this one has (from 2^19, 2^20, 2^21 and every multiple of 2^22 picks on a work group takes more, and they are fewer)
+inline int group_most_chunks(int64_t n_picks) { return n_picks > (int64_t)2 * kGroupUnit * kGroupMaxChunks ? kGroupMaxChunks : group_chunks(n_picks); }
 
 // Rows of x, by expert, times the experts' weights (see include/lora_experts.h).  starts == NULL: one expert that has all rows.
 struct ExpertsArgs {

@@ -226,3 +226,12 @@ def test_the_binding_refuses_more_picks_than_32_bits_count(monkeypatch):
     assert not told
     L.lora_experts_group(e(5, 1), e(9), e(5), e(5))
     assert told[0][2] == 5
+
+
+def test_a_workspace_of_more_picks_is_enough_for_fewer():
+    """by what the calls say of themselves: at every line where a work group takes more picks, and on either side of it"""
+    ends = sorted({max(0, m * 2 ** k + d) for k in range(9, 26) for m in (1, 3) for d in (-1, 0, 1)} | {65000 * 8, 66000 * 8, 2 ** 31 - 1})
+    for experts in (1, 256, 512):
+        said = [L.lora_experts_group_workspace_bytes(n, experts) for n in ends]
+        assert said == sorted(said)
+    assert L.lora_experts_group_workspace_bytes(10 ** 6, 7) <= L.lora_experts_group_workspace_bytes(10 ** 6, 8)

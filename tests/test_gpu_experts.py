@@ -585,3 +585,14 @@ def test_linear_scaled_on_the_columns_that_are_there_of_rows_of_whole_blocks(row
     L.lora_linear_scaled(q[:, :192], s, packed(w, 192), ws, y)
     w[:, :, 192:] = 0.0
     close(y, *product8(q, s, w[0], ws[0]))
+
+
+@pytest.mark.parametrize("tokens, room", [(65000, 66000), (131000, 140000), (262143, 262145)])
+def test_group_with_the_workspace_of_more_picks(tokens, room):
+    """what a program that makes its buffers once, for the most tokens it takes, has at hand"""
+    ids = torch.randint(-1, 256, (tokens, 8), generator=gen(tokens), device="cuda", dtype=torch.int32)
+    n = ids.numel()
+    st, od, pl = (torch.empty(k, dtype=torch.int32, device="cuda") for k in (257, n, n))
+    L.lora_experts_group(ids, st, od, pl, torch.empty(L.lora_experts_group_workspace_bytes(room * 8, 256), dtype=torch.uint8, device="cuda"))
+    for a, b in zip((st, od, pl), grouped(ids, 256)):
+        assert np.array_equal(a.cpu().numpy(), b)
