@@ -9,9 +9,13 @@ namespace lora {
 constexpr int kScaleBlock = 128;     // values of a row, or of a row and a column of a weight, that share a scale
 constexpr int kPieceBytes = 128;     // of a row: what the products walk k in (64 bf16 or 128 8-bit values)
 constexpr int kMaxExperts = 512;     // (a work group that groups picks has a count of each for 16 wavefronts in LDS)
+constexpr int kQuantizeBlocks = 2;   // of 128 values a thread that rounds to 8 bits has a part of, a sixteenth each
 constexpr int kGroupUnit = 1024;      // picks of a work group that groups them: 1, 2, 4, 8 or a multiple of 16 times as many
 constexpr int kGroupAlone = 8;        // up to so many work groups each look at all picks; with more a launch counts ahead
 constexpr int kGroupMaxChunks = 256;  // of either launch then
+
+// rows of a launch that rounds rows of so many blocks: the runtime launches fewer than 2^32 threads (256 for 16 kQuantizeBlocks blocks)
+inline int64_t quantize_rows_at_once(int blocks) { return ((int64_t)1 << 28) / blocks; }
 
 // picks of a work group
 inline int64_t group_chunk(int64_t n_picks)

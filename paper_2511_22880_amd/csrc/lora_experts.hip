@@ -1100,8 +1100,6 @@ hipError_t launch_experts_pack(const char *w, int64_t n_experts, int row_bytes, 
 static __device__ __forceinline__ float value_lo(uint32_t u) { return __uint_as_float(u << 16); }
 static __device__ __forceinline__ float value_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
 
-constexpr int kQuantizeBlocks = 2;  // of 128 a thread has a part of
-
 __global__ __launch_bounds__(256) void k_rows_quantize(const uint16_t *__restrict__ x, int64_t ldx, unsigned total, int in, unsigned blocks,
                                                        uint8_t *__restrict__ q, int64_t ldq, float *__restrict__ scales, int64_t ld_scales)
 {
@@ -1167,7 +1165,7 @@ hipError_t launch_rows_quantize(const uint16_t *x, int64_t ldx, int64_t rows, in
                                 int64_t ld_scales, hipStream_t stream)
 {
     const int blocks = (in + kScaleBlock - 1) / kScaleBlock;
-    const int64_t most = ((int64_t)1 << 31) / blocks;  // rows of a launch, whose blocks are counted in 32 bits
+    const int64_t most = quantize_rows_at_once(blocks);
     for (int64_t r = 0; r < rows; r += most) {
         const int64_t total = (rows - r < most ? rows - r : most) * blocks;
         hipLaunchKernelGGL(k_rows_quantize, dim3((unsigned)((total + 16 * kQuantizeBlocks - 1) / (16 * kQuantizeBlocks))), dim3(256), 0, stream,

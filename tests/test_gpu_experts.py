@@ -596,3 +596,26 @@ def test_group_with_the_workspace_of_more_picks(tokens, room):
     L.lora_experts_group(ids, st, od, pl, torch.empty(L.lora_experts_group_workspace_bytes(room * 8, 256), dtype=torch.uint8, device="cuda"))
     for a, b in zip((st, od, pl), grouped(ids, 256)):
         assert np.array_equal(a.cpu().numpy(), b)
+
+
+def test_quantize_more_rows_than_a_launch_takes():
+    """2^28 + 4099 blocks of 128: 64 GiB of x, in repetitions of 4096 rows, and other rows behind them"""
+    torch.cuda.empty_cache()
+    pattern = (torch.randn(4096, 128, generator=gen(1), device="cuda") * 30).to(BF)
+    rest = (torch.randn(4099, 128, generator=gen(2), device="cuda") * 3).to(BF)
+    n = 1 << 28
+    x = torch.empty(n + 4099, 128, dtype=BF, device="cuda")
+    x[:n].view(-1, 4096, 128).copy_(pattern)
+    x[n:] = rest
+    q = torch.empty(x.shape, dtype=torch.uint8, device="cuda")
+    s = torch.empty(x.shape[0], 1, device="cuda")
+    L.lora_rows_quantize(x, q, s)
+    del x
+    rq, rs = quantized(pattern)
+    rq = rq.float().to(F8).view(torch.uint8)
+    for a in range(0, n, 1 << 24):
+        assert (q[a:a + (1 << 24)].view(-1, 4096, 128) == rq).all() and (s[a:a + (1 << 24)].view(-1, 4096, 1) == rs).all(), a
+    rq, rs = quantized(rest)
+    assert torch.equal(q[n:].view(F8).double(), rq) and torch.equal(s[n:], rs)
+    del q, s
+    torch.cuda.empty_cache()
