@@ -164,6 +164,14 @@ static lora_status_t check_product(lora::ExpertsArgs &a, int bits, const void *x
     return LORA_OK;
 }
 
+static lora_status_t launch_product(const lora::ExpertsArgs &a, int bits, void *stream, const char *what)
+{
+    const hipError_t e = lora::launch_experts_linear(a, bits == 8, (hipStream_t)stream);
+    if (e == hipErrorInvalidConfiguration)
+        return fail(LORA_ERR_SHAPE, "%s: %d rows of %d experts x %d out_features are more tiles than a launch can have", what, a.n_rows, a.n_experts, a.out);
+    return of_hip(e, what);
+}
+
 extern "C" lora_status_t lora_linear_scaled(const void *q, int64_t ldq, const float *scales, int64_t ld_scales, int32_t rows, int32_t in_features,
                                             const void *w_packed, const float *w_scales, int32_t out_features, void *y, int64_t ldy, void *stream)
 {
@@ -171,7 +179,7 @@ extern "C" lora_status_t lora_linear_scaled(const void *q, int64_t ldq, const fl
     a.tokens = a.n_rows = rows;
     a.n_experts = a.picks = 1;
     TRY(check_product(a, 8, q, ldq, scales, ld_scales, in_features, w_packed, w_scales, out_features, y, ldy));
-    return a.n_rows == 0 ? LORA_OK : of_hip(lora::launch_experts_linear(a, true, (hipStream_t)stream), "lora_linear_scaled");
+    return a.n_rows == 0 ? LORA_OK : launch_product(a, 8, stream, "lora_linear_scaled");
 }
 
 static lora_status_t experts_linear(int bits, const void *x, int64_t ldx, const float *scales, int64_t ld_scales, int32_t tokens,
@@ -195,7 +203,7 @@ static lora_status_t experts_linear(int bits, const void *x, int64_t ldx, const 
     if (a.n_rows == 0) return LORA_OK;
     TRY(check_values(starts, "starts"));
     if (order) TRY(check_values(order, "order"));
-    return of_hip(lora::launch_experts_linear(a, bits == 8, (hipStream_t)stream), what);
+    return launch_product(a, bits, stream, what);
 }
 
 extern "C" lora_status_t lora_experts_linear(const void *x, int64_t ldx, int32_t tokens, const int32_t *starts, const int32_t *order, int32_t picks,

@@ -14,7 +14,10 @@ constexpr int kGroupUnit = 1024;      // picks of a work group that groups them:
 constexpr int kGroupAlone = 8;        // up to so many work groups each look at all picks; with more a launch counts ahead
 constexpr int kGroupMaxChunks = 256;  // of either launch then
 
-// rows of a launch that rounds rows of so many blocks: the runtime launches fewer than 2^32 threads (256 for 16 kQuantizeBlocks blocks)
+// the runtime launches fewer than 2^32 threads
+inline bool can_launch(int64_t work_groups, int threads) { return work_groups <= (int64_t)UINT32_MAX / threads; }
+
+// rows of a launch that rounds rows of so many blocks (256 threads for 16 kQuantizeBlocks blocks)
 inline int64_t quantize_rows_at_once(int blocks) { return ((int64_t)1 << 28) / blocks; }
 
 // picks of a work group
@@ -50,6 +53,7 @@ struct ExpertsArgs {
     uint16_t *y;
     int64_t ldy;
 };
+// hipErrorInvalidConfiguration, and nothing is launched, where there are more tiles than a launch can have.
 hipError_t launch_experts_linear(const ExpertsArgs &a, bool bits8, hipStream_t stream);
 
 // W [experts][out][row_bytes] -> operand order (see the kernels).  row_bytes: whole pieces, of which the bytes behind used_bytes become zero.

@@ -408,7 +408,7 @@ static hipError_t launch_thin(const ExpertsArgs &a, hipStream_t stream)
 {
     const int64_t row_tiles = (int64_t)(a.n_rows + 16 * RB - 1) / (16 * RB) + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
     const int64_t grid = (row_tiles * (a.out / (16 * CB)) + 7) / 8 * 8;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    if (!can_launch(grid, 64 * WAVES)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_experts_thin<F8, RB, CB, D, WAVES, ONCE>), dim3((unsigned)grid), dim3(64 * WAVES), 0, stream, a);
     return hipGetLastError();
 }
@@ -788,7 +788,7 @@ static hipError_t launch_wide(const ExpertsArgs &a, hipStream_t stream)
     const int64_t row_tiles = ((int64_t)a.n_rows + 255) / 256 + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0), n_ct = (a.out + 255) / 256;
     // an eighth of each kind is rounded up, and up to half a round of tiles cut in two
     int64_t grid = (row_tiles * n_ct + 7) / 8 * 8 + 16 + kComputeUnits / 2;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    if (!can_launch(grid, kWideThreads8)) return hipErrorInvalidConfiguration;
     if (!a.starts) {  // known here (150 work groups without a tile take about 1 us)
         const int whole = (int)(((int64_t)a.n_rows + 127) / 256 * n_ct), rest = (int)(row_tiles * n_ct) - whole;
         grid = (int64_t)(whole + 7) / 8 * 8 + (cut_tiles(whole, rest) + 7) / 8 * 8 + (rest + 7) / 8 * 8;
@@ -984,7 +984,7 @@ static hipError_t launch_mid(const ExpertsArgs &a, hipStream_t stream)
 {
     const int64_t row_tiles = (int64_t)(a.n_rows + 16 * RB - 1) / (16 * RB) + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
     const int64_t grid = (row_tiles * (a.out / (64 * CB)) + 7) / 8 * 8;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    if (!can_launch(grid, 64 * kMidWaves * KS)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_experts_mid<F8, RB, CB, D, KS, ONCE>), dim3((unsigned)grid), dim3(64 * kMidWaves * KS), 0, stream, a);
     return hipGetLastError();
 }

@@ -235,3 +235,17 @@ def test_a_workspace_of_more_picks_is_enough_for_fewer():
         said = [L.lora_experts_group_workspace_bytes(n, experts) for n in ends]
         assert said == sorted(said)
     assert L.lora_experts_group_workspace_bytes(10 ** 6, 7) <= L.lora_experts_group_workspace_bytes(10 ** 6, 8)
+
+
+F = 1 << 24  # LORA_EXPERTS_MAX_FEATURES
+
+
+@pytest.mark.parametrize("name, base, change", [
+    ("lora_linear_scaled", LINEAR, dict(rows=1 << 24, out=F, ldy=F)),                                                # tiles of 256 x 256: 2^32 of them
+    ("lora_linear_scaled", LINEAR, dict(rows=1 << 21, in_f=128, ldq=128, lds=1, out=F >> 2, ldy=F >> 2)),              # .. 2^27, of 512 threads
+    ("lora_experts_linear", EXPERTS, dict(tokens=3584, picks=1, rows=3584, experts=512, in_f=64, out=F, ldy=F)),     # of 32 x 128
+    ("lora_experts_linear_scaled", SCALED, dict(tokens=3584, picks=1, rows=3584, experts=512, out=F, ldy=F)),
+])
+def test_more_tiles_than_a_launch_can_have_are_refused(name, base, change):
+    assert status(name, *dict(base, **change).values(), None) == "LORA_ERR_SHAPE"
+    assert "tiles" in L.lib().lora_last_error().decode()
