@@ -80,6 +80,7 @@ class ExpertLayer:
         # (the rows behind the last expert's, where picks have none, are never written: they go through the activation and the second quantiser
         # with whatever they hold, and no product or sum reads them)
         self.h = torch.zeros(rows, 2 * inner, dtype=torch.bfloat16, device="cuda")
+        self.act32 = torch.empty(rows, inner, device="cuda")
         self.act = torch.empty(rows, inner, dtype=torch.bfloat16, device="cuda")
         self.y = torch.empty(rows, down.out_features, dtype=torch.bfloat16, device="cuda")
 
@@ -90,8 +91,9 @@ class ExpertLayer:
         L.lora_experts_group(ids, self.starts, self.order[:rows], self.place[:rows], self.workspace, stream)
         q, scales = self.x8.fill(x, stream)
         L.lora_experts_linear_scaled(q, scales, self.starts, self.order[:rows], self.picks, self.gate_up.packed, self.gate_up.scales, self.h[:rows], stream)
-        gate, up = self.h[:rows, :inner].float(), self.h[:rows, inner:].float()
-        self.act[:rows].copy_(torch.nn.functional.silu(gate) * up)
+        act = self.act32[:rows].copy_(self.h[:rows, :inner])  # silu(gate) * up in 32 bits, rounded once
+        torch.nn.functional.silu(act, inplace=True).mul_(self.h[:rows, inner:])
+        self.act[:rows].copy_(act)
         q, scales = self.h8.fill(self.act[:rows], stream)
         L.lora_experts_linear_scaled(q, scales, self.starts, None, 1, self.down.packed, self.down.scales, self.y[:rows], stream)
         L.lora_experts_combine(self.y[:rows], self.place[:rows].view(-1, self.picks), weights, z, stream)

@@ -619,3 +619,18 @@ def test_quantize_more_rows_than_a_launch_takes():
     assert torch.equal(q[n:].view(F8).double(), rq) and torch.equal(s[n:], rs)
     del q, s
     torch.cuda.empty_cache()
+
+
+def test_a_step_of_the_layer_of_experts_allocates_nothing():
+    from paper_2511_22880_amd import expert_layer as m
+    g = gen(32)
+    layer = m.ExpertLayer(m.Packed(*m.weights_to_8_bits(torch.randn(4, 512, 256, generator=g, device="cuda") * 0.05)),
+                          m.Packed(*m.weights_to_8_bits(torch.randn(4, 256, 256, generator=g, device="cuda") * 0.05)), 2, 50)
+    x, z = torch.randn(50, 256, generator=g, device="cuda").to(BF), torch.empty(50, 256, dtype=BF, device="cuda")
+    ids, w = torch.randint(-1, 4, (50, 2), generator=g, device="cuda", dtype=torch.int32), torch.rand(50, 2, generator=g, device="cuda")
+    for tokens in (50, 33):
+        before = torch.cuda.memory_stats()["allocation.all.allocated"]
+        layer(x[:tokens], ids[:tokens], w[:tokens], z[:tokens])
+        assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+        h = layer.h[:int(layer.starts[-1])].float()  # the same numbers as out of place
+        assert torch.equal(layer.act[:h.shape[0]], (torch.nn.functional.silu(h[:, :256]) * h[:, 256:]).to(BF))
