@@ -814,8 +814,9 @@ template <bool F8, int RB, int CB, int D, int KS, bool ONCE>
 __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsArgs a)
 {
     constexpr int R = 16 * RB, XBUF = R * kPieceBytes;
-    constexpr int NX = RB > 2 ? RB / 2 : 1;  // x loads of a wavefront per piece
-    constexpr int NS = (R + 63) / 64;        // .. of scales
+    constexpr int NX = RB / 2;  // x loads of a wavefront per piece
+    static_assert(RB % 2 == 0 && R <= 64, "whole loads of x, and a lane for the scale of every row");
+    static_assert(CB == 2 || CB == 4, "what a lane stores of a row");
     static_assert(D % 2 == 0, "slots of x by the place in the unrolled loop");
     __shared__ __attribute__((aligned(16))) char all_lds[kMidLds<F8, RB, CB, D, KS>];
     const int tid = threadIdx.x % (64 * kMidWaves), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -834,43 +835,36 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
 #pragma unroll
         for (int b = 0; b < CB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // x: 16 bytes a lane (8 where the tile has 16 rows), the tile's rows in order over the wavefronts; chunk c of row r goes to slot c XOR (r mod 8)
-    typedef __attribute__((ext_vector_type(RB == 1 ? 2 : 4))) unsigned XLoad;
-    constexpr int LPR = kPieceBytes / (int)sizeof(XLoad);  // lanes per row
+    // x: 16 bytes a lane, 8 lanes a row, the tile's rows in order over the wavefronts; chunk c of row r goes to slot c XOR (r mod 8)
     const char *xrow[NX];
     int xput[NX];
 #pragma unroll
     for (int q = 0; q < NX; ++q) {
-        const int l = q * 64 * kMidWaves + tid, r = l / LPR, at = l % LPR * (int)sizeof(XLoad);
+        const int l = q * 64 * kMidWaves + tid, r = l >> 3, c = l & 7;
         const int tok = token_at(a, t.row0 + (r < t.rows ? r : 0));
-        xrow[q] = a.x + (int64_t)max(tok, 0) * a.ldx_bytes + at;
-        xput[q] = r * kPieceBytes + (((at >> 4) ^ (r & 7)) << 4) + (at & 15);
+        xrow[q] = a.x + (int64_t)max(tok, 0) * a.ldx_bytes + 16 * c;
+        xput[q] = r * kPieceBytes + ((c ^ (r & 7)) << 4);
     }
     const char *wbase = a.w + ((int64_t)t.expert * (a.out >> 7) + strip) * np * 16384 + operand_at<F8>(0, b0);
     const unsigned lane16 = lane * 16;
-    [[maybe_unused]] const float *xs_at[NS], *ws_at = nullptr;
+    [[maybe_unused]] const float *xs_at = nullptr, *ws_at = nullptr;
     [[maybe_unused]] float *const sc = reinterpret_cast<float *>(lds + 2 * XBUF) + wave * R;
     if constexpr (F8) {
-#pragma unroll
-        for (int q = 0; q < NS; ++q) {
-            const int tok = token_at(a, t.row0 + (64 * q + lane < t.rows ? 64 * q + lane : 0));
-            xs_at[q] = a.x_scales + (int64_t)max(tok, 0) * a.ld_scales;
-        }
+        const int tok = token_at(a, t.row0 + (lane < t.rows ? lane : 0));
+        xs_at = a.x_scales + (int64_t)max(tok, 0) * a.ld_scales;
         int zero = 0;
         asm("" : "+v"(zero));  // (a vector load, counted in order with the others)
         ws_at = a.w_scales + ((int64_t)t.expert * (a.out >> 7) + strip) * np + zero;
     }
-    XLoad xq[D][NX];
-    uint4 wq[D][2][CB];
-    [[maybe_unused]] float sx[D][NS], sw[D];
+    uint4 xq[D][NX], wq[D][2][CB];
+    [[maybe_unused]] float sx[D], sw[D];
     // Loads without branches (around one the compiler would wait for everything in flight): past the last piece, the last one again.
     auto load_x = [&](int s, int d) __attribute__((always_inline)) {
         const int at = min(s * KS + ks, np - 1);
 #pragma unroll
-        for (int q = 0; q < NX; ++q) xq[d][q] = *reinterpret_cast<const XLoad *>(xrow[q] + (int64_t)at * kPieceBytes);
+        for (int q = 0; q < NX; ++q) xq[d][q] = ldb16(xrow[q] + (int64_t)at * kPieceBytes);
         if constexpr (F8) {
-#pragma unroll
-            for (int q = 0; q < NS; ++q) sx[d][q] = xs_at[q][at];
+            sx[d] = xs_at[at];
             sw[d] = ws_at[at];
         }
     };
@@ -883,7 +877,7 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
     };
     auto put_x = [&](int d, int slot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int q = 0; q < NX; ++q) *reinterpret_cast<XLoad *>(lds + slot * XBUF + xput[q]) = xq[d][q];
+        for (int q = 0; q < NX; ++q) *reinterpret_cast<uint4 *>(lds + slot * XBUF + xput[q]) = xq[d][q];
     };
     auto barrier = [&]() __attribute__((always_inline)) {
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
@@ -907,9 +901,7 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
             if constexpr (F8) {
                 const WeightScale s = weight_scale(sw[d]);
                 power = s.power;
-#pragma unroll
-                for (int q = 0; q < NS; ++q)
-                    if (64 * q + lane < R) sc[64 * q + lane] = sx[d][q] * s.factor;
+                if (lane < R) sc[lane] = sx[d] * s.factor;
             }
             load_x(s0 + d + D, d);
             // what a slot held two pieces ago has been read by everyone: each came to the barrier of the piece between behind its reads
@@ -969,13 +961,11 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
         for (int e = 0; e < 4; ++e) {
             const int r = 16 * i + 4 * kq + e;
             if (r >= t.rows || token_at(a, t.row0 + r) < 0) continue;
-            [[maybe_unused]] uint32_t *const dst = reinterpret_cast<uint32_t *>(y0 + (int64_t)r * a.ldy);
+            uint32_t *const dst = reinterpret_cast<uint32_t *>(y0 + (int64_t)r * a.ldy);
             if constexpr (CB == 4)
                 *reinterpret_cast<uint2 *>(dst) = uint2{pack_bf16_rne(acc[i][0][e], acc[i][1][e]), pack_bf16_rne(acc[i][2][e], acc[i][3][e])};
-            else if constexpr (CB == 2)
-                *dst = pack_bf16_rne(acc[i][0][e], acc[i][1][e]);
             else
-                y0[(int64_t)r * a.ldy] = (uint16_t)pack_bf16_rne(acc[i][0][e], 0.f);
+                *dst = pack_bf16_rne(acc[i][0][e], acc[i][1][e]);
         }
 }
 
