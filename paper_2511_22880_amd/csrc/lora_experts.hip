@@ -406,7 +406,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
 template <bool F8, int RB, int CB, int D, int WAVES, bool ONCE = false>
 static hipError_t launch_thin(const ExpertsArgs &a, hipStream_t stream)
 {
-    const int64_t row_tiles = (int64_t)(a.n_rows + 16 * RB - 1) / (16 * RB) + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
+    const int64_t row_tiles = ((int64_t)a.n_rows + 16 * RB - 1) / (16 * RB) + met_experts(a.starts ? a.n_experts : 0, a.n_rows);
     const int64_t grid = (row_tiles * (a.out / (16 * CB)) + 7) / 8 * 8;
     if (!can_launch(grid, 64 * WAVES)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_experts_thin<F8, RB, CB, D, WAVES, ONCE>), dim3((unsigned)grid), dim3(64 * WAVES), 0, stream, a);
@@ -772,7 +772,7 @@ __global__ __launch_bounds__(kWideThreads8, 1) void k_experts_wide(ExpertsArgs a
     const int n_ct = (a.out + 255) >> 8;
     Tile t;
     if (!find_wide_tile(a.starts, a.n_experts, a.n_rows, n_ct, threadIdx.x & 63, (int)blockIdx.x, t)) return;
-    // W past the caches where an expert has this one tile of rows and the weights are many (see launch_by_rows): us, 64 experts of 64 rows each,
+    // W past the caches where an expert has this one tile of rows and the weights are many (see large_weights): us, 64 experts of 64 rows each,
     // 2048 -> 1536, in bf16 90 / 83, in 8 bits 54.6 / 50.5
     if (t.rows > 128)
         t.only && a.large ? wide_body<F8, 4, 2, true>(a, t, lds) : wide_body<F8, 4, 2, false>(a, t, lds);
@@ -785,7 +785,7 @@ __global__ __launch_bounds__(kWideThreads8, 1) void k_experts_wide(ExpertsArgs a
 template <bool F8>
 static hipError_t launch_wide(const ExpertsArgs &a, hipStream_t stream)
 {
-    const int64_t row_tiles = ((int64_t)a.n_rows + 255) / 256 + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0), n_ct = (a.out + 255) / 256;
+    const int64_t row_tiles = ((int64_t)a.n_rows + 255) / 256 + met_experts(a.starts ? a.n_experts : 0, a.n_rows), n_ct = (a.out + 255) / 256;
     // an eighth of each kind is rounded up, and up to half a round of tiles cut in two
     int64_t grid = (row_tiles * n_ct + 7) / 8 * 8 + 16 + kComputeUnits / 2;
     if (!can_launch(grid, kWideThreads8)) return hipErrorInvalidConfiguration;
@@ -972,81 +972,48 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
 template <bool F8, int RB, int CB, int D, int KS = 1, bool ONCE = false>
 static hipError_t launch_mid(const ExpertsArgs &a, hipStream_t stream)
 {
-    const int64_t row_tiles = (int64_t)(a.n_rows + 16 * RB - 1) / (16 * RB) + (a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0);
+    const int64_t row_tiles = ((int64_t)a.n_rows + 16 * RB - 1) / (16 * RB) + met_experts(a.starts ? a.n_experts : 0, a.n_rows);
     const int64_t grid = (row_tiles * (a.out / (64 * CB)) + 7) / 8 * 8;
     if (!can_launch(grid, 64 * kMidWaves * KS)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_experts_mid<F8, RB, CB, D, KS, ONCE>), dim3((unsigned)grid), dim3(64 * kMidWaves * KS), 0, stream, a);
     return hipGetLastError();
 }
 
-// The tiles of a launch: the largest of which there are enough to occupy most compute units, no higher than an expert's rows in the mean ask for.  Row
-// tiles are counted as if every expert's last one were half there (the host does not know who picked what).  With one tile of 64 x 256, 64 x 128 or 32 x 128 on a
-// compute unit two groups of wavefronts share its pieces (two), unless k is short; with more of them the tiles' own wavefronts are enough (one).
-// Device time in us, one layer in 8 bits (wide: k_experts_wide, whose tiles are 256 x 256 or 128 x 256):
-//   rows, layer        wide        64 x 256, one / two   64 x 128, one / two   32 x 128, one / two   32 x 64   16 x 64   16 x 32   16 x 16
-//   1     4096 4096                                                                                            6.3       5.6       5.3
-//   64    4096 4096    36          32 / 25               21 / 17               12.6 / 12.5           8.9       7.3       9.2
-//   128   4096 4096    36          32 / 25               21 / 17               12.7 / 12.6           9.4       11.3      14.8
-//   256   4096 4096    33          33 / 25               21 / 17               13.4 / 13.1           15.0      19.1      26
-//   512   4096 4096    34          33 / 26               22 / 17.5             22 / 21               25        32        52
-//   1024  4096 4096    36          35 / 27               32 / 32               39 / 40               49        69        107
-//   2048  4096 4096    42          49 / 53               60 / 64               78 / 79               98        136       215
-//   64    16384 16384  131         132 / 122             90 / 86               75 / 66               70        90        117
-//   256   16384 16384  132         131 / 118             134 / 144             181 / 175             179       252       372
-//   115   5568 3584    43          42 / 32               27 / 21               16.3 / 15.5           11.6      13.8      17.4
-//   373   5440 640     41                                26 / 21               15.8 / 15.1           11.3      9.1       11.4
-//   1149  7232 512     54          54 / 41               33 / 27               20.3 / 19.4           24        24        33
-//   689   8128 14848   111         150 / 152             156 / 160             201 / 195             218       316       472
-//   10081 704 512      12.1        15.1 / 18.8           15.9 / 18.4           14.6 / 18.2           28        33        59
-//   7     3008 4352                                                                                            5.5       4.9       5.8
-// and of 64 experts 2048 -> 1536, rows each, in 8 bits: 8 49, - , 47, 39.9, 44, 41, 54; 64 54, 64, 71, 66, 82, 91, 170; in bf16: 8 81, - , 75, 75, 71, 73, 76;
-// 32 85, 86, 78, 90, 91, 104, 130; 64 90, 98, 102, 109, 115, 153, 200 (in the same order, one group of wavefronts, through the caches).
-// Over 50 random sizes of one layer the choice was 1.7 % from the best of all of these in the mean, over 50 of experts 7 % (a quarter of them with one pick in
-// ten here, which the host does not know: up to twice the best).
+// The kernel that a form names; every one that product_form gives is here.
 template <bool F8>
-static hipError_t launch_by_rows(ExpertsArgs a, hipStream_t stream)
+static hipError_t launch_form(const ExpertsArgs &a, ProductForm f, hipStream_t stream)
 {
-    const int met = a.starts ? (a.n_rows < a.n_experts ? a.n_rows : a.n_experts) : 0;
-    const int per = met ? a.n_rows / met : a.n_rows;
-    auto fills = [&](int rows, int columns, int least) {
-        const int64_t row_tiles = (int64_t)(a.n_rows + rows - 1) / rows + met / 2;
-        return (row_tiles > met ? row_tiles : met) * ((a.out + columns - 1) / columns) >= least;
-    };
-    constexpr int kMost = kComputeUnits * 9 / 16;
-    // Weights of more than half of what the chip's last cache holds are read past the caches where an expert has one tile of rows: they would leave
-    // there whatever else a layer keeps, and another pass would hardly find them.  us, through the caches / past them: 512 rows of 64 experts
-    // 2048 -> 1536 in bf16 72 / 64 (6.4 TB/s), 1024 78 / 69, 2048 81 / 72, in 8 bits 512 rows 40 / 36; 16 rows 16384 -> 16384 in 8 bits 50 / 44.  Smaller ones: one row
-    // 8192 -> 8192 (three such layers in turn, 201 MB) 11.9 / 15.5.
-    const bool large = a.large = (int64_t)(met ? met : 1) * a.out * a.pieces * kPieceBytes > ((int64_t)128 << 20);
-    auto once = [&](int rows) { return large && (met ? per <= rows * 3 / 4 : per <= rows); };
-    auto middle = [&](auto rb, auto cb) {
-        constexpr int RB = decltype(rb)::value, CB = decltype(cb)::value;
-        const bool two = a.pieces >= 16 && !fills(16 * RB, 64 * CB, 2 * kComputeUnits);
-        if constexpr (CB == 2)
-            if (once(16 * RB)) return two ? launch_mid<F8, RB, CB, 2, 2, true>(a, stream) : launch_mid<F8, RB, CB, 2, 1, true>(a, stream);
-        return two ? launch_mid<F8, RB, CB, 2, 2>(a, stream) : launch_mid<F8, RB, CB, 2, 1>(a, stream);
-    };
-    constexpr std::integral_constant<int, 2> two;
-    constexpr std::integral_constant<int, 4> four;
-    // (more tiles of 64 x 256 than one round: half as many of 128 x 256 or 256 x 256, in one, are earlier.  us, 64 x 256 / wide: 1024 rows 4096 -> 4096 in 8 bits 27 / 33,
-    // 1152 49 / 33, 2048 49 / 40, 1100 9152 -> 4480 92 / 67, 2000 of 8 experts 4096 -> 2048 in bf16 77 / 62, 1600 of them 58 / 60.  Few rows an expert, 64 experts
-    // 2048 -> 1536, what was taken else / wide: in 8 bits 20 rows 40 / 44, 30 51 / 45, 40 57 / 45, in bf16 30 72 / 78, 40 87 / 79)
-    if (per > (F8 ? 25 : 35) && (fills(256, 256, kMost) || fills(64, 256, kComputeUnits + 1))) return launch_wide<F8>(a, stream);
-    if (per > 32 && a.out % 256 == 0 && fills(64, 256, kMost)) return middle(four, four);
-    if (per > 24 && fills(64, 128, kMost)) return middle(four, two);
-    // (a row an expert, of large weights: 16 x 64 tiles cost up to a tenth more where all picks have an expert here, but where one in ten has, as with experts on
-    // eight chips, they are through in half to two thirds of the time.  us, 32 x 128 / 16 x 64, all and one in ten: 90 picks of 78 experts 3584 -> 512 in 8 bits
-    // 19.2 / 21.3 and 14.0 / 9.4, 64 of 64 2048 -> 1536 in bf16 50.7 / 50.1 and 17.8 / 11.3, 16 of 64 4096 -> 4096 75.2 / 78.7 and 25.4 / 14.0)
-    if ((per > 6 || (large && per > 1 && met)) && fills(32, 128, kMost)) return middle(two, two);
-    if (per > 16 && fills(32, 64, kMost)) return once(32) ? launch_thin<F8, 2, 4, 2, 4, true>(a, stream) : launch_thin<F8, 2, 4, 2, 4>(a, stream);
-    if (fills(16, 64, kMost)) return once(16) ? launch_thin<F8, 1, 4, 2, 4, true>(a, stream) : launch_thin<F8, 1, 4, 2, 4>(a, stream);
-    if (fills(16, 32, kMost)) return launch_thin<F8, 1, 2, 2, 8>(a, stream);
-    return launch_thin<F8, 1, 1, 2, 8>(a, stream);
+    const int which = f.rb * 1000 + f.cb * 100 + f.groups * 10 + f.once;
+    if (f.kind == ProductForm::kWide) return launch_wide<F8>(a, stream);
+    if (f.kind == ProductForm::kMid) switch (which) {
+        case 4410: return launch_mid<F8, 4, 4, 2, 1>(a, stream);
+        case 4420: return launch_mid<F8, 4, 4, 2, 2>(a, stream);
+        case 4210: return launch_mid<F8, 4, 2, 2, 1>(a, stream);
+        case 4220: return launch_mid<F8, 4, 2, 2, 2>(a, stream);
+        case 4211: return launch_mid<F8, 4, 2, 2, 1, true>(a, stream);
+        case 4221: return launch_mid<F8, 4, 2, 2, 2, true>(a, stream);
+        case 2210: return launch_mid<F8, 2, 2, 2, 1>(a, stream);
+        case 2220: return launch_mid<F8, 2, 2, 2, 2>(a, stream);
+        case 2211: return launch_mid<F8, 2, 2, 2, 1, true>(a, stream);
+        case 2221: return launch_mid<F8, 2, 2, 2, 2, true>(a, stream);
+        }
+    else switch (which) {
+        case 2440: return launch_thin<F8, 2, 4, 2, 4>(a, stream);
+        case 2441: return launch_thin<F8, 2, 4, 2, 4, true>(a, stream);
+        case 1440: return launch_thin<F8, 1, 4, 2, 4>(a, stream);
+        case 1441: return launch_thin<F8, 1, 4, 2, 4, true>(a, stream);
+        case 1280: return launch_thin<F8, 1, 2, 2, 8>(a, stream);
+        case 1180: return launch_thin<F8, 1, 1, 2, 8>(a, stream);
+        }
+    return hipErrorInvalidValue;
 }
 
-hipError_t launch_experts_linear(const ExpertsArgs &a, bool bits8, hipStream_t stream)
+hipError_t launch_experts_linear(ExpertsArgs a, bool bits8, hipStream_t stream)
 {
-    return bits8 ? launch_by_rows<true>(a, stream) : launch_by_rows<false>(a, stream);
+    const int met = met_experts(a.starts ? a.n_experts : 0, a.n_rows);
+    a.large = large_weights(met, a.out, a.pieces);
+    const ProductForm f = product_form(bits8, a.n_rows, met, a.out, a.pieces);
+    return bits8 ? launch_form<true>(a, f, stream) : launch_form<false>(a, f, stream);
 }
 
 // ------------------------------------------------------------------------------------------------
