@@ -671,7 +671,7 @@ def _blocks(n: int) -> int:
 
 
 # What a tensor is asked for costs 0.1 us each time, and so does a call of Python's: the calls below, which a decode step waits for, ask for shape and
-# strides once, in line, and compare; where anything is unusual _usable looks closer.
+# strides once, in line, and compare; where anything is unusual _usable, _whole and _packed look closer.
 def _names(types) -> str:
     return " or ".join(sorted(str(t).replace("torch.", "") for t in types))
 
@@ -692,27 +692,22 @@ def _usable(name: str, t, rows: int, columns: int, types: set) -> None:
     _on_gpu(name, t)
 
 
-def _whole(name: str, t, n: int, types: set):
-    """Address of a contiguous tensor of at least n elements of one of these types."""
+def _whole(name: str, t, n: int, types: set) -> None:
+    """Refuses a tensor that is not n contiguous elements, or more, of one of these types."""
+    if not types:
+        _know_types()
     if t.dtype not in types:
-        if not types:
-            _know_types()
-        if t.dtype not in types:
-            raise ValueError(f"{name}: {t.dtype} does not do: {_names(types)} is meant")
+        raise ValueError(f"{name}: {t.dtype} does not do: {_names(types)} is meant")
     if t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{name}: {tuple(t.shape)} with strides {t.stride()} does not do: {n} contiguous elements are meant")
-    if not t.is_cuda:
-        _on_gpu(name, t)
-    return t.data_ptr()
+    _on_gpu(name, t)
 
 
-def _packed(t, n: int):
-    """Address of packed weights, n bytes of whatever type."""
-    if t.itemsize != 1 or t.numel() < n or not t.is_contiguous():
+def _packed(t, n: int) -> None:
+    """Refuses packed weights that are not n contiguous bytes, of whatever type, or more."""
+    if t.nbytes < n or not t.is_contiguous():
         raise ValueError(f"w_packed: {tuple(t.shape)} of {t.dtype} does not do: {n} contiguous bytes are meant")
-    if not t.is_cuda:
-        _on_gpu("w_packed", t)
-    return t.data_ptr()
+    _on_gpu("w_packed", t)
 
 
 def _two(t, name: str):
@@ -769,7 +764,8 @@ def lora_experts_pack_weight(w, dev_packed, stream=None, in_features: Optional[i
     if row != (in_f if bits == 16 else _blocks(in_f) << 7):
         raise ValueError(f"w: rows of {row} elements are not those of {in_f} input features")
     _on_gpu("dev_packed", dev_packed)
-    _check(lib().lora_experts_pack_weight(_whole("w", w, 0, _BF16 if bits == 16 else _E4M3), e, in_f, out_f, bits, dev_packed.data_ptr(), _nbytes(dev_packed), _queue(stream)))
+    _whole("w", w, 0, _BF16 if bits == 16 else _E4M3)
+    _check(lib().lora_experts_pack_weight(w.data_ptr(), e, in_f, out_f, bits, dev_packed.data_ptr(), _nbytes(dev_packed), _queue(stream)))
 
 
 def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
@@ -795,8 +791,12 @@ def lora_linear_scaled(q, scales, w_packed, w_scales, y, stream=None) -> None:
         lds = sc
     if yr == 1:
         ldy = out_f
-    status = (_lib or lib()).lora_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, rows, in_f, _packed(w_packed, out_f * blocks << 7),
-                                                _whole("w_scales", w_scales, (out_f >> 7) * blocks, _F32), out_f, y.data_ptr(), ldy,
+    if w_packed.nbytes < out_f * blocks << 7 or not w_packed.is_contiguous() or not w_packed.is_cuda:
+        _packed(w_packed, out_f * blocks << 7)
+    if w_scales.dtype not in _F32 or w_scales.numel() < (out_f >> 7) * blocks or not w_scales.is_contiguous() or not w_scales.is_cuda:
+        _whole("w_scales", w_scales, (out_f >> 7) * blocks, _F32)
+    status = (_lib or lib()).lora_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, rows, in_f, w_packed.data_ptr(), w_scales.data_ptr(), out_f,
+                                                y.data_ptr(), ldy,
                                                 None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -826,8 +826,14 @@ def lora_experts_group(ids, starts, order, place, workspace=None, stream=None) -
             _on_gpu("workspace", workspace)
             raise ValueError(f"workspace: strides {workspace.stride()} do not do: contiguous bytes are meant")
         pw, nw = workspace.data_ptr(), workspace.nbytes
-    status = (_lib or lib()).lora_experts_group(ids.data_ptr(), ldi if tokens > 1 else picks, tokens, picks, n_experts, _whole("starts", starts, 1, _INT32),
-                                                _whole("order", order, n, _INT32), _whole("place", place, n, _INT32), pw, nw,
+    if starts.dtype not in _INT32 or n_experts < 0 or not starts.is_contiguous() or not starts.is_cuda:
+        _whole("starts", starts, 1, _INT32)
+    if order.dtype not in _INT32 or order.numel() < n or not order.is_contiguous() or not order.is_cuda:
+        _whole("order", order, n, _INT32)
+    if place.dtype not in _INT32 or place.numel() < n or not place.is_contiguous() or not place.is_cuda:
+        _whole("place", place, n, _INT32)
+    status = (_lib or lib()).lora_experts_group(ids.data_ptr(), ldi if tokens > 1 else picks, tokens, picks, n_experts, starts.data_ptr(), order.data_ptr(),
+                                                place.data_ptr(), pw, nw,
                                                 None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -849,9 +855,14 @@ def lora_experts_linear(x, starts, order, picks: int, w_packed, y, stream=None) 
         ldx = in_f
     if yr == 1:
         ldy = out_f
-    status = (_lib or lib()).lora_experts_linear(x.data_ptr(), ldx, tokens, _whole("starts", starts, 1, _INT32),
-                                                 None if order is None else _whole("order", order, n_rows, _INT32), picks, n_rows, n_experts, in_f,
-                                                 _packed(w_packed, n_experts * out_f * in_f << 1), out_f, y.data_ptr(), ldy,
+    if starts.dtype not in _INT32 or n_experts < 0 or not starts.is_contiguous() or not starts.is_cuda:
+        _whole("starts", starts, 1, _INT32)
+    if order is not None and (order.dtype not in _INT32 or order.numel() < n_rows or not order.is_contiguous() or not order.is_cuda):
+        _whole("order", order, n_rows, _INT32)
+    if w_packed.nbytes < n_experts * out_f * in_f << 1 or not w_packed.is_contiguous() or not w_packed.is_cuda:
+        _packed(w_packed, n_experts * out_f * in_f << 1)
+    status = (_lib or lib()).lora_experts_linear(x.data_ptr(), ldx, tokens, starts.data_ptr(), None if order is None else order.data_ptr(), picks, n_rows,
+                                                 n_experts, in_f, w_packed.data_ptr(), out_f, y.data_ptr(), ldy,
                                                  None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -880,10 +891,17 @@ def lora_experts_linear_scaled(q, scales, starts, order, picks: int, w_packed, w
         lds = sc
     if yr == 1:
         ldy = out_f
-    status = (_lib or lib()).lora_experts_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, tokens, _whole("starts", starts, 1, _INT32),
-                                                        None if order is None else _whole("order", order, n_rows, _INT32), picks, n_rows, n_experts, in_f,
-                                                        _packed(w_packed, n_experts * out_f * blocks << 7),
-                                                        _whole("w_scales", w_scales, n_experts * (out_f >> 7) * blocks, _F32), out_f, y.data_ptr(), ldy,
+    if starts.dtype not in _INT32 or n_experts < 0 or not starts.is_contiguous() or not starts.is_cuda:
+        _whole("starts", starts, 1, _INT32)
+    if order is not None and (order.dtype not in _INT32 or order.numel() < n_rows or not order.is_contiguous() or not order.is_cuda):
+        _whole("order", order, n_rows, _INT32)
+    if w_packed.nbytes < n_experts * out_f * blocks << 7 or not w_packed.is_contiguous() or not w_packed.is_cuda:
+        _packed(w_packed, n_experts * out_f * blocks << 7)
+    if w_scales.dtype not in _F32 or w_scales.numel() < n_experts * (out_f >> 7) * blocks or not w_scales.is_contiguous() or not w_scales.is_cuda:
+        _whole("w_scales", w_scales, n_experts * (out_f >> 7) * blocks, _F32)
+    status = (_lib or lib()).lora_experts_linear_scaled(q.data_ptr(), ldq, scales.data_ptr(), lds, tokens, starts.data_ptr(),
+                                                        None if order is None else order.data_ptr(), picks, n_rows, n_experts, in_f, w_packed.data_ptr(),
+                                                        w_scales.data_ptr(), out_f, y.data_ptr(), ldy,
                                                         None if stream is None else _queue(stream))
     if status:
         _check(status)
@@ -906,7 +924,11 @@ def lora_experts_combine(y, place, weights, z, stream=None) -> None:
         ldy = yc
     if zr == 1:
         ldz = out_f
-    status = (_lib or lib()).lora_experts_combine(y.data_ptr(), ldy, yr, _whole("place", place, n, _INT32), _whole("weights", weights, n, _F32), tokens, picks, out_f,
+    if place.dtype not in _INT32 or place.numel() < n or not place.is_contiguous() or not place.is_cuda:
+        _whole("place", place, n, _INT32)
+    if weights.dtype not in _F32 or weights.numel() < n or not weights.is_contiguous() or not weights.is_cuda:
+        _whole("weights", weights, n, _F32)
+    status = (_lib or lib()).lora_experts_combine(y.data_ptr(), ldy, yr, place.data_ptr(), weights.data_ptr(), tokens, picks, out_f,
                                                   z.data_ptr(), ldz, None if stream is None else _queue(stream))
     if status:
         _check(status)
