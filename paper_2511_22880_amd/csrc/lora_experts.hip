@@ -47,27 +47,28 @@ static __device__ __forceinline__ void in_order()
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
-// A weight's scale as 2^(power - 127), which the matrix instruction applies to its sum for nothing, times the factor left over: half to one, unless the scale
+// A weight's scale as 2^(power - 127) (power: the second byte of `powers`), which the matrix instruction applies to its sum for nothing, times the factor left over: half to one, unless the scale
 // is beyond 2^100 or 2^-100.  x's scale times the whole one can be far below 2^-126, where it would lose bits (x's alone goes down to that) though y does not:
 // a sum of 128 products of up to 448^2 lies up to 2^25 above it.  x's scale times the factor loses none to speak of, and never overflows where x's scale does not; a
 // sum times 2^-100 to 2^100 is still exact.  Zero, infinities and NaN stay in the factor.
 struct WeightScale {
     float factor;
-    int power;
+    int powers;  // of x's operand, one, and of W's: one register for both
 };
+constexpr int kPowersOne = 127 | 127 << 8;
 static __device__ __forceinline__ WeightScale weight_scale(float w)
 {
     const int e = min(max((int)((__float_as_uint(w) >> 23) & 0xFFu) - 126, -100), 100);
-    return WeightScale{w * __uint_as_float((uint32_t)(127 - e) << 23), e + 127};
+    return WeightScale{w * __uint_as_float((uint32_t)(127 - e) << 23), kPowersOne + (e << 8)};
 }
 
 // 16 x 16 products over 128 8-bit values of k (both operands E4M3, b's times 2^(power - 127)).  The instruction drops what lies 2^-17 below the
 // largest of an element's 128 products (all in all up to 2^-10 of that product was seen), and the ones for 32 values of k do the same: of those that take 8 bits there is
 // none more exact.  (E4M3 is exact in bf16, whose instruction adds in fp32: that would take twice as long at the matrix units and a conversion of
 // every operand.)  A block's sum is fp32 from there on.
-static __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, int power)
+static __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, int powers)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 127, 0, power);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, powers, 1, powers);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -317,13 +318,13 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
 #pragma unroll
                 for (int b = 0; b < CB; ++b) wq[d][h][b] = ldw16<ONCE>(wbase + at * (16384 * WAVES) + operand_at<F8>(h, b));
         };
-        [[maybe_unused]] int power = 127;  // of the staged piece's scale of W
+        [[maybe_unused]] int powers = kPowersOne;  // of the staged piece's scale of W
         auto stage = [&](int d) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < NX; ++q) *reinterpret_cast<uint4 *>(slab + (8 * q + lr) * 128 + ((lc ^ lr) << 4)) = xq[d][q];
             if constexpr (F8) {
                 const WeightScale s = weight_scale(sw[d]);
-                power = s.power;
+                powers = s.powers;
                 if (lane < R) reinterpret_cast<float *>(slab + kSlab)[lane] = sx[d] * s.factor;
             }
         };
@@ -340,7 +341,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void k_experts_thin(ExpertsArgs a)
                     const f32x4 s = *reinterpret_cast<const f32x4 *>(slab + kSlab + (16 * i + 4 * kq) * 4);
 #pragma unroll
                     for (int b = 0; b < CB; ++b)
-                        acc[i][b] += s * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), power);
+                        acc[i][b] += s * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), powers);
                 }
             } else {
 #pragma unroll
@@ -648,7 +649,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
     uint4 xo[XH][4], wo[WH][WB];
     [[maybe_unused]] f32x4 sc[4];
     int xget = 0, wget = 0;
-    [[maybe_unused]] int sget = 0, power = 127;
+    [[maybe_unused]] int sget = 0, powers = kPowersOne;
     const int xlane = (8 * rw + (n >> 3)) * 1024 + (n & 7) * 128;
     const int wlane = wave / WS * WPART + lane * 16;
     // row 16 i + n of this wavefront's: block 8 rw + 2 i + n / 8, row n mod 8 of it
@@ -701,7 +702,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         }
         if constexpr (F8 && q == 0) {
             const WeightScale w = weight_scale(wscale[P]);
-            power = w.power;
+            powers = w.powers;
 #pragma unroll
             for (int i = 0; i < 4; ++i) sc[i] = *reinterpret_cast<const f32x4 *>(sbuf + sget + (16 * i + 4 * kq) * 4) * w.factor;
             sget = (sget + 256) & (by16 ? 1023 : 2047);
@@ -719,7 +720,7 @@ static __device__ __forceinline__ void wide_body(const ExpertsArgs &a, const Til
         if constexpr (F8) {
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-                part[k % (kLag + 1)] = mfma_e4m3(as_i32x8(xo[0][k >> 2], xo[XH - 1][k >> 2]), as_i32x8(wo[0][k & 3], wo[WH - 1][k & 3]), power);
+                part[k % (kLag + 1)] = mfma_e4m3(as_i32x8(xo[0][k >> 2], xo[XH - 1][k >> 2]), as_i32x8(wo[0][k & 3], wo[WH - 1][k & 3]), powers);
                 __builtin_amdgcn_sched_barrier(0);
                 if (k >= kLag) add(q, k - kLag);
                 // these rows of x have been multiplied: the next piece's.  All of it has landed: W of this step, requested behind it, has been waited
@@ -897,10 +898,10 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
         for (int d = 0; d < D; ++d) {
             const int slot = d & 1;
             put_x(d, slot);
-            [[maybe_unused]] int power = 127;
+            [[maybe_unused]] int powers = kPowersOne;
             if constexpr (F8) {
                 const WeightScale s = weight_scale(sw[d]);
-                power = s.power;
+                powers = s.powers;
                 if (lane < R) sc[lane] = sx[d] * s.factor;
             }
             load_x(s0 + d + D, d);
@@ -920,7 +921,7 @@ __global__ __launch_bounds__(64 * kMidWaves * KS, 1) void k_experts_mid(ExpertsA
                         const f32x4 f = *reinterpret_cast<const f32x4 *>(sc + 16 * i + 4 * kq);
 #pragma unroll
                         for (int b = 0; b < CB; ++b)
-                            acc[i][b] += f * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), power);
+                            acc[i][b] += f * mfma_e4m3(as_i32x8(xo[0][i], xo[1][i]), as_i32x8(wq[d][0][b], wq[d][1][b]), powers);
                     }
                 } else {
 #pragma unroll
