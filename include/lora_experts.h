@@ -21,7 +21,8 @@
  * 8-bit format: OCP E4M3 (largest value 448, no infinities), fp32 scales.  value(q[t][k]) = q[t][k] * x_scales[t][k / 128],
  * value(w[e][o][k]) = w[e][o][k] * w_scales[e][o / 128][k / 128].  The 128 products of a block are added up by the matrix instruction, exact but for
  * what of each lies below 2^-17 of the block's largest (so a block is off by less than 2^-10 of its largest product; without cancellation a few 1e-5 of
- * the sum, measured); the block's sum times both scales is added to the row's in fp32, and y is rounded to bf16 once.
+ * the sum, measured); the block's sum times both scales is added to the row's in fp32, and y is rounded to bf16 once; the
+ * scales' own product may be below or beyond what fp32 holds.
  *
  * Device data that the calls read as indices (expert ids, starts, order, place) is checked where it is used: a place outside the rows, an order
  * entry outside the tokens or starts that do not fit the rows reach no memory outside the buffers; rows that would be meant are not written.

@@ -430,10 +430,10 @@ static hipError_t launch_thin(const ExpertsArgs &a, hipStream_t stream)
 //     time: every row's lie in cache lines of their own, and one copy a piece took as long as half of the others together (8192 tokens
 //     8192 -> 8192: copies alone 418 us with one a piece, 304 without any).  Rows of x enter registers while the piece before is multiplied
 //     (64 x 128): a piece's first reading phase had 20 of its 28 operands, and lasted longer than the products beside it.
-//   * What bounds it is the chip's power: 8192 tokens 8192 -> 8192 in 8 bits take 474 us (2.32 PFLOP/s) at 1.95 of 2.4 GHz, and the parts add up like
+//   * What bounds it is the chip's power: 8192 tokens 8192 -> 8192 in 8 bits take 476 us (2.31 PFLOP/s) at 2.0 of 2.4 GHz, and the parts add up like
 //     energies, not like times: products and LDS reads alone 278 (products from registers alone run at 4.05 PFLOP/s, 271 us), copies 105 more, the fp32
 //     sums 110 more, in phases or without, copies requested two steps ahead or four.  In bf16 8002 rows of 8 experts 4096 -> 14336 take 755 us
-//     (1.25 PFLOP/s; a library's product of their size 750, products from registers alone 1.90 PFLOP/s).
+//     (1.25 PFLOP/s; a library's product of 8192 such rows 719 to 767, products from registers alone 1.90 PFLOP/s).
 // ------------------------------------------------------------------------------------------------
 constexpr int kWideThreads8 = 512;
 constexpr int kRing = 3;
