@@ -741,7 +741,7 @@ def lora_rows_quantize(x, q, scales, stream=None) -> None:
     if rows == 1:  # (of a single row torch states any stride)
         ldx = in_f
     if qr == 1:
-        ldq = qc
+        ldq = blocks << 7
     if sr == 1:
         lds = sc
     status = (_lib or lib()).lora_rows_quantize(x.data_ptr(), ldx, rows, in_f, q.data_ptr(), ldq, scales.data_ptr(), lds,
@@ -921,7 +921,7 @@ def lora_experts_combine(y, place, weights, z, stream=None) -> None:
     if zr < tokens or z1 != 1 or z.dtype not in _BF16 or not z.is_cuda:
         _usable("z", z, tokens, out_f, _BF16)
     if yr == 1:
-        ldy = yc
+        ldy = out_f
     if zr == 1:
         ldz = out_f
     if place.dtype not in _INT32 or place.numel() < n or not place.is_contiguous() or not place.is_cuda:

@@ -249,3 +249,33 @@ F = 1 << 24  # LORA_EXPERTS_MAX_FEATURES
 def test_more_tiles_than_a_launch_can_have_are_refused(name, base, change):
     assert status(name, *dict(base, **change).values(), None) == "LORA_ERR_SHAPE"
     assert "tiles" in L.lib().lora_last_error().decode()
+
+
+@pytest.fixture
+def told(monkeypatch):
+    """what the binding tells the library, call by call"""
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: calls.append((name, *args)) or 0
+    monkeypatch.setattr(L, "_lib", Library())
+    return calls
+
+
+def test_the_binding_takes_a_single_row_of_any_stride(told):
+    e = lambda *shape, dtype=torch.float32: torch.zeros(*shape).to(dtype).as_subclass(OnGpu)  # noqa: E731
+    x, q, s = e(1, 128, dtype=torch.bfloat16), e(1, 130, dtype=torch.uint8), e(1, 1)
+    L.lora_rows_quantize(x, q, s)
+    assert told[-1][1:9] == (x.data_ptr(), 128, 1, 128, q.data_ptr(), 128, s.data_ptr(), 1)
+    y, place, z = e(1, 130, dtype=torch.bfloat16), e(1, 2, dtype=torch.int32), e(1, 128, dtype=torch.bfloat16)
+    L.lora_experts_combine(y, place, e(1, 2), z)
+    assert told[-1][1:4] == (y.data_ptr(), 128, 1) and told[-1][6:11] == (1, 2, 128, z.data_ptr(), 128)
+
+
+@pytest.mark.parametrize("call", good())
+def test_the_binding_takes_bits_for_bf16_and_8_bit_values(call, told):
+    given = {n: t.view({torch.bfloat16: torch.uint16, torch.float8_e4m3fn: torch.uint8}.get(t.dtype, t.dtype)) if isinstance(t, torch.Tensor) else t
+             for n, t in good()[call].items()}
+    getattr(L, call)(**given)
+    assert told[-1][0] == call and next(iter(given.values())).data_ptr() == told[-1][1]
