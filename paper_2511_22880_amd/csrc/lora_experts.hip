@@ -47,13 +47,13 @@ static __device__ __forceinline__ void in_order()
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
 
-// A weight's scale as 2^(power - 127) (power: the second byte of `powers`), which the matrix instruction applies to its sum for nothing, times the factor left over: half to one, unless the scale
-// is beyond 2^100 or 2^-100.  x's scale times the whole one can be far below 2^-126, where it would lose bits (x's alone goes down to that) though y does not:
-// a sum of 128 products of up to 448^2 lies up to 2^25 above it.  x's scale times the factor loses none to speak of, and never overflows where x's scale does not; a
-// sum times 2^-100 to 2^100 is still exact.  Zero, infinities and NaN stay in the factor.
+// A weight's scale as 2^(power - 127), which the matrix instruction applies to its sum for nothing, times the factor left over: half to one, unless the
+// scale is beyond 2^100 or 2^-100.  x's scale times the whole one can be far below 2^-126, where it would lose bits (x's alone goes down to that) though y does not: a
+// sum of 128 products of up to 448^2 lies up to 2^25 above it.  x's scale times the factor loses none to speak of, and never overflows where x's scale does
+// not; a sum times 2^-100 to 2^100 is still exact.  Zero, infinities and NaN stay in the factor.
 struct WeightScale {
     float factor;
-    int powers;  // of x's operand, one, and of W's: one register for both
+    int powers;  // of x's operand (127: times one) in the first byte, of W's in the second: one register for both
 };
 constexpr int kPowersOne = 127 | 127 << 8;
 static __device__ __forceinline__ WeightScale weight_scale(float w)
