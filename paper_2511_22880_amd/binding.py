@@ -27,6 +27,8 @@ _EXPERTS = (
     "lora_rows_quantize", "lora_experts_packed_bytes", "lora_experts_pack_weight", "lora_linear_scaled", "lora_experts_group_workspace_bytes",
     "lora_experts_group", "lora_experts_linear", "lora_experts_linear_scaled", "lora_experts_combine",
 )
+# include/lora_attention.h, on the same terms.
+_ATTENTION = ("lora_rotary_turns", "lora_rotary", "lora_cache_append", "lora_attention_workspace_bytes", "lora_attention")
 # every symbol include/*.h declare
 EXPORTS = (
     "lora_pool_bytes", "lora_pool_create", "lora_pool_create_live", "lora_pool_load", "lora_pool_evict",
@@ -43,7 +45,7 @@ EXPORTS = (
     "lora_status_string",
     "lora_last_error",
     "lora_place_extrapolate", "lora_place_assign",
-) + _EXPERTS
+) + _EXPERTS + _ATTENTION
 
 
 class LoraError(RuntimeError):
@@ -98,7 +100,7 @@ _lib = None
 # Argument types of the calls a serving loop makes for every projection or adapter: ctypes then converts plain
 # ints itself, without an object per argument made here (a decode step of one token waits for the host:
 # lora_apply of one token 9.8 -> 8.9 us a call, its launches included).
-_P, _I32, _I64, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+_P, _I32, _I64, _SZ, _F64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_double
 _ARGTYPES = {
     "lora_pool_load": (_P, _I32, _P, _P, ctypes.c_int, _P),
     "lora_pool_load_staged": (_P, _I32, _P, _P, _P, _SZ, _P),
@@ -118,6 +120,11 @@ _ARGTYPES = {
     "lora_experts_linear": (_P, _I64, _I32, _P, _P, _I32, _I32, _I32, _I32, _P, _I32, _P, _I64, _P),
     "lora_experts_linear_scaled": (_P, _I64, _P, _I64, _I32, _P, _P, _I32, _I32, _I32, _I32, _P, _P, _I32, _P, _I64, _P),
     "lora_experts_combine": (_P, _I64, _I32, _P, _P, _I32, _I32, _I32, _P, _I64, _P),
+    "lora_rotary_turns": (_I32, _F64, _I32, _F64, _F64, _F64, _F64, _P, _P),
+    "lora_rotary": (_P, _I64, _I64, _I32, _I32, _I32, _P, _P, _I32, _P, _I64, _I64, _P),
+    "lora_cache_append": (_P, _I64, _I64, _P, _I64, _I64, _I32, _P, _P, _P, _P, _P, _I64, _I64, _I32, _P, _I64, _I64, _P),
+    "lora_attention_workspace_bytes": (_I32, _I32, _I32, _I32, _P, _P),
+    "lora_attention": (_P, _I64, _I64, _I32, _I32, _P, _P, _I32, _P, _I64, _I32, _P, _I32, _P, ctypes.c_float, _P, _I64, _I64, _P, _SZ, _P),
 }
 
 
@@ -129,7 +136,7 @@ def lib() -> ctypes.CDLL:
                               "(there is no fallback path)")
         L = ctypes.CDLL(LIB_PATH)
         for name in EXPORTS:
-            if name in _EXPERTS and not hasattr(L, name):
+            if name in _EXPERTS + _ATTENTION and not hasattr(L, name):
                 continue
             fn = getattr(L, name)
             fn.restype = ctypes.c_char_p if name in ("lora_status_string", "lora_last_error") else ctypes.c_int
@@ -930,5 +937,206 @@ def lora_experts_combine(y, place, weights, z, stream=None) -> None:
         _whole("weights", weights, n, _F32)
     status = (_lib or lib()).lora_experts_combine(y.data_ptr(), ldy, yr, place.data_ptr(), weights.data_ptr(), tokens, picks, out_f,
                                                   z.data_ptr(), ldz, None if stream is None else _queue(stream))
+    if status:
+        _check(status)
+
+
+# ---- between the projections: rotary positions, the paged cache, attention (include/lora_attention.h) ----------------------
+# A call's tensors are all on one GPU, the current one: a launch goes there whatever the tensors' own device is.
+ROTARY_SCALING = ("none", "linear", "wavelength", "dimension")  # LORA_ROTARY_*, in that order
+
+
+class _RotaryArgs(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
+class _CacheArgs(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("bits", ctypes.c_int32)]
+
+
+def lora_rotary_turns(dims: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                      length: float = 8192.0):
+    """(uint64 [dims / 2], magnitude): the part of a turn, in units of 2^-64, that every pair makes in a position."""
+    turns, magnitude = np.zeros(max(0, dims // 2), dtype=np.uint64), ctypes.c_float(1.0)
+    if scaling not in ROTARY_SCALING:
+        raise ValueError(f"scaling: {scaling!r} is none of {', '.join(ROTARY_SCALING)}")
+    _check(lib().lora_rotary_turns(dims, base, ROTARY_SCALING.index(scaling), factor, low, high, length, turns.ctypes.data, ctypes.addressof(magnitude)))
+    return turns, float(magnitude.value)
+
+
+class Rotary:
+    """lora_rotary_t: the frequencies on the GPU (int64, the bits of lora_rotary_turns), and how a head's elements pair up."""
+
+    def __init__(self, dims: int, base: float = 10000.0, *, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                 high: float = 4.0, length: float = 8192.0, device="cuda"):
+        import torch
+        turns, magnitude = lora_rotary_turns(dims, base, scaling, factor, low, high, length)
+        self.turns, self.dims, self.interleaved, self.magnitude = torch.from_numpy(turns.view(np.int64)).to(device), dims, interleaved, magnitude
+        self.args = _RotaryArgs(self.turns.data_ptr(), dims, 1 if interleaved else 0, magnitude)
+        self.address, self.device = ctypes.addressof(self.args), self.turns.get_device()
+
+
+class Cache:
+    """lora_cache_t over the caller's tensors: k, v [pages][kv_heads][page_size][head_dim], bf16, or 8-bit with fp32 scales [pages][kv_heads][page_size]."""
+
+    def __init__(self, k, v, k_scales=None, v_scales=None):
+        if not _BF16:
+            _know_types()
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError(f"k, v: {tuple(k.shape)} of {k.dtype} and {tuple(v.shape)} of {v.dtype} do not do: contiguous [pages][heads][slots][dim] alike are meant")
+        if k.dtype not in _BF16 and k.dtype not in _E4M3:
+            raise ValueError(f"k: {k.dtype} does not do: {_names(_BF16 | _E4M3)} is meant")
+        bits = 16 if k.dtype in _BF16 else 8
+        _on_gpu("k", k)
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        if (k_scales is None) != (bits == 16) or (v_scales is None) != (bits == 16):
+            raise ValueError(f"k_scales, v_scales: a cache in {bits} bits has {'none' if bits == 16 else 'both'}")
+        for name, t in (("v", v), ("k_scales", k_scales), ("v_scales", v_scales)):
+            if t is None:
+                continue
+            if name != "v":
+                if t.shape != k.shape[:3]:
+                    raise ValueError(f"{name}: {tuple(t.shape)} does not do: {tuple(k.shape[:3])} is meant")
+                _whole(name, t, 0, _F32)
+            if t.get_device() != k.get_device():
+                raise ValueError(f"{name}: on another device than k")
+        self.args = _CacheArgs(k.data_ptr(), v.data_ptr(), *(None if t is None else t.data_ptr() for t in (k_scales, v_scales)),
+                               *(int(n) for n in (self.pages, self.page_size, self.kv_heads, self.head_dim)), bits)
+        self.address, self.device = ctypes.addressof(self.args), k.get_device()
+
+
+_current_device = None
+
+
+def _here(device: int, stream) -> None:
+    """Refuses tensors of another GPU than the one that the launch goes to."""
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = torch.cuda.current_device
+    if device < 0:
+        raise ValueError("a tensor on the CPU does not do: ones on the GPU are meant")
+    at = _current_device()
+    if device != at or getattr(stream, "device_index", at) != at:
+        raise ValueError(f"tensors on device {device}, stream {stream}: the current device is {at}")
+
+
+def _heads(name: str, t, device: int):
+    """Shape and strides of bf16 [tokens][heads][dim] on that device."""
+    if t.dtype not in _BF16:
+        if not _BF16:
+            _know_types()
+        if t.dtype not in _BF16:
+            raise ValueError(f"{name}: {t.dtype} does not do: {_names(_BF16)} is meant")
+    if t.dim() != 3 or t.get_device() != device:
+        raise ValueError(f"{name}: {tuple(t.shape)} on {t.device} does not do: [tokens][heads][dim] on the other tensors' GPU is meant")
+    (n, h, d), (s0, s1, s2) = t.shape, t.stride()
+    if s2 != 1 and d > 1:
+        raise ValueError(f"{name}: strides {t.stride()} do not do: a head's elements lie side by side")
+    # (of a dimension of one torch states any stride)
+    return n, h, d, s0 if n > 1 else h * d, s1 if h > 1 else d
+
+
+def _ints(name: str, t, n: int, device: int) -> int:
+    if t.dtype not in _INT32 or t.numel() < n or not t.is_contiguous() or t.get_device() != device:
+        _whole(name, t, n, _INT32)
+        raise ValueError(f"{name}: on another device than the other tensors")
+    return t.data_ptr()
+
+
+def lora_rotary(x, positions, rotary: Rotary, y=None, inverse: bool = False, stream=None) -> None:
+    """x, y: bf16 [tokens][heads][dim] (y None: x, in place); positions: int32 [tokens]; inverse: the gradient's way."""
+    device = x.get_device()
+    n, heads, dim, st, sh = _heads("x", x, device)
+    if y is None:
+        py, yt, yh = x.data_ptr(), st, sh
+    else:
+        yn, yheads, ydim, yt, yh = _heads("y", y, device)
+        if (yn, yheads, ydim) != (n, heads, dim):
+            raise ValueError(f"y: {tuple(y.shape)} does not do: {tuple(x.shape)} is meant")
+        py = y.data_ptr()
+    _here(device, stream)
+    if rotary.device != device:
+        raise ValueError("rotary: on another device than x")
+    status = (_lib or lib()).lora_rotary(x.data_ptr(), st, sh, n, heads, dim, _ints("positions", positions, n, device), rotary.address, 1 if inverse else 0,
+                                         py, yt, yh, None if stream is None else _queue(stream))
+    if status:
+        _check(status)
+
+
+def lora_cache_append(k, v, slots, cache: Cache, rotary: Optional[Rotary] = None, positions=None, q=None, y=None, stream=None) -> None:
+    """k, v: bf16 [tokens][kv_heads][dim]; slots, positions: int32 [tokens]; q: bf16 [tokens][q_heads][dim], turned into y (None: q, in place)."""
+    device = k.get_device()
+    n, heads, dim, kt, kh = _heads("k", k, device)
+    vn, vheads, vdim, vt, vh = _heads("v", v, device)
+    if (heads, dim, vn, vheads, vdim) != (cache.kv_heads, cache.head_dim, n, cache.kv_heads, cache.head_dim):
+        raise ValueError(f"k, v: {tuple(k.shape)} and {tuple(v.shape)} do not do: tokens x {cache.kv_heads} x {cache.head_dim} is meant")
+    pq = py = None
+    qt = qh = q_heads = yt = yh = 0
+    if q is not None:
+        qn, q_heads, qdim, qt, qh = _heads("q", q, device)
+        yn, yheads, ydim, yt, yh = (qn, q_heads, qdim, qt, qh) if y is None else _heads("y", y, device)
+        if (qn, qdim, yn, yheads, ydim) != (n, dim, n, q_heads, dim):
+            raise ValueError(f"q, y: {tuple(q.shape)} and {tuple((q if y is None else y).shape)} do not do: {n} tokens of heads of {dim}, alike, are meant")
+        pq, py = q.data_ptr(), (q if y is None else y).data_ptr()
+    elif y is not None:
+        raise ValueError("y: without q there is nothing for it")
+    _here(device, stream)
+    if cache.device != device or (rotary is not None and rotary.device != device):
+        raise ValueError("cache, rotary: on another device than k")
+    status = (_lib or lib()).lora_cache_append(k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, n, _ints("slots", slots, n, device),
+                                               None if positions is None else _ints("positions", positions, n, device),
+                                               None if rotary is None else rotary.address, cache.address, pq, qt, qh, q_heads, py, yt, yh,
+                                               None if stream is None else _queue(stream))
+    if status:
+        _check(status)
+
+
+def lora_attention_workspace_bytes(tokens: int, q_heads: int, requests: int, width: int, cache: Cache) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().lora_attention_workspace_bytes(tokens, q_heads, requests, width, cache.address, ctypes.addressof(n)))
+    return int(n.value)
+
+
+def lora_attention(q, starts, lengths, page_table, cache: Cache, y, workspace=None, scale: Optional[float] = None, tree=None, most: int = 0,
+                   stream=None) -> None:
+    """q, y: bf16 [tokens][q_heads][dim]; starts [requests + 1], lengths [requests], page_table [requests][width]: int32; tree: int64 [tokens], one
+    word of 64 bits a row (None: rows see their request's own keys up to themselves); scale None: 1 / sqrt(dim); most: the most rows of a request, 0 if unknown."""
+    device = q.get_device()
+    n, heads, dim, qt, qh = _heads("q", q, device)
+    yn, yheads, ydim, yt, yh = _heads("y", y, device)
+    if (dim, yn, yheads, ydim) != (cache.head_dim, n, heads, dim):
+        raise ValueError(f"q, y: {tuple(q.shape)} and {tuple(y.shape)} do not do: alike, of heads of {cache.head_dim}, is meant")
+    requests = lengths.numel()
+    if page_table.dim() != 2 or page_table.dtype not in _INT32 or page_table.shape[0] < requests or page_table.get_device() != device:
+        raise ValueError(f"page_table: {tuple(page_table.shape)} of {page_table.dtype} on {page_table.device} does not do: int32 [{requests}][width] is meant")
+    width, (ld, t1) = page_table.shape[1], page_table.stride()
+    if t1 != 1 and width > 1:
+        raise ValueError(f"page_table: strides {page_table.stride()} do not do: a request's pages lie side by side")
+    if requests <= 1 or ld < width:
+        if requests > 1 and width:
+            raise ValueError(f"page_table: strides {page_table.stride()} do not do: rows overlap")
+        ld = width
+    pt = None
+    if tree is not None:
+        if tree.element_size() != 8 or tree.is_floating_point() or tree.numel() < n or not tree.is_contiguous() or tree.get_device() != device:
+            raise ValueError(f"tree: {tuple(tree.shape)} of {tree.dtype} on {tree.device} does not do: {n} contiguous words of 64 bits are meant")
+        pt = tree.data_ptr()
+    if workspace is None:
+        pw, nw = None, 0
+    else:
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise ValueError("workspace: contiguous bytes on the other tensors' GPU are meant")
+        pw, nw = workspace.data_ptr(), workspace.nbytes
+    _here(device, stream)
+    if cache.device != device:
+        raise ValueError("cache: on another device than q")
+    status = (_lib or lib()).lora_attention(q.data_ptr(), qt, qh, n, heads, _ints("starts", starts, requests + 1, device),
+                                            _ints("lengths", lengths, requests, device), requests, page_table.data_ptr(), ld, width, pt, most, cache.address,
+                                            dim ** -0.5 if scale is None else scale, y.data_ptr(), yt, yh, pw, nw,
+                                            None if stream is None else _queue(stream))
     if status:
         _check(status)

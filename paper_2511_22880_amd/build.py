@@ -13,10 +13,12 @@ LIB = os.path.join(PKG, "liblora_gfx950.so")
 LIB_CLOCKS = os.path.join(PKG, "liblora_gfx950_clocks.so")
 SOURCES = [os.path.join(CSRC, "lora_host.cpp"), os.path.join(CSRC, "lora_place.cpp"),
            os.path.join(CSRC, "lora_memory.cpp"), os.path.join(CSRC, "lora_experts.cpp"),
-           os.path.join(CSRC, "lora_kernels.hip"), os.path.join(CSRC, "lora_experts.hip")]
+           os.path.join(CSRC, "lora_attention.cpp"), os.path.join(CSRC, "lora_kernels.hip"), os.path.join(CSRC, "lora_experts.hip"),
+           os.path.join(CSRC, "lora_attention.hip")]
 HEADERS = [os.path.join(CSRC, "lora_internal.h"), os.path.join(CSRC, "lora_device.h"), os.path.join(ROOT, "include", "lora.h"),
            os.path.join(ROOT, "include", "lora_placement.h"), os.path.join(CSRC, "lora_experts.h"),
-           os.path.join(ROOT, "include", "lora_experts.h")]
+           os.path.join(ROOT, "include", "lora_experts.h"), os.path.join(CSRC, "lora_attention.h"),
+           os.path.join(ROOT, "include", "lora_attention.h")]
 
 
 def build(verbose: bool = False, clocks: bool = False) -> str:

@@ -1,0 +1,120 @@
+// Launch entry points of the operators in include/lora_attention.h (lora_attention.hip), which their host side (lora_attention.cpp) calls.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lora_internal.h"
+
+namespace lora {
+
+// [tokens][heads][dim] in bf16: strides of a token and a head, in elements
+struct HeadRows {
+    uint16_t *p;
+    int64_t token, head;
+};
+
+struct PagedCache {
+    char *k, *v;
+    float *k_scales, *v_scales;
+    int pages, page_shift, kv_heads, dim;
+    bool bits8;
+};
+
+// Rows turned by their positions: q's into y, and (cache.k given) k's into the cache beside v's.
+struct TurnArgs {
+    HeadRows q, y, k, v;
+    int q_heads, heads;       // of q; of q, k and v together
+    uint32_t per_heads;       // 2^32 / heads, rounded up: numbers below 2^16 are divided by it
+    int tokens, dim;
+    const int32_t *positions, *slots;
+    const uint64_t *turns;    // NULL: nothing is turned
+    int dims;                 // turned elements of a head
+    float magnitude;
+    int inverse, interleaved;
+    PagedCache cache;
+    int rows;                 // (token, head) pairs of a work group (set by the launcher)
+};
+
+hipError_t launch_turn(TurnArgs a, hipStream_t stream);
+
+// ---- attention ------------------------------------------------------------------------------------------------
+// A tile: the columns (row of a request, query head of a key head's group), row by row, that a work group holds at a time.
+constexpr int kFewKeys = 128;    // keys a work group takes in a step, k_attend_few
+
+struct AttendArgs {
+    HeadRows q, y;
+    int tokens, q_heads, group;   // group: query heads per key head
+    const int32_t *starts, *lengths, *table;
+    int64_t ld_table;
+    int requests, width;
+    const uint64_t *tree;
+    PagedCache cache;
+    float scale;                  // times log2 e
+    int least, most;              // columns of the requests that this launch takes: least < rows * group <= most
+    int shares;                   // of a key head's work
+    float *parts;                 // workspace: [kv_heads * shares][2][columns][dim], then sums [..][2][columns][2]
+};
+
+// Which launches a call takes.
+struct AttendForm {
+    int columns;       // of a tile
+    int shares;        // of a key head's work
+    int least, most;
+    bool joins;        // some tile may be cut
+};
+struct AttendForms {
+    AttendForm f[2];
+    int n;
+};
+
+inline int64_t most_tiles(int64_t tokens, int group, int requests, int columns)
+{
+    const int64_t all = tokens * group;
+    return all / columns + (requests < tokens ? requests : tokens);
+}
+
+inline AttendForm attend_form(int columns, int keys, int work_groups, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys)
+{
+    const int64_t steps = (most_keys + keys - 1) / keys, work = most_tiles(tokens, group, requests, columns) * (steps ? steps : 1);
+    int64_t shares = work_groups / kv_heads;
+    if (shares < 1) shares = 1;
+    if (shares > work) shares = work;
+    return AttendForm{columns, (int)shares, 0, INT32_MAX, steps > 1 && shares > 1};
+}
+
+inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int64_t most_rows)
+{
+    const int64_t columns = (most_rows > 0 && most_rows < tokens ? most_rows : tokens) * group;
+    const int c = columns <= 16 ? 16 : columns <= 32 ? 32 : 64;
+    return AttendForms{{attend_form(c, kFewKeys, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys), {}}, 1};
+}
+
+inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
+{
+    return f.joins ? (size_t)kv_heads * f.shares * 2 * f.columns * (dim + 2) * sizeof(float) : 0;
+}
+
+// bytes that a call may need, whatever `most` says
+inline size_t attend_most_bytes(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int dim)
+{
+    size_t most = 0;
+    for (int64_t rows : {(int64_t)1, (int64_t)16 / group, (int64_t)32 / group, (int64_t)64 / group, (int64_t)0}) {
+        const AttendForms forms = attend_forms(tokens, group, kv_heads, requests, most_keys, rows);
+        for (int i = 0; i < forms.n; ++i) {
+            const size_t n = attend_parts_bytes(forms.f[i], kv_heads, dim);
+            if (n > most) most = n;
+        }
+    }
+    return most;
+}
+
+// steps of a key head's tiles, at most
+inline int64_t most_steps(int64_t tokens, int group, int requests, int64_t most_keys)
+{
+    return most_tiles(tokens, group, requests, 16) * ((most_keys + 63) / 64 + 1);
+}
+
+hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t stream);
+
+}  // namespace lora

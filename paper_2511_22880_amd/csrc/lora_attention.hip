@@ -1,0 +1,803 @@
+// gfx950 kernels between the adapted projections (include/lora_attention.h): rotary positions, the paged cache's append, attention over it.
+#include "lora_attention.h"
+#include "lora_device.h"
+#include "lora_internal.h"
+
+#include <type_traits>
+
+namespace lora {
+
+static __device__ __forceinline__ float value_lo(uint32_t u) { return __uint_as_float(u << 16); }
+static __device__ __forceinline__ float value_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
+
+// ------------------------------------------------------------------------------------------------
+// Rows turned by their positions.  A row is (token, head), heads counted over q, k and v; a thread has 16 elements of one, two pieces of 8: eight pairs that
+// are turned (half layout: the pieces are dims / 2 apart), or elements that pass.  A work group has `rows` consecutive rows; it asks for all of them, computes the
+// cosines and sines of its few tokens once into LDS (a pair's angle for all heads at once: 64 angles a token, not 64 a head), and turns.  The angle is the low
+// 64 bits of position * turns, of which the upper 32 count: exact to 2^-31 turns at any position, without a division or a table of positions.
+// ------------------------------------------------------------------------------------------------
+constexpr int kTurnThreads = 256;
+
+template <bool BITS8>
+static __device__ __forceinline__ void store_held(char *row, float *scale_at, const float (&a)[8], const float (&b)[8], int d0, int d1, int units, bool first)
+{
+    if constexpr (!BITS8) {
+        uint16_t *y = reinterpret_cast<uint16_t *>(row);
+        *reinterpret_cast<uint4 *>(y + d0) = uint4{pack_bf16_rne(a[0], a[1]), pack_bf16_rne(a[2], a[3]), pack_bf16_rne(a[4], a[5]), pack_bf16_rne(a[6], a[7])};
+        *reinterpret_cast<uint4 *>(y + d1) = uint4{pack_bf16_rne(b[0], b[1]), pack_bf16_rne(b[2], b[3]), pack_bf16_rne(b[4], b[5]), pack_bf16_rne(b[6], b[7])};
+    } else {
+        // x * 448 / d, d = m 2^(e - 127): the power of two is exact, the quotient by m is corrected once (see lora_rows_quantize, whose rounding this is)
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, max(__float_as_uint(a[i]) & 0x7FFFFFFFu, __float_as_uint(b[i]) & 0x7FFFFFFFu));
+        for (int d = 1; d < units; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+        const float largest = __uint_as_float(top);
+        float scale = largest;
+        uint32_t o[4] = {0u, 0u, 0u, 0u};
+        if (top < 0x7F800000u) {
+            const float d = fmaxf(largest, 448.f * 0x1p-126f);
+            scale = d / 448.f;
+            const uint32_t bits = __float_as_uint(d), e = bits >> 23;
+            const float m = __uint_as_float((bits & 0x007FFFFFu) | 0x3F800000u), f = 1.75f * __uint_as_float((262u - e) << 23), r = __builtin_amdgcn_rcpf(m);
+            auto quotient = [&](float x) __attribute__((always_inline)) {
+                const float n = x * f, t = n * r;
+                return fmaf(fmaf(-t, m, n), r, t);
+            };
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float *c = i < 2 ? a + 4 * i : b + 4 * (i - 2);
+                const int p = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(c[0]), quotient(c[1]), 0, false);
+                o[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(quotient(c[2]), quotient(c[3]), p, true);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float x = i < 8 ? a[i] : b[i - 8];
+                o[i >> 2] |= (top > 0x7F800000u || (__float_as_uint(x) & 0x7FFFFFFFu) >= 0x7F800000u ? 0x7Fu : 0u) << (8 * (i & 3));
+            }
+        }
+        *reinterpret_cast<uint2 *>(row + d0) = uint2{o[0], o[1]};
+        *reinterpret_cast<uint2 *>(row + d1) = uint2{o[2], o[3]};
+        if (first) *scale_at = scale;
+    }
+}
+
+// KIND 0: q alone; 1: with a cache in bf16; 2: in 8 bits.  PASSES: rows of a thread.
+template <int KIND, int PASSES>
+__global__ __launch_bounds__(kTurnThreads) void k_turn(TurnArgs a)
+{
+    extern __shared__ float2 turned[];  // [tokens here][pairs]: cosine and sine, times the magnitude
+    const int tid = threadIdx.x, units = a.dim >> 4, at_once = kTurnThreads / units;
+    const int r0 = tid / units, u = tid - r0 * units;
+    const uint32_t first = blockIdx.x * (uint32_t)a.rows;
+    const int t_first = (int)(first / (uint32_t)a.heads), h_first = (int)(first - (uint32_t)t_first * a.heads);
+    auto over_heads = [&](int flat) __attribute__((always_inline)) { return a.per_heads ? (int)__umulhi((uint32_t)flat, a.per_heads) : flat; };
+
+    uint4 lo[PASSES], hi[PASSES];
+    int token[PASSES], head[PASSES], slot[PASSES];
+    bool there[PASSES], turns[PASSES];
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int flat = h_first + r0 + i * at_once, t = over_heads(flat);
+        head[i] = flat - t * a.heads;
+        token[i] = t_first + t;
+        there[i] = token[i] < a.tokens && r0 < at_once;
+        const int tok = there[i] ? token[i] : 0;
+        const bool is_q = head[i] < a.q_heads, is_k = !is_q && (KIND == 0 || head[i] < a.q_heads + a.cache.kv_heads);
+        slot[i] = 0;
+        if constexpr (KIND > 0) {
+            slot[i] = a.slots[tok];
+            there[i] &= (uint32_t)slot[i] < (uint32_t)a.cache.pages << a.cache.page_shift;
+        }
+        if (a.positions) there[i] &= a.positions[tok] >= 0;
+        turns[i] = a.turns && (KIND == 0 || is_q || is_k) && u < a.dims >> 4;
+        HeadRows from = a.q;
+        int h = head[i];
+        if constexpr (KIND > 0) {
+            from = is_q ? a.q : is_k ? a.k : a.v;
+            h = is_q ? h : is_k ? h - a.q_heads : h - a.q_heads - a.cache.kv_heads;
+        }
+        const bool apart = turns[i] && !a.interleaved;
+        const int d0 = apart ? 8 * u : 16 * u, d1 = apart ? 8 * u + (a.dims >> 1) : 16 * u + 8;
+        if (there[i]) {
+            const uint16_t *row = from.p + tok * from.token + h * from.head;
+            lo[i] = ld16(row + d0);
+            hi[i] = ld16(row + d1);
+        }
+    }
+    if (a.turns) {
+        const int pairs = a.dims >> 1, n = (over_heads(h_first + at_once * PASSES - 1) + 1) * pairs;
+        for (int e = tid; e < n; e += kTurnThreads) {
+            const int t = e / pairs, p = e - t * pairs, tok = t_first + t < a.tokens ? t_first + t : 0;
+            const uint64_t all = (uint64_t)(uint32_t)a.positions[tok] * a.turns[p];
+            // quarters of a turn apart, what is left within an eighth either way: as a float it is off by 2^-28 turns at most
+            const uint32_t turn = (uint32_t)(all >> 32), quarter = (turn + 0x20000000u) >> 30;
+            float s, c;
+            sincospif((float)(int32_t)(turn - (quarter << 30)) * 0x1p-31f, &s, &c);
+            if (quarter & 1) {
+                const float was = c;
+                c = -s;
+                s = was;
+            }
+            if (quarter & 2) {
+                c = -c;
+                s = -s;
+            }
+            turned[e] = float2{c * a.magnitude, (a.inverse ? -s : s) * a.magnitude};
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        if (!there[i]) continue;
+        const uint32_t w[8] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w, hi[i].x, hi[i].y, hi[i].z, hi[i].w};
+        float x[8], z[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[2 * j] = value_lo(w[j]);
+            x[2 * j + 1] = value_hi(w[j]);
+            z[2 * j] = value_lo(w[4 + j]);
+            z[2 * j + 1] = value_hi(w[4 + j]);
+        }
+        const bool apart = turns[i] && !a.interleaved;
+        const int d0 = apart ? 8 * u : 16 * u, d1 = apart ? 8 * u + (a.dims >> 1) : 16 * u + 8;
+        if (turns[i]) {
+            const float2 *cs = turned + (token[i] - t_first) * (a.dims >> 1) + 8 * u;
+            if (a.interleaved) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 f = cs[j], g = cs[4 + j];
+                    const float x0 = x[2 * j], x1 = x[2 * j + 1], z0 = z[2 * j], z1 = z[2 * j + 1];
+                    x[2 * j] = x0 * f.x - x1 * f.y;
+                    x[2 * j + 1] = x0 * f.y + x1 * f.x;
+                    z[2 * j] = z0 * g.x - z1 * g.y;
+                    z[2 * j + 1] = z0 * g.y + z1 * g.x;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float2 f = cs[j];
+                    const float x0 = x[j], z0 = z[j];
+                    x[j] = x0 * f.x - z0 * f.y;
+                    z[j] = x0 * f.y + z0 * f.x;
+                }
+            }
+        }
+        if (KIND == 0 || head[i] < a.q_heads) {
+            store_held<false>(reinterpret_cast<char *>(a.y.p + token[i] * a.y.token + head[i] * a.y.head), nullptr, x, z, d0, d1, units, false);
+        } else if constexpr (KIND > 0) {
+            const int h = head[i] - a.q_heads;
+            const bool is_k = h < a.cache.kv_heads;
+            const int kh = is_k ? h : h - a.cache.kv_heads, page = slot[i] >> a.cache.page_shift;
+            const int64_t at = (((int64_t)page * a.cache.kv_heads + kh) << a.cache.page_shift) + (slot[i] & ((1 << a.cache.page_shift) - 1));
+            store_held<KIND == 2>((is_k ? a.cache.k : a.cache.v) + at * a.dim * (KIND == 2 ? 1 : 2), (is_k ? a.cache.k_scales : a.cache.v_scales) + at, x, z, d0, d1,
+                                  units, u == 0);
+        }
+    }
+}
+
+template <int KIND>
+static hipError_t launch_turn_kind(TurnArgs a, hipStream_t stream)
+{
+    const int at_once = kTurnThreads / (a.dim >> 4), pairs = a.turns ? a.dims >> 1 : 0;
+    const int64_t all = (int64_t)a.tokens * a.heads;
+    // tokens that a work group of so many passes meets, and LDS for their pairs
+    auto room = [&](int passes) { return (size_t)((passes * at_once - 2) / a.heads + 2) * pairs * sizeof(float2); };
+    int passes = 1;
+    while (passes < 4 && all > (int64_t)8 * kComputeUnits * passes * at_once && room(2 * passes) <= 32768) passes *= 2;
+    a.rows = passes * at_once;
+    const dim3 grid((unsigned)((all + a.rows - 1) / a.rows)), threads(kTurnThreads);
+    if (passes == 1)
+        hipLaunchKernelGGL((k_turn<KIND, 1>), grid, threads, room(1), stream, a);
+    else if (passes == 2)
+        hipLaunchKernelGGL((k_turn<KIND, 2>), grid, threads, room(2), stream, a);
+    else
+        hipLaunchKernelGGL((k_turn<KIND, 4>), grid, threads, room(4), stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_turn(TurnArgs a, hipStream_t stream)
+{
+    if (!a.cache.k) return launch_turn_kind<0>(a, stream);
+    return a.cache.bits8 ? launch_turn_kind<2>(a, stream) : launch_turn_kind<1>(a, stream);
+}
+
+// ------------------------------------------------------------------------------------------------
+// How the work of an attention call is dealt out.  A request's columns (row by row, the query heads of a key head's group side by side) are cut into tiles of
+// TC; a tile takes as many steps of KEYS keys as its last row sees, one at least.  The steps of all tiles of all requests, in that order, are one list for every key
+// head, and a head's `shares` work groups take equal runs of it.  A run that has all of a tile's steps writes its rows; otherwise it leaves sums, which
+// k_attend_join brings together.  The list follows from starts and lengths on the device alone: every work group adds up the requests' steps and finds
+// its place in it, so the host need not know any length, and a captured call follows them.
+// ------------------------------------------------------------------------------------------------
+struct Request {
+    int first, n, keys;  // first row, rows, keys
+};
+
+static __device__ __forceinline__ Request request_at(const AttendArgs &a, int r)
+{
+    const int s0 = min(max(a.starts[r], 0), a.tokens), s1 = min(max(a.starts[r + 1], 0), a.tokens);
+    const int64_t room = (int64_t)a.width << a.cache.page_shift;
+    const int64_t keys = a.lengths[r];
+    return Request{s0, max(s1 - s0, 0), (int)(keys < 0 ? 0 : keys < room ? keys : room)};
+}
+
+// sum of floor((a i + b) / m) for i < n: the part that whole multiples of m give, then the same question with the axes exchanged
+static __device__ __forceinline__ uint32_t sum_of_floors(uint32_t n, uint32_t m, uint32_t a, uint32_t b)
+{
+    uint32_t sum = 0;
+    while (true) {
+        if (a >= m) {
+            const uint32_t f = a / m;
+            sum += (n & 1 ? n * ((n - 1) >> 1) : (n >> 1) * (n - 1)) * f;
+            a -= f * m;
+        }
+        if (b >= m) {
+            const uint32_t f = b / m;
+            sum += n * f;
+            b -= f * m;
+        }
+        const uint32_t top = a * n + b;
+        if (top < m) return sum;
+        n = top / m;
+        b = top - n * m;
+        const uint32_t t = m;
+        m = a;
+        a = t;
+    }
+}
+
+template <int TC, int KEYS>
+struct Dealt {
+    // of a request
+    struct Tiles {
+        int n;          // tiles
+        uint32_t last;  // steps of the last one, and of all where rows do not see more and more
+        bool level;
+        uint32_t whole, part;  // steps before the request's own keys; (context mod KEYS) * group + TC
+    };
+    static __device__ __forceinline__ Tiles tiles(const AttendArgs &a, const Request &q)
+    {
+        const int columns = q.n * a.group;
+        if (q.n == 0 || columns <= a.least || columns > a.most) return Tiles{0, 0, true, 0, 0};
+        const int context = q.keys - q.n;
+        const uint32_t last = max(1u, (uint32_t)(q.keys + KEYS - 1) / KEYS);
+        return Tiles{(columns - 1) / TC + 1, last, a.tree != nullptr || context < 0, (uint32_t)context / KEYS, (uint32_t)(context & (KEYS - 1)) * a.group + TC};
+    }
+    // steps of the first t tiles, t < n
+    static __device__ __forceinline__ uint32_t before(const AttendArgs &a, const Tiles &s, uint32_t t)
+    {
+        const uint32_t m = (uint32_t)a.group * KEYS;
+        return s.level ? t * s.last : t * s.whole + sum_of_floors(t, m, TC, s.part + m - 1);
+    }
+    static __device__ __forceinline__ uint32_t steps(const AttendArgs &a, const Tiles &s, uint32_t t)
+    {
+        const uint32_t m = (uint32_t)a.group * KEYS;
+        return s.level || (int)t == s.n - 1 ? s.last : s.whole + (s.part + t * TC + m - 1) / m;
+    }
+    static __device__ __forceinline__ uint32_t all(const AttendArgs &a, const Tiles &s) { return s.n == 0 ? 0u : (s.n == 1 ? 0u : before(a, s, s.n - 1)) + s.last; }
+
+    // a place in the list
+    struct Place {
+        int r, t;
+        uint32_t at, of;  // step of the tile, its steps
+        Request q;
+        Tiles s;
+    };
+    struct Found {
+        uint32_t sums[16];
+        int r;
+        uint32_t at;
+    };
+
+    // Every thread of the work group: place(total) says which step of the list is meant, given how many there are (UINT32_MAX: none, and false is returned).
+    template <int THREADS, class Which>
+    static __device__ __forceinline__ bool find(const AttendArgs &a, Found &f, Which which, Place &p)
+    {
+        constexpr int kWaves = THREADS / 64;
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int each = (a.requests + THREADS - 1) / THREADS, r0 = tid * each, r1 = min(a.requests, r0 + each);
+        uint32_t mine = 0;
+        for (int r = r0; r < r1; ++r) mine += all(a, tiles(a, request_at(a, r)));
+        uint32_t upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
+            upto += lane >= d ? o : 0;
+        }
+        if (lane == 63) f.sums[wave] = upto;
+        __syncthreads();
+        uint32_t total = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w == wave) upto += total;
+            total += f.sums[w];
+        }
+        const uint32_t want = which(total);
+        if (want >= total) return false;
+        uint32_t from = upto - mine;
+        if (want >= from && want < upto) {
+            for (int r = r0; r < r1; ++r) {
+                const uint32_t n = all(a, tiles(a, request_at(a, r)));
+                if (want < from + n) {
+                    f.r = r;
+                    f.at = want - from;
+                    break;
+                }
+                from += n;
+            }
+        }
+        __syncthreads();
+        p.r = __builtin_amdgcn_readfirstlane(f.r);
+        uint32_t at = __builtin_amdgcn_readfirstlane(f.at);
+        p.q = request_at(a, p.r);
+        p.s = tiles(a, p.q);
+        // the last tile that begins at or before it, 64 at a time
+        int lo = 0, hi = p.s.n - 1;
+        while (hi > lo) {
+            const int step = (hi - lo + 63) >> 6, t = lo + (lane + 1) * step;
+            const int k = (int)__popcll(__ballot(t <= hi && before(a, p.s, t) <= at));
+            lo += k * step;
+            hi = min(hi, lo + step - 1);
+        }
+        p.t = lo;
+        p.at = lo > 0 ? __builtin_amdgcn_readfirstlane(at - before(a, p.s, lo)) : at;
+        p.of = steps(a, p.s, p.t);
+        return true;
+    }
+    // the tile behind it; false where there is none
+    static __device__ __forceinline__ bool next(const AttendArgs &a, Place &p)
+    {
+        p.at = 0;
+        if (++p.t >= p.s.n) {
+            p.t = 0;
+            do {
+                if (++p.r >= a.requests) return false;
+                p.q = request_at(a, p.r);
+                p.s = tiles(a, p.q);
+            } while (p.s.n == 0);
+        }
+        p.of = steps(a, p.s, p.t);
+        return true;
+    }
+};
+
+// first step of a share of `total`
+static __device__ __forceinline__ uint32_t share_at(uint32_t total, int share, int shares) { return (uint32_t)((uint64_t)total * share / shares); }
+
+// where a share leaves its sums: slot 1 of those of a tile that begins in it, slot 0 of one that began earlier
+static __device__ __forceinline__ int64_t part_of(int head, int shares, int share, bool begins) { return ((int64_t)head * shares + share) * 2 + begins; }
+
+// ------------------------------------------------------------------------------------------------
+// Attention of few columns: tiles of 16 C.  A wavefront takes 32 keys at a time, the work group's four 128, each with a running maximum and sum of its own; what
+// they have is brought together in LDS at the tile's end.  Nothing goes through LDS on the way: with S^T = K Q^T (16 x 16 x 32 matrix instructions) a lane
+// holds a column's scores of eight keys, and those are what O^T = V^T P^T takes as the operand of eight values of k from that lane, if row m of the score
+// tile t is key 8 (m / 4) + 4 t + m mod 4 and lane (quad, n) brings the keys 8 quad .. 8 quad + 7.  It reads their dims [n D / 16, (n + 1) D / 16): sixteen
+// lanes a whole row of v; the element c of each is the operand of tile c, whose row n is dim n D / 16 + c, put together by byte permutes.
+// ------------------------------------------------------------------------------------------------
+template <int BYTES>
+struct Bytes;
+template <>
+struct Bytes<4> {
+    uint32_t w[1];
+};
+template <>
+struct Bytes<8> {
+    uint32_t w[2];
+};
+template <>
+struct Bytes<16> {
+    uint32_t w[4];
+};
+template <int BYTES>
+static __device__ __forceinline__ Bytes<BYTES> ld_bytes(const char *p)
+{
+    typedef __attribute__((ext_vector_type(BYTES / 4))) uint32_t vec;
+    return __builtin_bit_cast(Bytes<BYTES>, *reinterpret_cast<const vec *>(p));
+}
+template <>
+__device__ __forceinline__ Bytes<4> ld_bytes<4>(const char *p)
+{
+    return Bytes<4>{{*reinterpret_cast<const uint32_t *>(p)}};
+}
+
+// two E4M3 values, of the low or the high half, as bf16: exact
+template <bool HIGH>
+static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t u)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HIGH));
+}
+
+static __device__ __forceinline__ bool odd16(uint32_t u) { return (u & 0x7F80u) == 0x7F80u || (u & 0x7F800000u) == 0x7F800000u; }  // an infinity or NaN
+
+template <int D, bool F8>
+struct FewShape {
+    static constexpr int kRowBytes = D * (F8 ? 1 : 2);
+    static constexpr int kLoadsK = kRowBytes / 64;   // of 16 bytes a lane, of a tile of 16 keys
+    static constexpr int kBytesV = kRowBytes / 16;   // of a key, a lane's
+    static constexpr int kSteps = D / 32;            // of k, of the scores
+    static constexpr int kTiles = D / 16;            // of v
+};
+
+template <int D, bool F8, int C>
+__global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a)
+{
+    using S = FewShape<D, F8>;
+    using W = Dealt<16 * C, kFewKeys>;
+    constexpr int TC = 16 * C;
+    __shared__ typename W::Found found;
+    __shared__ float2 sums[4][TC];
+    __shared__ float part[4][4 * S::kTiles][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, quad = lane >> 4;
+    const int kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
+    typename W::Place p;
+    uint32_t left = 0;
+    if (!W::template find<256>(a, found, [&](uint32_t total) {
+            const uint32_t from = share_at(total, share, a.shares);
+            left = share_at(total, share + 1, a.shares) - from;
+            return left ? from : UINT32_MAX;
+        }, p)) return;
+
+    const int page = 1 << a.cache.page_shift;
+    // a lane's keys of a step, and where their bytes are in 16 of them
+    const int k_in = ((8 * (n >> 2) + (n & 3)) & 15) * S::kRowBytes + quad * 16;
+    const int v_in = 8 * (quad & 1) * S::kRowBytes + n * S::kBytesV;
+
+    while (true) {
+        const uint32_t to = min(p.of, p.at + left);
+        const bool whole = p.at == 0 && to == p.of;
+        const int context = p.q.keys - p.q.n, columns = p.q.n * a.group, c0 = p.t * TC;
+        // queries: the scores' other operand
+        bf16x8 q[C][S::kSteps];
+        int sees[C];        // last key a column sees (no tree)
+        uint64_t word[C];   // which of its request's own keys (tree)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            int col = c0 + 16 * c + n;
+            if (col >= columns) col = c0;
+            const int i = col / a.group, row = p.q.first + i, h = kh * a.group + (col - i * a.group);
+            const uint16_t *at = a.q.p + row * a.q.token + h * a.q.head;
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s) q[c][s] = as_bf16x8(ld16(at + (F8 ? 64 * (s >> 1) + 16 * quad + 8 * (s & 1) : 32 * s + 8 * quad)));
+            sees[c] = context + i;
+            word[c] = a.tree ? a.tree[row] : 0;
+        }
+        // keys up to here are seen by all
+        const int open = min(p.q.keys, a.tree ? context : context + c0 / a.group + 1);
+
+        f32x4 o[C][S::kTiles];
+        float top[C], sum[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            top[c] = -INFINITY;
+            sum[c] = 0.f;
+#pragma unroll
+            for (int i = 0; i < S::kTiles; ++i) o[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        Bytes<16> k[2][S::kLoadsK];
+        Bytes<S::kBytesV> v[8];
+        float4 ks[2], vs[2];
+        // the two pages of a wavefront's 32 keys at step j, -1 where there is none
+        struct Pages {
+            int id[2];
+        };
+        const int32_t *table = a.table + p.r * a.ld_table;
+        auto pages_of = [&](uint32_t j) __attribute__((always_inline)) {
+            Pages g;
+            const int key = (int)j * kFewKeys + 32 * wave;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int at = key + 16 * i;
+                const int id = at < p.q.keys ? table[at >> a.cache.page_shift] : -1;
+                g.id[i] = (unsigned)id < (unsigned)a.cache.pages ? id : -1;
+            }
+            return g;
+        };
+        auto base_of = [&](const Pages &g, uint32_t j, int half) __attribute__((always_inline)) {
+            const int64_t in = ((int64_t)j * kFewKeys + 32 * wave + 16 * half) & (page - 1);
+            return ((int64_t)max(g.id[half], 0) * a.cache.kv_heads + kh) * page + in;  // in rows
+        };
+        auto load_k = [&](const Pages &g, uint32_t j) __attribute__((always_inline)) {
+            const int64_t r0 = base_of(g, j, 0), r1 = base_of(g, j, 1);
+            const char *at = a.cache.k + (n < 8 ? r0 : r1) * S::kRowBytes + k_in;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int s = 0; s < S::kLoadsK; ++s) k[t][s] = ld_bytes<16>(at + t * 4 * S::kRowBytes + s * 64);
+            if constexpr (F8) {
+                const float *sc = a.cache.k_scales + (quad < 2 ? r0 : r1) + 8 * (quad & 1);
+                ks[0] = *reinterpret_cast<const float4 *>(sc);
+                ks[1] = *reinterpret_cast<const float4 *>(sc + 4);
+            }
+        };
+        auto load_v = [&](const Pages &g, uint32_t j) __attribute__((always_inline)) {
+            const int64_t r0 = base_of(g, j, 0), r1 = base_of(g, j, 1), r = quad < 2 ? r0 : r1;
+            const char *at = a.cache.v + r * S::kRowBytes + v_in;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = ld_bytes<S::kBytesV>(at + i * S::kRowBytes);
+            if constexpr (F8) {
+                const float *sc = a.cache.v_scales + r + 8 * (quad & 1);
+                vs[0] = *reinterpret_cast<const float4 *>(sc);
+                vs[1] = *reinterpret_cast<const float4 *>(sc + 4);
+            }
+        };
+        auto four = [](const float4 &f, int i) __attribute__((always_inline)) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; };
+
+        if (p.q.keys > 0) {
+            Pages now = pages_of(p.at), then = pages_of(p.at + 1 < to ? p.at + 1 : p.at);
+            load_k(now, p.at);
+            load_v(now, p.at);
+            for (uint32_t j = p.at; j < to; ++j) {
+                const uint32_t j1 = j + 1 < to ? j + 1 : j, j2 = j + 2 < to ? j + 2 : j1;
+                const Pages after = pages_of(j2);
+                // scores
+                f32x4 sc[C][2];
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) sc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < S::kSteps; ++s)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        bf16x8 x;
+                        if constexpr (F8) {
+                            const uint32_t w0 = k[t][s >> 1].w[2 * (s & 1)], w1 = k[t][s >> 1].w[2 * (s & 1) + 1];
+                            x = as_bf16x8(uint4{two_of_e4m3<false>(w0), two_of_e4m3<true>(w0), two_of_e4m3<false>(w1), two_of_e4m3<true>(w1)});
+                        } else {
+                            x = __builtin_bit_cast(bf16x8, k[t][s]);
+                        }
+#pragma unroll
+                        for (int c = 0; c < C; ++c) sc[c][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[c][s], sc[c][t], 0, 0, 0);
+                    }
+                const int key0 = (int)j * kFewKeys + 32 * wave, mine = key0 + 8 * quad;
+                [[maybe_unused]] float4 kn[2] = {ks[0], ks[1]};
+                load_k(then, j1);
+                const bool plain = now.id[0] >= 0 && now.id[1] >= 0 && key0 + 32 <= open;
+                uint32_t seen[C];
+                const bool held = now.id[quad >> 1] >= 0;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    seen[c] = 0xFFu;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[c][t][i] *= F8 ? a.scale * four(kn[t], i) : a.scale;
+                    if (!plain) {
+                        seen[c] = 0;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int key = mine + i, own = key - context;
+                            bool s = held && key < p.q.keys;
+                            if (a.tree)
+                                s = s && (own < 0 || (own < 64 && (word[c] >> (own & 63) & 1)));
+                            else
+                                s = s && key <= sees[c];
+                            seen[c] |= (uint32_t)s << i;
+                            sc[c][i >> 2][i & 3] = s ? sc[c][i >> 2][i & 3] : -INFINITY;
+                        }
+                    }
+                }
+                // weights
+                uint4 w[C];
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    float t = fmaxf(fmaxf(fmaxf(sc[c][0][0], sc[c][0][1]), fmaxf(sc[c][0][2], sc[c][0][3])),
+                                    fmaxf(fmaxf(sc[c][1][0], sc[c][1][1]), fmaxf(sc[c][1][2], sc[c][1][3])));
+                    t = fmaxf(t, __shfl_xor(t, 16, 64));
+                    t = fmaxf(t, __shfl_xor(t, 32, 64));
+                    t = fmaxf(t, top[c]);
+                    if (__any(t > top[c])) {
+                        const float f = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[c] - t);
+                        sum[c] *= f;
+#pragma unroll
+                        for (int i = 0; i < S::kTiles; ++i) o[c][i] *= f;
+                        top[c] = t;
+                    }
+                    const float from = t == -INFINITY ? 0.f : t;
+                    float e[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        e[i] = __builtin_amdgcn_exp2f(sc[c][i >> 2][i & 3] - from);
+                        sum[c] += e[i];
+                        if constexpr (F8) e[i] = plain || (seen[c] >> i & 1) ? e[i] * four(vs[i >> 2], i & 3) : 0.f;
+                    }
+                    w[c] = uint4{pack_bf16_rne(e[0], e[1]), pack_bf16_rne(e[2], e[3]), pack_bf16_rne(e[4], e[5]), pack_bf16_rne(e[6], e[7])};
+                }
+                // values
+                if (!plain) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int x = 0; x < S::kBytesV / 4; ++x) v[i].w[x] = held && mine + i < p.q.keys ? v[i].w[x] : 0u;
+                }
+                uint4 vt[S::kTiles];
+                if constexpr (F8) {
+#pragma unroll
+                    for (int x = 0; x < S::kBytesV / 4; ++x) {
+                        uint32_t four_keys[2][4];
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const uint32_t v0 = v[4 * y].w[x], v1 = v[4 * y + 1].w[x], v2 = v[4 * y + 2].w[x], v3 = v[4 * y + 3].w[x];
+                            const uint32_t l01 = __builtin_amdgcn_perm(v1, v0, 0x05010400u), l23 = __builtin_amdgcn_perm(v3, v2, 0x05010400u);
+                            const uint32_t h01 = __builtin_amdgcn_perm(v1, v0, 0x07030602u), h23 = __builtin_amdgcn_perm(v3, v2, 0x07030602u);
+                            four_keys[y][0] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
+                            four_keys[y][1] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
+                            four_keys[y][2] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
+                            four_keys[y][3] = __builtin_amdgcn_perm(h23, h01, 0x07060302u);
+                        }
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+                            vt[4 * x + b] = uint4{two_of_e4m3<false>(four_keys[0][b]), two_of_e4m3<true>(four_keys[0][b]), two_of_e4m3<false>(four_keys[1][b]),
+                                                  two_of_e4m3<true>(four_keys[1][b])};
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < S::kTiles; ++i) {
+                        uint32_t d[4];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) d[y] = __builtin_amdgcn_perm(v[2 * y + 1].w[i >> 1], v[2 * y].w[i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
+                        vt[i] = uint4{d[0], d[1], d[2], d[3]};
+                    }
+                }
+                load_v(then, j1);
+                bool odd = false;
+                if (!plain) {
+                    // a weight of zero times an infinity is NaN: where a value is one, a key at a time, for the columns that see it
+#pragma unroll
+                    for (int i = 0; i < S::kTiles; ++i) odd |= odd16(vt[i].x) || odd16(vt[i].y) || odd16(vt[i].z) || odd16(vt[i].w);
+                    odd = __any(odd);
+                }
+                if (!odd) {
+#pragma unroll
+                    for (int i = 0; i < S::kTiles; ++i)
+#pragma unroll
+                        for (int c = 0; c < C; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt[i]), as_bf16x8(w[c]), o[c][i], 0, 0, 0);
+                } else {
+                    for (int key = 0; key < 32; ++key) {
+                        const bool here = quad == key >> 3;
+                        const uint32_t half = key & 1 ? 0xFFFF0000u : 0xFFFFu;
+                        const int dword = (key & 7) >> 1;
+                        const uint4 only{here && dword == 0 ? half : 0u, here && dword == 1 ? half : 0u, here && dword == 2 ? half : 0u, here && dword == 3 ? half : 0u};
+#pragma unroll
+                        for (int c = 0; c < C; ++c) {
+                            const bool s = (uint32_t)__shfl((int)seen[c], (key >> 3) * 16 + n, 64) >> (key & 7) & 1;
+                            const uint4 wk{w[c].x & only.x, w[c].y & only.y, w[c].z & only.z, w[c].w & only.w};
+#pragma unroll
+                            for (int i = 0; i < S::kTiles; ++i) {
+                                const uint4 vk{vt[i].x & only.x, vt[i].y & only.y, vt[i].z & only.z, vt[i].w & only.w};
+                                const f32x4 one = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vk), as_bf16x8(wk), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[c][i][e] += s ? one[e] : 0.f;
+                            }
+                        }
+                    }
+                }
+                now = then;
+                then = after;
+            }
+        }
+
+        // the four wavefronts' sums: each on the largest of their maxima, then one quarter of a column's dims a wavefront
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            sum[c] += __shfl_xor(sum[c], 16, 64);
+            sum[c] += __shfl_xor(sum[c], 32, 64);
+            if (quad == 0) sums[wave][16 * c + n] = float2{top[c], sum[c]};
+        }
+        __syncthreads();
+        const int64_t slot = part_of(kh, a.shares, share, p.at == 0);
+        float *slots = a.parts + (int64_t)a.cache.kv_heads * a.shares * 2 * TC * D;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float most = -INFINITY, all = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, sums[i][16 * c + n].x);
+            const float from = most == -INFINITY ? 0.f : most, f = __builtin_amdgcn_exp2f(top[c] - from);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) all += sums[i][16 * c + n].y * __builtin_amdgcn_exp2f(sums[i][16 * c + n].x - from);
+            if (c > 0) __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < S::kTiles; ++i) part[wave][e * S::kTiles + i][lane] = o[c][i][e] * f;
+            __syncthreads();
+            const int in = 16 * c + n, col = c0 + in;
+            if (col < columns) {
+                float z[S::kTiles];
+#pragma unroll
+                for (int i = 0; i < S::kTiles; ++i) {
+                    const int at = wave * S::kTiles + i;
+                    z[i] = part[0][at][lane] + part[1][at][lane] + part[2][at][lane] + part[3][at][lane];
+                }
+                const int dim = S::kTiles * (4 * quad + wave);
+                if (whole) {
+                    const float by = all == 0.f ? 0.f : 1.f / all;
+                    const int i = col / a.group, row = p.q.first + i, h = kh * a.group + (col - i * a.group);
+                    uint32_t *y = reinterpret_cast<uint32_t *>(a.y.p + row * a.y.token + h * a.y.head + dim);
+#pragma unroll
+                    for (int x = 0; x < S::kTiles; x += 4) *reinterpret_cast<uint2 *>(y + x / 2) = uint2{pack_bf16_rne(z[x] * by, z[x + 1] * by), pack_bf16_rne(z[x + 2] * by, z[x + 3] * by)};
+                } else {
+                    float *y = a.parts + (slot * TC + in) * D + dim;
+#pragma unroll
+                    for (int x = 0; x < S::kTiles; x += 4) *reinterpret_cast<float4 *>(y + x) = float4{z[x], z[x + 1], z[x + 2], z[x + 3]};
+                    if (wave == 0 && quad == 0) *reinterpret_cast<float2 *>(slots + (slot * TC + in) * 2) = float2{most, all};
+                }
+            }
+        }
+        left -= to - p.at;
+        if (left == 0 || !W::next(a, p)) return;
+        __syncthreads();
+    }
+}
+
+// Tiles that several shares have a part of: a work group has 16 columns of the tile that the first step of share s + 1 lies in, if that tile begins in share s.
+template <int D, int TC, int KEYS>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
+{
+    using W = Dealt<TC, KEYS>;
+    constexpr int kEach = D / 16;
+    __shared__ typename W::Found found;
+    const int kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
+    typename W::Place p;
+    uint32_t total = 0, step = 0;
+    if (!W::template find<256>(a, found, [&](uint32_t all) {
+            total = all;
+            return step = share_at(all, share + 1, a.shares);
+        }, p)) return;
+    if (p.at == 0 || step - p.at < share_at(total, share, a.shares)) return;
+    const uint32_t end = step - p.at + p.of;
+    int last = share + 1;
+    while (last + 1 < a.shares && share_at(total, last + 1, a.shares) < end) ++last;
+    const int in = 16 * blockIdx.y + (threadIdx.x >> 4), dim = (threadIdx.x & 15) * kEach, col = p.t * TC + in;
+    if (col >= p.q.n * a.group) return;
+    const float *slots = a.parts + (int64_t)a.cache.kv_heads * a.shares * 2 * TC * D;
+    auto slot_of = [&](int s) { return part_of(kh, a.shares, s, s == share) * TC + in; };
+    // (a share without steps has no part: where there are more shares than steps, some have none)
+    auto has = [&](int s) { return share_at(total, s, a.shares) < share_at(total, s + 1, a.shares); };
+    float most = -INFINITY;
+    for (int s = share; s <= last; ++s)
+        if (has(s)) most = fmaxf(most, slots[slot_of(s) * 2]);
+    const float from = most == -INFINITY ? 0.f : most;
+    float all = 0.f, z[kEach] = {};
+    for (int s = share; s <= last; ++s) {
+        if (!has(s)) continue;
+        const int64_t at = slot_of(s);
+        const float f = __builtin_amdgcn_exp2f(slots[at * 2] - from);
+        all += slots[at * 2 + 1] * f;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) z[i] += a.parts[at * D + dim + i] * f;
+    }
+    const float by = all == 0.f ? 0.f : 1.f / all;
+    const int i = col / a.group, row = p.q.first + i, h = kh * a.group + (col - i * a.group);
+    uint32_t *y = reinterpret_cast<uint32_t *>(a.y.p + row * a.y.token + h * a.y.head + dim);
+#pragma unroll
+    for (int x = 0; x < kEach; x += 2) y[x / 2] = pack_bf16_rne(z[x] * by, z[x + 1] * by);
+}
+
+template <int D, bool F8, int C>
+static hipError_t launch_few(const AttendArgs &a, bool joins, hipStream_t stream)
+{
+    hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(256), 0, stream, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
+    hipLaunchKernelGGL((k_attend_join<D, 16 * C, kFewKeys>), dim3((unsigned)(a.shares - 1) * a.cache.kv_heads, C), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t stream)
+{
+    a.shares = f.shares;
+    a.least = f.least;
+    a.most = f.most;
+    auto by_columns = [&](auto dim, auto f8) {
+        constexpr int D = decltype(dim)::value;
+        constexpr bool F8 = decltype(f8)::value;
+        return f.columns == 16   ? launch_few<D, F8, 1>(a, f.joins, stream)
+               : f.columns == 32 ? launch_few<D, F8, 2>(a, f.joins, stream)
+                                 : launch_few<D, F8, 4>(a, f.joins, stream);
+    };
+    auto by_bits = [&](auto dim) { return a.cache.bits8 ? by_columns(dim, std::true_type{}) : by_columns(dim, std::false_type{}); };
+    return a.cache.dim == 64 ? by_bits(std::integral_constant<int, 64>{}) : by_bits(std::integral_constant<int, 128>{});
+}
+
+}  // namespace lora

@@ -1,0 +1,262 @@
+"""include/lora_attention.h without a GPU: what the calls refuse, before the device is touched, the frequencies and the sizes they state."""
+import ctypes
+import math
+from fractions import Fraction
+
+import pytest
+import torch
+
+from paper_2511_22880_amd import binding as L
+
+P = 0x7F0000000000  # a 256-byte aligned address that is never dereferenced
+
+
+def status(name, *args):
+    return L.STATUS[getattr(L.lib(), name)(*args)]
+
+
+def rotary(turns=P, dims=64, interleaved=0, magnitude=1.0):
+    return L._RotaryArgs(turns, dims, interleaved, magnitude)
+
+
+def cache(k=P, v=P, ks=None, vs=None, pages=10, page=16, heads=2, dim=64, bits=16):
+    return L._CacheArgs(k, v, ks, vs, pages, page, heads, dim, bits)
+
+
+def call(name, given):
+    kept = [v for v in given.values()]
+    return status(name, *(ctypes.addressof(v) if isinstance(v, ctypes.Structure) else v for v in kept), None)
+
+
+ROTARY = dict(x=P, xt=256, xh=64, tokens=3, heads=4, dim=64, positions=P, rotary=rotary(), inverse=0, y=P + 4096, yt=256, yh=64)
+APPEND = dict(k=P, kt=256, kh=64, v=P, vt=256, vh=64, tokens=3, slots=P, positions=P, rotary=rotary(), cache=cache(), q=P, qt=256, qh=64, heads=4, y=P + 4096,
+              yt=256, yh=64)
+ATTEND = dict(q=P, qt=256, qh=64, tokens=3, heads=4, starts=P, lengths=P, requests=3, table=P, ld=10, width=10, tree=None, most=1, cache=cache(), scale=0.125,
+              y=P + 4096, yt=256, yh=64, work=P, nwork=1 << 40)
+
+CASES = [("lora_rotary", ROTARY, c, s) for c, s in [
+    (dict(x=None), "INVALID_ARG"), (dict(x=P + 8), "INVALID_ARG"), (dict(xt=252), "INVALID_ARG"), (dict(xh=60), "INVALID_ARG"), (dict(xh=56), "INVALID_ARG"),
+    (dict(xt=-256), "INVALID_ARG"), (dict(xt=1 << 62), "INVALID_ARG"), (dict(tokens=-1), "INVALID_ARG"), (dict(heads=0), "SHAPE"), (dict(heads=4097), "SHAPE"),
+    (dict(tokens=1 << 30), "SHAPE"), (dict(dim=0), "SHAPE"), (dict(dim=24), "SHAPE"), (dict(dim=272), "SHAPE"), (dict(positions=None), "INVALID_ARG"),
+    (dict(positions=P + 2), "INVALID_ARG"), (dict(rotary=None), "INVALID_ARG"), (dict(rotary=rotary(turns=None)), "INVALID_ARG"),
+    (dict(rotary=rotary(turns=P + 4)), "INVALID_ARG"), (dict(rotary=rotary(dims=0)), "SHAPE"), (dict(rotary=rotary(dims=24)), "SHAPE"),
+    (dict(rotary=rotary(dims=80)), "SHAPE"), (dict(y=None), "INVALID_ARG"), (dict(y=P + 4100), "INVALID_ARG"), (dict(yt=128), "INVALID_ARG"),
+    (dict(yt=0), "INVALID_ARG"), (dict(yt=64, yh=128), "INVALID_ARG"), (dict(y=P, yt=512), "INVALID_ARG")]]
+CASES += [("lora_cache_append", APPEND, c, s) for c, s in [
+    (dict(k=None), "INVALID_ARG"), (dict(v=P + 2), "INVALID_ARG"), (dict(kt=250), "INVALID_ARG"), (dict(vh=32), "INVALID_ARG"), (dict(tokens=-3), "INVALID_ARG"),
+    (dict(slots=None), "INVALID_ARG"), (dict(positions=None), "INVALID_ARG"), (dict(rotary=None), "INVALID_ARG"), (dict(rotary=rotary(dims=128)), "SHAPE"),
+    (dict(q=P + 1), "INVALID_ARG"), (dict(heads=0), "SHAPE"), (dict(y=None), "INVALID_ARG"), (dict(yt=192), "INVALID_ARG"), (dict(y=P, yh=128, yt=512), "INVALID_ARG"),
+    (dict(tokens=1 << 28, heads=8, qt=512, yt=512), "SHAPE")]]
+CASES += [("lora_attention", ATTEND, c, s) for c, s in [
+    (dict(q=None), "INVALID_ARG"), (dict(qt=100), "INVALID_ARG"), (dict(tokens=-1), "INVALID_ARG"), (dict(heads=3), "SHAPE"), (dict(heads=0), "SHAPE"),
+    (dict(starts=None), "INVALID_ARG"), (dict(lengths=P + 3), "INVALID_ARG"), (dict(requests=-1), "INVALID_ARG"), (dict(table=None), "INVALID_ARG"),
+    (dict(ld=9), "INVALID_ARG"), (dict(width=-1), "INVALID_ARG"), (dict(width=1 << 27, ld=1 << 27), "SHAPE"), (dict(tree=P + 4), "INVALID_ARG"), (dict(most=-1), "INVALID_ARG"),
+    (dict(scale=math.inf), "INVALID_ARG"), (dict(scale=math.nan), "INVALID_ARG"), (dict(y=None), "INVALID_ARG"), (dict(y=P), "INVALID_ARG"),
+    (dict(yt=128), "INVALID_ARG"), (dict(work=None), "WORKSPACE"), (dict(work=P + 4), "WORKSPACE"), (dict(nwork=100), "WORKSPACE"),
+    (dict(tokens=1 << 22, requests=1 << 22, width=1 << 17, ld=1 << 17), "SHAPE")]]
+for name, base in (("lora_cache_append", APPEND), ("lora_attention", ATTEND)):
+    CASES += [(name, base, dict(cache=c), s) for c, s in [
+        (None, "INVALID_ARG"), (cache(k=None), "INVALID_ARG"), (cache(v=P + 8), "INVALID_ARG"), (cache(bits=4), "INVALID_ARG"), (cache(bits=8), "INVALID_ARG"),
+        (cache(bits=8, ks=P), "INVALID_ARG"), (cache(bits=8, ks=P, vs=P + 4), "INVALID_ARG"), (cache(pages=0), "SHAPE"), (cache(pages=1 << 28), "SHAPE"),
+        (cache(page=8), "SHAPE"), (cache(page=48), "SHAPE"), (cache(page=2048), "SHAPE"), (cache(heads=0), "SHAPE"), (cache(heads=5000), "SHAPE"),
+        (cache(dim=96), "SHAPE"), (cache(dim=256), "SHAPE")]]
+
+
+@pytest.mark.parametrize("name, base, change, expected", CASES, ids=lambda v: str(v) if isinstance(v, str) else "")
+def test_refusals(name, base, change, expected):
+    assert call(name, dict(base, **change)) == "LORA_ERR_" + expected
+    assert len(L.lora_last_error()) > 5
+
+
+@pytest.mark.parametrize("name, base, change", [
+    ("lora_rotary", ROTARY, dict(tokens=0, x=None, y=None)), ("lora_cache_append", APPEND, dict(tokens=0, k=None, v=None, slots=None)),
+    ("lora_cache_append", APPEND, dict(tokens=0, q=None, heads=0, rotary=None)), ("lora_attention", ATTEND, dict(tokens=0, q=None, starts=None)),
+    ("lora_attention", ATTEND, dict(requests=0, lengths=None, table=None))])
+def test_nothing_to_do_is_no_error(name, base, change):
+    assert call(name, dict(base, **change)) == "LORA_OK"
+
+
+# ---- frequencies --------------------------------------------------------------------------------------------
+PI = Fraction(3141592653589793238462643383279502884197, 10 ** 39)
+
+
+def frequency(i, dims, base, kind, factor, low, high, length):
+    """(radians a position, to 2^-52 of it; magnitude) by the header's formulas"""
+    f = math.exp(-2 * i / dims * math.log(base))
+    if kind == "none":
+        return f
+    if kind == "linear":
+        return f / factor
+    if kind == "wavelength":
+        keep = min(1.0, max(0.0, (length * f / (2 * math.pi) - low) / (high - low)))
+    else:
+        pair = lambda n: dims * math.log(length / (2 * math.pi * n)) / (2 * math.log(base))  # noqa: E731
+        a, b = max(0, math.floor(pair(high))), min(dims - 1, math.ceil(pair(low)))
+        keep = 1.0 - min(1.0, max(0.0, (i - a) / max(b - a, 0.001)))
+    return keep * f + (1 - keep) * f / factor
+
+
+@pytest.mark.parametrize("kind", L.ROTARY_SCALING)
+@pytest.mark.parametrize("dims, base", [(16, 10000.0), (64, 10000.0), (128, 500000.0), (256, 1e6), (80, 2.0)])
+@pytest.mark.parametrize("factor, low, high, length", [(8.0, 1.0, 4.0, 8192.0), (40.0, 1.0, 32.0, 4096.0), (1.0, 0.5, 3.0, 100.0)])
+def test_frequencies(kind, dims, base, factor, low, high, length):
+    turns, magnitude = L.lora_rotary_turns(dims, base, kind, factor, low, high, length)
+    assert turns.shape == (dims // 2,) and turns[0] > 0
+    for i, t in enumerate(turns.tolist()):
+        f = frequency(i, dims, base, kind, factor, low, high, length)
+        exact = Fraction(f) / (2 * PI) * 2 ** 64
+        # the reference's own exp, logarithms and blends in 53 bits: 2^-48 of f at most, whose part between two borders is stretched by 1 / (high - low) turns of `length`
+        assert abs(t - exact) <= 1 + 2.0 ** -46 * float(exact) * max(1.0, length / (high - low))
+    assert magnitude == pytest.approx(0.1 * math.log(factor) + 1 if kind == "dimension" else 1.0, rel=2.0 ** -23)
+
+
+@pytest.mark.parametrize("change", [
+    dict(dims=0), dict(dims=24), dict(dims=272), dict(base=1.0), dict(base=math.inf), dict(base=math.nan), dict(scaling="linear", factor=0.5),
+    dict(scaling="linear", factor=math.inf), dict(scaling="wavelength", low=0.0), dict(scaling="wavelength", low=4.0, high=4.0), dict(scaling="dimension", length=0.0),
+    dict(scaling="dimension", high=math.inf), dict(scaling="twisted")])
+def test_frequencies_refused(change):
+    with pytest.raises((L.LoraError, ValueError)):
+        L.lora_rotary_turns(**dict(dict(dims=64), **change))
+    assert status("lora_rotary_turns", 64, 1e4, 0, 1.0, 1.0, 2.0, 3.0, None, None) == "LORA_ERR_INVALID_ARG"
+    room = (ctypes.c_uint64 * 32)()
+    assert status("lora_rotary_turns", 64, 1e4, 7, 1.0, 1.0, 2.0, 3.0, ctypes.addressof(room), None) == "LORA_ERR_INVALID_ARG"
+    assert status("lora_rotary_turns", 64, 1e4, 0, 0.0, 0.0, 0.0, 0.0, ctypes.addressof(room), None) == "LORA_OK"  # of no account without scaling
+
+
+# ---- workspaces ---------------------------------------------------------------------------------------------
+class Shape:
+    def __init__(self, heads=8, dim=128, page=16, pages=1000, bits=16):
+        self.args = cache(heads=heads, dim=dim, page=page, pages=pages, bits=bits, ks=P, vs=P)
+        self.address = ctypes.addressof(self.args)
+
+
+def test_a_workspace_of_more_is_enough_for_less():
+    for heads, group in ((8, 4), (1, 1), (1, 64), (4, 7), (300, 1), (9, 3)):
+        shape = Shape(heads)
+        said = {(t, r, w): L.lora_attention_workspace_bytes(t, heads * group, r, w, shape) for t in (0, 1, 2, 7, 64, 65, 300, 5000) for r in (0, 1, 3, 64, 300)
+                for w in (0, 1, 4, 8, 9, 100, 6000)}
+        for (t, r, w), n in said.items():
+            assert all(n <= m for (t2, r2, w2), m in said.items() if t2 >= t and r2 >= r and w2 >= w), (heads, group, t, r, w)
+        assert said[5000, 300, 6000] < 1 << 30
+
+
+def test_a_workspace_of_what_is_said_is_taken_and_less_is_not():
+    """whatever `most` says; the launch itself fails here, without a GPU, after the workspace was looked at"""
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are none")
+    shape = Shape()
+    for tokens, requests, width in ((1, 1, 100), (300, 300, 500), (5000, 4, 1000), (640, 10, 300)):
+        n = L.lora_attention_workspace_bytes(tokens, 32, requests, width, shape)
+        for most in (0, 1, 3, 4, 5, 8, 16, 17, 64, 500):
+            given = dict(ATTEND, tokens=tokens, heads=32, qt=4096, qh=128, yt=4096, yh=128, requests=requests, width=width, ld=width, most=most, cache=shape.args, nwork=n)
+            assert call("lora_attention", given) == "LORA_ERR_DEVICE"
+        assert call("lora_attention", dict(given, most=0, nwork=0)) == "LORA_ERR_WORKSPACE"
+
+
+# ---- the binding, on tensors that would do but for one thing ------------------------------------------------
+class OnGpu(torch.Tensor):
+    """A tensor that stands on the first GPU as far as the binding can tell."""
+    is_cuda = True
+
+    def get_device(self):
+        return 0
+
+
+@pytest.fixture
+def told(monkeypatch):
+    """what the binding tells the library, call by call"""
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: calls.append((name, *args)) or 0
+    monkeypatch.setattr(L, "_lib", Library())
+    monkeypatch.setattr(L, "_current_device", lambda: 0)
+    return calls
+
+
+def e(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape).to(dtype).as_subclass(OnGpu)
+
+
+def a_rotary():
+    r = L.Rotary.__new__(L.Rotary)
+    r.turns, r.address, r.device = e(32, dtype=torch.int64), 1234, 0
+    return r
+
+
+def good():
+    i32 = torch.int32
+    held = L.Cache(e(10, 2, 16, 64), e(10, 2, 16, 64))
+    return {
+        "lora_rotary": dict(x=e(3, 4, 64), positions=e(3, dtype=i32), rotary=a_rotary(), y=e(3, 4, 64)),
+        "lora_cache_append": dict(k=e(3, 2, 64), v=e(3, 2, 64), slots=e(3, dtype=i32), cache=held, rotary=a_rotary(), positions=e(3, dtype=i32), q=e(3, 4, 64), y=e(3, 4, 64)),
+        "lora_attention": dict(q=e(3, 4, 64), starts=e(4, dtype=i32), lengths=e(3, dtype=i32), page_table=e(3, 5, dtype=i32), cache=held, y=e(3, 4, 64),
+                               workspace=e(64, dtype=torch.uint8), tree=e(3, dtype=torch.int64)),
+    }
+
+
+TENSORS = [(c, n) for c, given in good().items() for n, t in given.items() if isinstance(t, torch.Tensor)]
+
+
+@pytest.mark.parametrize("call", good())
+def test_the_binding_passes_on_what_it_is_given(call, told):
+    given = good()[call]
+    getattr(L, call)(**given)
+    assert told[-1][0] == call
+    for t in given.values():
+        if isinstance(t, torch.Tensor):
+            assert t.data_ptr() in told[-1]
+
+
+@pytest.mark.parametrize("call, name", TENSORS)
+@pytest.mark.parametrize("wrong", ["on the host", "another device", "type", "short", "strided"])
+def test_the_binding_refuses(call, name, wrong, told):
+    given = good()[call]
+    t = given[name]
+    if wrong == "on the host":
+        t = t.as_subclass(torch.Tensor)
+    elif wrong == "another device":
+        t = t.as_subclass(type("OnAnother", (OnGpu,), {"get_device": lambda self: 1}))
+    elif wrong == "type":
+        if name == "workspace":
+            return
+        t = torch.zeros(t.shape, dtype={torch.bfloat16: torch.float16, torch.int32: torch.float32, torch.int64: torch.float64}[t.dtype]).as_subclass(OnGpu)
+    elif wrong == "short":
+        if name == "workspace" or (call == "lora_attention" and name in ("lengths",)):
+            return  # (the library counts its bytes; a request less)
+        t = t[:-1]
+    else:
+        t = torch.zeros(*t.shape, 2, dtype=t.dtype).as_subclass(OnGpu)[..., 0]
+    given[name] = t
+    with pytest.raises(ValueError):
+        getattr(L, call)(**given)
+    assert not told
+
+
+def test_the_binding_refuses_a_call_from_another_current_device(told, monkeypatch):
+    monkeypatch.setattr(L, "_current_device", lambda: 1)
+    for call, given in good().items():
+        with pytest.raises(ValueError, match="current device is 1"):
+            getattr(L, call)(**given)
+    monkeypatch.setattr(L, "_current_device", lambda: 0)
+    other = type("Stream", (), {"device_index": 1, "cuda_stream": 77})()
+    for call, given in good().items():
+        with pytest.raises(ValueError, match="current device is 0"):
+            getattr(L, call)(**given, stream=other)
+    assert not told
+
+
+def test_the_binding_takes_single_tokens_and_heads_of_any_stride(told):
+    x = torch.zeros(1, 5, 96, dtype=torch.bfloat16).as_subclass(OnGpu)[:, :1, :64]
+    L.lora_rotary(x, e(1, dtype=torch.int32), a_rotary())
+    assert told[-1][2:7] == (64, 64, 1, 1, 64)
+
+
+def test_caches_that_do_not_do():
+    k, f8, s = e(10, 2, 16, 64), e(10, 2, 16, 64, dtype=torch.float8_e4m3fn), e(10, 2, 16, dtype=torch.float32)
+    assert L.Cache(f8, f8, s, s).args.bits == 8 and L.Cache(k, k).args.bits == 16
+    for args in ((k, k[:9]), (k, f8), (k[0], k[0]), (k.transpose(1, 2), k.transpose(1, 2)), (k.float(), k.float()), (k, k, s, s), (f8, f8), (f8, f8, s), (f8, f8, s, s[:9]),
+                 (f8, f8, s.double(), s.double()), (k.as_subclass(torch.Tensor), k), (k, k.as_subclass(torch.Tensor)), (f8, f8, s, s.as_subclass(torch.Tensor))):
+        with pytest.raises(ValueError):
+            L.Cache(*args)
