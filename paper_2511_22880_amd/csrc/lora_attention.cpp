@@ -266,7 +266,7 @@ extern "C" lora_status_t lora_attention(const void *q, int64_t q_token, int64_t 
     a.tree = tree;
     a.cache = cache_of(cache);
     a.scale = scale * 1.44269504088896340736f;
-    const lora::AttendForms forms = lora::attend_forms(tokens, a.group, cache->kv_heads, requests, (int64_t)width * cache->page_size, most);
+    const lora::AttendForms forms = lora::attend_forms(tokens, a.group, cache->kv_heads, requests, (int64_t)width * cache->page_size, most, cache->head_dim);
     size_t need = 0;
     for (int i = 0; i < forms.n; ++i) {
         const size_t n = lora::attend_parts_bytes(forms.f[i], cache->kv_heads, cache->head_dim);

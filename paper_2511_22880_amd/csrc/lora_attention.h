@@ -83,11 +83,18 @@ inline AttendForm attend_form(int columns, int keys, int work_groups, int64_t to
     return AttendForm{columns, (int)shares, 0, INT32_MAX, steps > 1 && shares > 1};
 }
 
-inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int64_t most_rows)
+inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int64_t most_rows, int dim)
 {
-    const int64_t columns = (most_rows > 0 && most_rows < tokens ? most_rows : tokens) * group;
-    const int c = columns <= 16 ? 16 : columns <= 32 ? 32 : 64;
-    return AttendForms{{attend_form(c, kFewKeys, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys), {}}, 1};
+    const int64_t rows = most_rows > 0 && most_rows < tokens ? most_rows : tokens, columns = rows * group;
+    auto few = [&](int c) { return attend_form(c, kFewKeys, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys); };
+    if (columns <= 64) return AttendForms{{few(columns <= 16 ? 16 : columns <= 32 ? 32 : 64), {}}, 1};
+    const int c = columns <= 128 ? 128 : 256;
+    AttendForm wide = attend_form(c, 8192 / dim, c == 128 ? 2 * kComputeUnits : kComputeUnits, tokens, group, kv_heads, requests, most_keys);
+    if (requests == 1 || group > 16 || tokens > requests * rows / 2) return AttendForms{{wide, {}}, 1};
+    AttendForm narrow = few(16);
+    narrow.most = 16;
+    wide.least = 16;
+    return AttendForms{{narrow, wide}, 2};
 }
 
 inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
@@ -99,8 +106,8 @@ inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
 inline size_t attend_most_bytes(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int dim)
 {
     size_t most = 0;
-    for (int64_t rows : {(int64_t)1, (int64_t)16 / group, (int64_t)32 / group, (int64_t)64 / group, (int64_t)0}) {
-        const AttendForms forms = attend_forms(tokens, group, kv_heads, requests, most_keys, rows);
+    for (int64_t rows : {(int64_t)1, (int64_t)16 / group, (int64_t)32 / group, (int64_t)64 / group, (int64_t)128 / group, (int64_t)0}) {
+        const AttendForms forms = attend_forms(tokens, group, kv_heads, requests, most_keys, rows, dim);
         for (int i = 0; i < forms.n; ++i) {
             const size_t n = attend_parts_bytes(forms.f[i], kv_heads, dim);
             if (n > most) most = n;

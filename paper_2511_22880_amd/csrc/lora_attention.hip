@@ -409,6 +409,59 @@ static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t u)
 
 static __device__ __forceinline__ bool odd16(uint32_t u) { return (u & 0x7F80u) == 0x7F80u || (u & 0x7F800000u) == 0x7F800000u; }  // an infinity or NaN
 
+static __device__ __forceinline__ uint32_t finite_of(uint32_t u)  // two bf16, an infinity or NaN as zero
+{
+    return ((u & 0x7F80u) == 0x7F80u ? 0u : u & 0xFFFFu) | ((u & 0x7F800000u) == 0x7F800000u ? 0u : u & 0xFFFF0000u);
+}
+
+// A matrix instruction multiplies every column's weight by every value, and nought times an infinity is NaN: among keys that not all columns see, infinities and NaN
+// of v are taken as zero, and the steps that held some are remembered here.  Behind a tile's rows (or its sums), which are then written, such values are
+// added to the columns that see them, element by element, every element by one thread.  (Done between the steps instead, it takes 40 registers more.)
+struct OddSteps {
+    uint32_t from[2], to[2];  // of this tile and the next one
+    __device__ __forceinline__ void clear(int i)
+    {
+        from[i] = UINT32_MAX;
+        to[i] = 0;
+    }
+    __device__ __forceinline__ void note(int i, uint32_t step)
+    {
+        atomicMin(&from[i], step);
+        atomicMax(&to[i], step + 1);
+    }
+};
+
+// keys [from, to) of p's request; `whole`: y's rows, else the sums at `sums` [columns][D]
+template <int D, bool F8, class Place>
+static __device__ __forceinline__ void add_odd(const AttendArgs &a, const Place &p, int kh, int from, int to, int c0, int tile, bool whole, float *sums)
+{
+    const int dim = threadIdx.x % D, context = p.q.keys - p.q.n, columns = min(tile, p.q.n * a.group - c0);
+    for (int key = from; key < min(to, p.q.keys); ++key) {
+        const int id = a.table[p.r * a.ld_table + (key >> a.cache.page_shift)];
+        if ((unsigned)id >= (unsigned)a.cache.pages) continue;
+        const int64_t row = (((int64_t)id * a.cache.kv_heads + kh) << a.cache.page_shift) + (key & ((1 << a.cache.page_shift) - 1));
+        float v;
+        if constexpr (F8) {
+            if ((reinterpret_cast<const uint8_t *>(a.cache.v)[row * D + dim] & 0x7F) != 0x7F) continue;
+            v = __builtin_nanf("");
+        } else {
+            const uint32_t bits = reinterpret_cast<const uint16_t *>(a.cache.v)[row * D + dim];
+            if ((bits & 0x7F80u) != 0x7F80u) continue;
+            v = __uint_as_float(bits << 16);
+        }
+        for (int in = threadIdx.x / D; in < columns; in += 256 / D) {
+            const int i = (c0 + in) / a.group, own = key - context;
+            if (a.tree ? own >= 0 && (own >= 64 || !(a.tree[p.q.first + i] >> own & 1)) : own > i) continue;
+            if (whole) {
+                uint16_t *y = a.y.p + (p.q.first + i) * a.y.token + (kh * a.group + (c0 + in - i * a.group)) * a.y.head + dim;
+                *y = (uint16_t)pack_bf16_rne(__uint_as_float((uint32_t)*y << 16) + v, 0.f);
+            } else {
+                sums[(int64_t)in * D + dim] += v;
+            }
+        }
+    }
+}
+
 template <int D, bool F8>
 struct FewShape {
     static constexpr int kRowBytes = D * (F8 ? 1 : 2);
@@ -427,6 +480,9 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
     __shared__ typename W::Found found;
     __shared__ float2 sums[4][TC];
     __shared__ float part[4][4 * S::kTiles][64];
+    __shared__ OddSteps odd;
+    if (threadIdx.x == 0) odd.clear(0);
+    int turn = 0;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, quad = lane >> 4;
     const int kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
     typename W::Place p;
@@ -641,38 +697,19 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
                     }
                 }
                 load_v(then, j1);
-                bool odd = false;
                 if (!plain) {
-                    // a weight of zero times an infinity is NaN: where a value is one, a key at a time, for the columns that see it
+                    bool some = false;
 #pragma unroll
-                    for (int i = 0; i < S::kTiles; ++i) odd |= odd16(vt[i].x) || odd16(vt[i].y) || odd16(vt[i].z) || odd16(vt[i].w);
-                    odd = __any(odd);
-                }
-                if (!odd) {
-#pragma unroll
-                    for (int i = 0; i < S::kTiles; ++i)
-#pragma unroll
-                        for (int c = 0; c < C; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt[i]), as_bf16x8(w[c]), o[c][i], 0, 0, 0);
-                } else {
-                    for (int key = 0; key < 32; ++key) {
-                        const bool here = quad == key >> 3;
-                        const uint32_t half = key & 1 ? 0xFFFF0000u : 0xFFFFu;
-                        const int dword = (key & 7) >> 1;
-                        const uint4 only{here && dword == 0 ? half : 0u, here && dword == 1 ? half : 0u, here && dword == 2 ? half : 0u, here && dword == 3 ? half : 0u};
-#pragma unroll
-                        for (int c = 0; c < C; ++c) {
-                            const bool s = (uint32_t)__shfl((int)seen[c], (key >> 3) * 16 + n, 64) >> (key & 7) & 1;
-                            const uint4 wk{w[c].x & only.x, w[c].y & only.y, w[c].z & only.z, w[c].w & only.w};
-#pragma unroll
-                            for (int i = 0; i < S::kTiles; ++i) {
-                                const uint4 vk{vt[i].x & only.x, vt[i].y & only.y, vt[i].z & only.z, vt[i].w & only.w};
-                                const f32x4 one = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vk), as_bf16x8(wk), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) o[c][i][e] += s ? one[e] : 0.f;
-                            }
-                        }
+                    for (int i = 0; i < S::kTiles; ++i) {
+                        some |= odd16(vt[i].x) || odd16(vt[i].y) || odd16(vt[i].z) || odd16(vt[i].w);
+                        vt[i] = uint4{finite_of(vt[i].x), finite_of(vt[i].y), finite_of(vt[i].z), finite_of(vt[i].w)};
                     }
+                    if (some) odd.note(turn, j);
                 }
+#pragma unroll
+                for (int i = 0; i < S::kTiles; ++i)
+#pragma unroll
+                    for (int c = 0; c < C; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt[i]), as_bf16x8(w[c]), o[c][i], 0, 0, 0);
                 now = then;
                 then = after;
             }
@@ -725,9 +762,354 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
                 }
             }
         }
+        if (tid == 0) odd.clear(turn ^ 1);
+        __syncthreads();
+        if (odd.to[turn]) add_odd<D, F8>(a, p, kh, odd.from[turn] * kFewKeys, odd.to[turn] * kFewKeys, c0, TC, whole, a.parts + slot * TC * D);
+        turn ^= 1;
         left -= to - p.at;
         if (left == 0 || !W::next(a, p)) return;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Attention of many columns: tiles of 128 C, four wavefronts of 32 C columns, which share the keys and values of a step in LDS: 64 keys of 128 dims, or 128 of 64.
+// S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16 matrix instructions, 32 keys at a time.  A lane (half h, column n) ends up with the scores of keys
+// 8 i + 4 h + 0 .. 3 of those; as in k_attend_few they become an operand where they are, for V^T is laid out by the same order of keys: piece (2 ks + h) of a dim's row
+// has the keys 16 ks + 4 h + {0 .. 3, 8 .. 11}.  Two wavefronts fetch K and two V, through registers, a step ahead: V is turned there (a thread has 8 keys x 8 dims),
+// 8-bit values become bf16 there, once for all four.  In LDS 16-byte pieces of a row are exchanged by its number so that neither writes nor
+// reads meet in a bank.
+// ------------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+static __device__ __forceinline__ uint4 four_words(const uint32_t *w) { return uint4{w[0], w[1], w[2], w[3]}; }
+
+template <int D, bool F8>
+struct WideShape {
+    static constexpr int kKeys = 8192 / D;          // of a step
+    static constexpr int kRow = D * (F8 ? 1 : 2);   // bytes of a key or value in the cache
+    static constexpr int kGroups = kKeys / 16;      // that lie on one page
+    static constexpr int kSteps = D / 16;           // of k, of the scores
+    static constexpr int kDims = D / 32;            // tiles of O^T
+    static constexpr int kLoads = F8 ? 4 : 8;       // of 16 bytes, a thread's of K
+    // byte of 16-byte piece p of row r: K [key][dim], V^T [dim][key]
+    static __device__ __forceinline__ int k_at(int r, int p) { return r * (2 * D) + 16 * (p ^ (D == 128 ? r & 15 : (r >> 1) & 7)); }
+    static __device__ __forceinline__ int v_at(int r, int p) { return r * (2 * kKeys) + 16 * (D == 128 ? p ^ (((r >> 1) & 3) ^ ((r >> 3) & 7)) : p ^ ((r & 7) ^ ((r >> 3) & 7) << 1)); }
+};
+
+template <int D, bool F8, int C>
+__global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs a)
+{
+    using S = WideShape<D, F8>;
+    constexpr int TC = 128 * C, KEYS = S::kKeys;
+    using W = Dealt<TC, KEYS>;
+    __shared__ typename W::Found found;
+    __shared__ __attribute__((aligned(16))) char ks[2][16384], vs[2][16384];
+    __shared__ float scales[F8 ? 2 : 1][2][F8 ? KEYS : 1];
+    __shared__ OddSteps odd;
+    if (threadIdx.x == 0) odd.clear(0);
+    int turn = 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+    const int kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
+    typename W::Place p;
+    uint32_t left = 0;
+    if (!W::template find<256>(a, found, [&](uint32_t total) {
+            const uint32_t from = share_at(total, share, a.shares);
+            left = share_at(total, share + 1, a.shares) - from;
+            return left ? from : UINT32_MAX;
+        }, p)) return;
+    const int page = 1 << a.cache.page_shift;
+    const bool loads_v = wave < 2;
+    // V: keys of a thread, group of 16 and where in it; dims.  K: row within a load, piece
+    constexpr int kWide = D / 8;  // threads that have a row of V between them
+    const int vt = tid & 127, v_kg = vt / kWide, v_dims = (vt % kWide) * 8;
+    constexpr int kAcross = S::kRow / 16;  // .. of K
+    const int kt_row = (tid & 63) / kAcross, k_piece = (tid & 63) % kAcross;
+
+    while (true) {
+        const uint32_t to = min(p.of, p.at + left);
+        const bool whole = p.at == 0 && to == p.of;
+        const int context = p.q.keys - p.q.n, columns = p.q.n * a.group, c0 = p.t * TC, mine0 = c0 + wave * 32 * C;
+        const bool busy = mine0 < columns;
+        bf16x8 q[C][S::kSteps];
+        int sees[C];
+        uint64_t word[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            int col = mine0 + 32 * c + n;
+            if (col >= columns) col = c0;
+            const int i = col / a.group, row = p.q.first + i, hd = kh * a.group + (col - i * a.group);
+            const uint16_t *at = a.q.p + row * a.q.token + hd * a.q.head;
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s) q[c][s] = as_bf16x8(ld16(at + 16 * s + 8 * h));
+            sees[c] = context + i;
+            word[c] = a.tree ? a.tree[row] : 0;
+        }
+        // keys up to here are seen by all columns of the tile
+        const int open = min(p.q.keys, a.tree ? context : context + c0 / a.group + 1);
+
+        f32x16 o[C][S::kDims];
+        float top[C], sum[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            top[c] = -INFINITY;
+            sum[c] = 0.f;
+#pragma unroll
+            for (int i = 0; i < S::kDims; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[c][i][e] = 0.f;
+        }
+
+        const int32_t *table = a.table + p.r * a.ld_table;
+        // a lane has the page of 16 keys, group lane mod kGroups; -1 where there is none
+        auto page_of = [&](uint32_t j) __attribute__((always_inline)) {
+            const int key = (int)j * KEYS + 16 * (lane & (S::kGroups - 1));
+            const int id = key < p.q.keys ? table[key >> a.cache.page_shift] : -1;
+            return (unsigned)id < (unsigned)a.cache.pages ? id : -1;
+        };
+        uint32_t held[32];  // fetched for the next step: of K, or of V (a key's after the other's)
+        constexpr int kOfKey = F8 ? 2 : 4;
+        float sr[2];
+        auto row_of = [&](int id, uint32_t j, int group) __attribute__((always_inline)) {  // of the cache, of the first of 16 keys
+            const int in = ((int)j * KEYS + 16 * group) & (page - 1);
+            return ((int64_t)max(id, 0) * a.cache.kv_heads + kh) * page + in;
+        };
+        auto fetch = [&](int ids, uint32_t j) __attribute__((always_inline)) {
+            if (loads_v) {
+                const int group = v_kg >> 1, id = __shfl(ids, group, 64);
+                const char *at = a.cache.v + (row_of(id, j, group) + 4 * (v_kg & 1)) * S::kRow + v_dims * (F8 ? 1 : 2);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const auto got = ld_bytes<4 * kOfKey>(at + (i < 4 ? i : i + 4) * S::kRow);
+#pragma unroll
+                    for (int x = 0; x < kOfKey; ++x) held[kOfKey * i + x] = got.w[x];
+                }
+            } else {
+                // a wavefront has half of the step's keys; a load as many rows as fit 1 KB
+                constexpr int kRows = 64 / kAcross;
+#pragma unroll
+                for (int i = 0; i < S::kLoads; ++i) {
+                    const int key = (wave - 2) * (KEYS / 2) + i * kRows + kt_row, group = key >> 4, id = __shfl(ids, group, 64);
+                    const auto got = ld_bytes<16>(a.cache.k + (row_of(id, j, group) + (key & 15)) * S::kRow + 16 * k_piece);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) held[4 * i + x] = got.w[x];
+                }
+            }
+            if constexpr (F8) {
+                const int key = tid & (KEYS - 1), group = key >> 4, id = __shfl(ids, group, 64);
+                const int64_t row = row_of(id, j, group) + (key & 15);
+                sr[0] = a.cache.k_scales[row];
+                sr[1] = a.cache.v_scales[row];
+            }
+        };
+        // ids: of the step that was fetched
+        auto stage = [&](int ids, uint32_t j, int b) __attribute__((always_inline)) {
+            const int key0 = (int)j * KEYS;
+            const bool plain = key0 + KEYS <= open && __ballot(ids < 0) == 0;
+            if (loads_v) {
+                const int group = v_kg >> 1, first = key0 + 16 * group + 4 * (v_kg & 1);
+                if (!plain) {
+                    const bool there = __shfl(ids, group, 64) >= 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int x = 0; x < kOfKey; ++x) held[kOfKey * i + x] = there && first + (i < 4 ? i : i + 4) < p.q.keys ? held[kOfKey * i + x] : 0u;
+                }
+                bool some = false;
+                auto put = [&](int c, uint4 w) __attribute__((always_inline)) {
+                    if (!plain) {
+                        some |= odd16(w.x) || odd16(w.y) || odd16(w.z) || odd16(w.w);
+                        w = uint4{finite_of(w.x), finite_of(w.y), finite_of(w.z), finite_of(w.w)};
+                    }
+                    *reinterpret_cast<uint4 *>(vs[b] + S::v_at(v_dims + c, v_kg)) = w;
+                };
+                if constexpr (F8) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        uint32_t four_keys[2][4];
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const uint32_t *v = held + 8 * y + x;
+                            const uint32_t l01 = __builtin_amdgcn_perm(v[2], v[0], 0x05010400u), l23 = __builtin_amdgcn_perm(v[6], v[4], 0x05010400u);
+                            const uint32_t h01 = __builtin_amdgcn_perm(v[2], v[0], 0x07030602u), h23 = __builtin_amdgcn_perm(v[6], v[4], 0x07030602u);
+                            four_keys[y][0] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
+                            four_keys[y][1] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
+                            four_keys[y][2] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
+                            four_keys[y][3] = __builtin_amdgcn_perm(h23, h01, 0x07060302u);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            put(4 * x + c, uint4{two_of_e4m3<false>(four_keys[0][c]), two_of_e4m3<true>(four_keys[0][c]), two_of_e4m3<false>(four_keys[1][c]),
+                                                 two_of_e4m3<true>(four_keys[1][c])});
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t d[4];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) d[y] = __builtin_amdgcn_perm(held[8 * y + 4 + (c >> 1)], held[8 * y + (c >> 1)], c & 1 ? 0x07060302u : 0x05040100u);
+                        put(c, four_words(d));
+                    }
+                }
+                if (some) odd.note(turn, j);
+            } else {
+                constexpr int kRows = 64 / kAcross;
+#pragma unroll
+                for (int i = 0; i < S::kLoads; ++i) {
+                    const int key = (wave - 2) * (KEYS / 2) + i * kRows + kt_row;
+                    if constexpr (F8) {
+                        const uint32_t *w = held + 4 * i;
+                        *reinterpret_cast<uint4 *>(ks[b] + S::k_at(key, 2 * k_piece)) =
+                            uint4{two_of_e4m3<false>(w[0]), two_of_e4m3<true>(w[0]), two_of_e4m3<false>(w[1]), two_of_e4m3<true>(w[1])};
+                        *reinterpret_cast<uint4 *>(ks[b] + S::k_at(key, 2 * k_piece + 1)) =
+                            uint4{two_of_e4m3<false>(w[2]), two_of_e4m3<true>(w[2]), two_of_e4m3<false>(w[3]), two_of_e4m3<true>(w[3])};
+                    } else {
+                        *reinterpret_cast<uint4 *>(ks[b] + S::k_at(key, k_piece)) = four_words(held + 4 * i);
+                    }
+                }
+            }
+            if constexpr (F8) {
+                if (tid < KEYS) {
+                    scales[b][0][tid] = sr[0] * a.scale;
+                    scales[b][1][tid] = key0 + tid < p.q.keys && __shfl(ids, tid >> 4, 64) >= 0 ? sr[1] : 0.f;
+                }
+            }
+        };
+
+        if (p.q.keys > 0) {
+            int now = page_of(p.at), then = page_of(p.at + 1 < to ? p.at + 1 : p.at);
+            fetch(now, p.at);
+            stage(now, p.at, 0);
+            fetch(then, p.at + 1 < to ? p.at + 1 : p.at);
+            __syncthreads();
+            for (uint32_t j = p.at; j < to; ++j) {
+                const int b = (j - p.at) & 1;
+                const uint32_t j1 = j + 1 < to ? j + 1 : j, j2 = j + 2 < to ? j + 2 : j1;
+                const int after = page_of(j2);
+                const int key0 = (int)j * KEYS;
+                const uint64_t none = __ballot(now < 0);
+                const bool plain = none == 0 && key0 + KEYS <= open;
+                stage(then, j1, b ^ 1);
+                fetch(after, j2);
+                if (busy) {
+#pragma unroll 1
+                    for (int kt = 0; kt < KEYS / 32; ++kt) {
+                        f32x16 s[C];
+#pragma unroll
+                        for (int c = 0; c < C; ++c)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
+#pragma unroll
+                        for (int x = 0; x < S::kSteps; ++x) {
+                            const bf16x8 k = as_bf16x8(*reinterpret_cast<const uint4 *>(ks[b] + S::k_at(32 * kt + n, 2 * x + h)));
+#pragma unroll
+                            for (int c = 0; c < C; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c][x], s[c], 0, 0, 0);
+                        }
+                        [[maybe_unused]] float4 by_k[4], by_v[4];
+                        if constexpr (F8) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                by_k[i] = *reinterpret_cast<const float4 *>(&scales[b][0][32 * kt + 8 * i + 4 * h]);
+                                by_v[i] = *reinterpret_cast<const float4 *>(&scales[b][1][32 * kt + 8 * i + 4 * h]);
+                            }
+                        }
+                        auto four = [](const float4 &f, int i) __attribute__((always_inline)) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; };
+                        uint4 w[C][2];
+                        uint32_t seen[C];
+#pragma unroll
+                        for (int c = 0; c < C; ++c) {
+                            seen[c] = 0xFFFFu;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) s[c][e] *= F8 ? four(by_k[e >> 2], e & 3) : a.scale;
+                            if (!plain) {
+                                seen[c] = 0;
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) {
+                                    const int in = 32 * kt + 8 * (e >> 2) + 4 * h + (e & 3), key = key0 + in, own = key - context;
+                                    bool v = key < p.q.keys && !(none >> (in >> 4) & 1);
+                                    if (a.tree)
+                                        v = v && (own < 0 || (own < 64 && (word[c] >> (own & 63) & 1)));
+                                    else
+                                        v = v && key <= sees[c];
+                                    seen[c] |= (uint32_t)v << e;
+                                    s[c][e] = v ? s[c][e] : -INFINITY;
+                                }
+                            }
+                            float t = fmaxf(s[c][0], s[c][1]);
+#pragma unroll
+                            for (int e = 2; e < 16; e += 2) t = fmaxf(t, fmaxf(s[c][e], s[c][e + 1]));
+                            t = fmaxf(t, __shfl_xor(t, 32, 64));
+                            t = fmaxf(t, top[c]);
+                            if (__any(t > top[c])) {
+                                const float f = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[c] - t);
+                                sum[c] *= f;
+#pragma unroll
+                                for (int i = 0; i < S::kDims; ++i) o[c][i] *= f;
+                                top[c] = t;
+                            }
+                            const float from = t == -INFINITY ? 0.f : t;
+                            float e8[16];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                e8[e] = __builtin_amdgcn_exp2f(s[c][e] - from);
+                                sum[c] += e8[e];
+                                if constexpr (F8) e8[e] = plain || (seen[c] >> e & 1) ? e8[e] * four(by_v[e >> 2], e & 3) : 0.f;
+                            }
+#pragma unroll
+                            for (int y = 0; y < 2; ++y)
+                                w[c][y] = uint4{pack_bf16_rne(e8[8 * y], e8[8 * y + 1]), pack_bf16_rne(e8[8 * y + 2], e8[8 * y + 3]), pack_bf16_rne(e8[8 * y + 4], e8[8 * y + 5]),
+                                                pack_bf16_rne(e8[8 * y + 6], e8[8 * y + 7])};
+                        }
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int i = 0; i < S::kDims; ++i) {
+                                const bf16x8 v = as_bf16x8(*reinterpret_cast<const uint4 *>(vs[b] + S::v_at(32 * i + n, 2 * (2 * kt + y) + h)));
+#pragma unroll
+                                for (int c = 0; c < C; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(w[c][y]), o[c][i], 0, 0, 0);
+                            }
+                    }
+                }
+                __syncthreads();
+                now = then;
+                then = after;
+            }
+        }
+
+        const int64_t slot = part_of(kh, a.shares, share, p.at == 0);
+        if (busy) {
+            float *slots = a.parts + (int64_t)a.cache.kv_heads * a.shares * 2 * TC * D;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const float all = sum[c] + __shfl_xor(sum[c], 32, 64);
+                const int in = wave * 32 * C + 32 * c + n, col = c0 + in;
+                if (col >= columns) continue;
+                if (whole) {
+                    const float by = all == 0.f ? 0.f : 1.f / all;
+                    const int i = col / a.group, row = p.q.first + i, hd = kh * a.group + (col - i * a.group);
+                    uint16_t *y = a.y.p + row * a.y.token + hd * a.y.head + 4 * h;
+#pragma unroll
+                    for (int x = 0; x < S::kDims; ++x)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            *reinterpret_cast<uint2 *>(y + 32 * x + 8 * e) =
+                                uint2{pack_bf16_rne(o[c][x][4 * e] * by, o[c][x][4 * e + 1] * by), pack_bf16_rne(o[c][x][4 * e + 2] * by, o[c][x][4 * e + 3] * by)};
+                } else {
+                    float *y = a.parts + (slot * TC + in) * D + 4 * h;
+#pragma unroll
+                    for (int x = 0; x < S::kDims; ++x)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            *reinterpret_cast<float4 *>(y + 32 * x + 8 * e) = float4{o[c][x][4 * e], o[c][x][4 * e + 1], o[c][x][4 * e + 2], o[c][x][4 * e + 3]};
+                    if (h == 0) *reinterpret_cast<float2 *>(slots + (slot * TC + in) * 2) = float2{top[c], all};
+                }
+            }
+        }
+        if (tid == 0) odd.clear(turn ^ 1);
         __syncthreads();
+        if (odd.to[turn]) add_odd<D, F8>(a, p, kh, odd.from[turn] * KEYS, odd.to[turn] * KEYS, c0, TC, whole, a.parts + slot * TC * D);
+        turn ^= 1;
+        left -= to - p.at;
+        if (left == 0 || !W::next(a, p)) return;
     }
 }
 
@@ -784,6 +1166,15 @@ static hipError_t launch_few(const AttendArgs &a, bool joins, hipStream_t stream
     return hipGetLastError();
 }
 
+template <int D, bool F8, int C>
+static hipError_t launch_wide(const AttendArgs &a, bool joins, hipStream_t stream)
+{
+    hipLaunchKernelGGL((k_attend_wide<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(256), 0, stream, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
+    hipLaunchKernelGGL((k_attend_join<D, 128 * C, WideShape<D, F8>::kKeys>), dim3((unsigned)(a.shares - 1) * a.cache.kv_heads, 8 * C), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
 hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t stream)
 {
     a.shares = f.shares;
@@ -792,9 +1183,11 @@ hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t strea
     auto by_columns = [&](auto dim, auto f8) {
         constexpr int D = decltype(dim)::value;
         constexpr bool F8 = decltype(f8)::value;
-        return f.columns == 16   ? launch_few<D, F8, 1>(a, f.joins, stream)
-               : f.columns == 32 ? launch_few<D, F8, 2>(a, f.joins, stream)
-                                 : launch_few<D, F8, 4>(a, f.joins, stream);
+        return f.columns == 16    ? launch_few<D, F8, 1>(a, f.joins, stream)
+               : f.columns == 32  ? launch_few<D, F8, 2>(a, f.joins, stream)
+               : f.columns == 64  ? launch_few<D, F8, 4>(a, f.joins, stream)
+               : f.columns == 128 ? launch_wide<D, F8, 1>(a, f.joins, stream)
+                                  : launch_wide<D, F8, 2>(a, f.joins, stream);
     };
     auto by_bits = [&](auto dim) { return a.cache.bits8 ? by_columns(dim, std::true_type{}) : by_columns(dim, std::false_type{}); };
     return a.cache.dim == 64 ? by_bits(std::integral_constant<int, 64>{}) : by_bits(std::integral_constant<int, 128>{});
