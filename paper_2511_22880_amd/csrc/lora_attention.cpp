@@ -101,8 +101,8 @@ static void set_rotary(lora::TurnArgs &a, const lora_rotary_t *r)
     a.interleaved = r->interleaved != 0;
 }
 
-// the kernel divides numbers of up to 16 bits by it
-static uint32_t reciprocal(int32_t heads) { return heads == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + heads - 1) / heads); }
+// 2^32 / n, rounded up: the kernels' divisor
+static uint32_t reciprocal(int32_t n) { return n == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + n - 1) / n); }
 
 extern "C" lora_status_t lora_rotary_turns(int32_t dims, double base, int32_t scaling, double factor, double low, double high, double length,
                                            uint64_t *turns, float *magnitude)
@@ -255,8 +255,8 @@ extern "C" lora_status_t lora_attention(const void *q, int64_t q_token, int64_t 
     a.q = {(uint16_t *)q, q_token, q_head};
     a.y = {(uint16_t *)y, y_token, y_head};
     a.tokens = tokens;
-    a.q_heads = q_heads;
     a.group = q_heads / cache->kv_heads;
+    a.per_group = reciprocal(a.group);
     a.starts = starts;
     a.lengths = lengths;
     a.table = page_table;
@@ -265,7 +265,10 @@ extern "C" lora_status_t lora_attention(const void *q, int64_t q_token, int64_t 
     a.width = width;
     a.tree = tree;
     a.cache = cache_of(cache);
-    a.scale = scale * 1.44269504088896340736f;
+    // (nought times the -infinity of a key that is not seen would be NaN; times 2^-120 scores do not matter either)
+    a.scale = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 0x1p-120f);
+    a.flip = scale < 0.f ? 0x80008000u : 0u;
+    a.slack = 8.f / a.scale;
     const lora::AttendForms forms = lora::attend_forms(tokens, a.group, cache->kv_heads, requests, (int64_t)width * cache->page_size, most, cache->head_dim);
     size_t need = 0;
     for (int i = 0; i < forms.n; ++i) {

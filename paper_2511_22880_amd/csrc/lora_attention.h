@@ -44,13 +44,16 @@ constexpr int kFewKeys = 128;    // keys a work group takes in a step, k_attend_
 
 struct AttendArgs {
     HeadRows q, y;
-    int tokens, q_heads, group;   // group: query heads per key head
+    int tokens, group;            // group: query heads per key head
+    uint32_t per_group;           // 2^32 / group, rounded up (0 for 1): the upper half of a number's product with it is the quotient or one more
     const int32_t *starts, *lengths, *table;
     int64_t ld_table;
     int requests, width;
     const uint64_t *tree;
     PagedCache cache;
-    float scale;                  // times log2 e
+    float scale;                  // its magnitude times log2 e, never zero
+    uint32_t flip;                // the sign bits of q that a negative scale exchanges
+    float slack;                  // by how much a score may pass the maximum that weights are relative to: 8 / scale
     int least, most;              // columns of the requests that this launch takes: least < rows * group <= most
     int shares;                   // of a key head's work
     float *parts;                 // workspace: [kv_heads * shares][2][columns][dim], then sums [..][2][columns][2]

@@ -284,20 +284,24 @@ struct Dealt {
         Tiles s;
     };
     struct Found {
-        uint32_t sums[16];
+        uint32_t sums[8];
         int r;
         uint32_t at;
+        Request q;
     };
 
-    // Every thread of the work group: place(total) says which step of the list is meant, given how many there are (UINT32_MAX: none, and false is returned).
+    // Every thread of a work group: which(total) says which step of the list is meant, given how many there are (none: `total`, and false is returned).
     template <int THREADS, class Which>
     static __device__ __forceinline__ bool find(const AttendArgs &a, Found &f, Which which, Place &p)
     {
-        constexpr int kWaves = THREADS / 64;
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int each = (a.requests + THREADS - 1) / THREADS, r0 = tid * each, r1 = min(a.requests, r0 + each);
-        uint32_t mine = 0;
-        for (int r = r0; r < r1; ++r) mine += all(a, tiles(a, request_at(a, r)));
+        Request q{0, 0, 0};
+        uint32_t mine = 0, n = 0;  // (steps of this thread's requests; of the last of them)
+        for (int r = r0; r < r1; ++r) {
+            q = request_at(a, r);
+            mine += n = all(a, tiles(a, q));
+        }
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -308,28 +312,28 @@ struct Dealt {
         __syncthreads();
         uint32_t total = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < THREADS / 64; ++w) {
             if (w == wave) upto += total;
             total += f.sums[w];
         }
+        total = __builtin_amdgcn_readfirstlane(total);
         const uint32_t want = which(total);
         if (want >= total) return false;
-        uint32_t from = upto - mine;
-        if (want >= from && want < upto) {
-            for (int r = r0; r < r1; ++r) {
-                const uint32_t n = all(a, tiles(a, request_at(a, r)));
-                if (want < from + n) {
-                    f.r = r;
-                    f.at = want - from;
-                    break;
-                }
-                from += n;
+        if (want < upto && want >= upto - mine) {
+            int r = r1 - 1;
+            uint32_t from = upto - n;
+            while (want < from) {  // (no further than r0)
+                q = request_at(a, --r);
+                from -= all(a, tiles(a, q));
             }
+            f.r = r;
+            f.at = want - from;
+            f.q = q;
         }
         __syncthreads();
         p.r = __builtin_amdgcn_readfirstlane(f.r);
-        uint32_t at = __builtin_amdgcn_readfirstlane(f.at);
-        p.q = request_at(a, p.r);
+        const uint32_t at = __builtin_amdgcn_readfirstlane(f.at);
+        p.q = Request{__builtin_amdgcn_readfirstlane(f.q.first), __builtin_amdgcn_readfirstlane(f.q.n), __builtin_amdgcn_readfirstlane(f.q.keys)};
         p.s = tiles(a, p.q);
         // the last tile that begins at or before it, 64 at a time
         int lo = 0, hi = p.s.n - 1;
@@ -361,8 +365,12 @@ struct Dealt {
     }
 };
 
-// first step of a share of `total`
-static __device__ __forceinline__ uint32_t share_at(uint32_t total, int share, int shares) { return (uint32_t)((uint64_t)total * share / shares); }
+// first step of a share of `total` (the first ones have one more; with fewer steps than shares those have one each)
+static __device__ __forceinline__ uint32_t share_at(uint32_t total, int share, int shares)
+{
+    const uint32_t each = total / (uint32_t)shares, more = total - each * shares;
+    return each * share + min((uint32_t)share, more);
+}
 
 // where a share leaves its sums: slot 1 of those of a tile that begins in it, slot 0 of one that began earlier
 static __device__ __forceinline__ int64_t part_of(int head, int shares, int share, bool begins) { return ((int64_t)head * shares + share) * 2 + begins; }
@@ -407,11 +415,28 @@ static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t u)
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HIGH));
 }
 
-static __device__ __forceinline__ bool odd16(uint32_t u) { return (u & 0x7F80u) == 0x7F80u || (u & 0x7F800000u) == 0x7F800000u; }  // an infinity or NaN
+// two bf16: the sign bits of those that are an infinity or NaN
+static __device__ __forceinline__ uint32_t odd16(uint32_t u) { return ((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 
-static __device__ __forceinline__ uint32_t finite_of(uint32_t u)  // two bf16, an infinity or NaN as zero
+// .. as zero where `odd` says so
+static __device__ __forceinline__ uint32_t finite_of(uint32_t u, uint32_t odd) { return u & ~((odd - (odd >> 15)) | odd); }
+
+// eight bf16 values with their signs exchanged where `flip` says so
+static __device__ __forceinline__ uint4 flipped(uint4 u, uint32_t flip) { return uint4{u.x ^ flip, u.y ^ flip, u.z ^ flip, u.w ^ flip}; }
+
+// a column's row of its request: column / group
+static __device__ __forceinline__ int row_of_column(const AttendArgs &a, int column)
 {
-    return ((u & 0x7F80u) == 0x7F80u ? 0u : u & 0xFFFFu) | ((u & 0x7F800000u) == 0x7F800000u ? 0u : u & 0xFFFF0000u);
+    if (a.per_group == 0) return column;
+    const uint32_t i = __umulhi((uint32_t)column, a.per_group);
+    return (int)(i - (i * a.group > (uint32_t)column));
+}
+
+static __device__ __forceinline__ uint4 finite_of(uint4 u, uint32_t &some)
+{
+    const uint32_t x = odd16(u.x), y = odd16(u.y), z = odd16(u.z), w = odd16(u.w);
+    some |= x | y | z | w;
+    return uint4{finite_of(u.x, x), finite_of(u.y, y), finite_of(u.z, z), finite_of(u.w, w)};
 }
 
 // A matrix instruction multiplies every column's weight by every value, and nought times an infinity is NaN: among keys that not all columns see, infinities and NaN
@@ -432,7 +457,7 @@ struct OddSteps {
 };
 
 // keys [from, to) of p's request; `whole`: y's rows, else the sums at `sums` [columns][D]
-template <int D, bool F8, class Place>
+template <int D, bool F8, int THREADS, class Place>
 static __device__ __forceinline__ void add_odd(const AttendArgs &a, const Place &p, int kh, int from, int to, int c0, int tile, bool whole, float *sums)
 {
     const int dim = threadIdx.x % D, context = p.q.keys - p.q.n, columns = min(tile, p.q.n * a.group - c0);
@@ -449,8 +474,8 @@ static __device__ __forceinline__ void add_odd(const AttendArgs &a, const Place 
             if ((bits & 0x7F80u) != 0x7F80u) continue;
             v = __uint_as_float(bits << 16);
         }
-        for (int in = threadIdx.x / D; in < columns; in += 256 / D) {
-            const int i = (c0 + in) / a.group, own = key - context;
+        for (int in = threadIdx.x / D; in < columns; in += THREADS / D) {
+            const int i = row_of_column(a, c0 + in), own = key - context;
             if (a.tree ? own >= 0 && (own >= 64 || !(a.tree[p.q.first + i] >> own & 1)) : own > i) continue;
             if (whole) {
                 uint16_t *y = a.y.p + (p.q.first + i) * a.y.token + (kh * a.group + (c0 + in - i * a.group)) * a.y.head + dim;
@@ -460,6 +485,17 @@ static __device__ __forceinline__ void add_odd(const AttendArgs &a, const Place 
             }
         }
     }
+}
+
+// The first n bits, n held to 0 .. 32.
+static __device__ __forceinline__ uint32_t first_bits(int n) { return (uint32_t)((1ull << min(max(n, 0), 32)) - 1); }
+
+// Which of 32 keys from key0 on a column sees (`own` = key0 - context), those that there are: up to key `sees` without a tree.
+static __device__ __forceinline__ uint32_t seen_of(int key0, int keys, bool tree, int sees, uint64_t word, int own)
+{
+    if (!tree) return first_bits(min(keys, sees + 1) - key0);
+    const uint64_t mine = own >= 64 || own <= -64 ? 0 : own >= 0 ? word >> own : word << -own;
+    return first_bits(keys - key0) & ((uint32_t)mine | first_bits(-own));
 }
 
 template <int D, bool F8>
@@ -490,7 +526,7 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
     if (!W::template find<256>(a, found, [&](uint32_t total) {
             const uint32_t from = share_at(total, share, a.shares);
             left = share_at(total, share + 1, a.shares) - from;
-            return left ? from : UINT32_MAX;
+            return from;
         }, p)) return;
 
     const int page = 1 << a.cache.page_shift;
@@ -510,15 +546,15 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
         for (int c = 0; c < C; ++c) {
             int col = c0 + 16 * c + n;
             if (col >= columns) col = c0;
-            const int i = col / a.group, row = p.q.first + i, h = kh * a.group + (col - i * a.group);
+            const int i = row_of_column(a, col), row = p.q.first + i, h = kh * a.group + (col - i * a.group);
             const uint16_t *at = a.q.p + row * a.q.token + h * a.q.head;
 #pragma unroll
-            for (int s = 0; s < S::kSteps; ++s) q[c][s] = as_bf16x8(ld16(at + (F8 ? 64 * (s >> 1) + 16 * quad + 8 * (s & 1) : 32 * s + 8 * quad)));
+            for (int s = 0; s < S::kSteps; ++s) q[c][s] = as_bf16x8(flipped(ld16(at + (F8 ? 64 * (s >> 1) + 16 * quad + 8 * (s & 1) : 32 * s + 8 * quad)), a.flip));
             sees[c] = context + i;
             word[c] = a.tree ? a.tree[row] : 0;
         }
         // keys up to here are seen by all
-        const int open = min(p.q.keys, a.tree ? context : context + c0 / a.group + 1);
+        const int open = min(p.q.keys, a.tree ? context : context + row_of_column(a, c0) + 1);
 
         f32x4 o[C][S::kTiles];
         float top[C], sum[C];
@@ -620,18 +656,9 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
 #pragma unroll
                         for (int i = 0; i < 4; ++i) sc[c][t][i] *= F8 ? a.scale * four(kn[t], i) : a.scale;
                     if (!plain) {
-                        seen[c] = 0;
+                        seen[c] = seen_of(mine, held ? p.q.keys : 0, a.tree, sees[c], word[c], mine - context);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int key = mine + i, own = key - context;
-                            bool s = held && key < p.q.keys;
-                            if (a.tree)
-                                s = s && (own < 0 || (own < 64 && (word[c] >> (own & 63) & 1)));
-                            else
-                                s = s && key <= sees[c];
-                            seen[c] |= (uint32_t)s << i;
-                            sc[c][i >> 2][i & 3] = s ? sc[c][i >> 2][i & 3] : -INFINITY;
-                        }
+                        for (int i = 0; i < 8; ++i) sc[c][i >> 2][i & 3] = seen[c] >> i & 1 ? sc[c][i >> 2][i & 3] : -INFINITY;
                     }
                 }
                 // weights
@@ -662,10 +689,11 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
                 }
                 // values
                 if (!plain) {
+                    const uint32_t there = first_bits(held ? p.q.keys - mine : 0);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int x = 0; x < S::kBytesV / 4; ++x) v[i].w[x] = held && mine + i < p.q.keys ? v[i].w[x] : 0u;
+                        for (int x = 0; x < S::kBytesV / 4; ++x) v[i].w[x] &= 0u - (there >> i & 1);
                 }
                 uint4 vt[S::kTiles];
                 if constexpr (F8) {
@@ -698,12 +726,9 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
                 }
                 load_v(then, j1);
                 if (!plain) {
-                    bool some = false;
+                    uint32_t some = 0;
 #pragma unroll
-                    for (int i = 0; i < S::kTiles; ++i) {
-                        some |= odd16(vt[i].x) || odd16(vt[i].y) || odd16(vt[i].z) || odd16(vt[i].w);
-                        vt[i] = uint4{finite_of(vt[i].x), finite_of(vt[i].y), finite_of(vt[i].z), finite_of(vt[i].w)};
-                    }
+                    for (int i = 0; i < S::kTiles; ++i) vt[i] = finite_of(vt[i], some);
                     if (some) odd.note(turn, j);
                 }
 #pragma unroll
@@ -750,7 +775,7 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
                 const int dim = S::kTiles * (4 * quad + wave);
                 if (whole) {
                     const float by = all == 0.f ? 0.f : 1.f / all;
-                    const int i = col / a.group, row = p.q.first + i, h = kh * a.group + (col - i * a.group);
+                    const int i = row_of_column(a, col), row = p.q.first + i, h = kh * a.group + (col - i * a.group);
                     uint32_t *y = reinterpret_cast<uint32_t *>(a.y.p + row * a.y.token + h * a.y.head + dim);
 #pragma unroll
                     for (int x = 0; x < S::kTiles; x += 4) *reinterpret_cast<uint2 *>(y + x / 2) = uint2{pack_bf16_rne(z[x] * by, z[x + 1] * by), pack_bf16_rne(z[x + 2] * by, z[x + 3] * by)};
@@ -764,7 +789,7 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
         }
         if (tid == 0) odd.clear(turn ^ 1);
         __syncthreads();
-        if (odd.to[turn]) add_odd<D, F8>(a, p, kh, odd.from[turn] * kFewKeys, odd.to[turn] * kFewKeys, c0, TC, whole, a.parts + slot * TC * D);
+        if (odd.to[turn]) add_odd<D, F8, 256>(a, p, kh, odd.from[turn] * kFewKeys, odd.to[turn] * kFewKeys, c0, TC, whole, a.parts + slot * TC * D);
         turn ^= 1;
         left -= to - p.at;
         if (left == 0 || !W::next(a, p)) return;
@@ -772,39 +797,60 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
 }
 
 // ------------------------------------------------------------------------------------------------
-// Attention of many columns: tiles of 128 C, four wavefronts of 32 C columns, which share the keys and values of a step in LDS: 64 keys of 128 dims, or 128 of 64.
+// Attention of many columns: tiles of 32 a wavefront, whose four or eight wavefronts share the keys and values of a step in LDS: 64 keys of 128 dims, or 128 of 64.
 // S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16 matrix instructions, 32 keys at a time.  A lane (half h, column n) ends up with the scores of keys
 // 8 i + 4 h + 0 .. 3 of those; as in k_attend_few they become an operand where they are, for V^T is laid out by the same order of keys: piece (2 ks + h) of a dim's row
-// has the keys 16 ks + 4 h + {0 .. 3, 8 .. 11}.  Two wavefronts fetch K and two V, through registers, a step ahead: V is turned there (a thread has 8 keys x 8 dims),
-// 8-bit values become bf16 there, once for all four.  In LDS 16-byte pieces of a row are exchanged by its number so that neither writes nor
-// reads meet in a bank.
+// has the keys 16 ks + 4 h + {0 .. 3, 8 .. 11}.  Half of the wavefronts fetch V and half K, through registers, a step ahead: V is turned there (a thread has 8 keys x
+// kDimsV dims), 8-bit values become bf16 there, once for all wavefronts.  In LDS 16-byte pieces of a row are exchanged by its number so that neither writes nor reads
+// of eight lanes meet in a bank.
 // ------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
-static __device__ __forceinline__ uint4 four_words(const uint32_t *w) { return uint4{w[0], w[1], w[2], w[3]}; }
+// over a lane and the one 32 away
+static __device__ __forceinline__ float max_of_halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+static __device__ __forceinline__ float sum_of_halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
-template <int D, bool F8>
+template <int D, bool F8, int WAVES>
 struct WideShape {
-    static constexpr int kKeys = 8192 / D;          // of a step
-    static constexpr int kRow = D * (F8 ? 1 : 2);   // bytes of a key or value in the cache
-    static constexpr int kGroups = kKeys / 16;      // that lie on one page
-    static constexpr int kSteps = D / 16;           // of k, of the scores
-    static constexpr int kDims = D / 32;            // tiles of O^T
-    static constexpr int kLoads = F8 ? 4 : 8;       // of 16 bytes, a thread's of K
-    // byte of 16-byte piece p of row r: K [key][dim], V^T [dim][key]
-    static __device__ __forceinline__ int k_at(int r, int p) { return r * (2 * D) + 16 * (p ^ (D == 128 ? r & 15 : (r >> 1) & 7)); }
-    static __device__ __forceinline__ int v_at(int r, int p) { return r * (2 * kKeys) + 16 * (D == 128 ? p ^ (((r >> 1) & 3) ^ ((r >> 3) & 7)) : p ^ ((r & 7) ^ ((r >> 3) & 7) << 1)); }
+    static constexpr int kKeys = 8192 / D;               // of a step
+    static constexpr int kRow = D * (F8 ? 1 : 2);        // bytes of a key or value in the cache
+    static constexpr int kGroups = kKeys / 16;           // of keys that lie on one page
+    static constexpr int kSteps = D / 16;                // of k, of the scores
+    static constexpr int kDims = D / 32;                 // tiles of O^T
+    static constexpr int kDimsV = 32 / WAVES;            // a thread's of V
+    static constexpr int kWordsV = kDimsV * (F8 ? 1 : 2) / 4;  // .. of a key
+    static constexpr int kLoadsK = (F8 ? 16 : 32) / WAVES;     // of 16 bytes, a thread's
+    static constexpr int kAcross = kRow / 16;            // threads that have a row of K
+    static constexpr int kHeld = 8 * kWordsV > 4 * kLoadsK ? 8 * kWordsV : 4 * kLoadsK;
+    // by which a row's pieces are exchanged.  K [key][dim]; V^T [dim][key], which is also written across its rows: eight threads of one piece, kDimsV rows apart
+    static __device__ __forceinline__ int mix_k(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+    static __device__ __forceinline__ int mix_v(int r)
+    {
+        return D == 128 ? ((r >> 1) & 3) ^ ((r >> 3) & 1) ^ ((r >> 4) & 1) << 2 ^ ((r >> 5) & 1) << 1
+                        : (r & 7) ^ ((r >> 3) & 1) << 3 ^ ((r >> 4) & 1) << 1 ^ ((r >> 5) & 1) << 2;
+    }
+    static __device__ __forceinline__ int k_at(int r, int p) { return r * (2 * D) + 16 * (p ^ mix_k(r)); }
+    static __device__ __forceinline__ int v_at(int r, int p) { return r * (2 * kKeys) + 16 * (p ^ mix_v(r)); }
 };
 
-template <int D, bool F8, int C>
-__global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs a)
+template <int D, bool F8, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
 {
-    using S = WideShape<D, F8>;
-    constexpr int TC = 128 * C, KEYS = S::kKeys;
+    using S = WideShape<D, F8, WAVES>;
+    constexpr int TC = 32 * WAVES, KEYS = S::kKeys;
     using W = Dealt<TC, KEYS>;
     __shared__ typename W::Found found;
     __shared__ __attribute__((aligned(16))) char ks[2][16384], vs[2][16384];
-    __shared__ float scales[F8 ? 2 : 1][2][F8 ? KEYS : 1];
+    __shared__ __attribute__((aligned(16))) float scales[F8 ? 2 : 1][2][F8 ? KEYS : 4];
     __shared__ OddSteps odd;
     if (threadIdx.x == 0) odd.clear(0);
     int turn = 0;
@@ -812,52 +858,52 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs 
     const int kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
     typename W::Place p;
     uint32_t left = 0;
-    if (!W::template find<256>(a, found, [&](uint32_t total) {
+    if (!W::template find<64 * WAVES>(a, found, [&](uint32_t total) {
             const uint32_t from = share_at(total, share, a.shares);
             left = share_at(total, share + 1, a.shares) - from;
-            return left ? from : UINT32_MAX;
+            return from;
         }, p)) return;
     const int page = 1 << a.cache.page_shift;
-    const bool loads_v = wave < 2;
-    // V: keys of a thread, group of 16 and where in it; dims.  K: row within a load, piece
-    constexpr int kWide = D / 8;  // threads that have a row of V between them
-    const int vt = tid & 127, v_kg = vt / kWide, v_dims = (vt % kWide) * 8;
-    constexpr int kAcross = S::kRow / 16;  // .. of K
-    const int kt_row = (tid & 63) / kAcross, k_piece = (tid & 63) % kAcross;
+    const bool loads_v = wave < WAVES / 2;
+    // V: 8 keys and kDimsV dims of a thread.  K: its row and piece within a load
+    constexpr int kWide = D / S::kDimsV;  // threads that have a row of V
+    const int vt = tid & (32 * WAVES - 1), v_kg = vt / kWide, v_dims = (vt % kWide) * S::kDimsV;
+    const int k_row = lane / S::kAcross, k_piece = lane % S::kAcross, k_first = (wave - WAVES / 2) * (2 * KEYS / WAVES);
+    constexpr int kRows = 64 / S::kAcross;  // of K in a load: 16 at most
+    // where a lane's operands are
+    int k_off[S::kSteps], v_off[KEYS / 16];
+#pragma unroll
+    for (int x = 0; x < S::kSteps; ++x) k_off[x] = S::k_at(n, 2 * x + h);
+#pragma unroll
+    for (int z = 0; z < KEYS / 16; ++z) v_off[z] = S::v_at(n, 2 * z + h);
 
     while (true) {
         const uint32_t to = min(p.of, p.at + left);
         const bool whole = p.at == 0 && to == p.of;
-        const int context = p.q.keys - p.q.n, columns = p.q.n * a.group, c0 = p.t * TC, mine0 = c0 + wave * 32 * C;
-        const bool busy = mine0 < columns;
-        bf16x8 q[C][S::kSteps];
-        int sees[C];
-        uint64_t word[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            int col = mine0 + 32 * c + n;
+        const int context = p.q.keys - p.q.n, columns = p.q.n * a.group, c0 = p.t * TC;
+        const bool busy = c0 + wave * 32 < columns;
+        bf16x8 q[S::kSteps];
+        int sees;
+        uint64_t word;
+        {
+            int col = c0 + wave * 32 + n;
             if (col >= columns) col = c0;
-            const int i = col / a.group, row = p.q.first + i, hd = kh * a.group + (col - i * a.group);
+            const int i = row_of_column(a, col), row = p.q.first + i, hd = kh * a.group + (col - i * a.group);
             const uint16_t *at = a.q.p + row * a.q.token + hd * a.q.head;
 #pragma unroll
-            for (int s = 0; s < S::kSteps; ++s) q[c][s] = as_bf16x8(ld16(at + 16 * s + 8 * h));
-            sees[c] = context + i;
-            word[c] = a.tree ? a.tree[row] : 0;
+            for (int s = 0; s < S::kSteps; ++s) q[s] = as_bf16x8(flipped(ld16(at + 16 * s + 8 * h), a.flip));
+            sees = context + i;
+            word = a.tree ? a.tree[row] : 0;
         }
         // keys up to here are seen by all columns of the tile
-        const int open = min(p.q.keys, a.tree ? context : context + c0 / a.group + 1);
+        const int open = min(p.q.keys, a.tree ? context : context + row_of_column(a, c0) + 1);
 
-        f32x16 o[C][S::kDims];
-        float top[C], sum[C];
+        f32x16 o[S::kDims];
+        float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            top[c] = -INFINITY;
-            sum[c] = 0.f;
+        for (int i = 0; i < S::kDims; ++i)
 #pragma unroll
-            for (int i = 0; i < S::kDims; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[c][i][e] = 0.f;
-        }
+            for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
 
         const int32_t *table = a.table + p.r * a.ld_table;
         // a lane has the page of 16 keys, group lane mod kGroups; -1 where there is none
@@ -866,8 +912,7 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs 
             const int id = key < p.q.keys ? table[key >> a.cache.page_shift] : -1;
             return (unsigned)id < (unsigned)a.cache.pages ? id : -1;
         };
-        uint32_t held[32];  // fetched for the next step: of K, or of V (a key's after the other's)
-        constexpr int kOfKey = F8 ? 2 : 4;
+        uint32_t held[S::kHeld];  // fetched for the next step: of K, or of V (a key's after the other's)
         float sr[2];
         auto row_of = [&](int id, uint32_t j, int group) __attribute__((always_inline)) {  // of the cache, of the first of 16 keys
             const int in = ((int)j * KEYS + 16 * group) & (page - 1);
@@ -879,20 +924,20 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs 
                 const char *at = a.cache.v + (row_of(id, j, group) + 4 * (v_kg & 1)) * S::kRow + v_dims * (F8 ? 1 : 2);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const auto got = ld_bytes<4 * kOfKey>(at + (i < 4 ? i : i + 4) * S::kRow);
+                    const auto got = ld_bytes<4 * S::kWordsV>(at + (i < 4 ? i : i + 4) * S::kRow);
 #pragma unroll
-                    for (int x = 0; x < kOfKey; ++x) held[kOfKey * i + x] = got.w[x];
+                    for (int x = 0; x < S::kWordsV; ++x) held[S::kWordsV * i + x] = got.w[x];
                 }
+                asm volatile("; values");  // (the two ways end differently: the compiler would else join their loads, a register at a time)
             } else {
-                // a wavefront has half of the step's keys; a load as many rows as fit 1 KB
-                constexpr int kRows = 64 / kAcross;
 #pragma unroll
-                for (int i = 0; i < S::kLoads; ++i) {
-                    const int key = (wave - 2) * (KEYS / 2) + i * kRows + kt_row, group = key >> 4, id = __shfl(ids, group, 64);
-                    const auto got = ld_bytes<16>(a.cache.k + (row_of(id, j, group) + (key & 15)) * S::kRow + 16 * k_piece);
+                for (int i = 0; i < S::kLoadsK; ++i) {
+                    const int first = k_first + i * kRows, group = first >> 4, id = __builtin_amdgcn_readlane(ids, group);
+                    const auto got = ld_bytes<16>(a.cache.k + (row_of(id, j, group) + (first & 15) + k_row) * S::kRow + 16 * k_piece);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) held[4 * i + x] = got.w[x];
                 }
+                asm volatile("; keys");
             }
             if constexpr (F8) {
                 const int key = tid & (KEYS - 1), group = key >> 4, id = __shfl(ids, group, 64);
@@ -904,33 +949,26 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs 
         // ids: of the step that was fetched
         auto stage = [&](int ids, uint32_t j, int b) __attribute__((always_inline)) {
             const int key0 = (int)j * KEYS;
-            const bool plain = key0 + KEYS <= open && __ballot(ids < 0) == 0;
             if (loads_v) {
+                const bool plain = key0 + KEYS <= open && __ballot(ids < 0) == 0;
                 const int group = v_kg >> 1, first = key0 + 16 * group + 4 * (v_kg & 1);
                 if (!plain) {
-                    const bool there = __shfl(ids, group, 64) >= 0;
+                    const uint32_t there = first_bits(__shfl(ids, group, 64) >= 0 ? p.q.keys - first : 0);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int x = 0; x < kOfKey; ++x) held[kOfKey * i + x] = there && first + (i < 4 ? i : i + 4) < p.q.keys ? held[kOfKey * i + x] : 0u;
+                        for (int x = 0; x < S::kWordsV; ++x) held[S::kWordsV * i + x] &= 0u - (there >> (i < 4 ? i : i + 4) & 1);
                 }
-                bool some = false;
-                auto put = [&](int c, uint4 w) __attribute__((always_inline)) {
-                    if (!plain) {
-                        some |= odd16(w.x) || odd16(w.y) || odd16(w.z) || odd16(w.w);
-                        w = uint4{finite_of(w.x), finite_of(w.y), finite_of(w.z), finite_of(w.w)};
-                    }
-                    *reinterpret_cast<uint4 *>(vs[b] + S::v_at(v_dims + c, v_kg)) = w;
-                };
+                uint4 turned[S::kDimsV];
                 if constexpr (F8) {
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
+                    for (int x = 0; x < S::kWordsV; ++x) {
                         uint32_t four_keys[2][4];
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
-                            const uint32_t *v = held + 8 * y + x;
-                            const uint32_t l01 = __builtin_amdgcn_perm(v[2], v[0], 0x05010400u), l23 = __builtin_amdgcn_perm(v[6], v[4], 0x05010400u);
-                            const uint32_t h01 = __builtin_amdgcn_perm(v[2], v[0], 0x07030602u), h23 = __builtin_amdgcn_perm(v[6], v[4], 0x07030602u);
+                            auto v = [&](int i) __attribute__((always_inline)) { return held[S::kWordsV * (4 * y + i) + x]; };
+                            const uint32_t l01 = __builtin_amdgcn_perm(v(1), v(0), 0x05010400u), l23 = __builtin_amdgcn_perm(v(3), v(2), 0x05010400u);
+                            const uint32_t h01 = __builtin_amdgcn_perm(v(1), v(0), 0x07030602u), h23 = __builtin_amdgcn_perm(v(3), v(2), 0x07030602u);
                             four_keys[y][0] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
                             four_keys[y][1] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
                             four_keys[y][2] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
@@ -938,39 +976,49 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs 
                         }
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-                            put(4 * x + c, uint4{two_of_e4m3<false>(four_keys[0][c]), two_of_e4m3<true>(four_keys[0][c]), two_of_e4m3<false>(four_keys[1][c]),
-                                                 two_of_e4m3<true>(four_keys[1][c])});
+                            turned[4 * x + c] = uint4{two_of_e4m3<false>(four_keys[0][c]), two_of_e4m3<true>(four_keys[0][c]), two_of_e4m3<false>(four_keys[1][c]),
+                                                      two_of_e4m3<true>(four_keys[1][c])};
                     }
                 } else {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 0; c < S::kDimsV; ++c) {
                         uint32_t d[4];
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) d[y] = __builtin_amdgcn_perm(held[8 * y + 4 + (c >> 1)], held[8 * y + (c >> 1)], c & 1 ? 0x07060302u : 0x05040100u);
-                        put(c, four_words(d));
+                        for (int y = 0; y < 4; ++y)
+                            d[y] = __builtin_amdgcn_perm(held[S::kWordsV * (2 * y + 1) + (c >> 1)], held[S::kWordsV * 2 * y + (c >> 1)], c & 1 ? 0x07060302u : 0x05040100u);
+                        turned[c] = uint4{d[0], d[1], d[2], d[3]};
                     }
                 }
-                if (some) odd.note(turn, j);
-            } else {
-                constexpr int kRows = 64 / kAcross;
+                if (!plain) {
+                    uint32_t some = 0;
 #pragma unroll
-                for (int i = 0; i < S::kLoads; ++i) {
-                    const int key = (wave - 2) * (KEYS / 2) + i * kRows + kt_row;
+                    for (int c = 0; c < S::kDimsV; ++c) turned[c] = finite_of(turned[c], some);
+                    if (some) odd.note(turn, j);
+                }
+#pragma unroll
+                for (int c = 0; c < S::kDimsV; ++c) *reinterpret_cast<uint4 *>(vs[b] + S::v_at(v_dims + c, v_kg)) = turned[c];
+                asm volatile("; values");
+            } else {
+#pragma unroll
+                for (int i = 0; i < S::kLoadsK; ++i) {
+                    const int key = k_first + i * kRows + k_row;
+                    const uint32_t *w = held + 4 * i;
                     if constexpr (F8) {
-                        const uint32_t *w = held + 4 * i;
                         *reinterpret_cast<uint4 *>(ks[b] + S::k_at(key, 2 * k_piece)) =
                             uint4{two_of_e4m3<false>(w[0]), two_of_e4m3<true>(w[0]), two_of_e4m3<false>(w[1]), two_of_e4m3<true>(w[1])};
                         *reinterpret_cast<uint4 *>(ks[b] + S::k_at(key, 2 * k_piece + 1)) =
                             uint4{two_of_e4m3<false>(w[2]), two_of_e4m3<true>(w[2]), two_of_e4m3<false>(w[3]), two_of_e4m3<true>(w[3])};
                     } else {
-                        *reinterpret_cast<uint4 *>(ks[b] + S::k_at(key, k_piece)) = four_words(held + 4 * i);
+                        *reinterpret_cast<uint4 *>(ks[b] + S::k_at(key, k_piece)) = uint4{w[0], w[1], w[2], w[3]};
                     }
                 }
+                asm volatile("; keys");
             }
             if constexpr (F8) {
+                const bool there = __shfl(ids, (tid & (KEYS - 1)) >> 4, 64) >= 0 && key0 + (tid & (KEYS - 1)) < p.q.keys;
                 if (tid < KEYS) {
-                    scales[b][0][tid] = sr[0] * a.scale;
-                    scales[b][1][tid] = key0 + tid < p.q.keys && __shfl(ids, tid >> 4, 64) >= 0 ? sr[1] : 0.f;
+                    scales[b][0][tid] = sr[0];
+                    scales[b][1][tid] = there ? sr[1] : 0.f;
                 }
             }
         };
@@ -991,81 +1039,66 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs 
                 stage(then, j1, b ^ 1);
                 fetch(after, j2);
                 if (busy) {
-#pragma unroll 1
+                    const char *kb = ks[b], *vb = vs[b];
+#pragma unroll
                     for (int kt = 0; kt < KEYS / 32; ++kt) {
-                        f32x16 s[C];
+                        f32x16 s;
 #pragma unroll
-                        for (int c = 0; c < C; ++c)
+                        for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) s[c][e] = 0.f;
-#pragma unroll
-                        for (int x = 0; x < S::kSteps; ++x) {
-                            const bf16x8 k = as_bf16x8(*reinterpret_cast<const uint4 *>(ks[b] + S::k_at(32 * kt + n, 2 * x + h)));
-#pragma unroll
-                            for (int c = 0; c < C; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c][x], s[c], 0, 0, 0);
-                        }
-                        [[maybe_unused]] float4 by_k[4], by_v[4];
+                        for (int x = 0; x < S::kSteps; ++x)
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const uint4 *>(kb + k_off[x] + kt * 64 * D)), q[x], s, 0, 0, 0);
+                        [[maybe_unused]] float4 by_v[4];
+                        auto four = [](const float4 &f, int i) __attribute__((always_inline)) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; };
                         if constexpr (F8) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                by_k[i] = *reinterpret_cast<const float4 *>(&scales[b][0][32 * kt + 8 * i + 4 * h]);
+                                const float4 by_k = *reinterpret_cast<const float4 *>(&scales[b][0][32 * kt + 8 * i + 4 * h]);
                                 by_v[i] = *reinterpret_cast<const float4 *>(&scales[b][1][32 * kt + 8 * i + 4 * h]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) s[4 * i + e] *= four(by_k, e);
                             }
                         }
-                        auto four = [](const float4 &f, int i) __attribute__((always_inline)) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; };
-                        uint4 w[C][2];
-                        uint32_t seen[C];
+                        uint32_t seen = 0xFFFFFFFFu;
+                        if (!plain) {
+                            const int first = key0 + 32 * kt;
+                            const uint32_t there = ((none >> (2 * kt) & 1 ? 0u : 0xFFFFu) | (none >> (2 * kt + 1) & 1 ? 0u : 0xFFFF0000u)) >> (4 * h);
+                            seen = seen_of(first, p.q.keys, a.tree, sees, word, first - context) >> (4 * h) & there;
 #pragma unroll
-                        for (int c = 0; c < C; ++c) {
-                            seen[c] = 0xFFFFu;
+                            for (int e = 0; e < 16; ++e) s[e] = seen >> (8 * (e >> 2) + (e & 3)) & 1 ? s[e] : -INFINITY;
+                        }
+                        float t = fmaxf(s[0], s[1]);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) s[c][e] *= F8 ? four(by_k[e >> 2], e & 3) : a.scale;
-                            if (!plain) {
-                                seen[c] = 0;
+                        for (int e = 2; e < 16; e += 2) t = fmaxf(fmaxf(t, s[e]), s[e + 1]);
+                        t = max_of_halves(t);
+                        if (__any(t > top + a.slack)) {
+                            t = fmaxf(t, top);
+                            const float f = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - t) * a.scale);
+                            sum *= f;
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) {
-                                    const int in = 32 * kt + 8 * (e >> 2) + 4 * h + (e & 3), key = key0 + in, own = key - context;
-                                    bool v = key < p.q.keys && !(none >> (in >> 4) & 1);
-                                    if (a.tree)
-                                        v = v && (own < 0 || (own < 64 && (word[c] >> (own & 63) & 1)));
-                                    else
-                                        v = v && key <= sees[c];
-                                    seen[c] |= (uint32_t)v << e;
-                                    s[c][e] = v ? s[c][e] : -INFINITY;
-                                }
+                            for (int i = 0; i < S::kDims; ++i) o[i] *= f;
+                            top = t;
+                        }
+                        const float from = top == -INFINITY ? 0.f : -top * a.scale;
+                        uint32_t w[8];
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) {
+                            float e0 = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale, from)), e1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], a.scale, from));
+                            if constexpr (F8) {
+                                sum += e0 + e1;
+                                e0 = plain || (seen >> (8 * (e >> 2) + (e & 3)) & 1) ? e0 * four(by_v[e >> 2], e & 3) : 0.f;
+                                e1 = plain || (seen >> (8 * (e >> 2) + (e & 3) + 1) & 1) ? e1 * four(by_v[e >> 2], (e & 3) + 1) : 0.f;
                             }
-                            float t = fmaxf(s[c][0], s[c][1]);
-#pragma unroll
-                            for (int e = 2; e < 16; e += 2) t = fmaxf(t, fmaxf(s[c][e], s[c][e + 1]));
-                            t = fmaxf(t, __shfl_xor(t, 32, 64));
-                            t = fmaxf(t, top[c]);
-                            if (__any(t > top[c])) {
-                                const float f = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[c] - t);
-                                sum[c] *= f;
-#pragma unroll
-                                for (int i = 0; i < S::kDims; ++i) o[c][i] *= f;
-                                top[c] = t;
-                            }
-                            const float from = t == -INFINITY ? 0.f : t;
-                            float e8[16];
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                e8[e] = __builtin_amdgcn_exp2f(s[c][e] - from);
-                                sum[c] += e8[e];
-                                if constexpr (F8) e8[e] = plain || (seen[c] >> e & 1) ? e8[e] * four(by_v[e >> 2], e & 3) : 0.f;
-                            }
-#pragma unroll
-                            for (int y = 0; y < 2; ++y)
-                                w[c][y] = uint4{pack_bf16_rne(e8[8 * y], e8[8 * y + 1]), pack_bf16_rne(e8[8 * y + 2], e8[8 * y + 3]), pack_bf16_rne(e8[8 * y + 4], e8[8 * y + 5]),
-                                                pack_bf16_rne(e8[8 * y + 6], e8[8 * y + 7])};
+                            w[e / 2] = pack_bf16_rne(e0, e1);
+                            if constexpr (!F8) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e / 2]), bf16x2{(__bf16)1.f, (__bf16)1.f}, sum, false);
                         }
 #pragma unroll
                         for (int y = 0; y < 2; ++y)
 #pragma unroll
                             for (int i = 0; i < S::kDims; ++i) {
-                                const bf16x8 v = as_bf16x8(*reinterpret_cast<const uint4 *>(vs[b] + S::v_at(32 * i + n, 2 * (2 * kt + y) + h)));
-#pragma unroll
-                                for (int c = 0; c < C; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(w[c][y]), o[c][i], 0, 0, 0);
+                                const int z = (2 * kt + y) ^ (i & 1) << (D == 128 ? 0 : 1);  // (mix_v takes bit 5 of the row)
+                                const bf16x8 v = as_bf16x8(*reinterpret_cast<const uint4 *>(vb + v_off[z] + i * 64 * KEYS));
+                                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(uint4{w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]}), o[i], 0, 0, 0);
                             }
                     }
                 }
@@ -1076,51 +1109,49 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_wide(AttendArgs 
         }
 
         const int64_t slot = part_of(kh, a.shares, share, p.at == 0);
-        if (busy) {
-            float *slots = a.parts + (int64_t)a.cache.kv_heads * a.shares * 2 * TC * D;
+        const int in = wave * 32 + n, col = c0 + in;
+        const float all = sum_of_halves(sum);
+        if (col < columns) {
+            if (whole) {
+                const float by = all == 0.f ? 0.f : 1.f / all;
+                const int i = row_of_column(a, col), row = p.q.first + i, hd = kh * a.group + (col - i * a.group);
+                uint16_t *y = a.y.p + row * a.y.token + hd * a.y.head + 4 * h;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const float all = sum[c] + __shfl_xor(sum[c], 32, 64);
-                const int in = wave * 32 * C + 32 * c + n, col = c0 + in;
-                if (col >= columns) continue;
-                if (whole) {
-                    const float by = all == 0.f ? 0.f : 1.f / all;
-                    const int i = col / a.group, row = p.q.first + i, hd = kh * a.group + (col - i * a.group);
-                    uint16_t *y = a.y.p + row * a.y.token + hd * a.y.head + 4 * h;
+                for (int x = 0; x < S::kDims; ++x)
 #pragma unroll
-                    for (int x = 0; x < S::kDims; ++x)
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<uint2 *>(y + 32 * x + 8 * e) =
+                            uint2{pack_bf16_rne(o[x][4 * e] * by, o[x][4 * e + 1] * by), pack_bf16_rne(o[x][4 * e + 2] * by, o[x][4 * e + 3] * by)};
+            } else {
+                float *slots = a.parts + (int64_t)a.cache.kv_heads * a.shares * 2 * TC * D;
+                float *y = a.parts + (slot * TC + in) * D + 4 * h;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            *reinterpret_cast<uint2 *>(y + 32 * x + 8 * e) =
-                                uint2{pack_bf16_rne(o[c][x][4 * e] * by, o[c][x][4 * e + 1] * by), pack_bf16_rne(o[c][x][4 * e + 2] * by, o[c][x][4 * e + 3] * by)};
-                } else {
-                    float *y = a.parts + (slot * TC + in) * D + 4 * h;
+                for (int x = 0; x < S::kDims; ++x)
 #pragma unroll
-                    for (int x = 0; x < S::kDims; ++x)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            *reinterpret_cast<float4 *>(y + 32 * x + 8 * e) = float4{o[c][x][4 * e], o[c][x][4 * e + 1], o[c][x][4 * e + 2], o[c][x][4 * e + 3]};
-                    if (h == 0) *reinterpret_cast<float2 *>(slots + (slot * TC + in) * 2) = float2{top[c], all};
-                }
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<float4 *>(y + 32 * x + 8 * e) = float4{o[x][4 * e], o[x][4 * e + 1], o[x][4 * e + 2], o[x][4 * e + 3]};
+                if (h == 0) *reinterpret_cast<float2 *>(slots + (slot * TC + in) * 2) = float2{top * a.scale, all};
             }
         }
         if (tid == 0) odd.clear(turn ^ 1);
         __syncthreads();
-        if (odd.to[turn]) add_odd<D, F8>(a, p, kh, odd.from[turn] * KEYS, odd.to[turn] * KEYS, c0, TC, whole, a.parts + slot * TC * D);
+        if (odd.to[turn]) add_odd<D, F8, 64 * WAVES>(a, p, kh, odd.from[turn] * KEYS, odd.to[turn] * KEYS, c0, TC, whole, a.parts + slot * TC * D);
         turn ^= 1;
         left -= to - p.at;
         if (left == 0 || !W::next(a, p)) return;
     }
 }
 
-// Tiles that several shares have a part of: a work group has 16 columns of the tile that the first step of share s + 1 lies in, if that tile begins in share s.
-template <int D, int TC, int KEYS>
+// Tiles that several shares have a part of: a work group has CW columns of the tile that the first step of share s + 1 lies in, if that tile begins in share s.
+// 16 / CW groups of threads share the parts, four of which a thread asks for at a time.
+template <int D, int TC, int KEYS, int CW>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
 {
     using W = Dealt<TC, KEYS>;
-    constexpr int kEach = D / 16;
+    constexpr int kEach = D / 16, kGroups = 16 / CW;
     __shared__ typename W::Found found;
-    const int kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
+    __shared__ float tops[256 / CW][CW], sums[kGroups][CW], rows[kGroups][CW][D];
+    const int tid = threadIdx.x, kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
     typename W::Place p;
     uint32_t total = 0, step = 0;
     if (!W::template find<256>(a, found, [&](uint32_t all) {
@@ -1128,33 +1159,79 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
             return step = share_at(all, share + 1, a.shares);
         }, p)) return;
     if (p.at == 0 || step - p.at < share_at(total, share, a.shares)) return;
+    const int in0 = CW * blockIdx.y, columns = p.q.n * a.group - p.t * TC;
+    if (in0 >= columns) return;
     const uint32_t end = step - p.at + p.of;
+    // the share of the tile's last step: they are alike but for one step
     int last = share + 1;
-    while (last + 1 < a.shares && share_at(total, last + 1, a.shares) < end) ++last;
-    const int in = 16 * blockIdx.y + (threadIdx.x >> 4), dim = (threadIdx.x & 15) * kEach, col = p.t * TC + in;
-    if (col >= p.q.n * a.group) return;
+    {
+        const uint32_t least = max(1u, total / min((uint32_t)a.shares, total));
+        last = min((int)min((uint32_t)a.shares, total) - 1, share + 1 + (int)((end - 1 - step) / least));
+        while (share_at(total, last, a.shares) >= end) --last;
+    }
     const float *slots = a.parts + (int64_t)a.cache.kv_heads * a.shares * 2 * TC * D;
-    auto slot_of = [&](int s) { return part_of(kh, a.shares, s, s == share) * TC + in; };
-    // (a share without steps has no part: where there are more shares than steps, some have none)
-    auto has = [&](int s) { return share_at(total, s, a.shares) < share_at(total, s + 1, a.shares); };
+    auto slot_of = [&](int s) __attribute__((always_inline)) { return part_of(kh, a.shares, s, s == share) * TC + in0; };
+    {
+        const int c = tid % CW;
+        float most = -INFINITY;
+        for (int s = share + tid / CW; s <= last; s += 256 / CW) most = fmaxf(most, slots[(slot_of(s) + c) * 2]);
+        tops[tid / CW][c] = most;
+    }
+    __syncthreads();
+    const int c = tid / (16 * kGroups), grp = tid / 16 % kGroups, dim = (tid & 15) * kEach;
     float most = -INFINITY;
-    for (int s = share; s <= last; ++s)
-        if (has(s)) most = fmaxf(most, slots[slot_of(s) * 2]);
+    for (int i = 0; i < min(256 / CW, last - share + 1); ++i) most = fmaxf(most, tops[i][c]);
     const float from = most == -INFINITY ? 0.f : most;
     float all = 0.f, z[kEach] = {};
-    for (int s = share; s <= last; ++s) {
-        if (!has(s)) continue;
-        const int64_t at = slot_of(s);
-        const float f = __builtin_amdgcn_exp2f(slots[at * 2] - from);
-        all += slots[at * 2 + 1] * f;
+    for (int s = share + grp; s <= last; s += 4 * kGroups) {
+        float2 sum[4];
+        float part[4][kEach];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) z[i] += a.parts[at * D + dim + i] * f;
+        for (int i = 0; i < 4; ++i) {
+            const int64_t at = slot_of(min(s + i * kGroups, last)) + c;
+            sum[i] = *reinterpret_cast<const float2 *>(slots + at * 2);
+#pragma unroll
+            for (int x = 0; x < kEach; x += 4) *reinterpret_cast<float4 *>(part[i] + x) = *reinterpret_cast<const float4 *>(a.parts + at * D + dim + x);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool there = s + i * kGroups <= last;
+            const float f = __builtin_amdgcn_exp2f(sum[i].x - from);
+            all += there ? sum[i].y * f : 0.f;
+#pragma unroll
+            for (int x = 0; x < kEach; ++x) z[x] += there ? part[i][x] * f : 0.f;
+        }
     }
+    if constexpr (kGroups > 1) {
+        if ((tid & 15) == 0) sums[grp][c] = all;
+#pragma unroll
+        for (int x = 0; x < kEach; ++x) rows[grp][c][dim + x] = z[x];
+        __syncthreads();
+        if (grp > 0) return;
+        for (int g = 1; g < kGroups; ++g) {
+            all += sums[g][c];
+#pragma unroll
+            for (int x = 0; x < kEach; ++x) z[x] += rows[g][c][dim + x];
+        }
+    }
+    if (in0 + c >= columns) return;
     const float by = all == 0.f ? 0.f : 1.f / all;
-    const int i = col / a.group, row = p.q.first + i, h = kh * a.group + (col - i * a.group);
+    const int col = p.t * TC + in0 + c, i = row_of_column(a, col), row = p.q.first + i, h = kh * a.group + (col - i * a.group);
     uint32_t *y = reinterpret_cast<uint32_t *>(a.y.p + row * a.y.token + h * a.y.head + dim);
 #pragma unroll
-    for (int x = 0; x < kEach; x += 2) y[x / 2] = pack_bf16_rne(z[x] * by, z[x + 1] * by);
+    for (int x = 0; x < kEach; x += 4) *reinterpret_cast<uint2 *>(y + x / 2) = uint2{pack_bf16_rne(z[x] * by, z[x + 1] * by), pack_bf16_rne(z[x + 2] * by, z[x + 3] * by)};
+}
+
+template <int D, int TC, int KEYS>
+static hipError_t launch_join(const AttendArgs &a, hipStream_t stream)
+{
+    const unsigned ends = (unsigned)(a.shares - 1) * a.cache.kv_heads;
+    // few requests among many shares: a tile has many parts
+    if (TC <= 64 && 4 * a.requests < a.shares)
+        hipLaunchKernelGGL((k_attend_join<D, TC, KEYS, 4>), dim3(ends, TC / 4), dim3(256), 0, stream, a);
+    else
+        hipLaunchKernelGGL((k_attend_join<D, TC, KEYS, 16>), dim3(ends, TC / 16), dim3(256), 0, stream, a);
+    return hipGetLastError();
 }
 
 template <int D, bool F8, int C>
@@ -1162,17 +1239,15 @@ static hipError_t launch_few(const AttendArgs &a, bool joins, hipStream_t stream
 {
     hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(256), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
-    hipLaunchKernelGGL((k_attend_join<D, 16 * C, kFewKeys>), dim3((unsigned)(a.shares - 1) * a.cache.kv_heads, C), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    return launch_join<D, 16 * C, kFewKeys>(a, stream);
 }
 
-template <int D, bool F8, int C>
+template <int D, bool F8, int WAVES>
 static hipError_t launch_wide(const AttendArgs &a, bool joins, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_attend_wide<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((k_attend_wide<D, F8, WAVES>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * WAVES), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
-    hipLaunchKernelGGL((k_attend_join<D, 128 * C, WideShape<D, F8>::kKeys>), dim3((unsigned)(a.shares - 1) * a.cache.kv_heads, 8 * C), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    return launch_join<D, 32 * WAVES, WideShape<D, F8, WAVES>::kKeys>(a, stream);
 }
 
 hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t stream)
@@ -1186,8 +1261,8 @@ hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t strea
         return f.columns == 16    ? launch_few<D, F8, 1>(a, f.joins, stream)
                : f.columns == 32  ? launch_few<D, F8, 2>(a, f.joins, stream)
                : f.columns == 64  ? launch_few<D, F8, 4>(a, f.joins, stream)
-               : f.columns == 128 ? launch_wide<D, F8, 1>(a, f.joins, stream)
-                                  : launch_wide<D, F8, 2>(a, f.joins, stream);
+               : f.columns == 128 ? launch_wide<D, F8, 4>(a, f.joins, stream)
+                                  : launch_wide<D, F8, 8>(a, f.joins, stream);
     };
     auto by_bits = [&](auto dim) { return a.cache.bits8 ? by_columns(dim, std::true_type{}) : by_columns(dim, std::false_type{}); };
     return a.cache.dim == 64 ? by_bits(std::integral_constant<int, 64>{}) : by_bits(std::integral_constant<int, 128>{});
