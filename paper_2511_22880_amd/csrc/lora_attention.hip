@@ -1023,6 +1023,127 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
             }
         };
 
+        // A step's keys, 64 at a time.  The order of instructions is laid down: operands are read from LDS beside the matrix instructions in front of those that
+        // need them, and the second half's exponentials beside the first half's product with v.
+        auto take = [&](bool plain, int b, int key0, uint64_t none) __attribute__((always_inline)) {
+            constexpr int kPv = 2 * S::kDims;  // matrix instructions of 32 keys with v
+            constexpr bool kEarly = WAVES == 8;  // (with four wavefronts each holds twice as much of the next step: it would have to put registers by)
+            const char *kb = ks[b], *vb = vs[b];
+            auto four = [](const float4 &f, int i) __attribute__((always_inline)) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; };
+#pragma unroll
+            for (int u = 0; u < KEYS / 64; ++u) {
+                auto read_k = [&](int kt, int x) __attribute__((always_inline)) { return as_bf16x8(*reinterpret_cast<const uint4 *>(kb + k_off[x] + kt * 64 * D)); };
+                auto read_v = [&](int kt, int i) __attribute__((always_inline)) {
+                    const int z = (2 * kt + i / S::kDims) ^ (i % S::kDims & 1) << (D == 128 ? 0 : 1);  // (mix_v takes bit 5 of the row)
+                    return as_bf16x8(*reinterpret_cast<const uint4 *>(vb + v_off[z] + i % S::kDims * 64 * KEYS));
+                };
+                bf16x8 k[S::kSteps], v[kPv];
+                f32x16 s[2];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[0][e] = s[1][e] = 0.f;
+#pragma unroll
+                for (int x = 0; x < S::kSteps; ++x) k[x] = read_k(2 * u, x);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int x = 0; x < S::kSteps; ++x) {
+                    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[x], q[x], s[0], 0, 0, 0);
+                    k[x] = read_k(2 * u + 1, x);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int x = 0; x < S::kSteps; ++x) {
+                    s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[x], q[x], s[1], 0, 0, 0);
+                    if (kEarly && x < kPv) v[x] = read_v(2 * u, x);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                [[maybe_unused]] float4 by_v[4];
+                uint32_t seen[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    if constexpr (F8) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 by_k = *reinterpret_cast<const float4 *>(&scales[b][0][64 * u + 32 * y + 8 * i + 4 * h]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[y][4 * i + e] *= four(by_k, e);
+                        }
+                    }
+                    if (!plain) {
+                        const int kt = 2 * u + y, first = key0 + 32 * kt;
+                        const uint32_t there = ((none >> (2 * kt) & 1 ? 0u : 0xFFFFu) | (none >> (2 * kt + 1) & 1 ? 0u : 0xFFFF0000u)) >> (4 * h);
+                        seen[y] = seen_of(first, p.q.keys, a.tree, sees, word, first - context) >> (4 * h) & there;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[y][e] = seen[y] >> (8 * (e >> 2) + (e & 3)) & 1 ? s[y][e] : -INFINITY;
+                    }
+                }
+                float t = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+                for (int e = 1; e < 16; ++e) t = fmaxf(fmaxf(t, s[0][e]), s[1][e]);
+                t = max_of_halves(t);
+                if (__any(t > top + a.slack)) {
+                    t = fmaxf(t, top);
+                    const float f = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - t) * a.scale);
+                    sum *= f;
+#pragma unroll
+                    for (int i = 0; i < S::kDims; ++i) o[i] *= f;
+                    top = t;
+                }
+                const float from = top == -INFINITY ? 0.f : -top * a.scale;
+                uint32_t w[2][8];
+                // two weights
+                auto weigh = [&](int y, int e) __attribute__((always_inline)) {
+                    float e0 = __builtin_amdgcn_exp2f(fmaf(s[y][e], a.scale, from)), e1 = __builtin_amdgcn_exp2f(fmaf(s[y][e + 1], a.scale, from));
+                    if constexpr (F8) {
+                        sum += e0 + e1;
+                        e0 *= four(by_v[e >> 2], e & 3);
+                        e1 *= four(by_v[e >> 2], (e & 3) + 1);
+                    }
+                    w[y][e / 2] = pack_bf16_rne(e0, e1);
+                    if constexpr (!F8) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[y][e / 2]), bf16x2{(__bf16)1.f, (__bf16)1.f}, sum, false);
+                };
+                // (nought times a scale that is none is none)
+                auto only_seen = [&](int y) __attribute__((always_inline)) {
+                    if (F8 && !plain) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) {
+                            const uint32_t pair = seen[y] >> (8 * (e >> 2) + (e & 3));
+                            w[y][e / 2] &= (0u - (pair & 1) & 0xFFFFu) | (0u - (pair >> 1 & 1) & 0xFFFF0000u);
+                        }
+                    }
+                };
+                auto product = [&](int y, int i) __attribute__((always_inline)) {
+                    const uint32_t *x = w[y] + 4 * (i / S::kDims);
+                    o[i % S::kDims] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[i], as_bf16x8(uint4{x[0], x[1], x[2], x[3]}), o[i % S::kDims], 0, 0, 0);
+                };
+                auto read_scales = [&](int y) __attribute__((always_inline)) {
+                    if constexpr (F8) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) by_v[i] = *reinterpret_cast<const float4 *>(&scales[b][1][64 * u + 32 * y + 8 * i + 4 * h]);
+                    }
+                };
+                read_scales(0);
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) weigh(0, e);
+                only_seen(0);
+                if constexpr (!kEarly) {
+#pragma unroll
+                    for (int i = 0; i < kPv; ++i) v[i] = read_v(2 * u, i);
+                }
+                read_scales(1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < kPv; ++i) {
+                    product(0, i);
+                    v[i] = read_v(2 * u + 1, i);
+#pragma unroll
+                    for (int e = 16 / kPv * i; e < 16 / kPv * (i + 1); e += 2) weigh(1, e);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                only_seen(1);
+#pragma unroll
+                for (int i = 0; i < kPv; ++i) product(1, i);
+            }
+        };
         if (p.q.keys > 0) {
             int now = page_of(p.at), then = page_of(p.at + 1 < to ? p.at + 1 : p.at);
             fetch(now, p.at);
@@ -1038,70 +1159,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                 const bool plain = none == 0 && key0 + KEYS <= open;
                 stage(then, j1, b ^ 1);
                 fetch(after, j2);
-                if (busy) {
-                    const char *kb = ks[b], *vb = vs[b];
-#pragma unroll
-                    for (int kt = 0; kt < KEYS / 32; ++kt) {
-                        f32x16 s;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-                        for (int x = 0; x < S::kSteps; ++x)
-                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const uint4 *>(kb + k_off[x] + kt * 64 * D)), q[x], s, 0, 0, 0);
-                        [[maybe_unused]] float4 by_v[4];
-                        auto four = [](const float4 &f, int i) __attribute__((always_inline)) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; };
-                        if constexpr (F8) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float4 by_k = *reinterpret_cast<const float4 *>(&scales[b][0][32 * kt + 8 * i + 4 * h]);
-                                by_v[i] = *reinterpret_cast<const float4 *>(&scales[b][1][32 * kt + 8 * i + 4 * h]);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) s[4 * i + e] *= four(by_k, e);
-                            }
-                        }
-                        uint32_t seen = 0xFFFFFFFFu;
-                        if (!plain) {
-                            const int first = key0 + 32 * kt;
-                            const uint32_t there = ((none >> (2 * kt) & 1 ? 0u : 0xFFFFu) | (none >> (2 * kt + 1) & 1 ? 0u : 0xFFFF0000u)) >> (4 * h);
-                            seen = seen_of(first, p.q.keys, a.tree, sees, word, first - context) >> (4 * h) & there;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) s[e] = seen >> (8 * (e >> 2) + (e & 3)) & 1 ? s[e] : -INFINITY;
-                        }
-                        float t = fmaxf(s[0], s[1]);
-#pragma unroll
-                        for (int e = 2; e < 16; e += 2) t = fmaxf(fmaxf(t, s[e]), s[e + 1]);
-                        t = max_of_halves(t);
-                        if (__any(t > top + a.slack)) {
-                            t = fmaxf(t, top);
-                            const float f = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - t) * a.scale);
-                            sum *= f;
-#pragma unroll
-                            for (int i = 0; i < S::kDims; ++i) o[i] *= f;
-                            top = t;
-                        }
-                        const float from = top == -INFINITY ? 0.f : -top * a.scale;
-                        uint32_t w[8];
-#pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            float e0 = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale, from)), e1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], a.scale, from));
-                            if constexpr (F8) {
-                                sum += e0 + e1;
-                                e0 = plain || (seen >> (8 * (e >> 2) + (e & 3)) & 1) ? e0 * four(by_v[e >> 2], e & 3) : 0.f;
-                                e1 = plain || (seen >> (8 * (e >> 2) + (e & 3) + 1) & 1) ? e1 * four(by_v[e >> 2], (e & 3) + 1) : 0.f;
-                            }
-                            w[e / 2] = pack_bf16_rne(e0, e1);
-                            if constexpr (!F8) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e / 2]), bf16x2{(__bf16)1.f, (__bf16)1.f}, sum, false);
-                        }
-#pragma unroll
-                        for (int y = 0; y < 2; ++y)
-#pragma unroll
-                            for (int i = 0; i < S::kDims; ++i) {
-                                const int z = (2 * kt + y) ^ (i & 1) << (D == 128 ? 0 : 1);  // (mix_v takes bit 5 of the row)
-                                const bf16x8 v = as_bf16x8(*reinterpret_cast<const uint4 *>(vb + v_off[z] + i * 64 * KEYS));
-                                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(uint4{w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]}), o[i], 0, 0, 0);
-                            }
-                    }
-                }
+                if (busy) take(plain, b, key0, none);
                 __syncthreads();
                 now = then;
                 then = after;
