@@ -227,7 +227,7 @@ extern "C" lora_status_t lora_attention_workspace_bytes(int32_t tokens, int32_t 
 {
     if (!bytes) return fail(LORA_ERR_INVALID_ARG, "bytes is NULL");
     TRY(check_attention(tokens, q_heads, requests, width, cache));
-    *bytes = lora::attend_most_bytes(tokens, q_heads / cache->kv_heads, cache->kv_heads, requests, (int64_t)width * cache->page_size, cache->head_dim);
+    *bytes = lora::attend_most_bytes(tokens, q_heads / cache->kv_heads, cache->kv_heads, requests, (int64_t)width * cache->page_size, cache->head_dim, cache->bits == 8);
     return LORA_OK;
 }
 
@@ -269,7 +269,7 @@ extern "C" lora_status_t lora_attention(const void *q, int64_t q_token, int64_t 
     a.scale = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 0x1p-120f);
     a.flip = scale < 0.f ? 0x80008000u : 0u;
     a.slack = 8.f / a.scale;
-    const lora::AttendForms forms = lora::attend_forms(tokens, a.group, cache->kv_heads, requests, (int64_t)width * cache->page_size, most, cache->head_dim);
+    const lora::AttendForms forms = lora::attend_forms(tokens, a.group, cache->kv_heads, requests, (int64_t)width * cache->page_size, most, cache->head_dim, cache->bits == 8);
     size_t need = 0;
     for (int i = 0; i < forms.n; ++i) {
         const size_t n = lora::attend_parts_bytes(forms.f[i], cache->kv_heads, cache->head_dim);

@@ -40,7 +40,8 @@ hipError_t launch_turn(TurnArgs a, hipStream_t stream);
 
 // ---- attention ------------------------------------------------------------------------------------------------
 // A tile: the columns (row of a request, query head of a key head's group), row by row, that a work group holds at a time.
-constexpr int kFewKeys = 128;    // keys a work group takes in a step, k_attend_few
+constexpr int kFewWaves = 4;                                              // wavefronts of k_attend_few
+constexpr int few_keys(bool bits8) { return (bits8 ? 64 : 32) * kFewWaves; }  // that they take in a step
 
 struct AttendArgs {
     HeadRows q, y;
@@ -86,10 +87,10 @@ inline AttendForm attend_form(int columns, int keys, int work_groups, int64_t to
     return AttendForm{columns, (int)shares, 0, INT32_MAX, steps > 1 && shares > 1};
 }
 
-inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int64_t most_rows, int dim)
+inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int64_t most_rows, int dim, bool bits8)
 {
     const int64_t rows = most_rows > 0 && most_rows < tokens ? most_rows : tokens, columns = rows * group;
-    auto few = [&](int c) { return attend_form(c, kFewKeys, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys); };
+    auto few = [&](int c) { return attend_form(c, few_keys(bits8), 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys); };
     if (columns <= 64) return AttendForms{{few(columns <= 16 ? 16 : columns <= 32 ? 32 : 64), {}}, 1};
     const int c = columns <= 128 ? 128 : 256;
     AttendForm wide = attend_form(c, 8192 / dim, c == 128 ? 2 * kComputeUnits : kComputeUnits, tokens, group, kv_heads, requests, most_keys);
@@ -106,11 +107,11 @@ inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
 }
 
 // bytes that a call may need, whatever `most` says
-inline size_t attend_most_bytes(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int dim)
+inline size_t attend_most_bytes(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int dim, bool bits8)
 {
     size_t most = 0;
     for (int64_t rows : {(int64_t)1, (int64_t)16 / group, (int64_t)32 / group, (int64_t)64 / group, (int64_t)128 / group, (int64_t)0}) {
-        const AttendForms forms = attend_forms(tokens, group, kv_heads, requests, most_keys, rows, dim);
+        const AttendForms forms = attend_forms(tokens, group, kv_heads, requests, most_keys, rows, dim, bits8);
         for (int i = 0; i < forms.n; ++i) {
             const size_t n = attend_parts_bytes(forms.f[i], kv_heads, dim);
             if (n > most) most = n;

@@ -376,7 +376,7 @@ static __device__ __forceinline__ uint32_t share_at(uint32_t total, int share, i
 static __device__ __forceinline__ int64_t part_of(int head, int shares, int share, bool begins) { return ((int64_t)head * shares + share) * 2 + begins; }
 
 // ------------------------------------------------------------------------------------------------
-// Attention of few columns: tiles of 16 C.  A wavefront takes 32 keys at a time, the work group's four 128, each with a running maximum and sum of its own; what
+// Attention of few columns: tiles of 16 C.  A wavefront takes 32 keys (8 bits: twice) at a time, the work group's four as many times that, each with a running maximum and sum of its own; what
 // they have is brought together in LDS at the tile's end.  Nothing goes through LDS on the way: with S^T = K Q^T (16 x 16 x 32 matrix instructions) a lane
 // holds a column's scores of eight keys, and those are what O^T = V^T P^T takes as the operand of eight values of k from that lane, if row m of the score
 // tile t is key 8 (m / 4) + 4 t + m mod 4 and lane (quad, n) brings the keys 8 quad .. 8 quad + 7.  It reads their dims [n D / 16, (n + 1) D / 16): sixteen
@@ -408,6 +408,19 @@ __device__ __forceinline__ Bytes<4> ld_bytes<4>(const char *p)
     return Bytes<4>{{*reinterpret_cast<const uint32_t *>(p)}};
 }
 
+// .. past the caches (see ld16_stream): what one launch reads once
+template <int BYTES>
+static __device__ __forceinline__ Bytes<BYTES> ld_bytes_once(const char *p)
+{
+    typedef __attribute__((ext_vector_type(BYTES / 4))) uint32_t vec;
+    return __builtin_bit_cast(Bytes<BYTES>, __builtin_nontemporal_load(reinterpret_cast<const vec *>(p)));
+}
+template <>
+__device__ __forceinline__ Bytes<4> ld_bytes_once<4>(const char *p)
+{
+    return Bytes<4>{{__builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p))}};
+}
+
 // two E4M3 values, of the low or the high half, as bf16: exact
 template <bool HIGH>
 static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t u)
@@ -415,11 +428,7 @@ static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t u)
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HIGH));
 }
 
-// two bf16: the sign bits of those that are an infinity or NaN
-static __device__ __forceinline__ uint32_t odd16(uint32_t u) { return ((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 
-// .. as zero where `odd` says so
-static __device__ __forceinline__ uint32_t finite_of(uint32_t u, uint32_t odd) { return u & ~((odd - (odd >> 15)) | odd); }
 
 // eight bf16 values with their signs exchanged where `flip` says so
 static __device__ __forceinline__ uint4 flipped(uint4 u, uint32_t flip) { return uint4{u.x ^ flip, u.y ^ flip, u.z ^ flip, u.w ^ flip}; }
@@ -432,11 +441,13 @@ static __device__ __forceinline__ int row_of_column(const AttendArgs &a, int col
     return (int)(i - (i * a.group > (uint32_t)column));
 }
 
-static __device__ __forceinline__ uint4 finite_of(uint4 u, uint32_t &some)
+// Two bf16 or four E4M3 values with zero for each that is an infinity or NaN; `some` is set where one is.
+template <bool F8>
+static __device__ __forceinline__ uint32_t finite_of(uint32_t u, uint32_t &some)
 {
-    const uint32_t x = odd16(u.x), y = odd16(u.y), z = odd16(u.z), w = odd16(u.w);
-    some |= x | y | z | w;
-    return uint4{finite_of(u.x, x), finite_of(u.y, y), finite_of(u.z, z), finite_of(u.w, w)};
+    const uint32_t odd = F8 ? ((u & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u : ((u & 0x7F807F80u) + 0x00800080u) & 0x80008000u;  // their sign bits
+    some |= odd;
+    return u & ~((odd - (odd >> (F8 ? 7 : 15))) | odd);
 }
 
 // A matrix instruction multiplies every column's weight by every value, and nought times an infinity is NaN: among keys that not all columns see, infinities and NaN
@@ -498,6 +509,32 @@ static __device__ __forceinline__ uint32_t seen_of(int key0, int keys, bool tree
     return first_bits(keys - key0) & ((uint32_t)mine | first_bits(-own));
 }
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+// over a lane and the one 32 away
+static __device__ __forceinline__ float max_of_halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+static __device__ __forceinline__ float sum_of_halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// over the four lanes 16 apart
+static __device__ __forceinline__ float max_of_quads(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return max_of_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+static __device__ __forceinline__ float sum_of_quads(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return sum_of_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
 template <int D, bool F8>
 struct FewShape {
     static constexpr int kRowBytes = D * (F8 ? 1 : 2);
@@ -505,17 +542,18 @@ struct FewShape {
     static constexpr int kBytesV = kRowBytes / 16;   // of a key, a lane's
     static constexpr int kSteps = D / 32;            // of k, of the scores
     static constexpr int kTiles = D / 16;            // of v
+    static constexpr int kBlocks = F8 ? 2 : 1;       // of 32 keys a wavefront takes at a time: as many bytes either way
 };
 
 template <int D, bool F8, int C>
-__global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a)
+__global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a)
 {
     using S = FewShape<D, F8>;
-    using W = Dealt<16 * C, kFewKeys>;
-    constexpr int TC = 16 * C;
+    constexpr int TC = 16 * C, WAVES = kFewWaves, KEYS = few_keys(F8);
+    using W = Dealt<TC, KEYS>;
     __shared__ typename W::Found found;
-    __shared__ float2 sums[4][TC];
-    __shared__ float part[4][4 * S::kTiles][64];
+    __shared__ float2 sums[WAVES][TC];
+    __shared__ float part[WAVES][4 * S::kTiles][64];
     __shared__ OddSteps odd;
     if (threadIdx.x == 0) odd.clear(0);
     int turn = 0;
@@ -553,6 +591,7 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
             sees[c] = context + i;
             word[c] = a.tree ? a.tree[row] : 0;
         }
+        const int rows = row_of_column(a, min(columns, c0 + TC) - 1) - row_of_column(a, c0) + 1;  // that the tile is of
         // keys up to here are seen by all
         const int open = min(p.q.keys, a.tree ? context : context + row_of_column(a, c0) + 1);
 
@@ -566,51 +605,58 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
             for (int i = 0; i < S::kTiles; ++i) o[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        Bytes<16> k[2][S::kLoadsK];
-        Bytes<S::kBytesV> v[8];
-        float4 ks[2], vs[2];
-        // the two pages of a wavefront's 32 keys at step j, -1 where there is none
+        constexpr int B = S::kBlocks;
+        Bytes<16> k[B][2][S::kLoadsK];
+        Bytes<S::kBytesV> v[B][8];
+        float4 ks[B][2], vs[B][2];
+        // the pages of a wavefront's keys at step j, 16 by 16; -1 where there is none
         struct Pages {
-            int id[2];
+            int id[2 * B];
         };
         const int32_t *table = a.table + p.r * a.ld_table;
         auto pages_of = [&](uint32_t j) __attribute__((always_inline)) {
             Pages g;
-            const int key = (int)j * kFewKeys + 32 * wave;
+            const int key = (int)j * KEYS + 32 * B * wave;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < 2 * B; ++i) {
                 const int at = key + 16 * i;
                 const int id = at < p.q.keys ? table[at >> a.cache.page_shift] : -1;
                 g.id[i] = (unsigned)id < (unsigned)a.cache.pages ? id : -1;
             }
             return g;
         };
-        auto base_of = [&](const Pages &g, uint32_t j, int half) __attribute__((always_inline)) {
-            const int64_t in = ((int64_t)j * kFewKeys + 32 * wave + 16 * half) & (page - 1);
-            return ((int64_t)max(g.id[half], 0) * a.cache.kv_heads + kh) * page + in;  // in rows
+        auto base_of = [&](const Pages &g, uint32_t j, int i) __attribute__((always_inline)) {
+            const int in = ((int)j * KEYS + 32 * B * wave + 16 * i) & (page - 1);
+            return ((int64_t)max(g.id[i], 0) * a.cache.kv_heads + kh) * page + in;  // in rows
         };
         auto load_k = [&](const Pages &g, uint32_t j) __attribute__((always_inline)) {
-            const int64_t r0 = base_of(g, j, 0), r1 = base_of(g, j, 1);
-            const char *at = a.cache.k + (n < 8 ? r0 : r1) * S::kRowBytes + k_in;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int y = 0; y < B; ++y) {
+                const int64_t r0 = base_of(g, j, 2 * y), r1 = base_of(g, j, 2 * y + 1);
+                const char *at = a.cache.k + (n < 8 ? r0 : r1) * S::kRowBytes + k_in;
 #pragma unroll
-                for (int s = 0; s < S::kLoadsK; ++s) k[t][s] = ld_bytes<16>(at + t * 4 * S::kRowBytes + s * 64);
-            if constexpr (F8) {
-                const float *sc = a.cache.k_scales + (quad < 2 ? r0 : r1) + 8 * (quad & 1);
-                ks[0] = *reinterpret_cast<const float4 *>(sc);
-                ks[1] = *reinterpret_cast<const float4 *>(sc + 4);
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int s = 0; s < S::kLoadsK; ++s) k[y][t][s] = ld_bytes_once<16>(at + t * 4 * S::kRowBytes + s * 64);
+                if constexpr (F8) {
+                    const float *sc = a.cache.k_scales + (quad < 2 ? r0 : r1) + 8 * (quad & 1);
+                    ks[y][0] = *reinterpret_cast<const float4 *>(sc);
+                    ks[y][1] = *reinterpret_cast<const float4 *>(sc + 4);
+                }
             }
         };
         auto load_v = [&](const Pages &g, uint32_t j) __attribute__((always_inline)) {
-            const int64_t r0 = base_of(g, j, 0), r1 = base_of(g, j, 1), r = quad < 2 ? r0 : r1;
-            const char *at = a.cache.v + r * S::kRowBytes + v_in;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = ld_bytes<S::kBytesV>(at + i * S::kRowBytes);
-            if constexpr (F8) {
-                const float *sc = a.cache.v_scales + r + 8 * (quad & 1);
-                vs[0] = *reinterpret_cast<const float4 *>(sc);
-                vs[1] = *reinterpret_cast<const float4 *>(sc + 4);
+            for (int y = 0; y < B; ++y) {
+                const int64_t r0 = base_of(g, j, 2 * y), r1 = base_of(g, j, 2 * y + 1), r = quad < 2 ? r0 : r1;
+                const char *at = a.cache.v + r * S::kRowBytes + v_in;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[y][i] = ld_bytes_once<S::kBytesV>(at + i * S::kRowBytes);
+                if constexpr (F8) {
+                    const float *sc = a.cache.v_scales + r + 8 * (quad & 1);
+                    vs[y][0] = *reinterpret_cast<const float4 *>(sc);
+                    vs[y][1] = *reinterpret_cast<const float4 *>(sc + 4);
+                }
             }
         };
         auto four = [](const float4 &f, int i) __attribute__((always_inline)) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; };
@@ -622,129 +668,154 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
             for (uint32_t j = p.at; j < to; ++j) {
                 const uint32_t j1 = j + 1 < to ? j + 1 : j, j2 = j + 2 < to ? j + 2 : j1;
                 const Pages after = pages_of(j2);
+                const int key0 = (int)j * KEYS + 32 * B * wave, mine = key0 + 8 * quad;
+                bool plain = key0 + 32 * B <= open;
+#pragma unroll
+                for (int i = 0; i < 2 * B; ++i) plain &= now.id[i] >= 0;
                 // scores
-                f32x4 sc[C][2];
+                f32x4 sc[C][B][2];
 #pragma unroll
                 for (int c = 0; c < C; ++c)
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) sc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int y = 0; y < B; ++y) sc[c][y][0] = sc[c][y][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s = 0; s < S::kSteps; ++s)
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        bf16x8 x;
-                        if constexpr (F8) {
-                            const uint32_t w0 = k[t][s >> 1].w[2 * (s & 1)], w1 = k[t][s >> 1].w[2 * (s & 1) + 1];
-                            x = as_bf16x8(uint4{two_of_e4m3<false>(w0), two_of_e4m3<true>(w0), two_of_e4m3<false>(w1), two_of_e4m3<true>(w1)});
-                        } else {
-                            x = __builtin_bit_cast(bf16x8, k[t][s]);
+                    for (int y = 0; y < B; ++y)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            bf16x8 x;
+                            if constexpr (F8) {
+                                const uint32_t w0 = k[y][t][s >> 1].w[2 * (s & 1)], w1 = k[y][t][s >> 1].w[2 * (s & 1) + 1];
+                                x = as_bf16x8(uint4{two_of_e4m3<false>(w0), two_of_e4m3<true>(w0), two_of_e4m3<false>(w1), two_of_e4m3<true>(w1)});
+                            } else {
+                                x = __builtin_bit_cast(bf16x8, k[y][t][s]);
+                            }
+#pragma unroll
+                            for (int c = 0; c < C; ++c) sc[c][y][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[c][s], sc[c][y][t], 0, 0, 0);
                         }
+                if constexpr (F8) {
 #pragma unroll
-                        for (int c = 0; c < C; ++c) sc[c][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[c][s], sc[c][t], 0, 0, 0);
-                    }
-                const int key0 = (int)j * kFewKeys + 32 * wave, mine = key0 + 8 * quad;
-                [[maybe_unused]] float4 kn[2] = {ks[0], ks[1]};
+                    for (int c = 0; c < C; ++c)
+#pragma unroll
+                        for (int y = 0; y < B; ++y)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) sc[c][y][i >> 2][i & 3] *= four(ks[y][i >> 2], i & 3);
+                }
                 load_k(then, j1);
-                const bool plain = now.id[0] >= 0 && now.id[1] >= 0 && key0 + 32 <= open;
-                uint32_t seen[C];
-                const bool held = now.id[quad >> 1] >= 0;
+                uint32_t seen[C][B];
+                if (!plain) {
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    seen[c] = 0xFFu;
+                    for (int y = 0; y < B; ++y) {
+                        const bool held = now.id[2 * y + (quad >> 1)] >= 0;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
+                        for (int c = 0; c < C; ++c) {
+                            seen[c][y] = seen_of(mine + 32 * y, held ? p.q.keys : 0, a.tree, sees[c], word[c], mine + 32 * y - context);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sc[c][t][i] *= F8 ? a.scale * four(kn[t], i) : a.scale;
-                    if (!plain) {
-                        seen[c] = seen_of(mine, held ? p.q.keys : 0, a.tree, sees[c], word[c], mine - context);
+                            for (int i = 0; i < 8; ++i) sc[c][y][i >> 2][i & 3] = seen[c][y] >> i & 1 ? sc[c][y][i >> 2][i & 3] : -INFINITY;
+                        }
+                        // values of keys that there are none of are taken as zero, and (see OddSteps) infinities and NaN where the columns differ in what they see
+                        const uint32_t there = first_bits(held ? p.q.keys - (mine + 32 * y) : 0);
+                        uint32_t some = 0;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) sc[c][i >> 2][i & 3] = seen[c] >> i & 1 ? sc[c][i >> 2][i & 3] : -INFINITY;
+                        for (int i = 0; i < 8; ++i)
+#pragma unroll
+                            for (int x = 0; x < S::kBytesV / 4; ++x) {
+                                v[y][i].w[x] &= 0u - (there >> i & 1);
+                                if (rows > 1) v[y][i].w[x] = finite_of<F8>(v[y][i].w[x], some);
+                            }
+                        if (some) odd.note(turn, j);
                     }
                 }
                 // weights
-                uint4 w[C];
+                uint4 w[C][B];
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
-                    float t = fmaxf(fmaxf(fmaxf(sc[c][0][0], sc[c][0][1]), fmaxf(sc[c][0][2], sc[c][0][3])),
-                                    fmaxf(fmaxf(sc[c][1][0], sc[c][1][1]), fmaxf(sc[c][1][2], sc[c][1][3])));
-                    t = fmaxf(t, __shfl_xor(t, 16, 64));
-                    t = fmaxf(t, __shfl_xor(t, 32, 64));
-                    t = fmaxf(t, top[c]);
-                    if (__any(t > top[c])) {
-                        const float f = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top[c] - t);
+                    float t = sc[c][0][0][0];
+#pragma unroll
+                    for (int i = 1; i < 8 * B; ++i) t = fmaxf(t, sc[c][i >> 3][i >> 2 & 1][i & 3]);
+                    t = max_of_quads(t);
+                    if (__any(t > top[c] + a.slack)) {
+                        t = fmaxf(t, top[c]);
+                        const float f = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top[c] - t) * a.scale);
                         sum[c] *= f;
 #pragma unroll
                         for (int i = 0; i < S::kTiles; ++i) o[c][i] *= f;
                         top[c] = t;
                     }
-                    const float from = t == -INFINITY ? 0.f : t;
-                    float e[8];
+                    const float from = top[c] == -INFINITY ? 0.f : -top[c] * a.scale;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        e[i] = __builtin_amdgcn_exp2f(sc[c][i >> 2][i & 3] - from);
-                        sum[c] += e[i];
-                        if constexpr (F8) e[i] = plain || (seen[c] >> i & 1) ? e[i] * four(vs[i >> 2], i & 3) : 0.f;
+                    for (int y = 0; y < B; ++y) {
+                        uint32_t pairs[4];
+#pragma unroll
+                        for (int i = 0; i < 8; i += 2) {
+                            float e0 = __builtin_amdgcn_exp2f(fmaf(sc[c][y][i >> 2][i & 3], a.scale, from));
+                            float e1 = __builtin_amdgcn_exp2f(fmaf(sc[c][y][i >> 2][(i & 3) + 1], a.scale, from));
+                            if constexpr (F8) {
+                                sum[c] += e0 + e1;
+                                e0 *= four(vs[y][i >> 2], i & 3);
+                                e1 *= four(vs[y][i >> 2], (i & 3) + 1);
+                            }
+                            pairs[i / 2] = pack_bf16_rne(e0, e1);
+                            if constexpr (!F8) sum[c] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pairs[i / 2]), bf16x2{(__bf16)1.f, (__bf16)1.f}, sum[c], false);
+                        }
+                        if (F8 && !plain) {  // (nought times a scale that is none is none)
+#pragma unroll
+                            for (int i = 0; i < 8; i += 2) {
+                                const uint32_t two = seen[c][y] >> i;
+                                pairs[i / 2] &= ((0u - (two & 1)) & 0xFFFFu) | ((0u - (two >> 1 & 1)) & 0xFFFF0000u);
+                            }
+                        }
+                        w[c][y] = uint4{pairs[0], pairs[1], pairs[2], pairs[3]};
                     }
-                    w[c] = uint4{pack_bf16_rne(e[0], e[1]), pack_bf16_rne(e[2], e[3]), pack_bf16_rne(e[4], e[5]), pack_bf16_rne(e[6], e[7])};
                 }
                 // values
-                if (!plain) {
-                    const uint32_t there = first_bits(held ? p.q.keys - mine : 0);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                for (int y = 0; y < B; ++y) {
+                    auto add = [&](int i, uint4 vt) __attribute__((always_inline)) {
 #pragma unroll
-                        for (int x = 0; x < S::kBytesV / 4; ++x) v[i].w[x] &= 0u - (there >> i & 1);
-                }
-                uint4 vt[S::kTiles];
-                if constexpr (F8) {
+                        for (int c = 0; c < C; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt), as_bf16x8(w[c][y]), o[c][i], 0, 0, 0);
+                    };
+                    if constexpr (F8) {
 #pragma unroll
-                    for (int x = 0; x < S::kBytesV / 4; ++x) {
-                        uint32_t four_keys[2][4];
+                        for (int x = 0; x < S::kBytesV / 4; ++x) {
+                            uint32_t four_keys[2][4];
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const uint32_t v0 = v[4 * y].w[x], v1 = v[4 * y + 1].w[x], v2 = v[4 * y + 2].w[x], v3 = v[4 * y + 3].w[x];
-                            const uint32_t l01 = __builtin_amdgcn_perm(v1, v0, 0x05010400u), l23 = __builtin_amdgcn_perm(v3, v2, 0x05010400u);
-                            const uint32_t h01 = __builtin_amdgcn_perm(v1, v0, 0x07030602u), h23 = __builtin_amdgcn_perm(v3, v2, 0x07030602u);
-                            four_keys[y][0] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
-                            four_keys[y][1] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
-                            four_keys[y][2] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
-                            four_keys[y][3] = __builtin_amdgcn_perm(h23, h01, 0x07060302u);
+                            for (int z = 0; z < 2; ++z) {
+                                const uint32_t v0 = v[y][4 * z].w[x], v1 = v[y][4 * z + 1].w[x], v2 = v[y][4 * z + 2].w[x], v3 = v[y][4 * z + 3].w[x];
+                                const uint32_t l01 = __builtin_amdgcn_perm(v1, v0, 0x05010400u), l23 = __builtin_amdgcn_perm(v3, v2, 0x05010400u);
+                                const uint32_t h01 = __builtin_amdgcn_perm(v1, v0, 0x07030602u), h23 = __builtin_amdgcn_perm(v3, v2, 0x07030602u);
+                                four_keys[z][0] = __builtin_amdgcn_perm(l23, l01, 0x05040100u);
+                                four_keys[z][1] = __builtin_amdgcn_perm(l23, l01, 0x07060302u);
+                                four_keys[z][2] = __builtin_amdgcn_perm(h23, h01, 0x05040100u);
+                                four_keys[z][3] = __builtin_amdgcn_perm(h23, h01, 0x07060302u);
+                            }
+#pragma unroll
+                            for (int b = 0; b < 4; ++b)
+                                add(4 * x + b, uint4{two_of_e4m3<false>(four_keys[0][b]), two_of_e4m3<true>(four_keys[0][b]), two_of_e4m3<false>(four_keys[1][b]),
+                                                     two_of_e4m3<true>(four_keys[1][b])});
                         }
+                    } else {
 #pragma unroll
-                        for (int b = 0; b < 4; ++b)
-                            vt[4 * x + b] = uint4{two_of_e4m3<false>(four_keys[0][b]), two_of_e4m3<true>(four_keys[0][b]), two_of_e4m3<false>(four_keys[1][b]),
-                                                  two_of_e4m3<true>(four_keys[1][b])};
-                    }
-                } else {
+                        for (int i = 0; i < S::kTiles; ++i) {
+                            uint32_t d[4];
 #pragma unroll
-                    for (int i = 0; i < S::kTiles; ++i) {
-                        uint32_t d[4];
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) d[y] = __builtin_amdgcn_perm(v[2 * y + 1].w[i >> 1], v[2 * y].w[i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
-                        vt[i] = uint4{d[0], d[1], d[2], d[3]};
+                            for (int z = 0; z < 4; ++z) d[z] = __builtin_amdgcn_perm(v[y][2 * z + 1].w[i >> 1], v[y][2 * z].w[i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
+                            add(i, uint4{d[0], d[1], d[2], d[3]});
+                        }
                     }
                 }
                 load_v(then, j1);
-                if (!plain) {
-                    uint32_t some = 0;
-#pragma unroll
-                    for (int i = 0; i < S::kTiles; ++i) vt[i] = finite_of(vt[i], some);
-                    if (some) odd.note(turn, j);
-                }
-#pragma unroll
-                for (int i = 0; i < S::kTiles; ++i)
-#pragma unroll
-                    for (int c = 0; c < C; ++c) o[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt[i]), as_bf16x8(w[c]), o[c][i], 0, 0, 0);
                 now = then;
                 then = after;
             }
         }
 
-        // the four wavefronts' sums: each on the largest of their maxima, then one quarter of a column's dims a wavefront
+        // the wavefronts' sums: each on the largest of their maxima, then a quarter of a column's dims a wavefront
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            sum[c] += __shfl_xor(sum[c], 16, 64);
-            sum[c] += __shfl_xor(sum[c], 32, 64);
+            sum[c] = sum_of_quads(sum[c]);
+            top[c] *= a.scale;
             if (quad == 0) sums[wave][16 * c + n] = float2{top[c], sum[c]};
         }
         __syncthreads();
@@ -754,10 +825,10 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
         for (int c = 0; c < C; ++c) {
             float most = -INFINITY, all = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, sums[i][16 * c + n].x);
+            for (int i = 0; i < WAVES; ++i) most = fmaxf(most, sums[i][16 * c + n].x);
             const float from = most == -INFINITY ? 0.f : most, f = __builtin_amdgcn_exp2f(top[c] - from);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) all += sums[i][16 * c + n].y * __builtin_amdgcn_exp2f(sums[i][16 * c + n].x - from);
+            for (int i = 0; i < WAVES; ++i) all += sums[i][16 * c + n].y * __builtin_amdgcn_exp2f(sums[i][16 * c + n].x - from);
             if (c > 0) __syncthreads();
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -767,14 +838,14 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
             const int in = 16 * c + n, col = c0 + in;
             if (col < columns) {
                 float z[S::kTiles];
+                const int dim = S::kTiles * (4 * quad + wave);
 #pragma unroll
                 for (int i = 0; i < S::kTiles; ++i) {
                     const int at = wave * S::kTiles + i;
                     z[i] = part[0][at][lane] + part[1][at][lane] + part[2][at][lane] + part[3][at][lane];
                 }
-                const int dim = S::kTiles * (4 * quad + wave);
                 if (whole) {
-                    const float by = all == 0.f ? 0.f : 1.f / all;
+                    const float by = all == 0.f ? 0.f : __builtin_amdgcn_rcpf(all);
                     const int i = row_of_column(a, col), row = p.q.first + i, h = kh * a.group + (col - i * a.group);
                     uint32_t *y = reinterpret_cast<uint32_t *>(a.y.p + row * a.y.token + h * a.y.head + dim);
 #pragma unroll
@@ -789,7 +860,7 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
         }
         if (tid == 0) odd.clear(turn ^ 1);
         __syncthreads();
-        if (odd.to[turn]) add_odd<D, F8, 256>(a, p, kh, odd.from[turn] * kFewKeys, odd.to[turn] * kFewKeys, c0, TC, whole, a.parts + slot * TC * D);
+        if (odd.to[turn]) add_odd<D, F8, 256>(a, p, kh, odd.from[turn] * KEYS, odd.to[turn] * KEYS, c0, TC, whole, a.parts + slot * TC * D);
         turn ^= 1;
         left -= to - p.at;
         if (left == 0 || !W::next(a, p)) return;
@@ -805,19 +876,6 @@ __global__ __launch_bounds__(256, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a
 // of eight lanes meet in a bank.
 // ------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(16))) float f32x16;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-
-// over a lane and the one 32 away
-static __device__ __forceinline__ float max_of_halves(float v)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-static __device__ __forceinline__ float sum_of_halves(float v)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 
 template <int D, bool F8, int WAVES>
 struct WideShape {
@@ -954,10 +1012,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                 const int group = v_kg >> 1, first = key0 + 16 * group + 4 * (v_kg & 1);
                 if (!plain) {
                     const uint32_t there = first_bits(__shfl(ids, group, 64) >= 0 ? p.q.keys - first : 0);
+                    uint32_t some = 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int x = 0; x < S::kWordsV; ++x) held[S::kWordsV * i + x] &= 0u - (there >> (i < 4 ? i : i + 4) & 1);
+                        for (int x = 0; x < S::kWordsV; ++x)
+                            held[S::kWordsV * i + x] = finite_of<F8>(held[S::kWordsV * i + x] & (0u - (there >> (i < 4 ? i : i + 4) & 1)), some);
+                    if (some) odd.note(turn, j);
                 }
                 uint4 turned[S::kDimsV];
                 if constexpr (F8) {
@@ -988,12 +1049,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                             d[y] = __builtin_amdgcn_perm(held[S::kWordsV * (2 * y + 1) + (c >> 1)], held[S::kWordsV * 2 * y + (c >> 1)], c & 1 ? 0x07060302u : 0x05040100u);
                         turned[c] = uint4{d[0], d[1], d[2], d[3]};
                     }
-                }
-                if (!plain) {
-                    uint32_t some = 0;
-#pragma unroll
-                    for (int c = 0; c < S::kDimsV; ++c) turned[c] = finite_of(turned[c], some);
-                    if (some) odd.note(turn, j);
                 }
 #pragma unroll
                 for (int c = 0; c < S::kDimsV; ++c) *reinterpret_cast<uint4 *>(vs[b] + S::v_at(v_dims + c, v_kg)) = turned[c];
@@ -1171,7 +1226,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
         const float all = sum_of_halves(sum);
         if (col < columns) {
             if (whole) {
-                const float by = all == 0.f ? 0.f : 1.f / all;
+                const float by = all == 0.f ? 0.f : __builtin_amdgcn_rcpf(all);
                 const int i = row_of_column(a, col), row = p.q.first + i, hd = kh * a.group + (col - i * a.group);
                 uint16_t *y = a.y.p + row * a.y.token + hd * a.y.head + 4 * h;
 #pragma unroll
@@ -1273,7 +1328,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
         }
     }
     if (in0 + c >= columns) return;
-    const float by = all == 0.f ? 0.f : 1.f / all;
+    const float by = all == 0.f ? 0.f : __builtin_amdgcn_rcpf(all);
     const int col = p.t * TC + in0 + c, i = row_of_column(a, col), row = p.q.first + i, h = kh * a.group + (col - i * a.group);
     uint32_t *y = reinterpret_cast<uint32_t *>(a.y.p + row * a.y.token + h * a.y.head + dim);
 #pragma unroll
@@ -1295,9 +1350,9 @@ static hipError_t launch_join(const AttendArgs &a, hipStream_t stream)
 template <int D, bool F8, int C>
 static hipError_t launch_few(const AttendArgs &a, bool joins, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * kFewWaves), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
-    return launch_join<D, 16 * C, kFewKeys>(a, stream);
+    return launch_join<D, 16 * C, few_keys(F8)>(a, stream);
 }
 
 template <int D, bool F8, int WAVES>
