@@ -262,7 +262,7 @@ extern "C" lora_status_t lora_attention(const void *q, int64_t q_token, int64_t 
     a.table = page_table;
     a.ld_table = ld_table;
     a.requests = requests;
-    a.width = width;
+    a.room = width * cache->page_size;
     a.tree = tree;
     a.cache = cache_of(cache);
     // (nought times the -infinity of a key that is not seen would be NaN; times 2^-120 scores do not matter either)

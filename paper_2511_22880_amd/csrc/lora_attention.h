@@ -49,7 +49,7 @@ struct AttendArgs {
     uint32_t per_group;           // 2^32 / group, rounded up (0 for 1): the upper half of a number's product with it is the quotient or one more
     const int32_t *starts, *lengths, *table;
     int64_t ld_table;
-    int requests, width;
+    int requests, room;           // room: slots of a row of the table
     const uint64_t *tree;
     PagedCache cache;
     float scale;                  // its magnitude times log2 e, never zero

@@ -213,12 +213,23 @@ struct Request {
     int first, n, keys;  // first row, rows, keys
 };
 
+// What a work group needs before it has anything else to ask for: arguments in front of the struct, which arrive in registers.  The others are in memory, five lines of 64
+// bytes, and would be asked for one after the other as they are used, a trip to memory each (one token over 1500 keys: 17.3 us a call so, see lines_of).
+#define ATTEND_LIST const int32_t *__restrict__ starts, const int32_t *__restrict__ lengths, int requests, int tokens, int room, int group, int shares, int kv_heads
+#define ATTEND_LIST_OF(a) (a).starts, (a).lengths, (a).requests, (a).tokens, (a).room, (a).group, (a).shares, (a).cache.kv_heads
+#define ATTEND_LIST_TO(a) \
+    (a).starts = starts, (a).lengths = lengths, (a).requests = requests, (a).tokens = tokens, (a).room = room, (a).group = group, (a).shares = shares, (a).cache.kv_heads = kv_heads
+
+// asks for all lines of the arguments at once
+static __device__ __forceinline__ void lines_of(const AttendArgs &a)
+{
+    asm volatile("" ::"s"(a.q.p), "s"(a.table), "s"(a.cache.k), "s"(a.cache.pages), "s"(a.least), "s"(a.parts) : "memory");
+}
+
 static __device__ __forceinline__ Request request_at(const AttendArgs &a, int r)
 {
     const int s0 = min(max(a.starts[r], 0), a.tokens), s1 = min(max(a.starts[r + 1], 0), a.tokens);
-    const int64_t room = (int64_t)a.width << a.cache.page_shift;
-    const int64_t keys = a.lengths[r];
-    return Request{s0, max(s1 - s0, 0), (int)(keys < 0 ? 0 : keys < room ? keys : room)};
+    return Request{s0, max(s1 - s0, 0), min(max(a.lengths[r], 0), a.room)};
 }
 
 // sum of floor((a i + b) / m) for i < n: the part that whole multiples of m give, then the same question with the axes exchanged
@@ -298,8 +309,10 @@ struct Dealt {
         const int each = (a.requests + THREADS - 1) / THREADS, r0 = tid * each, r1 = min(a.requests, r0 + each);
         Request q{0, 0, 0};
         uint32_t mine = 0, n = 0;  // (steps of this thread's requests; of the last of them)
+        if (r0 < r1) q = request_at(a, r0);
+        lines_of(a);
         for (int r = r0; r < r1; ++r) {
-            q = request_at(a, r);
+            if (r > r0) q = request_at(a, r);
             mine += n = all(a, tiles(a, q));
         }
         uint32_t upto = mine;
@@ -546,8 +559,9 @@ struct FewShape {
 };
 
 template <int D, bool F8, int C>
-__global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a)
+__global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(ATTEND_LIST, AttendArgs a)
 {
+    ATTEND_LIST_TO(a);
     using S = FewShape<D, F8>;
     constexpr int TC = 16 * C, WAVES = kFewWaves, KEYS = few_keys(F8);
     using W = Dealt<TC, KEYS>;
@@ -707,7 +721,7 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
                 if (!plain) {
 #pragma unroll
                     for (int y = 0; y < B; ++y) {
-                        const bool held = now.id[2 * y + (quad >> 1)] >= 0;
+                        const bool held = (quad < 2 ? now.id[2 * y] : now.id[2 * y + 1]) >= 0;  // (an index by lane would put them into memory)
 #pragma unroll
                         for (int c = 0; c < C; ++c) {
                             seen[c][y] = seen_of(mine + 32 * y, held ? p.q.keys : 0, a.tree, sees[c], word[c], mine + 32 * y - context);
@@ -901,8 +915,9 @@ struct WideShape {
 };
 
 template <int D, bool F8, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(ATTEND_LIST, AttendArgs a)
 {
+    ATTEND_LIST_TO(a);
     using S = WideShape<D, F8, WAVES>;
     constexpr int TC = 32 * WAVES, KEYS = S::kKeys;
     using W = Dealt<TC, KEYS>;
@@ -1258,8 +1273,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
 // Tiles that several shares have a part of: a work group has CW columns of the tile that the first step of share s + 1 lies in, if that tile begins in share s.
 // 16 / CW groups of threads share the parts, four of which a thread asks for at a time.
 template <int D, int TC, int KEYS, int CW>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
+__global__ __launch_bounds__(256) void k_attend_join(ATTEND_LIST, AttendArgs a)
 {
+    ATTEND_LIST_TO(a);
     using W = Dealt<TC, KEYS>;
     constexpr int kEach = D / 16, kGroups = 16 / CW;
     __shared__ typename W::Found found;
@@ -1341,16 +1357,16 @@ static hipError_t launch_join(const AttendArgs &a, hipStream_t stream)
     const unsigned ends = (unsigned)(a.shares - 1) * a.cache.kv_heads;
     // few requests among many shares: a tile has many parts
     if (TC <= 64 && 4 * a.requests < a.shares)
-        hipLaunchKernelGGL((k_attend_join<D, TC, KEYS, 4>), dim3(ends, TC / 4), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((k_attend_join<D, TC, KEYS, 4>), dim3(ends, TC / 4), dim3(256), 0, stream, ATTEND_LIST_OF(a), a);
     else
-        hipLaunchKernelGGL((k_attend_join<D, TC, KEYS, 16>), dim3(ends, TC / 16), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((k_attend_join<D, TC, KEYS, 16>), dim3(ends, TC / 16), dim3(256), 0, stream, ATTEND_LIST_OF(a), a);
     return hipGetLastError();
 }
 
 template <int D, bool F8, int C>
 static hipError_t launch_few(const AttendArgs &a, bool joins, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * kFewWaves), 0, stream, a);
+    hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * kFewWaves), 0, stream, ATTEND_LIST_OF(a), a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
     return launch_join<D, 16 * C, few_keys(F8)>(a, stream);
 }
@@ -1358,7 +1374,7 @@ static hipError_t launch_few(const AttendArgs &a, bool joins, hipStream_t stream
 template <int D, bool F8, int WAVES>
 static hipError_t launch_wide(const AttendArgs &a, bool joins, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_attend_wide<D, F8, WAVES>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * WAVES), 0, stream, a);
+    hipLaunchKernelGGL((k_attend_wide<D, F8, WAVES>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * WAVES), 0, stream, ATTEND_LIST_OF(a), a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
     return launch_join<D, 32 * WAVES, WideShape<D, F8, WAVES>::kKeys>(a, stream);
 }
