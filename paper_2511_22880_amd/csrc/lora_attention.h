@@ -57,6 +57,7 @@ struct AttendArgs {
     float slack;                  // by how much a score may pass the maximum that weights are relative to: 8 / scale
     int least, most;              // columns of the requests that this launch takes: least < rows * group <= most
     int shares;                   // of a key head's work
+    bool cut;                     // shares are of steps, and tiles cut where those end; else every tile is a share
     float *parts;                 // workspace: [kv_heads * shares][2][columns][dim], then sums [..][2][columns][2]
 };
 
@@ -65,7 +66,7 @@ struct AttendForm {
     int columns;       // of a tile
     int shares;        // of a key head's work
     int least, most;
-    bool joins;        // some tile may be cut
+    bool cut;          // tiles may be cut (see AttendArgs)
 };
 struct AttendForms {
     AttendForm f[2];
@@ -78,22 +79,23 @@ inline int64_t most_tiles(int64_t tokens, int group, int requests, int columns)
     return all / columns + (requests < tokens ? requests : tokens);
 }
 
-inline AttendForm attend_form(int columns, int keys, int work_groups, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys)
+inline AttendForm attend_form(int columns, int keys, int whole_steps, int work_groups, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys)
 {
-    const int64_t steps = (most_keys + keys - 1) / keys, work = most_tiles(tokens, group, requests, columns) * (steps ? steps : 1);
+    const int64_t steps = (most_keys + keys - 1) / keys, tiles = most_tiles(tokens, group, requests, columns);
     int64_t shares = work_groups / kv_heads;
     if (shares < 1) shares = 1;
-    if (shares > work) shares = work;
-    return AttendForm{columns, (int)shares, 0, INT32_MAX, steps > 1 && shares > 1};
+    if (shares > tiles * steps) shares = tiles * steps;
+    if (steps <= whole_steps || shares <= 1) return AttendForm{columns, (int)tiles, 0, INT32_MAX, false};
+    return AttendForm{columns, (int)shares, 0, INT32_MAX, true};
 }
 
 inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int64_t most_rows, int dim, bool bits8)
 {
     const int64_t rows = most_rows > 0 && most_rows < tokens ? most_rows : tokens, columns = rows * group;
-    auto few = [&](int c) { return attend_form(c, few_keys(bits8), 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys); };
-    if (columns <= 64) return AttendForms{{few(columns <= 16 ? 16 : columns <= 32 ? 32 : 64), {}}, 1};
+    auto few = [&](int c) { return attend_form(c, few_keys(bits8), 4, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys); };
+    if (columns <= 32) return AttendForms{{few(columns <= 16 ? 16 : 32), {}}, 1};
     const int c = columns <= 128 ? 128 : 256;
-    AttendForm wide = attend_form(c, 8192 / dim, c == 128 ? 2 * kComputeUnits : kComputeUnits, tokens, group, kv_heads, requests, most_keys);
+    AttendForm wide = attend_form(c, 8192 / dim, 16, c == 128 ? 2 * kComputeUnits : kComputeUnits, tokens, group, kv_heads, requests, most_keys);
     if (requests == 1 || group > 16 || tokens > requests * rows / 2) return AttendForms{{wide, {}}, 1};
     AttendForm narrow = few(16);
     narrow.most = 16;
@@ -103,14 +105,14 @@ inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int req
 
 inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
 {
-    return f.joins ? (size_t)kv_heads * f.shares * 2 * f.columns * (dim + 2) * sizeof(float) : 0;
+    return f.cut ? (size_t)kv_heads * f.shares * 2 * f.columns * (dim + 2) * sizeof(float) : 0;
 }
 
 // bytes that a call may need, whatever `most` says
 inline size_t attend_most_bytes(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int dim, bool bits8)
 {
     size_t most = 0;
-    for (int64_t rows : {(int64_t)1, (int64_t)16 / group, (int64_t)32 / group, (int64_t)64 / group, (int64_t)128 / group, (int64_t)0}) {
+    for (int64_t rows : {(int64_t)1, (int64_t)16 / group, (int64_t)32 / group, (int64_t)128 / group, (int64_t)0}) {
         const AttendForms forms = attend_forms(tokens, group, kv_heads, requests, most_keys, rows, dim, bits8);
         for (int i = 0; i < forms.n; ++i) {
             const size_t n = attend_parts_bytes(forms.f[i], kv_heads, dim);

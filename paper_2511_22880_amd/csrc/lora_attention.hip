@@ -206,7 +206,7 @@ hipError_t launch_turn(TurnArgs a, hipStream_t stream)
 // How the work of an attention call is dealt out.  A request's columns (row by row, the query heads of a key head's group side by side) are cut into tiles of
 // TC; a tile takes as many steps of KEYS keys as its last row sees, one at least.  The steps of all tiles of all requests, in that order, are one list for every key
 // head, and a head's `shares` work groups take equal runs of it.  A run that has all of a tile's steps writes its rows; otherwise it leaves sums, which
-// k_attend_join brings together.  The list follows from starts and lengths on the device alone: every work group adds up the requests' steps and finds
+// k_attend_join brings together.  Where no tile has many steps (see attend_form) none is cut, and every tile has a work group.  The list follows from starts and lengths on the device alone: every work group adds up the requests' steps and finds
 // its place in it, so the host need not know any length, and a captured call follows them.
 // ------------------------------------------------------------------------------------------------
 struct Request {
@@ -285,7 +285,11 @@ struct Dealt {
         const uint32_t m = (uint32_t)a.group * KEYS;
         return s.level || (int)t == s.n - 1 ? s.last : s.whole + (s.part + t * TC + m - 1) / m;
     }
-    static __device__ __forceinline__ uint32_t all(const AttendArgs &a, const Tiles &s) { return s.n == 0 ? 0u : (s.n == 1 ? 0u : before(a, s, s.n - 1)) + s.last; }
+    // of a request: its steps, or its tiles where those are not cut
+    static __device__ __forceinline__ uint32_t all(const AttendArgs &a, const Tiles &s)
+    {
+        return s.n == 0 || !a.cut ? (uint32_t)s.n : (s.n == 1 ? 0u : before(a, s, s.n - 1)) + s.last;
+    }
 
     // a place in the list
     struct Place {
@@ -348,6 +352,12 @@ struct Dealt {
         const uint32_t at = __builtin_amdgcn_readfirstlane(f.at);
         p.q = Request{__builtin_amdgcn_readfirstlane(f.q.first), __builtin_amdgcn_readfirstlane(f.q.n), __builtin_amdgcn_readfirstlane(f.q.keys)};
         p.s = tiles(a, p.q);
+        if (!a.cut) {
+            p.t = (int)at;
+            p.at = 0;
+            p.of = steps(a, p.s, p.t);
+            return true;
+        }
         // the last tile that begins at or before it, 64 at a time
         int lo = 0, hi = p.s.n - 1;
         while (hi > lo) {
@@ -576,10 +586,12 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
     typename W::Place p;
     uint32_t left = 0;
     if (!W::template find<256>(a, found, [&](uint32_t total) {
+            if (!a.cut) return (uint32_t)share;
             const uint32_t from = share_at(total, share, a.shares);
             left = share_at(total, share + 1, a.shares) - from;
             return from;
         }, p)) return;
+    if (!a.cut) left = p.of;
 
     const int page = 1 << a.cache.page_shift;
     // a lane's keys of a step, and where their bytes are in 16 of them
@@ -932,10 +944,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(ATTEND_LIST, Atte
     typename W::Place p;
     uint32_t left = 0;
     if (!W::template find<64 * WAVES>(a, found, [&](uint32_t total) {
+            if (!a.cut) return (uint32_t)share;
             const uint32_t from = share_at(total, share, a.shares);
             left = share_at(total, share + 1, a.shares) - from;
             return from;
         }, p)) return;
+    if (!a.cut) left = p.of;
     const int page = 1 << a.cache.page_shift;
     const bool loads_v = wave < WAVES / 2;
     // V: 8 keys and kDimsV dims of a thread.  K: its row and piece within a load
@@ -1218,7 +1232,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(ATTEND_LIST, Atte
             int now = page_of(p.at), then = page_of(p.at + 1 < to ? p.at + 1 : p.at);
             fetch(now, p.at);
             stage(now, p.at, 0);
-            fetch(then, p.at + 1 < to ? p.at + 1 : p.at);
+            if (p.at + 1 < to) fetch(then, p.at + 1);
             __syncthreads();
             for (uint32_t j = p.at; j < to; ++j) {
                 const int b = (j - p.at) & 1;
@@ -1227,8 +1241,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(ATTEND_LIST, Atte
                 const int key0 = (int)j * KEYS;
                 const uint64_t none = __ballot(now < 0);
                 const bool plain = none == 0 && key0 + KEYS <= open;
-                stage(then, j1, b ^ 1);
-                fetch(after, j2);
+                if (j + 1 < to) stage(then, j1, b ^ 1);
+                if (j + 2 < to) fetch(after, j2);
                 if (busy) take(plain, b, key0, none);
                 __syncthreads();
                 now = then;
@@ -1364,34 +1378,34 @@ static hipError_t launch_join(const AttendArgs &a, hipStream_t stream)
 }
 
 template <int D, bool F8, int C>
-static hipError_t launch_few(const AttendArgs &a, bool joins, hipStream_t stream)
+static hipError_t launch_few(const AttendArgs &a, hipStream_t stream)
 {
     hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * kFewWaves), 0, stream, ATTEND_LIST_OF(a), a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut) return e;
     return launch_join<D, 16 * C, few_keys(F8)>(a, stream);
 }
 
 template <int D, bool F8, int WAVES>
-static hipError_t launch_wide(const AttendArgs &a, bool joins, hipStream_t stream)
+static hipError_t launch_wide(const AttendArgs &a, hipStream_t stream)
 {
     hipLaunchKernelGGL((k_attend_wide<D, F8, WAVES>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * WAVES), 0, stream, ATTEND_LIST_OF(a), a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || !joins) return e;
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut) return e;
     return launch_join<D, 32 * WAVES, WideShape<D, F8, WAVES>::kKeys>(a, stream);
 }
 
 hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t stream)
 {
     a.shares = f.shares;
+    a.cut = f.cut;
     a.least = f.least;
     a.most = f.most;
     auto by_columns = [&](auto dim, auto f8) {
         constexpr int D = decltype(dim)::value;
         constexpr bool F8 = decltype(f8)::value;
-        return f.columns == 16    ? launch_few<D, F8, 1>(a, f.joins, stream)
-               : f.columns == 32  ? launch_few<D, F8, 2>(a, f.joins, stream)
-               : f.columns == 64  ? launch_few<D, F8, 4>(a, f.joins, stream)
-               : f.columns == 128 ? launch_wide<D, F8, 4>(a, f.joins, stream)
-                                  : launch_wide<D, F8, 8>(a, f.joins, stream);
+        return f.columns == 16    ? launch_few<D, F8, 1>(a, stream)
+               : f.columns == 32  ? launch_few<D, F8, 2>(a, stream)
+               : f.columns == 128 ? launch_wide<D, F8, 4>(a, stream)
+                                  : launch_wide<D, F8, 8>(a, stream);
     };
     auto by_bits = [&](auto dim) { return a.cache.bits8 ? by_columns(dim, std::true_type{}) : by_columns(dim, std::false_type{}); };
     return a.cache.dim == 64 ? by_bits(std::integral_constant<int, 64>{}) : by_bits(std::integral_constant<int, 128>{});
