@@ -141,6 +141,13 @@ extern "C" lora_status_t lora_rotary_turns(int32_t dims, double base, int32_t sc
     return LORA_OK;
 }
 
+static lora_status_t launch_turn(const lora::TurnArgs &a, void *stream, const char *what)
+{
+    const hipError_t e = lora::launch_turn(a, (hipStream_t)stream);
+    if (e == hipErrorInvalidConfiguration) return fail(LORA_ERR_SHAPE, "%s: %d tokens x %d heads are more rows than a launch can have", what, a.tokens, a.heads);
+    return of_hip(e, what);
+}
+
 extern "C" lora_status_t lora_rotary(const void *x, int64_t x_token, int64_t x_head, int32_t tokens, int32_t heads, int32_t head_dim,
                                      const int32_t *positions, const lora_rotary_t *rotary, int32_t inverse, void *y, int64_t y_token, int64_t y_head,
                                      void *stream)
@@ -165,7 +172,7 @@ extern "C" lora_status_t lora_rotary(const void *x, int64_t x_token, int64_t x_h
     a.positions = positions;
     a.inverse = inverse != 0;
     set_rotary(a, rotary);
-    return of_hip(lora::launch_turn(a, (hipStream_t)stream), "lora_rotary");
+    return launch_turn(a, stream, "lora_rotary");
 }
 
 extern "C" lora_status_t lora_cache_append(const void *k, int64_t k_token, int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
@@ -203,7 +210,7 @@ extern "C" lora_status_t lora_cache_append(const void *k, int64_t k_token, int64
     a.slots = slots;
     if (rotary) set_rotary(a, rotary);
     a.cache = cache_of(cache);
-    return of_hip(lora::launch_turn(a, (hipStream_t)stream), "lora_cache_append");
+    return launch_turn(a, stream, "lora_cache_append");
 }
 
 static lora_status_t check_attention(int32_t tokens, int32_t q_heads, int32_t requests, int32_t width, const lora_cache_t *cache)

@@ -84,8 +84,9 @@ inline AttendForm attend_form(int columns, int keys, int whole_steps, int work_g
     const int64_t steps = (most_keys + keys - 1) / keys, tiles = most_tiles(tokens, group, requests, columns);
     int64_t shares = work_groups / kv_heads;
     if (shares < 1) shares = 1;
-    if (shares > tiles * steps) shares = tiles * steps;
-    if (steps <= whole_steps || shares <= 1) return AttendForm{columns, (int)tiles, 0, INT32_MAX, false};
+    if (shares > tiles * steps) shares = tiles * steps > 0 ? tiles * steps : 1;
+    // (a launch has fewer than 2^32 threads, of 512 at most a work group)
+    if (steps <= whole_steps && tiles * kv_heads < (int64_t)1 << 22) return AttendForm{columns, (int)tiles, 0, INT32_MAX, false};
     return AttendForm{columns, (int)shares, 0, INT32_MAX, true};
 }
 
@@ -105,7 +106,7 @@ inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int req
 
 inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
 {
-    return f.cut ? (size_t)kv_heads * f.shares * 2 * f.columns * (dim + 2) * sizeof(float) : 0;
+    return f.cut && f.shares > 1 ? (size_t)kv_heads * f.shares * 2 * f.columns * (dim + 2) * sizeof(float) : 0;
 }
 
 // bytes that a call may need, whatever `most` says

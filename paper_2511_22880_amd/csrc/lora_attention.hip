@@ -186,6 +186,7 @@ static hipError_t launch_turn_kind(TurnArgs a, hipStream_t stream)
     int passes = 1;
     while (passes < 4 && all > (int64_t)8 * kComputeUnits * passes * at_once && room(2 * passes) <= 32768) passes *= 2;
     a.rows = passes * at_once;
+    if ((all + a.rows - 1) / a.rows > (int64_t)UINT32_MAX / kTurnThreads) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)((all + a.rows - 1) / a.rows)), threads(kTurnThreads);
     if (passes == 1)
         hipLaunchKernelGGL((k_turn<KIND, 1>), grid, threads, room(1), stream, a);
@@ -1381,7 +1382,7 @@ template <int D, bool F8, int C>
 static hipError_t launch_few(const AttendArgs &a, hipStream_t stream)
 {
     hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * kFewWaves), 0, stream, ATTEND_LIST_OF(a), a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut) return e;
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut || a.shares == 1) return e;
     return launch_join<D, 16 * C, few_keys(F8)>(a, stream);
 }
 
@@ -1389,7 +1390,7 @@ template <int D, bool F8, int WAVES>
 static hipError_t launch_wide(const AttendArgs &a, hipStream_t stream)
 {
     hipLaunchKernelGGL((k_attend_wide<D, F8, WAVES>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * WAVES), 0, stream, ATTEND_LIST_OF(a), a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut) return e;
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut || a.shares == 1) return e;
     return launch_join<D, 32 * WAVES, WideShape<D, F8, WAVES>::kKeys>(a, stream);
 }
 

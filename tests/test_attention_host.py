@@ -46,13 +46,15 @@ CASES += [("lora_cache_append", APPEND, c, s) for c, s in [
     (dict(k=None), "INVALID_ARG"), (dict(v=P + 2), "INVALID_ARG"), (dict(kt=250), "INVALID_ARG"), (dict(vh=32), "INVALID_ARG"), (dict(tokens=-3), "INVALID_ARG"),
     (dict(slots=None), "INVALID_ARG"), (dict(positions=None), "INVALID_ARG"), (dict(rotary=None), "INVALID_ARG"), (dict(rotary=rotary(dims=128)), "SHAPE"),
     (dict(q=P + 1), "INVALID_ARG"), (dict(heads=0), "SHAPE"), (dict(y=None), "INVALID_ARG"), (dict(yt=192), "INVALID_ARG"), (dict(y=P, yh=128, yt=512), "INVALID_ARG"),
-    (dict(tokens=1 << 28, heads=8, qt=512, yt=512), "SHAPE")]]
+    (dict(tokens=1 << 28, heads=8, qt=512, yt=512), "SHAPE"),
+    (dict(tokens=(1 << 30) - 1, cache=cache(heads=1), q=None, kt=0, vt=0), "SHAPE")]]  # (2^31 rows, 128 a work group: more threads than a launch has)
 CASES += [("lora_attention", ATTEND, c, s) for c, s in [
     (dict(q=None), "INVALID_ARG"), (dict(qt=100), "INVALID_ARG"), (dict(tokens=-1), "INVALID_ARG"), (dict(heads=3), "SHAPE"), (dict(heads=0), "SHAPE"),
     (dict(starts=None), "INVALID_ARG"), (dict(lengths=P + 3), "INVALID_ARG"), (dict(requests=-1), "INVALID_ARG"), (dict(table=None), "INVALID_ARG"),
     (dict(ld=9), "INVALID_ARG"), (dict(width=-1), "INVALID_ARG"), (dict(width=1 << 27, ld=1 << 27), "SHAPE"), (dict(tree=P + 4), "INVALID_ARG"), (dict(most=-1), "INVALID_ARG"),
     (dict(scale=math.inf), "INVALID_ARG"), (dict(scale=math.nan), "INVALID_ARG"), (dict(y=None), "INVALID_ARG"), (dict(y=P), "INVALID_ARG"),
-    (dict(yt=128), "INVALID_ARG"), (dict(work=None), "WORKSPACE"), (dict(work=P + 4), "WORKSPACE"), (dict(nwork=100), "WORKSPACE"),
+    (dict(yt=128), "INVALID_ARG"), (dict(width=1000, ld=1000, work=None), "WORKSPACE"), (dict(width=1000, ld=1000, work=P + 4), "WORKSPACE"),
+    (dict(width=1000, ld=1000, nwork=100), "WORKSPACE"),
     (dict(tokens=1 << 22, requests=1 << 22, width=1 << 17, ld=1 << 17), "SHAPE")]]
 for name, base in (("lora_cache_append", APPEND), ("lora_attention", ATTEND)):
     CASES += [(name, base, dict(cache=c), s) for c, s in [
