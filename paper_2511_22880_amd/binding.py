@@ -1016,7 +1016,7 @@ def _here(device: int, stream) -> None:
     global _current_device
     if _current_device is None:
         import torch
-        _current_device = torch.cuda.current_device
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (the latter asks first whether torch is at work there)
     if device < 0:
         raise ValueError("a tensor on the CPU does not do: ones on the GPU are meant")
     at = _current_device()
@@ -1024,73 +1024,119 @@ def _here(device: int, stream) -> None:
         raise ValueError(f"tensors on device {device}, stream {stream}: the current device is {at}")
 
 
-def _heads(name: str, t, device: int):
-    """Shape and strides of bf16 [tokens][heads][dim] on that device."""
+def _heads(name: str, t, device: int) -> None:
+    """Refuses a tensor that is not bf16 [tokens][heads][dim] on that device, a head's elements side by side."""
+    if not _BF16:
+        _know_types()
     if t.dtype not in _BF16:
-        if not _BF16:
-            _know_types()
-        if t.dtype not in _BF16:
-            raise ValueError(f"{name}: {t.dtype} does not do: {_names(_BF16)} is meant")
+        raise ValueError(f"{name}: {t.dtype} does not do: {_names(_BF16)} is meant")
     if t.dim() != 3 or t.get_device() != device:
         raise ValueError(f"{name}: {tuple(t.shape)} on {t.device} does not do: [tokens][heads][dim] on the other tensors' GPU is meant")
-    (n, h, d), (s0, s1, s2) = t.shape, t.stride()
-    if s2 != 1 and d > 1:
+    if t.stride(2) != 1 and t.shape[2] > 1:
         raise ValueError(f"{name}: strides {t.stride()} do not do: a head's elements lie side by side")
-    # (of a dimension of one torch states any stride)
-    return n, h, d, s0 if n > 1 else h * d, s1 if h > 1 else d
 
 
-def _ints(name: str, t, n: int, device: int) -> int:
-    if t.dtype not in _INT32 or t.numel() < n or not t.is_contiguous() or t.get_device() != device:
-        _whole(name, t, n, _INT32)
+def _three(t, name: str):
+    """Shape and strides of a tensor of heads."""
+    if t.dim() != 3:
+        raise ValueError(f"{name}: {tuple(t.shape)} does not do: [tokens][heads][dim] is meant")
+    return t.shape, t.stride()
+
+
+def _ints(name: str, t, n: int, device: int) -> None:
+    _whole(name, t, n, _INT32)
+    if t.get_device() != device:
         raise ValueError(f"{name}: on another device than the other tensors")
-    return t.data_ptr()
 
 
+# (these calls too ask their tensors in line, and look closer where anything is unusual; of a dimension of one torch states any stride)
 def lora_rotary(x, positions, rotary: Rotary, y=None, inverse: bool = False, stream=None) -> None:
     """x, y: bf16 [tokens][heads][dim] (y None: x, in place); positions: int32 [tokens]; inverse: the gradient's way."""
-    device = x.get_device()
-    n, heads, dim, st, sh = _heads("x", x, device)
     if y is None:
-        py, yt, yh = x.data_ptr(), st, sh
-    else:
-        yn, yheads, ydim, yt, yh = _heads("y", y, device)
-        if (yn, yheads, ydim) != (n, heads, dim):
-            raise ValueError(f"y: {tuple(y.shape)} does not do: {tuple(x.shape)} is meant")
-        py = y.data_ptr()
+        y = x
+    try:
+        (n, heads, dim), (xt, xh, x1) = x.shape, x.stride()
+        (yn, yheads, ydim), (yt, yh, y1) = y.shape, y.stride()
+    except ValueError:
+        (n, heads, dim), (xt, xh, x1), (yn, yheads, ydim), (yt, yh, y1) = _three(x, "x") + _three(y, "y")
+    device = x.get_device()
+    if x1 != 1 or x.dtype not in _BF16:
+        _heads("x", x, device)
+    if y1 != 1 or y.dtype not in _BF16 or y.get_device() != device:
+        _heads("y", y, device)
+    if yn != n or yheads != heads or ydim != dim:
+        raise ValueError(f"y: {tuple(y.shape)} does not do: {tuple(x.shape)} is meant")
+    if positions.dtype not in _INT32 or positions.numel() < n or not positions.is_contiguous() or positions.get_device() != device:
+        _ints("positions", positions, n, device)
     _here(device, stream)
     if rotary.device != device:
         raise ValueError("rotary: on another device than x")
-    status = (_lib or lib()).lora_rotary(x.data_ptr(), st, sh, n, heads, dim, _ints("positions", positions, n, device), rotary.address, 1 if inverse else 0,
-                                         py, yt, yh, None if stream is None else _queue(stream))
+    if heads == 1:
+        xh = yh = dim
+    if n == 1:
+        xt, yt = heads * xh, heads * yh
+    status = (_lib or lib()).lora_rotary(x.data_ptr(), xt, xh, n, heads, dim, positions.data_ptr(), rotary.address, 1 if inverse else 0, y.data_ptr(), yt, yh,
+                                         None if stream is None else _queue(stream))
     if status:
         _check(status)
 
 
 def lora_cache_append(k, v, slots, cache: Cache, rotary: Optional[Rotary] = None, positions=None, q=None, y=None, stream=None) -> None:
     """k, v: bf16 [tokens][kv_heads][dim]; slots, positions: int32 [tokens]; q: bf16 [tokens][q_heads][dim], turned into y (None: q, in place)."""
+    try:
+        (n, heads, dim), (kt, kh, k1) = k.shape, k.stride()
+        (vn, vheads, vdim), (vt, vh, v1) = v.shape, v.stride()
+    except ValueError:
+        (n, heads, dim), (kt, kh, k1), (vn, vheads, vdim), (vt, vh, v1) = _three(k, "k") + _three(v, "v")
     device = k.get_device()
-    n, heads, dim, kt, kh = _heads("k", k, device)
-    vn, vheads, vdim, vt, vh = _heads("v", v, device)
-    if (heads, dim, vn, vheads, vdim) != (cache.kv_heads, cache.head_dim, n, cache.kv_heads, cache.head_dim):
+    if k1 != 1 or k.dtype not in _BF16:
+        _heads("k", k, device)
+    if v1 != 1 or v.dtype not in _BF16 or v.get_device() != device:
+        _heads("v", v, device)
+    if heads != cache.kv_heads or dim != cache.head_dim or vn != n or vheads != heads or vdim != dim:
         raise ValueError(f"k, v: {tuple(k.shape)} and {tuple(v.shape)} do not do: tokens x {cache.kv_heads} x {cache.head_dim} is meant")
-    pq = py = None
+    if heads == 1:
+        kh = vh = dim
+    if n == 1:
+        kt, vt = heads * kh, heads * vh
+    pq = py = pp = pr = None
     qt = qh = q_heads = yt = yh = 0
     if q is not None:
-        qn, q_heads, qdim, qt, qh = _heads("q", q, device)
-        yn, yheads, ydim, yt, yh = (qn, q_heads, qdim, qt, qh) if y is None else _heads("y", y, device)
-        if (qn, qdim, yn, yheads, ydim) != (n, dim, n, q_heads, dim):
-            raise ValueError(f"q, y: {tuple(q.shape)} and {tuple((q if y is None else y).shape)} do not do: {n} tokens of heads of {dim}, alike, are meant")
-        pq, py = q.data_ptr(), (q if y is None else y).data_ptr()
+        if y is None:
+            y = q
+        try:
+            (qn, q_heads, qdim), (qt, qh, q1) = q.shape, q.stride()
+            (yn, yheads, ydim), (yt, yh, y1) = y.shape, y.stride()
+        except ValueError:
+            (qn, q_heads, qdim), (qt, qh, q1), (yn, yheads, ydim), (yt, yh, y1) = _three(q, "q") + _three(y, "y")
+        if q1 != 1 or q.dtype not in _BF16 or q.get_device() != device:
+            _heads("q", q, device)
+        if y1 != 1 or y.dtype not in _BF16 or y.get_device() != device:
+            _heads("y", y, device)
+        if qn != n or qdim != dim or yn != n or yheads != q_heads or ydim != dim:
+            raise ValueError(f"q, y: {tuple(q.shape)} and {tuple(y.shape)} do not do: {n} tokens of heads of {dim}, alike, are meant")
+        if q_heads == 1:
+            qh = yh = dim
+        if n == 1:
+            qt, yt = q_heads * qh, q_heads * yh
+        pq, py = q.data_ptr(), y.data_ptr()
     elif y is not None:
         raise ValueError("y: without q there is nothing for it")
+    if slots.dtype not in _INT32 or slots.numel() < n or not slots.is_contiguous() or slots.get_device() != device:
+        _ints("slots", slots, n, device)
+    if positions is not None:
+        if positions.dtype not in _INT32 or positions.numel() < n or not positions.is_contiguous() or positions.get_device() != device:
+            _ints("positions", positions, n, device)
+        pp = positions.data_ptr()
+    if rotary is not None:
+        if rotary.device != device:
+            raise ValueError("rotary: on another device than k")
+        pr = rotary.address
     _here(device, stream)
-    if cache.device != device or (rotary is not None and rotary.device != device):
-        raise ValueError("cache, rotary: on another device than k")
-    status = (_lib or lib()).lora_cache_append(k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, n, _ints("slots", slots, n, device),
-                                               None if positions is None else _ints("positions", positions, n, device),
-                                               None if rotary is None else rotary.address, cache.address, pq, qt, qh, q_heads, py, yt, yh,
-                                               None if stream is None else _queue(stream))
+    if cache.device != device:
+        raise ValueError("cache: on another device than k")
+    status = (_lib or lib()).lora_cache_append(k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, n, slots.data_ptr(), pp, pr, cache.address, pq, qt, qh, q_heads, py, yt,
+                                               yh, None if stream is None else _queue(stream))
     if status:
         _check(status)
 
@@ -1105,21 +1151,35 @@ def lora_attention(q, starts, lengths, page_table, cache: Cache, y, workspace=No
                    stream=None) -> None:
     """q, y: bf16 [tokens][q_heads][dim]; starts [requests + 1], lengths [requests], page_table [requests][width]: int32; tree: int64 [tokens], one
     word of 64 bits a row (None: rows see their request's own keys up to themselves); scale None: 1 / sqrt(dim); most: the most rows of a request, 0 if unknown."""
+    try:
+        (n, heads, dim), (qt, qh, q1) = q.shape, q.stride()
+        (yn, yheads, ydim), (yt, yh, y1) = y.shape, y.stride()
+        (rows, width), (ld, t1) = page_table.shape, page_table.stride()
+    except ValueError:
+        (n, heads, dim), (qt, qh, q1), (yn, yheads, ydim), (yt, yh, y1), (rows, width), (ld, t1) = _three(q, "q") + _three(y, "y") + _two(page_table, "page_table")
     device = q.get_device()
-    n, heads, dim, qt, qh = _heads("q", q, device)
-    yn, yheads, ydim, yt, yh = _heads("y", y, device)
-    if (dim, yn, yheads, ydim) != (cache.head_dim, n, heads, dim):
+    if q1 != 1 or q.dtype not in _BF16:
+        _heads("q", q, device)
+    if y1 != 1 or y.dtype not in _BF16 or y.get_device() != device:
+        _heads("y", y, device)
+    if dim != cache.head_dim or yn != n or yheads != heads or ydim != dim:
         raise ValueError(f"q, y: {tuple(q.shape)} and {tuple(y.shape)} do not do: alike, of heads of {cache.head_dim}, is meant")
+    if heads == 1:
+        qh = yh = dim
+    if n == 1:
+        qt, yt = heads * qh, heads * yh
     requests = lengths.numel()
-    if page_table.dim() != 2 or page_table.dtype not in _INT32 or page_table.shape[0] < requests or page_table.get_device() != device:
-        raise ValueError(f"page_table: {tuple(page_table.shape)} of {page_table.dtype} on {page_table.device} does not do: int32 [{requests}][width] is meant")
-    width, (ld, t1) = page_table.shape[1], page_table.stride()
-    if t1 != 1 and width > 1:
-        raise ValueError(f"page_table: strides {page_table.stride()} do not do: a request's pages lie side by side")
-    if requests <= 1 or ld < width:
-        if requests > 1 and width:
-            raise ValueError(f"page_table: strides {page_table.stride()} do not do: rows overlap")
+    if page_table.dtype not in _INT32 or rows < requests or page_table.get_device() != device or (t1 != 1 and width > 1):
+        _usable("page_table", page_table, requests, width, _INT32)
+        raise ValueError("page_table: on another device than q")
+    if requests <= 1 or width == 0:
         ld = width
+    elif ld < width:
+        raise ValueError(f"page_table: strides {page_table.stride()} do not do: rows overlap")
+    if starts.dtype not in _INT32 or starts.numel() <= requests or not starts.is_contiguous() or starts.get_device() != device:
+        _ints("starts", starts, requests + 1, device)
+    if lengths.dtype not in _INT32 or not lengths.is_contiguous() or lengths.get_device() != device:
+        _ints("lengths", lengths, requests, device)
     pt = None
     if tree is not None:
         if tree.element_size() != 8 or tree.is_floating_point() or tree.numel() < n or not tree.is_contiguous() or tree.get_device() != device:
@@ -1134,9 +1194,8 @@ def lora_attention(q, starts, lengths, page_table, cache: Cache, y, workspace=No
     _here(device, stream)
     if cache.device != device:
         raise ValueError("cache: on another device than q")
-    status = (_lib or lib()).lora_attention(q.data_ptr(), qt, qh, n, heads, _ints("starts", starts, requests + 1, device),
-                                            _ints("lengths", lengths, requests, device), requests, page_table.data_ptr(), ld, width, pt, most, cache.address,
-                                            dim ** -0.5 if scale is None else scale, y.data_ptr(), yt, yh, pw, nw,
+    status = (_lib or lib()).lora_attention(q.data_ptr(), qt, qh, n, heads, starts.data_ptr(), lengths.data_ptr(), requests, page_table.data_ptr(), ld, width, pt,
+                                            most, cache.address, dim ** -0.5 if scale is None else scale, y.data_ptr(), yt, yh, pw, nw,
                                             None if stream is None else _queue(stream))
     if status:
         _check(status)

@@ -33,10 +33,9 @@ struct TurnArgs {
     float magnitude;
     int inverse, interleaved;
     PagedCache cache;
-    int rows;                 // (token, head) pairs of a work group (set by the launcher)
 };
 
-hipError_t launch_turn(TurnArgs a, hipStream_t stream);
+hipError_t launch_turn(const TurnArgs &a, hipStream_t stream);
 
 // ---- attention ------------------------------------------------------------------------------------------------
 // A tile: the columns (row of a request, query head of a key head's group), row by row, that a work group holds at a time.

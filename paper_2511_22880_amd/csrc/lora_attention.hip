@@ -12,7 +12,7 @@ static __device__ __forceinline__ float value_hi(uint32_t u) { return __uint_as_
 
 // ------------------------------------------------------------------------------------------------
 // Rows turned by their positions.  A row is (token, head), heads counted over q, k and v; a thread has 16 elements of one, two pieces of 8: eight pairs that
-// are turned (half layout: the pieces are dims / 2 apart), or elements that pass.  A work group has `rows` consecutive rows; it asks for all of them, computes the
+// are turned (half layout: the pieces are dims / 2 apart), or elements that pass.  A work group has as many consecutive rows as its threads hold; it asks for all of them, computes the
 // cosines and sines of its few tokens once into LDS (a pair's angle for all heads at once: 64 angles a token, not 64 a head), and turns.  The angle is the low
 // 64 bits of position * turns, of which the upper 32 count: exact to 2^-31 turns at any position, without a division or a table of positions.
 // ------------------------------------------------------------------------------------------------
@@ -62,54 +62,46 @@ static __device__ __forceinline__ void store_held(char *row, float *scale_at, co
     }
 }
 
-// KIND 0: q alone; 1: with a cache in bf16; 2: in 8 bits.  PASSES: rows of a thread.
-template <int KIND, int PASSES>
+// KIND 0: q alone; 1: with a cache in bf16; 2: in 8 bits.
+template <int KIND>
 __global__ __launch_bounds__(kTurnThreads) void k_turn(TurnArgs a)
 {
     extern __shared__ float2 turned[];  // [tokens here][pairs]: cosine and sine, times the magnitude
     const int tid = threadIdx.x, units = a.dim >> 4, at_once = kTurnThreads / units;
     const int r0 = tid / units, u = tid - r0 * units;
-    const uint32_t first = blockIdx.x * (uint32_t)a.rows;
+    const uint32_t first = blockIdx.x * (uint32_t)at_once;
     const int t_first = (int)(first / (uint32_t)a.heads), h_first = (int)(first - (uint32_t)t_first * a.heads);
     auto over_heads = [&](int flat) __attribute__((always_inline)) { return a.per_heads ? (int)__umulhi((uint32_t)flat, a.per_heads) : flat; };
 
-    uint4 lo[PASSES], hi[PASSES];
-    int token[PASSES], head[PASSES], slot[PASSES];
-    bool there[PASSES], turns[PASSES];
-#pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-        const int flat = h_first + r0 + i * at_once, t = over_heads(flat);
-        head[i] = flat - t * a.heads;
-        token[i] = t_first + t;
-        there[i] = token[i] < a.tokens && r0 < at_once;
-        const int tok = there[i] ? token[i] : 0;
-        const bool is_q = head[i] < a.q_heads, is_k = !is_q && (KIND == 0 || head[i] < a.q_heads + a.cache.kv_heads);
-        slot[i] = 0;
-        if constexpr (KIND > 0) {
-            slot[i] = a.slots[tok];
-            there[i] &= (uint32_t)slot[i] < (uint32_t)a.cache.pages << a.cache.page_shift;
-        }
-        if (a.positions) there[i] &= a.positions[tok] >= 0;
-        turns[i] = a.turns && (KIND == 0 || is_q || is_k) && u < a.dims >> 4;
+    const int t = over_heads(h_first + r0), head = h_first + r0 - t * a.heads, token = t_first + t;
+    const bool is_q = head < a.q_heads, is_k = !is_q && (KIND == 0 || head < a.q_heads + a.cache.kv_heads);
+    bool there = token < a.tokens && r0 < at_once;
+    const int tok = there ? token : 0;
+    int slot = 0;
+    if constexpr (KIND > 0) {
+        slot = a.slots[tok];
+        there &= (uint32_t)slot < (uint32_t)a.cache.pages << a.cache.page_shift;
+    }
+    if (a.positions) there &= a.positions[tok] >= 0;
+    const bool turns = a.turns && (KIND == 0 || is_q || is_k) && u < a.dims >> 4, apart = turns && !a.interleaved;
+    const int d0 = apart ? 8 * u : 16 * u, d1 = apart ? 8 * u + (a.dims >> 1) : 16 * u + 8;
+    uint4 lo, hi;
+    if (there) {
         HeadRows from = a.q;
-        int h = head[i];
+        int h = head;
         if constexpr (KIND > 0) {
             from = is_q ? a.q : is_k ? a.k : a.v;
             h = is_q ? h : is_k ? h - a.q_heads : h - a.q_heads - a.cache.kv_heads;
         }
-        const bool apart = turns[i] && !a.interleaved;
-        const int d0 = apart ? 8 * u : 16 * u, d1 = apart ? 8 * u + (a.dims >> 1) : 16 * u + 8;
-        if (there[i]) {
-            const uint16_t *row = from.p + tok * from.token + h * from.head;
-            lo[i] = ld16(row + d0);
-            hi[i] = ld16(row + d1);
-        }
+        const uint16_t *row = from.p + tok * from.token + h * from.head;
+        lo = ld16(row + d0);
+        hi = ld16(row + d1);
     }
     if (a.turns) {
-        const int pairs = a.dims >> 1, n = (over_heads(h_first + at_once * PASSES - 1) + 1) * pairs;
+        const int pairs = a.dims >> 1, n = (over_heads(h_first + at_once - 1) + 1) * pairs;
         for (int e = tid; e < n; e += kTurnThreads) {
-            const int t = e / pairs, p = e - t * pairs, tok = t_first + t < a.tokens ? t_first + t : 0;
-            const uint64_t all = (uint64_t)(uint32_t)a.positions[tok] * a.turns[p];
+            const int te = e / pairs, p = e - te * pairs, at = t_first + te < a.tokens ? t_first + te : 0;
+            const uint64_t all = (uint64_t)(uint32_t)a.positions[at] * a.turns[p];
             // quarters of a turn apart, what is left within an eighth either way: as a float it is off by 2^-28 turns at most
             const uint32_t turn = (uint32_t)(all >> 32), quarter = (turn + 0x20000000u) >> 30;
             float s, c;
@@ -127,80 +119,58 @@ __global__ __launch_bounds__(kTurnThreads) void k_turn(TurnArgs a)
         }
         __syncthreads();
     }
+    if (!there) return;
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    float x[8], z[8];
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-        if (!there[i]) continue;
-        const uint32_t w[8] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w, hi[i].x, hi[i].y, hi[i].z, hi[i].w};
-        float x[8], z[8];
+    for (int j = 0; j < 4; ++j) {
+        x[2 * j] = value_lo(w[j]);
+        x[2 * j + 1] = value_hi(w[j]);
+        z[2 * j] = value_lo(w[4 + j]);
+        z[2 * j + 1] = value_hi(w[4 + j]);
+    }
+    if (turns) {
+        const float2 *cs = turned + t * (a.dims >> 1) + 8 * u;
+        if (a.interleaved) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x[2 * j] = value_lo(w[j]);
-            x[2 * j + 1] = value_hi(w[j]);
-            z[2 * j] = value_lo(w[4 + j]);
-            z[2 * j + 1] = value_hi(w[4 + j]);
-        }
-        const bool apart = turns[i] && !a.interleaved;
-        const int d0 = apart ? 8 * u : 16 * u, d1 = apart ? 8 * u + (a.dims >> 1) : 16 * u + 8;
-        if (turns[i]) {
-            const float2 *cs = turned + (token[i] - t_first) * (a.dims >> 1) + 8 * u;
-            if (a.interleaved) {
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = cs[j], g = cs[4 + j];
+                const float x0 = x[2 * j], x1 = x[2 * j + 1], z0 = z[2 * j], z1 = z[2 * j + 1];
+                x[2 * j] = x0 * f.x - x1 * f.y;
+                x[2 * j + 1] = x0 * f.y + x1 * f.x;
+                z[2 * j] = z0 * g.x - z1 * g.y;
+                z[2 * j + 1] = z0 * g.y + z1 * g.x;
+            }
+        } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = cs[j], g = cs[4 + j];
-                    const float x0 = x[2 * j], x1 = x[2 * j + 1], z0 = z[2 * j], z1 = z[2 * j + 1];
-                    x[2 * j] = x0 * f.x - x1 * f.y;
-                    x[2 * j + 1] = x0 * f.y + x1 * f.x;
-                    z[2 * j] = z0 * g.x - z1 * g.y;
-                    z[2 * j + 1] = z0 * g.y + z1 * g.x;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float2 f = cs[j];
-                    const float x0 = x[j], z0 = z[j];
-                    x[j] = x0 * f.x - z0 * f.y;
-                    z[j] = x0 * f.y + z0 * f.x;
-                }
+            for (int j = 0; j < 8; ++j) {
+                const float2 f = cs[j];
+                const float x0 = x[j], z0 = z[j];
+                x[j] = x0 * f.x - z0 * f.y;
+                z[j] = x0 * f.y + z0 * f.x;
             }
         }
-        if (KIND == 0 || head[i] < a.q_heads) {
-            store_held<false>(reinterpret_cast<char *>(a.y.p + token[i] * a.y.token + head[i] * a.y.head), nullptr, x, z, d0, d1, units, false);
-        } else if constexpr (KIND > 0) {
-            const int h = head[i] - a.q_heads;
-            const bool is_k = h < a.cache.kv_heads;
-            const int kh = is_k ? h : h - a.cache.kv_heads, page = slot[i] >> a.cache.page_shift;
-            const int64_t at = (((int64_t)page * a.cache.kv_heads + kh) << a.cache.page_shift) + (slot[i] & ((1 << a.cache.page_shift) - 1));
-            store_held<KIND == 2>((is_k ? a.cache.k : a.cache.v) + at * a.dim * (KIND == 2 ? 1 : 2), (is_k ? a.cache.k_scales : a.cache.v_scales) + at, x, z, d0, d1,
-                                  units, u == 0);
-        }
+    }
+    if (KIND == 0 || is_q) {
+        store_held<false>(reinterpret_cast<char *>(a.y.p + token * a.y.token + head * a.y.head), nullptr, x, z, d0, d1, units, false);
+    } else if constexpr (KIND > 0) {
+        const int kh = head - a.q_heads - (is_k ? 0 : a.cache.kv_heads), page = slot >> a.cache.page_shift;
+        const int64_t at = (((int64_t)page * a.cache.kv_heads + kh) << a.cache.page_shift) + (slot & ((1 << a.cache.page_shift) - 1));
+        store_held<KIND == 2>((is_k ? a.cache.k : a.cache.v) + at * a.dim * (KIND == 2 ? 1 : 2), (is_k ? a.cache.k_scales : a.cache.v_scales) + at, x, z, d0, d1, units,
+                              u == 0);
     }
 }
 
-template <int KIND>
-static hipError_t launch_turn_kind(TurnArgs a, hipStream_t stream)
+hipError_t launch_turn(const TurnArgs &a, hipStream_t stream)
 {
-    const int at_once = kTurnThreads / (a.dim >> 4), pairs = a.turns ? a.dims >> 1 : 0;
-    const int64_t all = (int64_t)a.tokens * a.heads;
-    // tokens that a work group of so many passes meets, and LDS for their pairs
-    auto room = [&](int passes) { return (size_t)((passes * at_once - 2) / a.heads + 2) * pairs * sizeof(float2); };
-    int passes = 1;
-    while (passes < 4 && all > (int64_t)8 * kComputeUnits * passes * at_once && room(2 * passes) <= 32768) passes *= 2;
-    a.rows = passes * at_once;
-    if ((all + a.rows - 1) / a.rows > (int64_t)UINT32_MAX / kTurnThreads) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)((all + a.rows - 1) / a.rows)), threads(kTurnThreads);
-    if (passes == 1)
-        hipLaunchKernelGGL((k_turn<KIND, 1>), grid, threads, room(1), stream, a);
-    else if (passes == 2)
-        hipLaunchKernelGGL((k_turn<KIND, 2>), grid, threads, room(2), stream, a);
-    else
-        hipLaunchKernelGGL((k_turn<KIND, 4>), grid, threads, room(4), stream, a);
+    const int at_once = kTurnThreads / (a.dim >> 4);
+    const int64_t grid = ((int64_t)a.tokens * a.heads + at_once - 1) / at_once;
+    if (grid > (int64_t)UINT32_MAX / kTurnThreads) return hipErrorInvalidConfiguration;
+    // tokens that a work group meets at most, and LDS for their pairs: 16 KB where there is one head, a little more where tokens begin in its middle
+    const size_t lds = a.turns ? (size_t)((at_once - 2) / a.heads + 2) * (a.dims >> 1) * sizeof(float2) : 0;
+    auto *kernel = !a.cache.k ? k_turn<0> : a.cache.bits8 ? k_turn<2> : k_turn<1>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kTurnThreads), lds, stream, a);
     return hipGetLastError();
-}
-
-hipError_t launch_turn(TurnArgs a, hipStream_t stream)
-{
-    if (!a.cache.k) return launch_turn_kind<0>(a, stream);
-    return a.cache.bits8 ? launch_turn_kind<2>(a, stream) : launch_turn_kind<1>(a, stream);
 }
 
 // ------------------------------------------------------------------------------------------------

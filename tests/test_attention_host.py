@@ -47,7 +47,7 @@ CASES += [("lora_cache_append", APPEND, c, s) for c, s in [
     (dict(slots=None), "INVALID_ARG"), (dict(positions=None), "INVALID_ARG"), (dict(rotary=None), "INVALID_ARG"), (dict(rotary=rotary(dims=128)), "SHAPE"),
     (dict(q=P + 1), "INVALID_ARG"), (dict(heads=0), "SHAPE"), (dict(y=None), "INVALID_ARG"), (dict(yt=192), "INVALID_ARG"), (dict(y=P, yh=128, yt=512), "INVALID_ARG"),
     (dict(tokens=1 << 28, heads=8, qt=512, yt=512), "SHAPE"),
-    (dict(tokens=(1 << 30) - 1, cache=cache(heads=1), q=None, kt=0, vt=0), "SHAPE")]]  # (2^31 rows, 128 a work group: more threads than a launch has)
+    (dict(tokens=(1 << 30) - 1, cache=cache(heads=1), q=None, kt=0, vt=0), "SHAPE")]]  # (2^31 rows, 64 a work group: more threads than a launch has)
 CASES += [("lora_attention", ATTEND, c, s) for c, s in [
     (dict(q=None), "INVALID_ARG"), (dict(qt=100), "INVALID_ARG"), (dict(tokens=-1), "INVALID_ARG"), (dict(heads=3), "SHAPE"), (dict(heads=0), "SHAPE"),
     (dict(starts=None), "INVALID_ARG"), (dict(lengths=P + 3), "INVALID_ARG"), (dict(requests=-1), "INVALID_ARG"), (dict(table=None), "INVALID_ARG"),
