@@ -57,7 +57,7 @@ struct AttendArgs {
     int least, most;              // columns of the requests that this launch takes: least < rows * group <= most
     int shares;                   // of a key head's work
     bool cut;                     // shares are of steps, and tiles cut where those end; else every tile is a share
-    float *parts;                 // workspace: [kv_heads * shares][2][columns][dim], then sums [..][2][columns][2]
+    float *parts;                 // workspace: [kv_heads * shares][2][columns][dim], then sums [..][2][columns][2], then 16 bytes each (CutTile)
 };
 
 // Which launches a call takes.
@@ -105,7 +105,7 @@ inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int req
 
 inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
 {
-    return f.cut && f.shares > 1 ? (size_t)kv_heads * f.shares * 2 * f.columns * (dim + 2) * sizeof(float) : 0;
+    return f.cut && f.shares > 1 ? (size_t)kv_heads * f.shares * (2 * f.columns * (dim + 2) * sizeof(float) + 16) : 0;
 }
 
 // bytes that a call may need, whatever `most` says

@@ -366,6 +366,28 @@ static __device__ __forceinline__ uint32_t share_at(uint32_t total, int share, i
     return each * share + min((uint32_t)share, more);
 }
 
+// What a share leaves for k_attend_join: the tile that it began and did not end, whose last steps are in the shares up to `last` (-1: there is none).
+struct CutTile {
+    int first, columns, c0, last;  // its request's first row and columns, its own first column
+};
+static __device__ __forceinline__ CutTile *cut_tiles(const AttendArgs &a, int columns, int dim)
+{
+    return reinterpret_cast<CutTile *>(a.parts + (int64_t)a.cache.kv_heads * a.shares * 2 * columns * (dim + 2));
+}
+// one thread: the share ended `behind` steps before its tile does (0: with it)
+template <class Place>
+static __device__ __forceinline__ void leave_cut(const AttendArgs &a, CutTile *to, uint32_t total, int share, const Place &p, int c0, uint32_t behind)
+{
+    CutTile t{p.q.first, p.q.n * a.group, c0, -1};
+    if (behind > 0 && p.at == 0) {
+        // (shares are alike but for one step)
+        const uint32_t begin = share_at(total, share + 1, a.shares), end = begin + behind, some = min((uint32_t)a.shares, total);
+        t.last = min((int)some - 1, share + 1 + (int)((behind - 1) / (total / some)));
+        while (share_at(total, t.last, a.shares) >= end) --t.last;
+    }
+    *to = t;
+}
+
 // where a share leaves its sums: slot 1 of those of a tile that begins in it, slot 0 of one that began earlier
 static __device__ __forceinline__ int64_t part_of(int head, int shares, int share, bool begins) { return ((int64_t)head * shares + share) * 2 + begins; }
 
@@ -555,13 +577,17 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, quad = lane >> 4;
     const int kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
     typename W::Place p;
-    uint32_t left = 0;
+    uint32_t left = 0, all_steps = 0;
     if (!W::template find<256>(a, found, [&](uint32_t total) {
             if (!a.cut) return (uint32_t)share;
+            all_steps = total;
             const uint32_t from = share_at(total, share, a.shares);
             left = share_at(total, share + 1, a.shares) - from;
             return from;
-        }, p)) return;
+        }, p)) {
+        if (a.cut && a.shares > 1 && tid == 0) cut_tiles(a, TC, D)[kh * a.shares + share].last = -1;
+        return;
+    }
     if (!a.cut) left = p.of;
 
     const int page = 1 << a.cache.page_shift;
@@ -860,7 +886,11 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
         if (odd.to[turn]) add_odd<D, F8, 256>(a, p, kh, odd.from[turn] * KEYS, odd.to[turn] * KEYS, c0, TC, whole, a.parts + slot * TC * D);
         turn ^= 1;
         left -= to - p.at;
-        if (left == 0 || !W::next(a, p)) return;
+        if (left == 0) {
+            if (a.cut && a.shares > 1 && tid == 0) leave_cut(a, cut_tiles(a, TC, D) + kh * a.shares + share, all_steps, share, p, c0, p.of - to);
+            return;
+        }
+        if (!W::next(a, p)) return;  // (steps are left, so there is a tile)
     }
 }
 
@@ -913,13 +943,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(ATTEND_LIST, Atte
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const int kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
     typename W::Place p;
-    uint32_t left = 0;
+    uint32_t left = 0, all_steps = 0;
     if (!W::template find<64 * WAVES>(a, found, [&](uint32_t total) {
             if (!a.cut) return (uint32_t)share;
+            all_steps = total;
             const uint32_t from = share_at(total, share, a.shares);
             left = share_at(total, share + 1, a.shares) - from;
             return from;
-        }, p)) return;
+        }, p)) {
+        if (a.cut && a.shares > 1 && tid == 0) cut_tiles(a, TC, D)[kh * a.shares + share].last = -1;
+        return;
+    }
     if (!a.cut) left = p.of;
     const int page = 1 << a.cache.page_shift;
     const bool loads_v = wave < WAVES / 2;
@@ -1251,38 +1285,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(ATTEND_LIST, Atte
         if (odd.to[turn]) add_odd<D, F8, 64 * WAVES>(a, p, kh, odd.from[turn] * KEYS, odd.to[turn] * KEYS, c0, TC, whole, a.parts + slot * TC * D);
         turn ^= 1;
         left -= to - p.at;
-        if (left == 0 || !W::next(a, p)) return;
+        if (left == 0) {
+            if (a.cut && a.shares > 1 && tid == 0) leave_cut(a, cut_tiles(a, TC, D) + kh * a.shares + share, all_steps, share, p, c0, p.of - to);
+            return;
+        }
+        if (!W::next(a, p)) return;  // (steps are left, so there is a tile)
     }
 }
 
-// Tiles that several shares have a part of: a work group has CW columns of the tile that the first step of share s + 1 lies in, if that tile begins in share s.
-// 16 / CW groups of threads share the parts, four of which a thread asks for at a time.
-template <int D, int TC, int KEYS, int CW>
-__global__ __launch_bounds__(256) void k_attend_join(ATTEND_LIST, AttendArgs a)
+// Tiles that several shares have a part of: a work group has CW columns of the one that a share began and did not end.  16 / CW groups of threads share the parts,
+// four of which a thread asks for at a time.
+template <int D, int TC, int CW>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
 {
-    ATTEND_LIST_TO(a);
-    using W = Dealt<TC, KEYS>;
     constexpr int kEach = D / 16, kGroups = 16 / CW;
-    __shared__ typename W::Found found;
     __shared__ float tops[256 / CW][CW], sums[kGroups][CW], rows[kGroups][CW][D];
     const int tid = threadIdx.x, kh = (int)(blockIdx.x % (unsigned)a.cache.kv_heads), share = (int)(blockIdx.x / (unsigned)a.cache.kv_heads);
-    typename W::Place p;
-    uint32_t total = 0, step = 0;
-    if (!W::template find<256>(a, found, [&](uint32_t all) {
-            total = all;
-            return step = share_at(all, share + 1, a.shares);
-        }, p)) return;
-    if (p.at == 0 || step - p.at < share_at(total, share, a.shares)) return;
-    const int in0 = CW * blockIdx.y, columns = p.q.n * a.group - p.t * TC;
-    if (in0 >= columns) return;
-    const uint32_t end = step - p.at + p.of;
-    // the share of the tile's last step: they are alike but for one step
-    int last = share + 1;
-    {
-        const uint32_t least = max(1u, total / min((uint32_t)a.shares, total));
-        last = min((int)min((uint32_t)a.shares, total) - 1, share + 1 + (int)((end - 1 - step) / least));
-        while (share_at(total, last, a.shares) >= end) --last;
-    }
+    const CutTile tile = cut_tiles(a, TC, D)[kh * a.shares + share];
+    const int in0 = CW * blockIdx.y, columns = tile.columns - tile.c0, last = tile.last;
+    if (last < 0 || in0 >= columns) return;
     const float *slots = a.parts + (int64_t)a.cache.kv_heads * a.shares * 2 * TC * D;
     auto slot_of = [&](int s) __attribute__((always_inline)) { return part_of(kh, a.shares, s, s == share) * TC + in0; };
     {
@@ -1330,21 +1351,21 @@ __global__ __launch_bounds__(256) void k_attend_join(ATTEND_LIST, AttendArgs a)
     }
     if (in0 + c >= columns) return;
     const float by = all == 0.f ? 0.f : __builtin_amdgcn_rcpf(all);
-    const int col = p.t * TC + in0 + c, i = row_of_column(a, col), row = p.q.first + i, h = kh * a.group + (col - i * a.group);
+    const int col = tile.c0 + in0 + c, i = row_of_column(a, col), row = tile.first + i, h = kh * a.group + (col - i * a.group);
     uint32_t *y = reinterpret_cast<uint32_t *>(a.y.p + row * a.y.token + h * a.y.head + dim);
 #pragma unroll
     for (int x = 0; x < kEach; x += 4) *reinterpret_cast<uint2 *>(y + x / 2) = uint2{pack_bf16_rne(z[x] * by, z[x + 1] * by), pack_bf16_rne(z[x + 2] * by, z[x + 3] * by)};
 }
 
-template <int D, int TC, int KEYS>
+template <int D, int TC>
 static hipError_t launch_join(const AttendArgs &a, hipStream_t stream)
 {
     const unsigned ends = (unsigned)(a.shares - 1) * a.cache.kv_heads;
     // few requests among many shares: a tile has many parts
     if (TC <= 64 && 4 * a.requests < a.shares)
-        hipLaunchKernelGGL((k_attend_join<D, TC, KEYS, 4>), dim3(ends, TC / 4), dim3(256), 0, stream, ATTEND_LIST_OF(a), a);
+        hipLaunchKernelGGL((k_attend_join<D, TC, 4>), dim3(ends, TC / 4), dim3(256), 0, stream, a);
     else
-        hipLaunchKernelGGL((k_attend_join<D, TC, KEYS, 16>), dim3(ends, TC / 16), dim3(256), 0, stream, ATTEND_LIST_OF(a), a);
+        hipLaunchKernelGGL((k_attend_join<D, TC, 16>), dim3(ends, TC / 16), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -1353,7 +1374,7 @@ static hipError_t launch_few(const AttendArgs &a, hipStream_t stream)
 {
     hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * kFewWaves), 0, stream, ATTEND_LIST_OF(a), a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut || a.shares == 1) return e;
-    return launch_join<D, 16 * C, few_keys(F8)>(a, stream);
+    return launch_join<D, 16 * C>(a, stream);
 }
 
 template <int D, bool F8, int WAVES>
@@ -1361,7 +1382,7 @@ static hipError_t launch_wide(const AttendArgs &a, hipStream_t stream)
 {
     hipLaunchKernelGGL((k_attend_wide<D, F8, WAVES>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * WAVES), 0, stream, ATTEND_LIST_OF(a), a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut || a.shares == 1) return e;
-    return launch_join<D, 32 * WAVES, WideShape<D, F8, WAVES>::kKeys>(a, stream);
+    return launch_join<D, 32 * WAVES>(a, stream);
 }
 
 hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t stream)
