@@ -184,19 +184,6 @@ struct Request {
     int first, n, keys;  // first row, rows, keys
 };
 
-// What a work group needs before it has anything else to ask for: arguments in front of the struct, which arrive in registers.  The others are in memory, five lines of 64
-// bytes, and would be asked for one after the other as they are used, a trip to memory each (one token over 1500 keys: 17.3 us a call so, see lines_of).
-#define ATTEND_LIST const int32_t *__restrict__ starts, const int32_t *__restrict__ lengths, int requests, int tokens, int room, int group, int shares, int kv_heads
-#define ATTEND_LIST_OF(a) (a).starts, (a).lengths, (a).requests, (a).tokens, (a).room, (a).group, (a).shares, (a).cache.kv_heads
-#define ATTEND_LIST_TO(a) \
-    (a).starts = starts, (a).lengths = lengths, (a).requests = requests, (a).tokens = tokens, (a).room = room, (a).group = group, (a).shares = shares, (a).cache.kv_heads = kv_heads
-
-// asks for all lines of the arguments at once
-static __device__ __forceinline__ void lines_of(const AttendArgs &a)
-{
-    asm volatile("" ::"s"(a.q.p), "s"(a.table), "s"(a.cache.k), "s"(a.cache.pages), "s"(a.least), "s"(a.parts) : "memory");
-}
-
 static __device__ __forceinline__ Request request_at(const AttendArgs &a, int r)
 {
     const int s0 = min(max(a.starts[r], 0), a.tokens), s1 = min(max(a.starts[r + 1], 0), a.tokens);
@@ -284,10 +271,8 @@ struct Dealt {
         const int each = (a.requests + THREADS - 1) / THREADS, r0 = tid * each, r1 = min(a.requests, r0 + each);
         Request q{0, 0, 0};
         uint32_t mine = 0, n = 0;  // (steps of this thread's requests; of the last of them)
-        if (r0 < r1) q = request_at(a, r0);
-        lines_of(a);
         for (int r = r0; r < r1; ++r) {
-            if (r > r0) q = request_at(a, r);
+            q = request_at(a, r);
             mine += n = all(a, tiles(a, q));
         }
         uint32_t upto = mine;
@@ -562,9 +547,8 @@ struct FewShape {
 };
 
 template <int D, bool F8, int C>
-__global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(ATTEND_LIST, AttendArgs a)
+__global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(AttendArgs a)
 {
-    ATTEND_LIST_TO(a);
     using S = FewShape<D, F8>;
     constexpr int TC = 16 * C, WAVES = kFewWaves, KEYS = few_keys(F8);
     using W = Dealt<TC, KEYS>;
@@ -928,9 +912,8 @@ struct WideShape {
 };
 
 template <int D, bool F8, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(ATTEND_LIST, AttendArgs a)
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
 {
-    ATTEND_LIST_TO(a);
     using S = WideShape<D, F8, WAVES>;
     constexpr int TC = 32 * WAVES, KEYS = S::kKeys;
     using W = Dealt<TC, KEYS>;
@@ -1372,7 +1355,7 @@ static hipError_t launch_join(const AttendArgs &a, hipStream_t stream)
 template <int D, bool F8, int C>
 static hipError_t launch_few(const AttendArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * kFewWaves), 0, stream, ATTEND_LIST_OF(a), a);
+    hipLaunchKernelGGL((k_attend_few<D, F8, C>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * kFewWaves), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut || a.shares == 1) return e;
     return launch_join<D, 16 * C>(a, stream);
 }
@@ -1380,7 +1363,7 @@ static hipError_t launch_few(const AttendArgs &a, hipStream_t stream)
 template <int D, bool F8, int WAVES>
 static hipError_t launch_wide(const AttendArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_attend_wide<D, F8, WAVES>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * WAVES), 0, stream, ATTEND_LIST_OF(a), a);
+    hipLaunchKernelGGL((k_attend_wide<D, F8, WAVES>), dim3((unsigned)a.shares * a.cache.kv_heads), dim3(64 * WAVES), 0, stream, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.cut || a.shares == 1) return e;
     return launch_join<D, 32 * WAVES>(a, stream);
 }
