@@ -1,14 +1,16 @@
-"""A block of a mixture-of-experts model whose frozen weights are held in 8 bits, with LoRA adapters on its projection.
+"""A block of a mixture-of-experts model whose frozen weights are held in 8 bits, with LoRA adapters on its projections.
 
-Two parts, each one path through the library as a serving program takes it; every buffer is made once, nothing is allocated or waited
+Three parts, each one path through the library as a serving program takes it; every buffer is made once, nothing is allocated or waited
 for in a step, and the host never learns which tokens picked which experts:
 
     AdaptedProjection   y = x W + s_a (x A_a) B_a     lora_rows_quantize, lora_linear_scaled, lora_apply
+    AdaptedAttention    y = attention(x W_q, x W_k, x W_v) W_o, all four adapted, over a paged cache
+                        three projections, lora_cache_append (which turns queries and keys), lora_attention, the fourth
     ExpertLayer         z = sum over picks of weight * W_down_e (silu(W_gate_e x) * W_up_e x)
                         lora_experts_group, lora_rows_quantize, lora_experts_linear_scaled (gate and up side by side), the
                         activation, lora_rows_quantize, lora_experts_linear_scaled on rows in expert order, lora_experts_combine
 
-``python -m paper_2511_22880_amd.expert_layer`` runs both on random weights and checks them against 64 bits.
+``python -m paper_2511_22880_amd.expert_layer`` runs them on random weights and checks them against 64 bits.
 """
 from __future__ import annotations
 
@@ -67,6 +69,32 @@ class AdaptedProjection:
         L.lora_apply(self.pool, segments, x, y, workspace, stream)
 
 
+class AdaptedAttention:
+    """What stands between a layer's norm and its experts: queries, keys and values, the cache, attention, the output projection."""
+
+    def __init__(self, q: AdaptedProjection, k: AdaptedProjection, v: AdaptedProjection, o: AdaptedProjection, cache: L.Cache, rotary: L.Rotary, most_tokens: int,
+                 most_requests: int, width: int):
+        """width: pages a request has at most."""
+        self.projections, self.cache, self.rotary, self.width = (q, k, v, o), cache, rotary, width
+        self.heads = q.w.out_features // cache.head_dim
+        rows = lambda n: torch.empty(most_tokens, n, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+        self.q, self.k, self.v, self.turned, self.z = (rows(p.w.out_features) for p in (q, k, v, q, q))
+        n = L.lora_attention_workspace_bytes(most_tokens, self.heads, most_requests, width, cache)
+        self.workspace = torch.empty(max(16, n), dtype=torch.uint8, device="cuda")
+
+    def __call__(self, x: torch.Tensor, segments, positions: torch.Tensor, slots: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor,
+                 page_table: torch.Tensor, y: torch.Tensor, apply_workspace: torch.Tensor, tree=None, most: int = 0) -> None:
+        """x: bf16 [tokens][hidden]; segments: the batch's plans on the pools of q, k, v and o; positions, slots: int32 [tokens]; starts, lengths, page_table, tree,
+        most: of lora_attention, lengths with this step's tokens; y: bf16 [tokens][hidden], written."""
+        stream, n, dim = torch.cuda.current_stream(), x.shape[0], self.cache.head_dim
+        for projection, segment, out in zip(self.projections, segments, (self.q, self.k, self.v)):
+            projection(x, segment, out[:n], apply_workspace)
+        heads = lambda t: t[:n].view(n, -1, dim)  # noqa: E731
+        L.lora_cache_append(heads(self.k), heads(self.v), slots, self.cache, self.rotary, positions, heads(self.q), heads(self.turned), stream)
+        L.lora_attention(heads(self.turned), starts, lengths, page_table, self.cache, heads(self.z), self.workspace, tree=tree, most=most, stream=stream)
+        self.projections[3](self.z[:n], segments[3], y, apply_workspace)
+
+
 class ExpertLayer:
     """The experts: gate_up holds W_gate and W_up of an expert one behind the other ([experts][2 * inner][hidden]), down [experts][hidden][inner]."""
 
@@ -114,36 +142,111 @@ def reference(x, ids, weights, gate_up, down):
     return z
 
 
-def main() -> None:
-    import numpy as np
+class Adapters:
+    """Random adapters of the given ranks on a layer of this shape, and the plan of a batch on them."""
 
+    def __init__(self, in_f: int, out_f: int, ranks, token_adapter, rand):
+        import numpy as np
+        self.ranks, self.token_adapter = np.asarray(ranks, dtype=np.int32), np.asarray(token_adapter, dtype=np.int32)
+        self.scales = (2.0 / self.ranks).astype(np.float32)
+        self.arena = torch.zeros(L.lora_pool_bytes(in_f, out_f, self.ranks, self.scales), dtype=torch.uint8, device="cuda")
+        self.pool = L.lora_pool_create(in_f, out_f, self.ranks, self.scales, self.arena)
+        self.A = [(rand(in_f, int(r)) * 0.02).to(torch.bfloat16) for r in self.ranks]
+        self.B = [(rand(int(r), out_f) * 0.02).to(torch.bfloat16) for r in self.ranks]
+        for a in range(len(self.ranks)):
+            L.lora_pool_load(self.pool, a, self.A[a], self.B[a], src_is_device=True, stream=torch.cuda.current_stream())
+        self.segments = L.lora_segments_build(self.pool, self.token_adapter, torch.cuda.current_stream())
+        self.workspace_bytes = L.lora_apply_workspace_bytes(self.pool, self.segments)
+
+    def add(self, x: torch.Tensor, y: torch.Tensor) -> torch.Tensor:
+        """fp64 y with the deltas of x"""
+        for t, a in enumerate(self.token_adapter):
+            if a >= 0:
+                y[t] += float(self.scales[a]) * (x[t].double() @ self.A[a].double()) @ self.B[a].double()
+        return y
+
+    def close(self) -> None:
+        L.lora_segments_destroy(self.segments)
+        L.lora_pool_destroy(self.pool)
+
+
+def attention_reference(q, k, v, cached, positions, sizes, dims: int, base: float = 10000.0):
+    """Attention in 64 bits: q [tokens][heads][dim], k and v [tokens][kv_heads][dim] of the new tokens, not yet turned; cached: a request's context, (k, v)
+    [keys][kv_heads][dim] as the cache holds it; sizes: (rows, keys) of the requests."""
+    f = base ** (-torch.arange(0, dims, 2, dtype=torch.float64, device=q.device) / dims)
+    angle = positions.double()[:, None, None] * f
+
+    def turned(x):
+        x1, x2 = x[..., :dims // 2].double(), x[..., dims // 2:dims].double()
+        return torch.cat([x1 * angle.cos() - x2 * angle.sin(), x1 * angle.sin() + x2 * angle.cos(), x[..., dims:].double()], dim=2)
+
+    q, k, z, at = turned(q), turned(k), torch.zeros(q.shape, dtype=torch.float64, device=q.device), 0
+    group = q.shape[1] // k.shape[1]
+    for (n, keys), (ck, cv) in zip(sizes, cached):
+        rows = slice(at, at + n)
+        kk, vv = (torch.cat([c.double(), t[rows].double()]).repeat_interleave(group, dim=1).permute(1, 0, 2) for c, t in ((ck, k), (cv, v)))
+        s = q[rows].permute(1, 0, 2) @ kk.transpose(1, 2).contiguous() / q.shape[2] ** 0.5
+        late = torch.arange(keys, device=q.device)[None] > keys - n + torch.arange(n, device=q.device)[:, None]
+        z[rows] = (torch.softmax(s.masked_fill(late, float("-inf")), dim=2) @ vv).permute(1, 0, 2)
+        at += n
+    return z
+
+
+def attention_example(rand, seed: int = 1):
+    """A prompt, a piece of one and some single tokens through an AdaptedAttention.  (the block, its adapters and weights, x, y, what attention_reference takes
+    of the batch)"""
+    hidden, heads, kv_heads, dim, page, width = 1024, 8, 2, 128, 16, 20
+    sizes = [(90, 90), (40, 200)] + [(1, 17 + 9 * i) for i in range(30)]  # (new tokens, with their context)
+    tokens, ranks = sum(n for n, _ in sizes), [8, 16, 32, 64] * 2
+    token_adapter = [-1 if t % 5 == 4 else t % len(ranks) for t in range(tokens)]
+    x = rand(tokens, hidden).to(torch.bfloat16)
+    shapes = [(hidden, heads * dim), (hidden, kv_heads * dim), (hidden, kv_heads * dim), (heads * dim, hidden)]
+    adapters = [Adapters(*shape, ranks, token_adapter, rand) for shape in shapes]
+    weights = [weights_to_8_bits(rand(1, out_f, in_f) * 0.03) for in_f, out_f in shapes]
+    projections = [AdaptedProjection(Packed(*w), a.pool, tokens) for w, a in zip(weights, adapters)]
+    pages = width * len(sizes)
+    k, v = (rand(pages, kv_heads, page, dim).to(torch.bfloat16) for _ in range(2))
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(seed)).view(len(sizes), width)
+    where = [[(int(table[r, j // page]), j % page) for j in range(keys)] for r, (_, keys) in enumerate(sizes)]
+    cached = []
+    for (n, keys), slots in zip(sizes, where):
+        ids, places = (torch.tensor([s[i] for s in slots[:keys - n]], dtype=torch.long, device="cuda") for i in (0, 1))
+        cached.append((k[ids, :, places], v[ids, :, places]))
+    ints = lambda values: torch.tensor(values, dtype=torch.int32, device="cuda")  # noqa: E731
+    positions = ints([j for n, keys in sizes for j in range(keys - n, keys)])
+    slots = ints([p * page + j for (n, keys), s in zip(sizes, where) for p, j in s[keys - n:]])
+    starts = ints([sum(n for n, _ in sizes[:r]) for r in range(len(sizes) + 1)])
+    block = AdaptedAttention(*projections, L.Cache(k, v), L.Rotary(dim), tokens, len(sizes), width)
+    y = torch.empty(tokens, hidden, dtype=torch.bfloat16, device="cuda")
+    room = torch.empty(max(256, *(a.workspace_bytes for a in adapters)), dtype=torch.uint8, device="cuda")
+    block(x, [a.segments for a in adapters], positions, slots, starts, ints([keys for _, keys in sizes]), table.to(torch.int32).cuda(), y, room, most=90)
+    return block, adapters, weights, x, y, (cached, positions, sizes, dim)
+
+
+def main() -> None:
     g = torch.Generator(device="cuda").manual_seed(1)
     rand = lambda *shape: torch.randn(*shape, generator=g, device="cuda")  # noqa: E731
     hidden, inner, experts, picks, tokens = 1024, 512, 16, 4, 200
     x = rand(tokens, hidden).to(torch.bfloat16)
 
     # the projection: 8 adapters of ranks 8 to 64, every fifth token without one
-    ranks = np.array([8, 16, 32, 64] * 2, dtype=np.int32)
-    scales = (2.0 / ranks).astype(np.float32)
-    arena = torch.zeros(L.lora_pool_bytes(hidden, hidden, ranks, scales), dtype=torch.uint8, device="cuda")
-    pool = L.lora_pool_create(hidden, hidden, ranks, scales, arena)
-    A = [(rand(hidden, int(r)) * 0.02).to(torch.bfloat16) for r in ranks]
-    B = [(rand(int(r), hidden) * 0.02).to(torch.bfloat16) for r in ranks]
-    for a in range(len(ranks)):
-        L.lora_pool_load(pool, a, A[a], B[a], src_is_device=True, stream=torch.cuda.current_stream())
-    token_adapter = np.array([-1 if t % 5 == 4 else t % len(ranks) for t in range(tokens)], dtype=np.int32)
-    seg = L.lora_segments_build(pool, token_adapter, torch.cuda.current_stream())
-    workspace = torch.empty(max(256, L.lora_apply_workspace_bytes(pool, seg)), dtype=torch.uint8, device="cuda")
+    adapters = Adapters(hidden, hidden, [8, 16, 32, 64] * 2, [-1 if t % 5 == 4 else t % 8 for t in range(tokens)], rand)
+    workspace = torch.empty(max(256, adapters.workspace_bytes), dtype=torch.uint8, device="cuda")
     w8, ws = weights_to_8_bits(rand(1, hidden, hidden) * 0.03)
     y = torch.empty(tokens, hidden, dtype=torch.bfloat16, device="cuda")
-    AdaptedProjection(Packed(w8, ws), pool, tokens)(x, seg, y, workspace)
-    ref = x.double() @ _values(w8, ws)[0].t()
-    for t, a in enumerate(token_adapter):
-        if a >= 0:
-            ref[t] += float(scales[a]) * (x[t].double() @ A[a].double()) @ B[a].double()
+    AdaptedProjection(Packed(w8, ws), adapters.pool, tokens)(x, adapters.segments, y, workspace)
+    ref = adapters.add(x, x.double() @ _values(w8, ws)[0].t())
     print(f"adapted projection in 8 bits: relative error {((y.double() - ref).norm() / ref.norm()).item():.4f}")
-    L.lora_segments_destroy(seg)
-    L.lora_pool_destroy(pool)
+    adapters.close()
+
+    # attention between four adapted projections
+    block, four, layers, x4, y4, batch = attention_example(rand)
+    through = lambda i, rows: four[i].add(rows, rows.double() @ _values(*layers[i])[0].t())  # noqa: E731
+    q64, k64, v64 = (through(i, x4).view(x4.shape[0], -1, 128) for i in range(3))
+    ref = through(3, attention_reference(q64, k64, v64, *batch).flatten(1))
+    print(f"attention between adapted projections in 8 bits: off by {((y4.double() - ref).norm() / ref.norm()).item():.4f} of the result")
+    for a in four:
+        a.close()
 
     # the experts
     gate_up, gs = weights_to_8_bits(rand(experts, 2 * inner, hidden) * 0.03)

@@ -622,3 +622,35 @@ def test_a_prompt_in_pieces_gives_what_the_whole_prompt_gives():
     d = (results[0][0].double() - results[1][0].double()).abs()
     # each is off by 2^-8 |y| + 2^-8 M and a little; M is at most the largest |v|
     assert (d <= 4 * 2.0 ** -8 * x[:, kv_heads:].abs().max().double() * (1 + 2.0 ** -4)).all()
+
+
+# ---- between the adapted projections ------------------------------------------------------------------------
+def test_attention_between_adapted_projections():
+    """All of a block's calls on one batch, a part at a time: what the projections give against 64 bits within what an 8-bit row leaves (2^-3 / sqrt(12) of the
+    power of two below a value, in the mean), attention on what they gave within this file's bound, and the turned keys in the cache."""
+    from paper_2511_22880_amd import expert_layer as m
+    g = gen(17)
+    block, adapters, weights, x, y, batch = m.attention_example(lambda *shape: torch.randn(*shape, generator=g, device="cuda"))
+    cached, positions, sizes, dim = batch
+    step, n = 2.0 ** -3 / 12 ** 0.5, x.shape[0]
+    for i, (rows, out) in enumerate(((x, block.q), (x, block.k), (x, block.v), (block.z, y))):
+        ref = adapters[i].add(rows, rows.double() @ m._values(*weights[i])[0].t())
+        assert (out.double() - ref).norm() <= step * ref.norm()
+    q, k, v = (t.view(n, -1, dim) for t in (block.q, block.k, block.v))
+    z = m.attention_reference(q, k, v, cached, positions, sizes, dim)
+    # (here the queries and keys that attention sees were rounded to bf16 after they were turned, 2^-8 each: their scores are off by twice that of scale sum |q||k|)
+    group, at = block.heads // block.cache.kv_heads, 0
+    got = block.z.view(n, -1, dim).double()
+    for (rows, keys), (ck, cv) in zip(sizes, cached):
+        part = slice(at, at + rows)
+        # |q . k| <= |q||k| by element, and a turn leaves a pair's length: sum |q||k| <= 2 |q| |k| by pairs
+        pairs = lambda t: (t[..., :dim // 2].double() ** 2 + t[..., dim // 2:].double() ** 2).sqrt()  # noqa: E731
+        kk = torch.cat([pairs(ck), pairs(k[part])]).repeat_interleave(group, dim=1).permute(1, 0, 2)
+        a = (2 * pairs(q[part]).permute(1, 0, 2) @ kk.transpose(1, 2).contiguous()).amax(dim=2).t()[..., None] / dim ** 0.5
+        top = torch.cat([cv, v[part]]).abs().double().amax()
+        d = (2.0 ** -7 + (dim + 4) * U) * a * (1 + 2.0 ** -3)
+        bound = (2.0 ** -8 * z[part].abs() + (2.0 ** -8 + 2 * torch.expm1(d) + 2.0 ** -19 + 4 * keys * U) * top) * (1 + 2.0 ** -6)
+        assert ((got[part] - z[part]).abs() <= bound).all()
+        at += rows
+    for a in adapters:
+        a.close()
