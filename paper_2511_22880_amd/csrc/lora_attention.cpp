@@ -272,10 +272,10 @@ extern "C" lora_status_t lora_attention(const void *q, int64_t q_token, int64_t 
     a.room = width * cache->page_size;
     a.tree = tree;
     a.cache = cache_of(cache);
-    // (nought times the -infinity of a key that is not seen would be NaN; times 2^-120 scores do not matter either)
-    a.scale = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 0x1p-120f);
+    // (nought times the -infinity of a key that is not seen would be NaN; times 2^-126 scores do not matter either)
+    a.scale = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 0x1p-126f);
     a.flip = scale < 0.f ? 0x80008000u : 0u;
-    a.slack = 8.f / a.scale;
+    a.slack = std::fmin(8.f / a.scale, 1e38f);
     const lora::AttendForms forms = lora::attend_forms(tokens, a.group, cache->kv_heads, requests, (int64_t)width * cache->page_size, most, cache->head_dim, cache->bits == 8);
     size_t need = 0;
     for (int i = 0; i < forms.n; ++i) {

@@ -72,35 +72,39 @@ struct AttendForms {
     int n;
 };
 
-inline int64_t most_tiles(int64_t tokens, int group, int requests, int columns)
+// Tiles of a key head, at most: those that rows fill, and a last one for every request of more than `least` columns.
+inline int64_t most_tiles(int64_t tokens, int group, int requests, int columns, int least)
 {
-    const int64_t all = tokens * group;
-    return all / columns + (requests < tokens ? requests : tokens);
+    const int64_t all = tokens * group, with = all / (least + 1);
+    return all / columns + (requests < with ? requests : with);
 }
 
-inline AttendForm attend_form(int columns, int keys, int whole_steps, int work_groups, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys)
+// Whether tiles are cut.  Tiles of few steps are not, if there are not too many of them for a work group each (a work group that finds none takes 2 us to see that; the host's
+// count can be far above what there are): the parts that cut ones leave cost a launch to join them, and for 256 columns 128 KB each way.
+inline AttendForm attend_form(int columns, int keys, int whole_steps, int work_groups, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int least, int most)
 {
-    const int64_t steps = (most_keys + keys - 1) / keys, tiles = most_tiles(tokens, group, requests, columns);
-    int64_t shares = work_groups / kv_heads;
+    const int64_t steps = (most_keys + keys - 1) / keys;
+    int64_t tiles = most_tiles(tokens, group, requests, columns, least), shares = work_groups / kv_heads;
+    if (most <= columns && tiles > requests) tiles = requests;
+    if (tiles < 1) tiles = 1;
+    if (steps <= whole_steps && tiles * kv_heads <= 8 * work_groups) return AttendForm{columns, (int)tiles, least, most, false};
     if (shares < 1) shares = 1;
-    if (shares > tiles * steps) shares = tiles * steps > 0 ? tiles * steps : 1;
-    // (a launch has fewer than 2^32 threads, of 512 at most a work group)
-    if (steps <= whole_steps && tiles * kv_heads < (int64_t)1 << 22) return AttendForm{columns, (int)tiles, 0, INT32_MAX, false};
-    return AttendForm{columns, (int)shares, 0, INT32_MAX, true};
+    if (shares > tiles * steps) shares = tiles * steps;
+    return AttendForm{columns, (int)shares, least, most, true};
 }
 
 inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int64_t most_rows, int dim, bool bits8)
 {
     const int64_t rows = most_rows > 0 && most_rows < tokens ? most_rows : tokens, columns = rows * group;
-    auto few = [&](int c) { return attend_form(c, few_keys(bits8), 4, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys); };
-    if (columns <= 32) return AttendForms{{few(columns <= 16 ? 16 : 32), {}}, 1};
+    auto few = [&](int c, int most) { return attend_form(c, few_keys(bits8), 4, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys, 0, most); };
+    auto wide = [&](int c, int least) {
+        return attend_form(c, 8192 / dim, 16, c == 128 ? 2 * kComputeUnits : kComputeUnits, tokens, group, kv_heads, requests, most_keys, least, INT32_MAX);
+    };
+    if (columns <= 32) return AttendForms{{few(columns <= 16 ? 16 : 32, INT32_MAX), {}}, 1};
     const int c = columns <= 128 ? 128 : 256;
-    AttendForm wide = attend_form(c, 8192 / dim, 16, c == 128 ? 2 * kComputeUnits : kComputeUnits, tokens, group, kv_heads, requests, most_keys);
-    if (requests == 1 || group > 16 || tokens > requests * rows / 2) return AttendForms{{wide, {}}, 1};
-    AttendForm narrow = few(16);
-    narrow.most = 16;
-    wide.least = 16;
-    return AttendForms{{narrow, wide}, 2};
+    // requests of very different sizes: those of up to 16 columns in a launch of their own
+    if (requests == 1 || group > 16 || tokens > requests * rows / 2) return AttendForms{{wide(c, 0), {}}, 1};
+    return AttendForms{{few(16, 16), wide(c, 16)}, 2};
 }
 
 inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
@@ -125,7 +129,7 @@ inline size_t attend_most_bytes(int64_t tokens, int group, int kv_heads, int req
 // steps of a key head's tiles, at most
 inline int64_t most_steps(int64_t tokens, int group, int requests, int64_t most_keys)
 {
-    return most_tiles(tokens, group, requests, 16) * ((most_keys + 63) / 64 + 1);
+    return most_tiles(tokens, group, requests, 16, 0) * ((most_keys + 63) / 64 + 1);
 }
 
 hipError_t launch_attention(AttendArgs a, const AttendForm &f, hipStream_t stream);
