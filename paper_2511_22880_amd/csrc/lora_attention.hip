@@ -721,8 +721,9 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
 #pragma unroll
                             for (int i = 0; i < 8; ++i) sc[c][y][i >> 2][i & 3] = seen[c][y] >> i & 1 ? sc[c][y][i >> 2][i & 3] : -INFINITY;
                         }
-                        // values of keys that there are none of are taken as zero, and (see OddSteps) infinities and NaN where the columns differ in what they see
-                        const uint32_t there = first_bits(held ? p.q.keys - (mine + 32 * y) : 0);
+                        // values that no column sees are taken as zero: of one row's columns those that it does not see, of more the keys that there are none of, and
+                        // (see OddSteps) infinities and NaN
+                        const uint32_t there = rows > 1 ? first_bits(held ? p.q.keys - (mine + 32 * y) : 0) : seen[0][y];
                         uint32_t some = 0;
 #pragma unroll
                         for (int i = 0; i < 8; ++i)

@@ -422,6 +422,31 @@ def test_what_a_row_does_not_see_has_no_part_in_it(bits, tree):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("heads, dim, most", [(16, 64, 1), (32, 128, 1), (8, 64, 1), (8, 128, 40)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_a_row_alone_in_its_tile_does_not_see_later_keys(heads, dim, most, bits, tree):
+    """one key head: 16 heads are a tile's columns, and 32 keys of a step are looked at by one row only.  Its request's later keys, or (tree) its own, hold infinities"""
+    batch = Batch([(2, 20), (1, 33), (3, 75), (1, 1)], heads, 1, dim, bits=bits, tree=tree, seed=6)
+    if tree:
+        batch.tree.copy_(torch.tensor([1, 1, 0, 1, 0, 1, 0]))
+    for r, own in ((0, 1), (1, 0), (2, 1), (2, 2), (3, 0)):
+        if not tree and own == 0:
+            continue
+        n, keys = batch.sizes[r]
+        key = keys - n + own
+        page, at = int(batch.table[r, key // 16]), key % 16
+        if bits == 8:
+            batch.tensors["v"].view(torch.uint8)[page, 0, at, 9] = 0x7F
+        else:
+            batch.tensors["v"][page, 0, at, 9] = float("inf")
+    ref, bound = batch.reference()
+    y = batch.run(most).double()
+    assert torch.isfinite(ref[0]).all() and torch.equal(torch.isfinite(y), torch.isfinite(ref))
+    fine = torch.isfinite(ref)
+    assert ((y - ref).abs()[fine] <= bound[fine]).all()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("most", [1, 40])
 def test_pages_that_are_none_are_seen_by_nobody(bits, most):
     batch = Batch([(1, 200), (1, 16), (40, 500), (2, 90), (1, 30)], 8, 2, 64, bits=bits)
