@@ -1237,6 +1237,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                 now = then;
                 then = after;
             }
+        } else {
+            __syncthreads();  // (what the tile before noted in `odd` has been read by all, and is cleared below)
         }
 
         const int64_t slot = part_of(kh, a.shares, share, p.at == 0);

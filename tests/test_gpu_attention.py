@@ -446,6 +446,21 @@ def test_a_row_alone_in_its_tile_does_not_see_later_keys(heads, dim, most, bits,
     assert ((y - ref).abs()[fine] <= bound[fine]).all()
 
 
+@pytest.mark.parametrize("most", [1, 8, 40])
+def test_infinities_before_requests_without_keys(most):
+    """work groups that have several tiles, some of them of rows that see nothing, behind one whose later keys hold infinities"""
+    sizes = [(20, 64), (20, 0), (20, 64), (20, 0), (20, 0)] * 240 + [(1, 9000)]
+    batch = Batch(sizes, 4, 2, 128, seed=8)
+    for r in range(0, 1200, 5):
+        for x in (0, 2):
+            batch.tensors["v"][int(batch.table[r + x, 3]), :, 15, r % 128] = float("inf")  # the last key
+    ref, bound = batch.reference()
+    y = batch.run(most).double()
+    assert torch.equal(torch.isfinite(y), torch.isfinite(ref)) and torch.isinf(ref).any()
+    fine = torch.isfinite(ref)
+    assert ((y - ref).abs()[fine] <= bound[fine]).all()
+
+
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("most", [1, 40])
 def test_pages_that_are_none_are_seen_by_nobody(bits, most):
