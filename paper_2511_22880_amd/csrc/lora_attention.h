@@ -93,18 +93,24 @@ inline AttendForm attend_form(int columns, int keys, int whole_steps, int work_g
     return AttendForm{columns, (int)shares, least, most, true};
 }
 
+// of tiles of up to 32 columns, and of more
+inline AttendForm few_form(int columns, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, bool bits8, int most)
+{
+    return attend_form(columns, few_keys(bits8), 4, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys, 0, most);
+}
+inline AttendForm wide_form(int columns, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int dim, int least)
+{
+    return attend_form(columns, 8192 / dim, 16, columns == 128 ? 2 * kComputeUnits : kComputeUnits, tokens, group, kv_heads, requests, most_keys, least, INT32_MAX);
+}
+
 inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int64_t most_rows, int dim, bool bits8)
 {
     const int64_t rows = most_rows > 0 && most_rows < tokens ? most_rows : tokens, columns = rows * group;
-    auto few = [&](int c, int most) { return attend_form(c, few_keys(bits8), 4, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys, 0, most); };
-    auto wide = [&](int c, int least) {
-        return attend_form(c, 8192 / dim, 16, c == 128 ? 2 * kComputeUnits : kComputeUnits, tokens, group, kv_heads, requests, most_keys, least, INT32_MAX);
-    };
-    if (columns <= 32) return AttendForms{{few(columns <= 16 ? 16 : 32, INT32_MAX), {}}, 1};
+    if (columns <= 32) return AttendForms{{few_form(columns <= 16 ? 16 : 32, tokens, group, kv_heads, requests, most_keys, bits8, INT32_MAX), {}}, 1};
     const int c = columns <= 128 ? 128 : 256;
     // requests of very different sizes: those of up to 16 columns in a launch of their own
-    if (requests == 1 || group > 16 || tokens > requests * rows / 2) return AttendForms{{wide(c, 0), {}}, 1};
-    return AttendForms{{few(16, 16), wide(c, 16)}, 2};
+    if (requests == 1 || group > 16 || tokens > requests * rows / 2) return AttendForms{{wide_form(c, tokens, group, kv_heads, requests, most_keys, dim, 0), {}}, 1};
+    return AttendForms{{few_form(16, tokens, group, kv_heads, requests, most_keys, bits8, 16), wide_form(c, tokens, group, kv_heads, requests, most_keys, dim, 16)}, 2};
 }
 
 inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
@@ -112,16 +118,15 @@ inline size_t attend_parts_bytes(const AttendForm &f, int kv_heads, int dim)
     return f.cut && f.shares > 1 ? (size_t)kv_heads * f.shares * (2 * f.columns * (dim + 2) * sizeof(float) + 16) : 0;
 }
 
-// bytes that a call may need, whatever `most` says
+// bytes that a call may need, whatever `most` says: a launch of some of the requests has no more tiles, nor shares, than one of all
 inline size_t attend_most_bytes(int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int dim, bool bits8)
 {
     size_t most = 0;
-    for (int64_t rows : {(int64_t)1, (int64_t)16 / group, (int64_t)32 / group, (int64_t)128 / group, (int64_t)0}) {
-        const AttendForms forms = attend_forms(tokens, group, kv_heads, requests, most_keys, rows, dim, bits8);
-        for (int i = 0; i < forms.n; ++i) {
-            const size_t n = attend_parts_bytes(forms.f[i], kv_heads, dim);
-            if (n > most) most = n;
-        }
+    for (int columns : {16, 32, 128, 256}) {
+        if (columns > 32 && tokens * group <= columns / (columns == 128 ? 4 : 2)) break;  // (no request has so many)
+        const size_t n = attend_parts_bytes(columns <= 32 ? few_form(columns, tokens, group, kv_heads, requests, most_keys, bits8, INT32_MAX)
+                                                          : wide_form(columns, tokens, group, kv_heads, requests, most_keys, dim, 0), kv_heads, dim);
+        if (n > most) most = n;
     }
     return most;
 }
