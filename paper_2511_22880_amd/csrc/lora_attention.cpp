@@ -218,13 +218,15 @@ static lora_status_t check_attention(int32_t tokens, int32_t q_heads, int32_t re
     TRY(check_cache(cache));
     TRY(check_count(tokens, q_heads));
     if (q_heads % cache->kv_heads) return fail(LORA_ERR_SHAPE, "q_heads (%d) is no multiple of kv_heads (%d)", q_heads, cache->kv_heads);
-    if ((int64_t)tokens * q_heads > INT32_MAX) return fail(LORA_ERR_SHAPE, "%d tokens x %d heads do not fit 32 bits", tokens, q_heads);
+    // (a tile's columns are counted past the last one, and requests in equal parts for a work group's threads)
+    if ((int64_t)tokens * q_heads > INT32_MAX - 1024) return fail(LORA_ERR_SHAPE, "%d tokens x %d heads do not fit 32 bits", tokens, q_heads);
+    if (requests > INT32_MAX - 1024) return fail(LORA_ERR_SHAPE, "requests = %d", requests);
     if (requests < 0 || width < 0) return fail(LORA_ERR_INVALID_ARG, "requests = %d, width = %d", requests, width);
     if ((int64_t)width * cache->page_size > INT32_MAX - 2 * LORA_MAX_PAGE)
         return fail(LORA_ERR_SHAPE, "%d pages of %d slots a request: more keys than 32 bits count", width, cache->page_size);
     // (steps of the tiles are counted in 32 bits)
     const int64_t keys = (int64_t)width * cache->page_size;
-    if (lora::most_steps(tokens, q_heads / cache->kv_heads, requests, keys) > INT32_MAX)
+    if (lora::most_steps(tokens, q_heads / cache->kv_heads, requests, keys) >= INT32_MAX)
         return fail(LORA_ERR_SHAPE, "%d tokens x %d heads of %d requests over %lld keys are more work than 32 bits count", tokens, q_heads, requests, (long long)keys);
     return LORA_OK;
 }
@@ -274,6 +276,7 @@ extern "C" lora_status_t lora_attention(const void *q, int64_t q_token, int64_t 
     a.cache = cache_of(cache);
     // (nought times the -infinity of a key that is not seen would be NaN; times 2^-126 scores do not matter either)
     a.scale = std::fmax(std::fabs(scale) * 1.44269504088896340736f, 0x1p-126f);
+    if (!std::isfinite(a.scale)) return fail(LORA_ERR_INVALID_ARG, "scale = %g: too large for its multiple by log2 e", (double)scale);
     a.flip = scale < 0.f ? 0x80008000u : 0u;
     a.slack = std::fmin(8.f / a.scale, 1e38f);
     const lora::AttendForms forms = lora::attend_forms(tokens, a.group, cache->kv_heads, requests, (int64_t)width * cache->page_size, most, cache->head_dim, cache->bits == 8);

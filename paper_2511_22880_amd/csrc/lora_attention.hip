@@ -263,6 +263,9 @@ struct Dealt {
         Request q;
     };
 
+    // Rows that starts in order give are fewer steps; where requests share rows there can be more, and nothing is done.
+    static constexpr uint32_t kTooMany = 0x7FFFFFFFu;
+
     // Every thread of a work group: which(total) says which step of the list is meant, given how many there are (none: `total`, and false is returned).
     template <int THREADS, class Which>
     static __device__ __forceinline__ bool find(const AttendArgs &a, Found &f, Which which, Place &p)
@@ -273,13 +276,13 @@ struct Dealt {
         uint32_t mine = 0, n = 0;  // (steps of this thread's requests; of the last of them)
         for (int r = r0; r < r1; ++r) {
             q = request_at(a, r);
-            mine += n = all(a, tiles(a, q));
+            mine = min(mine + (n = all(a, tiles(a, q))), kTooMany);
         }
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
-            upto += lane >= d ? o : 0;
+            upto = min(upto + (lane >= d ? o : 0), kTooMany);
         }
         if (lane == 63) f.sums[wave] = upto;
         __syncthreads();
@@ -287,11 +290,11 @@ struct Dealt {
 #pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) {
             if (w == wave) upto += total;
-            total += f.sums[w];
+            total = min(total + f.sums[w], kTooMany);
         }
         total = __builtin_amdgcn_readfirstlane(total);
         const uint32_t want = which(total);
-        if (want >= total) return false;
+        if (want >= total || total == kTooMany) return false;
         if (want < upto && want >= upto - mine) {
             int r = r1 - 1;
             uint32_t from = upto - n;

@@ -55,7 +55,8 @@ CASES += [("lora_attention", ATTEND, c, s) for c, s in [
     (dict(scale=math.inf), "INVALID_ARG"), (dict(scale=math.nan), "INVALID_ARG"), (dict(y=None), "INVALID_ARG"), (dict(y=P), "INVALID_ARG"),
     (dict(yt=128), "INVALID_ARG"), (dict(width=1000, ld=1000, work=None), "WORKSPACE"), (dict(width=1000, ld=1000, work=P + 4), "WORKSPACE"),
     (dict(width=1000, ld=1000, nwork=100), "WORKSPACE"),
-    (dict(tokens=1 << 22, requests=1 << 22, width=1 << 17, ld=1 << 17), "SHAPE")]]
+    (dict(tokens=1 << 22, requests=1 << 22, width=1 << 17, ld=1 << 17), "SHAPE"), (dict(requests=(1 << 31) - 1000), "SHAPE"),
+    (dict(tokens=((1 << 31) - 1000) // 4, width=1, ld=1), "SHAPE"), (dict(scale=3e38), "INVALID_ARG")]]
 for name, base in (("lora_cache_append", APPEND), ("lora_attention", ATTEND)):
     CASES += [(name, base, dict(cache=c), s) for c, s in [
         (None, "INVALID_ARG"), (cache(k=None), "INVALID_ARG"), (cache(v=P + 8), "INVALID_ARG"), (cache(bits=4), "INVALID_ARG"), (cache(bits=8), "INVALID_ARG"),

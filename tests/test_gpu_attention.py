@@ -486,6 +486,20 @@ def test_indices_that_fit_nothing_reach_nothing():
     assert all(torch.equal(a, b) for a, b in zip(guard, batch.tensors.values()))
 
 
+@pytest.mark.parametrize("most", [1, 30])
+def test_requests_that_share_rows_without_end(most):
+    """10000 requests that each claim all of 20000 rows over 60000 keys: more steps than 32 bits count, which is found, and nothing is done"""
+    batch = Batch([(1, 60000)], 4, 1, 64, page=1024)
+    n, requests = 20000, 20001
+    batch.q = torch.zeros(n, 4, 64, dtype=BF, device="cuda")
+    batch.y = torch.full_like(batch.q, 9.0)
+    batch.starts, batch.lengths = ints([0, n] * (requests // 2) + [0, n]), ints([60000] * requests)
+    batch.table = batch.table.expand(requests, -1).contiguous()
+    batch.workspace = torch.empty(L.lora_attention_workspace_bytes(n, 4, requests, batch.table.shape[1], batch.cache), dtype=torch.uint8, device="cuda")
+    batch.run(most)
+    assert (batch.y == 9).all()
+
+
 def test_rows_behind_the_last_request_stay_as_they_are():
     for sizes, most in (([(1, 40), (1, 9)], 1), ([(30, 40), (5, 9)], 30), ([(100, 400)], 100)):
         batch = Batch(sizes, 8, 2, 64, spare=5)
