@@ -336,11 +336,16 @@ struct Dealt {
         p.at = 0;
         if (++p.t >= p.s.n) {
             p.t = 0;
-            do {
+            while (true) {
                 if (++p.r >= a.requests) return false;
                 p.q = request_at(a, p.r);
                 p.s = tiles(a, p.q);
-            } while (p.s.n == 0);
+                if (p.s.n > 0) break;
+                // over those behind it that have none either, 64 at a time
+                const int r = p.r + 1 + (int)(threadIdx.x & 63);
+                const uint64_t some = __ballot(r < a.requests && tiles(a, request_at(a, r)).n > 0);
+                p.r += some ? __builtin_ctzll(some) : 64;
+            }
         }
         p.of = steps(a, p.s, p.t);
         return true;

@@ -46,3 +46,56 @@ def test_a_workspace_is_enough_whatever_most_says(rules):
         said = rules.rule_most_bytes(*sizes, dim, bits)
         for rows in (most, 0, 1, max(1, 16 // sizes[1]), max(1, 40 // sizes[1]), max(1, 128 // sizes[1]), max(1, 2 * sizes[0] // sizes[3])):
             assert rules.rule_bytes(*sizes, rows, dim, bits) <= said, (sizes, rows, dim, bits)
+
+
+# Calls that take each kind of launch, which test_gpu_attention_forms.py runs: requests of (rows, keys), most rows as the host says.  8 query heads on 2 key heads.
+LONG = {"cut": 2500, "whole": 300}
+FORMS = {f"few {c} {how}": ([(1, keys), (rows, 40), (0, 9), (rows, keys - 7), (1, 1)], rows) for c, rows in ((16, 4), (32, 8)) for how, keys in LONG.items()}
+FORMS |= {f"wide {c} {how}": ([(rows, keys), (rows, rows), (rows - 3, 80), (1, 17)], rows) for c, rows in ((128, 32), (256, 77)) for how, keys in LONG.items()}
+FORMS |= {f"few 16 {how}, wide {c} {how}": ([(1, keys), (1, 1), (rows, keys), (3, 290), (0, 0), (4, 4), (5, 5), (1, 33), (2, 100), (rows, 90)], rows)
+          for c, rows in ((128, 27), (256, 91)) for how, keys in LONG.items()}
+# .. with a table that has room for more: tiles of many columns have more keys in 16 steps than those of few in 4
+FORMS |= {f"few 16 cut, wide {c} whole": ([(1, 1020), (1, 1), (rows, 1000), (3, 290), (4, 4), (5, 5), (1, 33), (2, 100)], rows) for c, rows in ((128, 31), (256, 300))}
+
+
+def form_of(rules, name, dim, bits, page=16):
+    sizes, most = FORMS[name]
+    keys = -(-max(k for _, k in sizes) // page) * page
+    return rules.rule_forms(sum(n for n, _ in sizes), 4, 2, len(sizes), keys, most, dim, bits).decode()
+
+
+def taken(name, bits):
+    return bits == 16 or name.split(",")[0] != "few 16 cut" or "whole" not in name  # (few columns in 8 bits take 256 keys a step: 1020 are 4)
+
+
+@needs_headers
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("name, bits", [(name, bits) for name in FORMS for bits in (8, 16) if taken(name, bits)])
+def test_these_calls_take_the_launches_they_stand_for(rules, name, dim, bits):
+    assert form_of(rules, name, dim, bits) == name
+
+
+@needs_headers
+def test_no_call_takes_launches_that_are_not_among_them(rules):
+    seen = {rules.rule_forms(*c).decode() for c in calls(20000, seed=2)}
+    # (few columns whole and many cut, by the number of their tiles alone: each is among them)
+    assert {form for forms in seen for form in forms.split(", ")} == {f"{kind} {c} {how}" for kind, c in (("few", 16), ("few", 32), ("wide", 128), ("wide", 256))
+                                                                    for how in ("cut", "whole")}
+    assert set(FORMS) <= seen
+
+
+@needs_headers
+def test_launches_have_work_groups_for_what_there_may_be_and_no_more_than_a_grid_has(rules):
+    """whole tiles: one work group for each that the host cannot rule out; cut ones: a share of a key head's is never empty by rule alone"""
+    for c in calls(20000, seed=3):
+        tokens, group, heads, requests, keys, most, dim, bits = c
+        for i, form in enumerate(rules.rule_forms(*c).decode().split(", ")):
+            columns, shares = int(form.split()[1]), rules.rule_shares(*c, i)
+            assert shares >= 1 and shares * heads * 512 < 2 ** 32
+            if form.endswith("whole"):
+                # requests of one token each, and one of all others
+                filled, up = min(requests, tokens), lambda n: -(-n * group // columns)  # noqa: E731
+                if "," not in rules.rule_forms(*c).decode():
+                    assert shares >= (filled - 1) * up(1) + up(tokens - filled + 1)
+            else:
+                assert shares <= max(1, 512 // heads)
