@@ -102,8 +102,9 @@ lora_status_t lora_cache_append(const void *k, int64_t k_token, int64_t k_head, 
  * [requests + 1]; lengths: device, int32, [requests]; page_table: device, int32, [requests][width], row stride ld_table; tree: device, 8-byte aligned, [tokens].
  * most: the most rows of a request, as far as the host knows (0: it does not): with it the call chooses its tiles, and more rows are no error.
  * workspace: device, 16-byte aligned, of lora_attention_workspace_bytes() or more; its contents are of no account, and calls that may run at the same time need one each.
- * Products are bf16 x bf16 (E4M3 is exact there) with fp32 sums; scores, weights' sum and the running maximum are fp32; a weight, times its value's
- * scale in 8 bits, is rounded to bf16 for its product with v, relative to the largest so far; y is rounded once.  The same call gives the same bits. */
+ * Products are bf16 x bf16 (E4M3 is exact there) with fp32 sums; scores, weights' sum and the running maximum are fp32.  Weights are relative to a maximum that may lag behind the true
+ * one by 2^8, and a weight (in 8 bits times its value's scale) is rounded to bf16 for its product with v; in bf16 the weights' sum is of the rounded ones; y is rounded once.
+ * scale: finite, and so are its multiple by log2 e and that times any score; a negative one is one of -q.  The same call gives the same bits. */
 lora_status_t lora_attention_workspace_bytes(int32_t tokens, int32_t q_heads, int32_t requests, int32_t width, const lora_cache_t *cache,
                                              size_t *bytes);
 lora_status_t lora_attention(const void *q, int64_t q_token, int64_t q_head, int32_t tokens, int32_t q_heads, const int32_t *starts,

@@ -15,6 +15,9 @@ static __device__ __forceinline__ float value_hi(uint32_t u) { return __uint_as_
 // are turned (half layout: the pieces are dims / 2 apart), or elements that pass.  A work group has as many consecutive rows as its threads hold; it asks for all of them, computes the
 // cosines and sines of its few tokens once into LDS (a pair's angle for all heads at once: 64 angles a token, not 64 a head), and turns.  The angle is the low
 // 64 bits of position * turns, of which the upper 32 count: exact to 2^-31 turns at any position, without a division or a table of positions.
+// Bound by memory where there is much: 19675 tokens x 32 heads of 128, 322 MB, 56 us (5.7 TB/s, a half written); the same tokens' q, k and v into a cache in 8 bits, 445 MB,
+// 87 us (5.1 TB/s: the maxima, quotients and conversions of k and v do not all hide).  One token 3.4 us, 256 tokens 4.5.  Four rows of a thread one after the other: 62 and 105 us; two: 55 and 90;
+// loads and stores past the caches 72 to 80 and level.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTurnThreads = 256;
 
@@ -177,8 +180,9 @@ hipError_t launch_turn(const TurnArgs &a, hipStream_t stream)
 // How the work of an attention call is dealt out.  A request's columns (row by row, the query heads of a key head's group side by side) are cut into tiles of
 // TC; a tile takes as many steps of KEYS keys as its last row sees, one at least.  The steps of all tiles of all requests, in that order, are one list for every key
 // head, and a head's `shares` work groups take equal runs of it.  A run that has all of a tile's steps writes its rows; otherwise it leaves sums, which
-// k_attend_join brings together.  Where no tile has many steps (see attend_form) none is cut, and every tile has a work group.  The list follows from starts and lengths on the device alone: every work group adds up the requests' steps and finds
-// its place in it, so the host need not know any length, and a captured call follows them.
+// k_attend_join brings together.  Where no tile has many steps (see attend_form) none is cut, and every tile has a work group.  The list follows from starts and lengths on the device
+// alone: every work group adds up the requests' steps and finds its place in it, so the host need not know any length, and a captured call follows them: one trip to
+// memory before the first page number.
 // ------------------------------------------------------------------------------------------------
 struct Request {
     int first, n, keys;  // first row, rows, keys
@@ -390,6 +394,13 @@ static __device__ __forceinline__ int64_t part_of(int head, int shares, int shar
 // holds a column's scores of eight keys, and those are what O^T = V^T P^T takes as the operand of eight values of k from that lane, if row m of the score
 // tile t is key 8 (m / 4) + 4 t + m mod 4 and lane (quad, n) brings the keys 8 quad .. 8 quad + 7.  It reads their dims [n D / 16, (n + 1) D / 16): sixteen
 // lanes a whole row of v; the element c of each is the operand of tile c, whose row n is dim n D / 16 + c, put together by byte permutes.
+//
+// The maximum that weights are relative to follows only when a score passes it by more than 2^8 (`slack`): weights are up to 2^8 then, which bf16 and fp32 hold as well as 1, and the sums
+// are not rescaled at every step.  A weight is rounded to bf16 for its product with v, half a step of its own value, and in bf16 caches the sum is of the rounded ones: y is then a mean by
+// weights that add up to one exactly.  In 8 bits the value's scale goes into the weight before that rounding, so the sum is of those before.
+//
+// Bound by memory.  256 requests of 200 to 8000 keys in bf16, 2.29 GB: 388 us, 5.9 TB/s; five of 60,000 to 130,000 in 8 bits, 810 MB: 138 us, 5.9 TB/s.  The loads alone, nothing computed:
+// 403 against 410 then, and 140 against 157.  Loads of what is read once go past the caches (400 against 408).
 // ------------------------------------------------------------------------------------------------
 template <int BYTES>
 struct Bytes;
@@ -436,8 +447,6 @@ static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t u)
 {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HIGH));
 }
-
-
 
 // eight bf16 values with their signs exchanged where `flip` says so
 static __device__ __forceinline__ uint4 flipped(uint4 u, uint32_t flip) { return uint4{u.x ^ flip, u.y ^ flip, u.z ^ flip, u.w ^ flip}; }
@@ -893,7 +902,12 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
 // 8 i + 4 h + 0 .. 3 of those; as in k_attend_few they become an operand where they are, for V^T is laid out by the same order of keys: piece (2 ks + h) of a dim's row
 // has the keys 16 ks + 4 h + {0 .. 3, 8 .. 11}.  Half of the wavefronts fetch V and half K, through registers, a step ahead: V is turned there (a thread has 8 keys x
 // kDimsV dims), 8-bit values become bf16 there, once for all wavefronts.  In LDS 16-byte pieces of a row are exchanged by its number so that neither writes nor reads
-// of eight lanes meet in a bank.
+// of eight lanes meet in a bank.  Maxima and roundings are k_attend_few's.
+//
+// Bound by the matrix units and the exponentials between them, which one wavefront's order of instructions and the two on a SIMD overlap in part: pieces of 2000 to 4096 rows behind 4000 to
+// 16000 keys, 961 GFLOP, 1030 us, 0.93 PFLOP/s (a large library product 1.23); the matrix units are busy 42 % of the cycles.  The order laid down in `take` took it from 1200.  Trees of
+// 8 to 24 tokens, 289 MB: 67 us, 4.3 TB/s, by the 64 KB that a compute unit's two work groups have on the way (registers are full: 64 keys more would spill).  64 columns a
+// wavefront instead of 32, half as many reads of LDS a product: 2066 to 2700 against 1435 then, one wavefront a SIMD; loads past the caches 1202 against 1080.
 // ------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
@@ -1288,7 +1302,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
 }
 
 // Tiles that several shares have a part of: a work group has CW columns of the one that a share began and did not end.  16 / CW groups of threads share the parts,
-// four of which a thread asks for at a time.
+// four of which a thread asks for at a time.  Bound by its own start and three trips to memory: 2.6 to 5 us behind few columns, 6 to 15 behind many (256 columns of
+// 128 dims are 133 KB a part; 28 MB of them behind the trees of k_attend_wide's comment, 8 us).  Done by the last share to end instead, it would need counters that someone has cleared.
 template <int D, int TC, int CW>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
 {
@@ -1355,11 +1370,15 @@ template <int D, int TC>
 static hipError_t launch_join(const AttendArgs &a, hipStream_t stream)
 {
     const unsigned ends = (unsigned)(a.shares - 1) * a.cache.kv_heads;
-    // few requests among many shares: a tile has many parts
-    if (TC <= 64 && 4 * a.requests < a.shares)
-        hipLaunchKernelGGL((k_attend_join<D, TC, 4>), dim3(ends, TC / 4), dim3(256), 0, stream, a);
-    else
-        hipLaunchKernelGGL((k_attend_join<D, TC, 16>), dim3(ends, TC / 16), dim3(256), 0, stream, a);
+    // Columns of a work group, 4 / 16, us a call.  Few requests among many shares, whose tiles have many parts: one token of 1500 keys 10.5 / 11.0, five long requests 142.2 / 143.4; more requests: 42 trees of up
+    // to 7 tokens 35.8 / 34.4, 83 of 2 48.6 / 47.6; tiles of many columns: trees 79 / 76 and 79 / 74.
+    if constexpr (TC <= 32) {
+        if (4 * (int64_t)a.requests < a.shares) {
+            hipLaunchKernelGGL((k_attend_join<D, TC, 4>), dim3(ends, TC / 4), dim3(256), 0, stream, a);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((k_attend_join<D, TC, 16>), dim3(ends, TC / 16), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

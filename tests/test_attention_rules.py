@@ -50,12 +50,13 @@ def test_a_workspace_is_enough_whatever_most_says(rules):
 
 # Calls that take each kind of launch, which test_gpu_attention_forms.py runs: requests of (rows, keys), most rows as the host says.  8 query heads on 2 key heads.
 LONG = {"cut": 2500, "whole": 300}
+MORE = [(1, 7 * i + 1) for i in range(28)]  # (up to 32 requests with little to read are one launch, and up to 256 of few steps here)
 FORMS = {f"few {c} {how}": ([(1, keys), (rows, 40), (0, 9), (rows, keys - 7), (1, 1)], rows) for c, rows in ((16, 4), (32, 8)) for how, keys in LONG.items()}
 FORMS |= {f"wide {c} {how}": ([(rows, keys), (rows, rows), (rows - 3, 80), (1, 17)], rows) for c, rows in ((128, 32), (256, 77)) for how, keys in LONG.items()}
-FORMS |= {f"few 16 {how}, wide {c} {how}": ([(1, keys), (1, 1), (rows, keys), (3, 290), (0, 0), (4, 4), (5, 5), (1, 33), (2, 100), (rows, 90)], rows)
+FORMS |= {f"few 16 {how}, wide {c} {how}": ([(1, keys), (1, 1), (rows, keys), (3, 290), (0, 0), (4, 4), (5, 5), (1, 33), (2, 100), (rows, 90)] + MORE * (10 if how == "whole" else 1), rows)
           for c, rows in ((128, 27), (256, 91)) for how, keys in LONG.items()}
 # .. with a table that has room for more: tiles of many columns have more keys in 16 steps than those of few in 4
-FORMS |= {f"few 16 cut, wide {c} whole": ([(1, 1020), (1, 1), (rows, 1000), (3, 290), (4, 4), (5, 5), (1, 33), (2, 100)], rows) for c, rows in ((128, 31), (256, 300))}
+FORMS |= {f"few 16 cut, wide {c} whole": ([(1, 1020), (1, 1), (rows, 1000), (3, 290), (4, 4), (5, 5), (1, 33), (2, 100)] + MORE, rows) for c, rows in ((128, 31), (256, 300))}
 
 
 def form_of(rules, name, dim, bits, page=16):
