@@ -399,7 +399,7 @@ static __device__ __forceinline__ int64_t part_of(int head, int shares, int shar
 // are not rescaled at every step.  A weight is rounded to bf16 for its product with v, half a step of its own value, and in bf16 caches the sum is of the rounded ones: y is then a mean by
 // weights that add up to one exactly.  In 8 bits the value's scale goes into the weight before that rounding, so the sum is of those before.
 //
-// Bound by memory.  256 requests of 200 to 8000 keys in bf16, 2.29 GB: 388 us, 5.9 TB/s; five of 60,000 to 130,000 in 8 bits, 810 MB: 138 us, 5.9 TB/s.  The loads alone, nothing computed:
+// Bound by memory.  256 requests of 200 to 8000 keys in bf16, 2.29 GB: 388 to 398 us, 5.8 to 5.9 TB/s; five of 60,000 to 130,000 in 8 bits, 810 MB: 138 us, 5.9 TB/s.  The loads alone, nothing computed:
 // 403 against 410 then, and 140 against 157.  Loads of what is read once go past the caches (400 against 408).
 // ------------------------------------------------------------------------------------------------
 template <int BYTES>
@@ -905,7 +905,7 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
 // of eight lanes meet in a bank.  Maxima and roundings are k_attend_few's.
 //
 // Bound by the matrix units and the exponentials between them, which one wavefront's order of instructions and the two on a SIMD overlap in part: pieces of 2000 to 4096 rows behind 4000 to
-// 16000 keys, 961 GFLOP, 1030 us, 0.93 PFLOP/s (a large library product 1.23); the matrix units are busy 42 % of the cycles.  The order laid down in `take` took it from 1200.  Trees of
+// 16000 keys, 961 GFLOP, 1027 to 1054 us, 0.91 to 0.94 PFLOP/s (a large library product 1.23); the matrix units are busy 42 % of the cycles.  The order laid down in `take` took it from 1200.  Trees of
 // 8 to 24 tokens, 289 MB: 67 us, 4.3 TB/s, by the 64 KB that a compute unit's two work groups have on the way (registers are full: 64 keys more would spill).  64 columns a
 // wavefront instead of 32, half as many reads of LDS a product: 2066 to 2700 against 1435 then, one wavefront a SIMD; loads past the caches 1202 against 1080.
 // ------------------------------------------------------------------------------------------------
