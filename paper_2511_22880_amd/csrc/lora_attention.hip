@@ -11,13 +11,13 @@ static __device__ __forceinline__ float value_lo(uint32_t u) { return __uint_as_
 static __device__ __forceinline__ float value_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
 
 // ------------------------------------------------------------------------------------------------
-// Rows turned by their positions.  A row is (token, head), heads counted over q, k and v; a thread has 16 elements of one, two pieces of 8: eight pairs that
-// are turned (half layout: the pieces are dims / 2 apart), or elements that pass.  A work group has as many consecutive rows as its threads hold; it asks for all of them, computes the
-// cosines and sines of its few tokens once into LDS (a pair's angle for all heads at once: 64 angles a token, not 64 a head), and turns.  The angle is the low
-// 64 bits of position * turns, of which the upper 32 count: exact to 2^-31 turns at any position, without a division or a table of positions.
-// Bound by memory where there is much: 19675 tokens x 32 heads of 128, 322 MB, 56 us (5.7 TB/s, a half written); the same tokens' q, k and v into a cache in 8 bits, 445 MB,
-// 87 us (5.1 TB/s: the maxima, quotients and conversions of k and v do not all hide).  One token 3.4 us, 256 tokens 4.5.  Four rows of a thread one after the other: 62 and 105 us; two: 55 and 90;
-// loads and stores past the caches 72 to 80 and level.
+// Rows turned by their positions.  A row is (token, head), heads counted over q, k and v; a thread has 16 elements of one, two pieces of 8: eight pairs that are turned
+// (half layout: the pieces are dims / 2 apart), or elements that pass.  A work group has as many consecutive rows as its threads hold; it asks for all of them,
+// computes the cosines and sines of its few tokens once into LDS (a pair's angle for all heads at once: 64 angles a token, not 64 a head), and turns.  The angle is the
+// low 64 bits of position * turns, of which the upper 32 count: exact to 2^-31 turns at any position, without a division or a table of positions. Bound by memory where
+// there is much: 19675 tokens x 32 heads of 128, 322 MB, 56 us (5.7 TB/s, a half written); the same tokens' q, k and v into a cache in 8 bits, 445 MB, 87 us (5.1 TB/s:
+// the maxima, quotients and conversions of k and v do not all hide).  One token 3.4 us, 256 tokens 4.5.  Four rows of a thread one after the other: 62 and 105 us; two:
+// 55 and 90; loads and stores past the caches 72 to 80 and level.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTurnThreads = 256;
 
@@ -177,10 +177,10 @@ hipError_t launch_turn(const TurnArgs &a, hipStream_t stream)
 }
 
 // ------------------------------------------------------------------------------------------------
-// How the work of an attention call is dealt out.  A request's columns (row by row, the query heads of a key head's group side by side) are cut into tiles of
-// TC; a tile takes as many steps of KEYS keys as its last row sees, one at least.  The steps of all tiles of all requests, in that order, are one list for every key
-// head, and a head's `shares` work groups take equal runs of it.  A run that has all of a tile's steps writes its rows; otherwise it leaves sums, which
-// k_attend_join brings together.  Where no tile has many steps (see attend_form) none is cut, and every tile has a work group.  The list follows from starts and lengths on the device
+// How the work of an attention call is dealt out.  A request's columns (row by row, the query heads of a key head's group side by side) are cut into tiles of TC; a
+// tile takes as many steps of KEYS keys as its last row sees, one at least.  The steps of all tiles of all requests, in that order, are one list for every key head,
+// and a head's `shares` work groups take equal runs of it.  A run that has all of a tile's steps writes its rows; otherwise it leaves sums, which k_attend_join brings
+// together.  Where no tile has many steps (see attend_form) none is cut, and every tile has a work group.  The list follows from starts and lengths on the device
 // alone: every work group adds up the requests' steps and finds its place in it, so the host need not know any length, and a captured call follows them: one trip to
 // memory before the first page number.
 // ------------------------------------------------------------------------------------------------
@@ -389,18 +389,19 @@ static __device__ __forceinline__ void leave_cut(const AttendArgs &a, CutTile *t
 static __device__ __forceinline__ int64_t part_of(int head, int shares, int share, bool begins) { return ((int64_t)head * shares + share) * 2 + begins; }
 
 // ------------------------------------------------------------------------------------------------
-// Attention of few columns: tiles of 16 C.  A wavefront takes 32 keys (8 bits: twice) at a time, the work group's four as many times that, each with a running maximum and sum of its own; what
-// they have is brought together in LDS at the tile's end.  Nothing goes through LDS on the way: with S^T = K Q^T (16 x 16 x 32 matrix instructions) a lane
-// holds a column's scores of eight keys, and those are what O^T = V^T P^T takes as the operand of eight values of k from that lane, if row m of the score
-// tile t is key 8 (m / 4) + 4 t + m mod 4 and lane (quad, n) brings the keys 8 quad .. 8 quad + 7.  It reads their dims [n D / 16, (n + 1) D / 16): sixteen
+// Attention of few columns: tiles of 16 C.  A wavefront takes 32 keys (8 bits: twice) at a time, the work group's four as many times that, each with a running maximum
+// and sum of its own; what they have is brought together in LDS at the tile's end.  Nothing goes through LDS on the way: with S^T = K Q^T (16 x 16 x 32 matrix
+// instructions) a lane holds a column's scores of eight keys, and those are what O^T = V^T P^T takes as the operand of eight values of k from that lane, if row m of
+// the score tile t is key 8 (m / 4) + 4 t + m mod 4 and lane (quad, n) brings the keys 8 quad .. 8 quad + 7.  It reads their dims [n D / 16, (n + 1) D / 16): sixteen
 // lanes a whole row of v; the element c of each is the operand of tile c, whose row n is dim n D / 16 + c, put together by byte permutes.
 //
-// The maximum that weights are relative to follows only when a score passes it by more than 2^8 (`slack`): weights are up to 2^8 then, which bf16 and fp32 hold as well as 1, and the sums
-// are not rescaled at every step.  A weight is rounded to bf16 for its product with v, half a step of its own value, and in bf16 caches the sum is of the rounded ones: y is then a mean by
-// weights that add up to one exactly.  In 8 bits the value's scale goes into the weight before that rounding, so the sum is of those before.
+// The maximum that weights are relative to follows only when a score passes it by more than 2^8 (`slack`): weights are up to 2^8 then, which bf16 and fp32 hold as well
+// as 1, and the sums are not rescaled at every step.  A weight is rounded to bf16 for its product with v, half a step of its own value, and in bf16 caches the sum is
+// of the rounded ones: y is then a mean by weights that add up to one exactly.  In 8 bits the value's scale goes into the weight before that rounding, so the sum is of
+// those before.
 //
-// Bound by memory.  256 requests of 200 to 8000 keys in bf16, 2.29 GB: 388 to 398 us, 5.8 to 5.9 TB/s; five of 60,000 to 130,000 in 8 bits, 810 MB: 138 us, 5.9 TB/s.  The loads alone, nothing computed:
-// 403 against 410 then, and 140 against 157.  Loads of what is read once go past the caches (400 against 408).
+// Bound by memory.  256 requests of 200 to 8000 keys in bf16, 2.29 GB: 388 to 398 us, 5.8 to 5.9 TB/s; five of 60,000 to 130,000 in 8 bits, 810 MB: 138 us, 5.9 TB/s.
+// The loads alone, nothing computed: 403 against 410 then, and 140 against 157.  Loads of what is read once go past the caches (400 against 408).
 // ------------------------------------------------------------------------------------------------
 template <int BYTES>
 struct Bytes;
@@ -900,14 +901,18 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
 // Attention of many columns: tiles of 32 a wavefront, whose four or eight wavefronts share the keys and values of a step in LDS: 64 keys of 128 dims, or 128 of 64.
 // S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16 matrix instructions, 32 keys at a time.  A lane (half h, column n) ends up with the scores of keys
 // 8 i + 4 h + 0 .. 3 of those; as in k_attend_few they become an operand where they are, for V^T is laid out by the same order of keys: piece (2 ks + h) of a dim's row
-// has the keys 16 ks + 4 h + {0 .. 3, 8 .. 11}.  Half of the wavefronts fetch V and half K, through registers, a step ahead: V is turned there (a thread has 8 keys x
+// has the keys 16 ks + 4 h + {0 .. 3, 8 .. 11}.  Half of the wavefronts fetch V and half K, through registers, a step ahead of LDS: V is turned there (a thread has 8 keys x
 // kDimsV dims), 8-bit values become bf16 there, once for all wavefronts.  In LDS 16-byte pieces of a row are exchanged by its number so that neither writes nor reads
 // of eight lanes meet in a bank.  Maxima and roundings are k_attend_few's.
 //
-// Bound by the matrix units and the exponentials between them, which one wavefront's order of instructions and the two on a SIMD overlap in part: pieces of 2000 to 4096 rows behind 4000 to
-// 16000 keys, 961 GFLOP, 1027 to 1054 us, 0.91 to 0.94 PFLOP/s (a large library product 1.23); the matrix units are busy 42 % of the cycles.  The order laid down in `take` took it from 1200.  Trees of
-// 8 to 24 tokens, 289 MB: 67 us, 4.3 TB/s, by the 64 KB that a compute unit's two work groups have on the way (registers are full: 64 keys more would spill).  64 columns a
-// wavefront instead of 32, half as many reads of LDS a product: 2066 to 2700 against 1435 then, one wavefront a SIMD; loads past the caches 1202 against 1080.
+// Bound by one wavefront's chain of instructions and the two on a SIMD, which overlap products and the rest in part only: pieces of 2000 to 4096 rows behind 4000 to
+// 16000 keys, 961 GFLOP, 1020 to 1040 us, 0.92 to 0.94 PFLOP/s (a large library product 1.23).  Of an earlier 1035 us the exponentials were 65, putting keys and values
+// into LDS 135 and asking for them 125, though they were near (the same keys over and over: level).  So addresses come from lanes that have them (by a few instructions
+// on one lane's value: trees 75.7 to 72.8), and eight wavefronts wait for each other every second step (with that 1065 to 1035; 131 KB of LDS, which one work group a
+// compute unit has to itself).  The order laid down in `take` took it from 1200.  Trees of 8 to 24 tokens, 289 MB: 64 us, 4.5 TB/s, by the 64 KB that a compute unit's
+// two work groups have on the way (registers are full: 64 keys more would spill).  64 columns a wavefront instead of 32, half as many reads of LDS a product: 2066 to
+// 2700 against 1435 then, one wavefront a SIMD; loads past the caches 1202 against 1080.  32 keys at a time with the exponentials beside the next ones' products: 1033
+// against 1023, trees 76 against 73.6; the wavefronts that bring K doing so behind their products, those that bring V before: 1046 against 1030.
 // ------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
@@ -941,8 +946,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
     constexpr int TC = 32 * WAVES, KEYS = S::kKeys;
     using W = Dealt<TC, KEYS>;
     __shared__ typename W::Found found;
-    __shared__ __attribute__((aligned(16))) char ks[2][16384], vs[2][16384];
-    __shared__ __attribute__((aligned(16))) float scales[F8 ? 2 : 1][2][F8 ? KEYS : 4];
+    constexpr int kBuffers = WAVES == 8 ? 4 : 2, kAhead = kBuffers / 2;  // steps that are in LDS; half of them are being read, and the wavefronts wait for each other once they were
+    __shared__ __attribute__((aligned(16))) char ks[kBuffers][16384], vs[kBuffers][16384];
+    __shared__ __attribute__((aligned(16))) float scales[F8 ? kBuffers : 1][2][F8 ? KEYS : 4];
     __shared__ OddSteps odd;
     if (threadIdx.x == 0) odd.clear(0);
     int turn = 0;
@@ -1012,14 +1018,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
         };
         uint32_t held[S::kHeld];  // fetched for the next step: of K, or of V (a key's after the other's)
         float sr[2];
-        auto row_of = [&](int id, uint32_t j, int group) __attribute__((always_inline)) {  // of the cache, of the first of 16 keys
-            const int in = ((int)j * KEYS + 16 * group) & (page - 1);
-            return ((int64_t)max(id, 0) * a.cache.kv_heads + kh) * page + in;
+        // rows of the cache in front of a lane's 16 keys (as page_of); one wavefront's loads take a lane's value as theirs
+        auto rows_of = [&](int id, uint32_t j) __attribute__((always_inline)) {
+            const int in = ((int)j * KEYS + 16 * (lane & (S::kGroups - 1))) & (page - 1);
+            return (((int64_t)max(id, 0) * a.cache.kv_heads + kh) << a.cache.page_shift) + in;
+        };
+        auto lane_of = [&](int64_t v, int of) __attribute__((always_inline)) {
+            return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), of) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, of));
+        };
+        auto any_lane_of = [&](int64_t v, int of) __attribute__((always_inline)) {
+            return (int64_t)((uint64_t)(uint32_t)__shfl((int)(v >> 32), of, 64) << 32 | (uint32_t)__shfl((int)v, of, 64));
         };
         auto fetch = [&](int ids, uint32_t j) __attribute__((always_inline)) {
+            const int64_t rows = rows_of(ids, j);
             if (loads_v) {
-                const int group = v_kg >> 1, id = __shfl(ids, group, 64);
-                const char *at = a.cache.v + (row_of(id, j, group) + 4 * (v_kg & 1)) * S::kRow + v_dims * (F8 ? 1 : 2);
+                const uint32_t in = (4 * (v_kg & 1)) * S::kRow + v_dims * (F8 ? 1 : 2);
+                const char *at;
+                if constexpr (2 * kWide >= 64)
+                    at = a.cache.v + lane_of(rows, wave * (64 / kWide) >> 1) * S::kRow + in;
+                else
+                    at = a.cache.v + any_lane_of(rows, v_kg >> 1) * S::kRow + in;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const auto got = ld_bytes<4 * S::kWordsV>(at + (i < 4 ? i : i + 4) * S::kRow);
@@ -1028,20 +1046,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                 }
                 asm volatile("; values");  // (the two ways end differently: the compiler would else join their loads, a register at a time)
             } else {
+                const uint32_t in = k_row * S::kRow + 16 * k_piece;
 #pragma unroll
                 for (int i = 0; i < S::kLoadsK; ++i) {
-                    const int first = k_first + i * kRows, group = first >> 4, id = __builtin_amdgcn_readlane(ids, group);
-                    const auto got = ld_bytes<16>(a.cache.k + (row_of(id, j, group) + (first & 15) + k_row) * S::kRow + 16 * k_piece);
+                    const int first = k_first + i * kRows;
+                    const auto got = ld_bytes<16>(a.cache.k + (lane_of(rows, first >> 4) + (first & 15)) * S::kRow + in);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) held[4 * i + x] = got.w[x];
                 }
                 asm volatile("; keys");
             }
             if constexpr (F8) {
-                const int key = tid & (KEYS - 1), group = key >> 4, id = __shfl(ids, group, 64);
-                const int64_t row = row_of(id, j, group) + (key & 15);
-                sr[0] = a.cache.k_scales[row];
-                sr[1] = a.cache.v_scales[row];
+                if (tid < KEYS) {
+                    const int64_t row = any_lane_of(rows, tid >> 4) + (tid & 15);
+                    sr[0] = a.cache.k_scales[row];
+                    sr[1] = a.cache.v_scales[row];
+                }
             }
         };
         // ids: of the step that was fetched
@@ -1136,21 +1156,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                 f32x16 s[2];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[0][e] = s[1][e] = 0.f;
+                constexpr int kHalf = S::kSteps / 2;
 #pragma unroll
-                for (int x = 0; x < S::kSteps; ++x) k[x] = read_k(2 * u, x);
+                for (int x = 0; x < S::kSteps; ++x) k[x] = read_k(2 * u + (x & 1), x >> 1);
                 __builtin_amdgcn_sched_barrier(0);
+                // (the two tiles' products in turn: the next one of a sum would wait for the one before; trees 73.6 to 72.2 us)
 #pragma unroll
-                for (int x = 0; x < S::kSteps; ++x) {
-                    s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[x], q[x], s[0], 0, 0, 0);
-                    k[x] = read_k(2 * u + 1, x);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int x = 0; x < S::kSteps; ++x)
 #pragma unroll
-                for (int x = 0; x < S::kSteps; ++x) {
-                    s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[x], q[x], s[1], 0, 0, 0);
-                    if (kEarly && x < kPv) v[x] = read_v(2 * u, x);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                    for (int y = 0; y < 2; ++y) {
+                        bf16x8 &at = k[2 * (x % kHalf) + y];
+                        s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at, q[x], s[y], 0, 0, 0);
+                        if (x < kHalf)
+                            at = read_k(2 * u + y, x + kHalf);
+                        else if (kEarly && 2 * (x - kHalf) + y < kPv)
+                            v[2 * (x - kHalf) + y] = read_v(2 * u, 2 * (x - kHalf) + y);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 [[maybe_unused]] float4 by_v[4];
                 uint32_t seen[2];
 #pragma unroll
@@ -1240,24 +1262,29 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
             }
         };
         if (p.q.keys > 0) {
-            int now = page_of(p.at), then = page_of(p.at + 1 < to ? p.at + 1 : p.at);
-            fetch(now, p.at);
-            stage(now, p.at, 0);
-            if (p.at + 1 < to) fetch(then, p.at + 1);
+            int ids[kAhead + 1];  // pages of the steps from j on
+#pragma unroll
+            for (int i = 0; i <= kAhead; ++i) ids[i] = page_of(p.at + i < to ? p.at + i : to - 1);
+#pragma unroll
+            for (int i = 0; i <= kAhead; ++i)
+                if (p.at + i < to) {
+                    fetch(ids[i], p.at + i);
+                    if (i < kAhead) stage(ids[i], p.at + i, i);
+                }
             __syncthreads();
             for (uint32_t j = p.at; j < to; ++j) {
-                const int b = (j - p.at) & 1;
-                const uint32_t j1 = j + 1 < to ? j + 1 : j, j2 = j + 2 < to ? j + 2 : j1;
-                const int after = page_of(j2);
+                const int b = (j - p.at) & (kBuffers - 1);
+                const int after = page_of(j + kAhead + 1 < to ? j + kAhead + 1 : to - 1);
                 const int key0 = (int)j * KEYS;
-                const uint64_t none = __ballot(now < 0);
+                const uint64_t none = __ballot(ids[0] < 0);
                 const bool plain = none == 0 && key0 + KEYS <= open;
-                if (j + 1 < to) stage(then, j1, b ^ 1);
-                if (j + 2 < to) fetch(after, j2);
+                if (j + kAhead < to) stage(ids[kAhead], j + kAhead, b ^ kAhead);
+                if (j + kAhead + 1 < to) fetch(after, j + kAhead + 1);
                 if (busy) take(plain, b, key0, none);
-                __syncthreads();
-                now = then;
-                then = after;
+                if ((b & (kAhead - 1)) == kAhead - 1) __syncthreads();
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) ids[i] = ids[i + 1];
+                ids[kAhead] = after;
             }
         } else {
             __syncthreads();  // (what the tile before noted in `odd` has been read by all, and is cleared below)
@@ -1301,9 +1328,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
     }
 }
 
-// Tiles that several shares have a part of: a work group has CW columns of the one that a share began and did not end.  16 / CW groups of threads share the parts,
-// four of which a thread asks for at a time.  Bound by its own start and three trips to memory: 2.6 to 5 us behind few columns, 6 to 15 behind many (256 columns of
-// 128 dims are 133 KB a part; 28 MB of them behind the trees of k_attend_wide's comment, 8 us).  Done by the last share to end instead, it would need counters that someone has cleared.
+// Tiles that several shares have a part of: a work group has CW columns of the one that a share began and did not end.  16 / CW groups of threads share the parts, four
+// of which a thread asks for at a time.  Bound by its own start and three trips to memory: 2.6 to 5 us behind few columns, 6 to 15 behind many (256 columns of 128 dims
+// are 133 KB a part; 28 MB of them behind the trees of k_attend_wide's comment, 8 us).  Done by the last share to end instead, it would need counters that someone has
+// cleared.
 template <int D, int TC, int CW>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a)
 {
@@ -1370,8 +1398,8 @@ template <int D, int TC>
 static hipError_t launch_join(const AttendArgs &a, hipStream_t stream)
 {
     const unsigned ends = (unsigned)(a.shares - 1) * a.cache.kv_heads;
-    // Columns of a work group, 4 / 16, us a call.  Few requests among many shares, whose tiles have many parts: one token of 1500 keys 10.5 / 11.0, five long requests 142.2 / 143.4; more requests: 42 trees of up
-    // to 7 tokens 35.8 / 34.4, 83 of 2 48.6 / 47.6; tiles of many columns: trees 79 / 76 and 79 / 74.
+    // Columns of a work group, 4 / 16, us a call.  Few requests among many shares, whose tiles have many parts: one token of 1500 keys 10.5 / 11.0, five long
+    // requests 142.2 / 143.4; more requests: 42 trees of up to 7 tokens 35.8 / 34.4, 83 of 2 48.6 / 47.6; tiles of many columns: trees 79 / 76 and 79 / 74.
     if constexpr (TC <= 32) {
         if (4 * (int64_t)a.requests < a.shares) {
             hipLaunchKernelGGL((k_attend_join<D, TC, 4>), dim3(ends, TC / 4), dim3(256), 0, stream, a);
