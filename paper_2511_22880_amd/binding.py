@@ -1182,7 +1182,7 @@ def lora_attention(q, starts, lengths, page_table, cache: Cache, y, workspace=No
         _ints("lengths", lengths, requests, device)
     pt = None
     if tree is not None:
-        if tree.element_size() != 8 or tree.is_floating_point() or tree.numel() < n or not tree.is_contiguous() or tree.get_device() != device:
+        if tree.element_size() != 8 or tree.is_floating_point() or tree.is_complex() or tree.numel() < n or not tree.is_contiguous() or tree.get_device() != device:
             raise ValueError(f"tree: {tuple(tree.shape)} of {tree.dtype} on {tree.device} does not do: {n} contiguous words of 64 bits are meant")
         pt = tree.data_ptr()
     if workspace is None:

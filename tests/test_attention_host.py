@@ -237,6 +237,13 @@ def test_the_binding_refuses(call, name, wrong, told):
     assert not told
 
 
+def test_the_binding_refuses_words_of_ancestors_that_are_no_integers(told):
+    for dtype in (torch.complex64, torch.float64, torch.int32):
+        with pytest.raises(ValueError, match="tree"):
+            L.lora_attention(**dict(good()["lora_attention"], tree=torch.zeros(3, dtype=dtype).as_subclass(OnGpu)))
+    assert not told
+
+
 def test_the_binding_refuses_a_call_from_another_current_device(told, monkeypatch):
     monkeypatch.setattr(L, "_current_device", lambda: 1)
     for call, given in good().items():
