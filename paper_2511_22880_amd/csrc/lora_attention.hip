@@ -906,7 +906,7 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
 // of eight lanes meet in a bank.  Maxima and roundings are k_attend_few's.
 //
 // Bound by one wavefront's chain of instructions and the two on a SIMD, which overlap products and the rest in part only: pieces of 2000 to 4096 rows behind 4000 to
-// 16000 keys, 961 GFLOP, 1020 to 1040 us, 0.92 to 0.94 PFLOP/s (a large library product 1.23).  Of an earlier 1035 us the exponentials were 65, putting keys and values
+// 16000 keys, 961 GFLOP, 990 to 1040 us, 0.92 to 0.97 PFLOP/s (a large library product 1.23).  Of an earlier 1035 us the exponentials were 65, putting keys and values
 // into LDS 135 and asking for them 125, though they were near (the same keys over and over: level).  So addresses come from lanes that have them (by a few instructions
 // on one lane's value: trees 75.7 to 72.8), and eight wavefronts wait for each other every second step (with that 1065 to 1035; 131 KB of LDS, which one work group a
 // compute unit has to itself).  The order laid down in `take` took it from 1200.  Trees of 8 to 24 tokens, 289 MB: 64 us, 4.5 TB/s, by the 64 KB that a compute unit's
@@ -1160,6 +1160,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
 #pragma unroll
                 for (int x = 0; x < S::kSteps; ++x) k[x] = read_k(2 * u + (x & 1), x >> 1);
                 __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);  // products before what else the SIMD's other wavefront has (pieces 1002 to 989 us, large trees 72.5 to 70.1)
                 // (the two tiles' products in turn: the next one of a sum would wait for the one before; trees 73.6 to 72.2 us)
 #pragma unroll
                 for (int x = 0; x < S::kSteps; ++x)
@@ -1173,6 +1174,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                             v[2 * (x - kHalf) + y] = read_v(2 * u, 2 * (x - kHalf) + y);
                         __builtin_amdgcn_sched_barrier(0);
                     }
+                __builtin_amdgcn_s_setprio(0);
                 [[maybe_unused]] float4 by_v[4];
                 uint32_t seen[2];
 #pragma unroll
@@ -1247,6 +1249,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                     for (int i = 0; i < kPv; ++i) v[i] = read_v(2 * u, i);
                 }
                 read_scales(1);
+                __builtin_amdgcn_s_setprio(1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < kPv; ++i) {
@@ -1259,6 +1262,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_wide(AttendArgs a)
                 only_seen(1);
 #pragma unroll
                 for (int i = 0; i < kPv; ++i) product(1, i);
+                __builtin_amdgcn_s_setprio(0);
             }
         };
         if (p.q.keys > 0) {
