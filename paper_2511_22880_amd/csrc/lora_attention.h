@@ -86,7 +86,7 @@ inline int64_t most_tiles(int64_t tokens, int group, int requests, int columns, 
 // times is between.
 inline AttendForm attend_form(int columns, int keys, int whole_steps, int work_groups, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int least, int most)
 {
-    const int64_t steps = (most_keys + keys - 1) / keys;
+    const int64_t steps = most_keys > 0 ? (most_keys + keys - 1) / keys : 1;  // (a tile without keys is one too: its rows are written)
     int64_t tiles = most_tiles(tokens, group, requests, columns, least), shares = work_groups / kv_heads;
     if (most <= columns && tiles > requests) tiles = requests;
     if (tiles < 1) tiles = 1;

@@ -100,3 +100,13 @@ def test_launches_have_work_groups_for_what_there_may_be_and_no_more_than_a_grid
                     assert shares >= (filled - 1) * up(1) + up(tokens - filled + 1)
             else:
                 assert shares <= max(1, 512 // heads)
+
+
+@needs_headers
+def test_a_table_without_pages_has_its_launches_too(rules):
+    """no request has a key then, and every row is written, with zeros: a tile is a step for that, in as many launches of a work group at least, with room for what they leave"""
+    for tokens, group, heads, requests, _, most, dim, bits in calls(20000, seed=4):
+        sizes = tokens, group, heads, requests, 0
+        forms = rules.rule_forms(*sizes, most, dim, bits).decode().split(", ")
+        assert all(1 <= rules.rule_shares(*sizes, most, dim, bits, i) <= 2 ** 23 // heads for i in range(len(forms))), (sizes, most, dim, bits, forms)
+        assert rules.rule_bytes(*sizes, most, dim, bits) <= rules.rule_most_bytes(*sizes, dim, bits)

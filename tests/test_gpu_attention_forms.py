@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2511_22880_amd import binding as L
 from test_attention_rules import FORMS, taken
 from test_gpu_attention import Batch
 
@@ -57,3 +58,19 @@ def test_pages_that_requests_share(most):
     batch.table[1, :10] = batch.table[0, :10]
     batch.table[2] = batch.table[0]
     batch.check(most)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("n, requests, heads, kv_heads, most", [
+    (1, 3, 32, 8, 1), (1, 600, 32, 8, 1), (8, 150, 64, 8, 8), (4096, 1, 64, 2, 4096), (4096, 1, 256, 8, 4096), (30, 300, 32, 8, 30), (0, 5, 8, 2, 0)])
+def test_a_table_without_pages(n, requests, heads, kv_heads, most, bits):
+    """no request has a key, whatever its length says: zeros, of as many rows as there are, up to more tiles than work groups"""
+    batch = Batch([(n, 0)] * requests, heads, kv_heads, 64, bits=bits, spare=2, seed=45)
+    batch.table = batch.table[:, :0]
+    batch.lengths += 40
+    size = L.lora_attention_workspace_bytes(batch.tokens, heads, requests, 0, batch.cache)
+    batch.workspace = torch.full((max(16, size) // 4,), float("nan"), device="cuda")
+    for said in (most, 0, 1):
+        batch.y.fill_(9.0)
+        y = batch.run(said)
+        assert (y[:-2] == 0).all() and (y[-2:] == 9).all()
