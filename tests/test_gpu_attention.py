@@ -474,6 +474,52 @@ def test_pages_that_are_none_are_seen_by_nobody(bits, most):
     assert (batch.y[batch.first[4]] == 0).all() and (batch.y[batch.first[1]] == 0).all()
 
 
+def within_guards(batch):
+    """The batch's y between other rows, and its workspace, as many bytes as the library asks for, between other bytes.  What asks whether those are as they were."""
+    room = torch.full((batch.tokens + 64, batch.heads, batch.dim), 9.0, dtype=BF, device="cuda")
+    n = L.lora_attention_workspace_bytes(batch.tokens, batch.heads, batch.lengths.numel(), batch.table.shape[1], batch.cache)
+    work = torch.full((4096 + n + 4096,), 0xFF, dtype=torch.uint8, device="cuda")  # (NaN, as sums)
+    batch.y, batch.workspace = room[32:-32], work[4096:4096 + n]
+    return lambda: bool((room[:32] == 9).all() and (room[-32:] == 9).all() and (work[:4096] == 0xFF).all() and (work[4096 + n:] == 0xFF).all())
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("page, dim", [(16, 64), (64, 128)])
+def test_indices_that_fit_nothing_write_nothing_beside_the_rows_and_the_workspace(page, dim, bits):
+    """starts that are negative, descend, or lie behind the rows, lengths likewise, pages that are none: y's neighbours, the workspace's and the cache stay as they are"""
+    for sizes in ([(3, 50), (1, 20), (70, 90)], [(1, 4000), (1, 3), (1, 9)], [(2, 2500), (200, 3000), (5, 700)]):
+        batch = Batch(sizes, 4, 2, dim, page=page, bits=bits)
+        held, n = copied(batch.tensors), batch.tokens
+        untouched = within_guards(batch)
+        batch.table[0, ::2] = batch.cache.pages
+        batch.table[2] = ints([-1, (1 << 31) - 1, 3, -(1 << 31), batch.cache.pages - 1]).repeat(batch.table.shape[1])[:batch.table.shape[1]]
+        for starts, lengths in (([-5, 9, 3, 1 << 30], [1 << 30, -4, 7]), ([n + 6, 20, n, n], [50, (1 << 31) - 1, 90]), ([0, n, 0, n], [90, 90, 90]),
+                                ([0, n, 0, n], [4000, -(1 << 31), 4000]), ([-(1 << 31), (1 << 31) - 1, -(1 << 31), (1 << 31) - 1], [(1 << 31) - 1] * 3)):
+            batch.starts, batch.lengths = ints(starts), ints(lengths)
+            for most in (0, 1, 8, 70):
+                batch.run(most)
+                assert untouched(), (sizes, starts, lengths, most)
+        assert same(held, batch.tensors)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_append_writes_nothing_beside_the_cache(bits):
+    """slots just outside the cache, and far from it: the memory in front of it and behind it stays as it is"""
+    pages, heads, page, dim, n = 3, 2, 16, 64, 9
+    room = new_cache(pages + 4, heads, page, dim, bits, seed=5)
+    held, cache = copied(room), {name: t[2:-2] for name, t in room.items()}
+    kv, q = normal(6, n, 2 * heads, dim), normal(7, n, 4, dim)
+    y = torch.full((n + 8, 4, dim), 9.0, dtype=BF, device="cuda")
+    last = pages * page
+    slots = ints([-1, last, last + 1, -page, 1 << 30, -(1 << 31), (1 << 31) - 1, last + page, -2])
+    positions = torch.arange(n, device="cuda", dtype=I32)
+    L.lora_cache_append(kv[:, :heads], kv[:, heads:], slots, L.Cache(**cache), L.Rotary(dim), positions, q, y[4:-4])
+    assert same(held, room) and (y == 9).all()
+    L.lora_cache_append(kv[:, :heads], kv[:, heads:], ints([last - 1, 0, -1, last] + [-1] * 5), L.Cache(**cache), L.Rotary(dim), positions, q, y[4:-4])
+    assert all(same({name: t[part] for name, t in held.items()}, {name: t[part] for name, t in room.items()}) for part in (slice(0, 2), slice(-2, None)))
+    assert not same(held, room) and (y[:4] == 9).all() and (y[6:] == 9).all() and not (y[4:6] == 9).any()
+
+
 def test_indices_that_fit_nothing_reach_nothing():
     batch = Batch([(3, 50), (1, 20), (70, 90)], 4, 2, 64)
     guard = [t.clone() for t in batch.tensors.values()]

@@ -4,7 +4,7 @@ import torch
 
 from paper_2511_22880_amd import binding as L
 from test_attention_rules import FORMS, taken
-from test_gpu_attention import Batch
+from test_gpu_attention import Batch, within_guards
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,14 @@ def test_a_table_without_pages(n, requests, heads, kv_heads, most, bits):
         batch.y.fill_(9.0)
         y = batch.run(said)
         assert (y[:-2] == 0).all() and (y[-2:] == 9).all()
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("name, bits", [(name, bits) for name in FORMS for bits in (8, 16) if taken(name, bits)])
+def test_form_writes_its_rows_and_its_workspace_alone(name, dim, bits, tree):
+    sizes, most = FORMS[name]
+    batch = Batch(sizes, 8, 2, dim, bits=bits, tree=tree, seed=46)
+    ref = batch.run(most).clone()
+    untouched = within_guards(batch)
+    assert torch.equal(batch.run(most), ref) and untouched()
