@@ -97,6 +97,8 @@ lora_status_t lora_cache_append(const void *k, int64_t k_token, int64_t k_head, 
  * A row that sees no key, or only keys whose score is -infinity, is zeros.  Keys that a row does not see have no part in it, whatever their slots hold.
  * Keys on pages outside 0 .. pages - 1 are seen by none; lengths behind page_table's width * page_size count as that; rows of q behind the last request's are
  * left as they are in y.  A request may have no rows, and lengths[r] may be less than n (key j of its own is then key lengths[r] - n + j, where there is one).
+ * starts must not descend: the host counts tiles and work groups by that.  Where they do, requests share rows, the call still returns LORA_OK, and any row, also one of a request
+ * that shares none, may stay as it was in y or hold, by element, what one of the requests that claim it gives; nothing outside y and the workspace is written.
  *
  * q, y: device, bf16, 16-byte aligned, [tokens][q_heads][head_dim], strides as above, not overlapping; q_heads a multiple of kv_heads.  starts: device, int32,
  * [requests + 1]; lengths: device, int32, [requests]; page_table: device, int32, [requests][width], row stride ld_table; tree: device, 8-byte aligned, [tokens].

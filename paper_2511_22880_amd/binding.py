@@ -1150,7 +1150,8 @@ def lora_attention_workspace_bytes(tokens: int, q_heads: int, requests: int, wid
 def lora_attention(q, starts, lengths, page_table, cache: Cache, y, workspace=None, scale: Optional[float] = None, tree=None, most: int = 0,
                    stream=None) -> None:
     """q, y: bf16 [tokens][q_heads][dim]; starts [requests + 1], lengths [requests], page_table [requests][width]: int32; tree: int64 [tokens], one
-    word of 64 bits a row (None: rows see their request's own keys up to themselves); scale None: 1 / sqrt(dim); most: the most rows of a request, 0 if unknown."""
+    word of 64 bits a row (None: rows see their request's own keys up to themselves); scale None: 1 / sqrt(dim); most: the most rows of a request, 0 if unknown.
+    starts must not descend: where they do (nothing says so, they are on the GPU), any row of y may stay as it was."""
     try:
         (n, heads, dim), (qt, qh, q1) = q.shape, q.stride()
         (yn, yheads, ydim), (yt, yh, y1) = y.shape, y.stride()

@@ -532,6 +532,31 @@ def test_indices_that_fit_nothing_reach_nothing():
     assert all(torch.equal(a, b) for a, b in zip(guard, batch.tensors.values()))
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("keys", [90, 3000])
+@pytest.mark.parametrize("starts", [[0, 74, 0, 74], [0, 74, 20, 74, 74], [70, 74, 0, 70], [10, 4, 60, 30, 74]])
+def test_rows_that_requests_share_hold_what_one_of_them_gives_or_stay(starts, keys, bits):
+    """starts that descend: every element of a row is what it was, or what one of the requests that claim the row gives it by itself"""
+    requests, n = len(starts) - 1, 74
+    batch = Batch([(1, keys)] * requests, 4, 2, 64, bits=bits, spare=n - requests, seed=9)
+    claims = [(r, a, b) for r, (a, b) in enumerate(zip(starts, starts[1:])) if b > a]
+    refs = []
+    for r, a, b in claims:
+        alone = Batch([(b - a, keys)], 4, 2, 64, bits=bits, seed=9)
+        alone.tensors, alone.cache, alone.table, alone.first = batch.tensors, batch.cache, batch.table[r:r + 1], [0, b - a]
+        alone.q = batch.q[a:b]
+        refs.append((a, b, *alone.reference()))
+    batch.starts, batch.lengths = ints(starts), ints([keys] * requests)
+    for most in (0, 1, 8, 74):
+        untouched = within_guards(batch)
+        batch.y.fill_(9.0)
+        y = batch.run(most).double()
+        fits = y == 9
+        for a, b, ref, bound in refs:
+            fits[a:b] |= (y[a:b] - ref).abs() <= bound
+        assert fits.all() and untouched(), most
+
+
 @pytest.mark.parametrize("most", [1, 30])
 def test_requests_that_share_rows_without_end(most):
     """10000 requests that each claim all of 20000 rows over 60000 keys: more steps than 32 bits count, which is found, and nothing is done"""
