@@ -1151,6 +1151,7 @@ def lora_attention(q, starts, lengths, page_table, cache: Cache, y, workspace=No
                    stream=None) -> None:
     """q, y: bf16 [tokens][q_heads][dim]; starts [requests + 1], lengths [requests], page_table [requests][width]: int32; tree: int64 [tokens], one
     word of 64 bits a row (None: rows see their request's own keys up to themselves); scale None: 1 / sqrt(dim); most: the most rows of a request, 0 if unknown.
+    page_table's width stands for the longest request's keys: a view of the columns that the batch needs (page_table[:, :n]) takes short ones faster.
     starts must not descend: where they do (nothing says so, they are on the GPU), any row of y may stay as it was."""
     try:
         (n, heads, dim), (qt, qh, q1) = q.shape, q.stride()

@@ -85,7 +85,8 @@ class AdaptedAttention:
     def __call__(self, x: torch.Tensor, segments, positions: torch.Tensor, slots: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor,
                  page_table: torch.Tensor, y: torch.Tensor, apply_workspace: torch.Tensor, tree=None, most: int = 0) -> None:
         """x: bf16 [tokens][hidden]; segments: the batch's plans on the pools of q, k, v and o; positions, slots: int32 [tokens]; starts, lengths, page_table, tree,
-        most: of lora_attention, lengths with this step's tokens; y: bf16 [tokens][hidden], written."""
+        most: of lora_attention, lengths with this step's tokens, page_table a view of the columns that the longest request needs, where the caller knows that; y: bf16
+        [tokens][hidden], written."""
         stream, n, dim = torch.cuda.current_stream(), x.shape[0], self.cache.head_dim
         for projection, segment, out in zip(self.projections, segments, (self.q, self.k, self.v)):
             projection(x, segment, out[:n], apply_workspace)

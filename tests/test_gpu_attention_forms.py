@@ -85,3 +85,20 @@ def test_form_writes_its_rows_and_its_workspace_alone(name, dim, bits, tree):
     ref = batch.run(most).clone()
     untouched = within_guards(batch)
     assert torch.equal(batch.run(most), ref) and untouched()
+
+
+@pytest.mark.parametrize("page, slots", [(16, 8192), (64, 131072)])
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("sizes, heads, kv_heads, most", [
+    ([(1, 40), (1, 300), (1, 5)], 8, 2, 1), ([(3, 40), (8, 200), (5, 5)], 8, 2, 8), ([(600, 600)], 8, 2, 600), ([(1, 9)] * 40 + [(200, 250), (30, 30)], 8, 2, 200), ([(2, 33)] * 50, 16, 16, 2)])
+def test_a_table_wider_than_its_requests(sizes, heads, kv_heads, most, bits, page, slots):
+    """as wide as the longest context that a server allows, and a view of the columns that the requests need: the same rows within the bound, pages that are none behind them"""
+    batch = Batch(sizes, heads, kv_heads, 64, page=page, bits=bits, seed=47)
+    needed = batch.table.shape[1]
+    wide = torch.full((len(sizes), slots // page), -7, dtype=torch.int32, device="cuda")
+    wide[:, :needed] = batch.table
+    size = L.lora_attention_workspace_bytes(batch.tokens, heads, len(sizes), slots // page, batch.cache)
+    batch.workspace = torch.full((max(16, size) // 4,), float("nan"), device="cuda")
+    for table in (wide, wide[:, :needed]):
+        batch.table = table
+        batch.check(most)
