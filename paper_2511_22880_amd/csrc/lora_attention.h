@@ -80,10 +80,16 @@ inline int64_t most_tiles(int64_t tokens, int group, int requests, int columns, 
 }
 
 // Whether tiles are cut.  Tiles of few steps are not, if there are not too many of them for a work group each (one that finds none takes 2 us to see that; the host's
-// count can be far above what there are): the parts that cut ones leave cost a launch to join them, and for 256 columns 128 KB each way.
-// us a call, cut / whole, wide tiles: 4 prompts of 307 to 922 tokens 45 / 28.  Up to 16 steps of them; up to 8 / 16: 4 prompts on 9 key heads 47 / 35.5, 9 prompts beside 92 single tokens
-// 76 / 54; up to 16 / 32: few requests of so many keys 23 / 47 and 19 / 54.  Up to so many tiles, four / sixteen times the work groups: 6 prompts beside 148 single tokens 42 / 55; eight
-// times is between.
+// count can be far above what there are): the parts that cut ones leave cost a launch to join them, and for 256 columns 128 KB each way.  The steps are those of
+// the longest request that the page table has room for, which is all that the host knows of lengths.  us a call, wide tiles, cut / whole:
+//   4 prompts of 307 to 922 tokens, table as wide   45 / 28
+// Up to so many steps, 16 / 8:
+//   4 prompts on 9 key heads                        35.5 / 47
+//   9 prompts beside 92 single tokens               54 / 76
+// Up to so many steps, 16 / 32:
+//   few requests of so many keys                    23 / 47, 19 / 54
+// Up to so many tiles, four / sixteen times the work groups (eight times is between):
+//   6 prompts beside 148 single tokens              42 / 55
 inline AttendForm attend_form(int columns, int keys, int whole_steps, int work_groups, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, int least, int most)
 {
     const int64_t steps = most_keys > 0 ? (most_keys + keys - 1) / keys : 1;  // (a tile without keys is one too: its rows are written)
@@ -96,9 +102,16 @@ inline AttendForm attend_form(int columns, int keys, int whole_steps, int work_g
     return AttendForm{columns, (int)shares, least, most, true};
 }
 
-// Tiles of up to 32 columns (k_attend_few) on two work groups a compute unit: three were level, and three, four or eight times as many shares of a decode step as that 410, 414 and 433 us
-// against 400.  More columns share keys through LDS (k_attend_wide): 33 to 64 columns as four tiles of 16 that hold their own keys / as one of 128, 6 trees of up to 11 tokens on 4 query
-// heads a key head: 36 / 25 us.
+// Tiles of up to 32 columns (k_attend_few): shares for two work groups a compute unit.  Of 16 columns two fit at least; for three was level, and three, four or eight
+// times as many shares of a decode step took 410, 414 and 433 us against 400.  Of 32 columns two fit with heads of 64 in bf16 (200 registers a wavefront), otherwise one
+// (280 to 386), and half of the shares begin when the others end.  us a call, shares for two / for one, trees of 5 to 8 tokens on 4 query heads a key head:
+//   requests x keys    64 x 300 to 6000   256 x 200 to 8000   1 x 8000
+//   bf16, heads of 128     129 / 117          523 / 514      28.5 / 18.1
+//   bf16, heads of 64       63 / 78           264 / 315      15.8 / 12.7
+//   8 bits, of 128          99 / 87.5         350 / 352      18.4 / 16.3
+//   8 bits, of 64         62.5 / 54           212 / 211      15.1 / 13.2
+// (all take those for two.)  More columns share keys through LDS (k_attend_wide): 33 to 64 columns as four tiles of 16 that hold their own keys / as one of 128,
+// 6 trees of up to 11 tokens on 4 query heads a key head: 36 / 25 us.
 inline AttendForm few_form(int columns, int64_t tokens, int group, int kv_heads, int requests, int64_t most_keys, bool bits8, int most)
 {
     return attend_form(columns, few_keys(bits8), 4, 2 * kComputeUnits, tokens, group, kv_heads, requests, most_keys, 0, most);
@@ -115,12 +128,18 @@ inline AttendForms attend_forms(int64_t tokens, int group, int kv_heads, int req
     // (128 / 256 columns: pieces of long prompts 1200 / 1034 us, prompts beside single tokens 511 / 488, trees of 280 to 448 columns 71 / 78; where no request has more than 128 half of
     // 256 would idle)
     const int c = columns <= 128 ? 128 : 256;
-    // Requests of very different sizes: those of up to 16 columns in a launch of their own, which reads a single token's keys faster than wide tiles of mostly empty columns, in 8 bits above all,
-    // where a step of those has half as many bytes.  The second launch costs its start and end, more than that where a tile of each request finds a compute unit at once and there is
-    // little to read.  us, two launches / one, single tokens + prompts (8 key heads of 128 in bf16 unless said): 384 + 8 466 / 615, 200 + 40 406 / 512, 64 + 1 146 / 177, 20 + 2 of 16000 keys 134 / 171,
-    // 32 + 2 81.5 / 86, 24 + 1 65 / 70, dim 64 24 + 2 51 / 73, 2 key heads 60 + 2 68 / 103, in 8 bits 16 + 1 48 / 66, 8 + 1 of dim 64 26 / 33; 16 + 1 of 4000 keys 68 / 60, 8 + 1 of
-    // 2000 53 / 42, 2 + 2 39 / 28.  1 to 64 rows, 20 requests 58 / 42, 100 requests 292 / 274; 1 to 500 rows, 30 and 100 requests 87 / 84 and 352 / 329.  Few steps in all: trees of 1 to 22 rows
-    // behind up to 161 keys, 40 requests, dim 64 16.6 / 10.7, in 8 bits 23 / 15; 200 + 1 of 400 keys in 8 bits 56 / 67.
+    // Requests of very different sizes: those of up to 16 columns in a launch of their own, which reads a single token's keys faster than wide tiles of mostly empty
+    // columns, in 8 bits above all, where a step of those has half as many bytes.  The second launch costs its start and end, more than that where a tile of each
+    // request finds a compute unit at once and there is little to read.  Here too the table's width stands for the longest request.  us a call, two launches / one, 8
+    // key heads of 128 in bf16 unless said, tables as wide as the longest request:
+    //   single tokens + prompts   384 + 8               466 / 615      20 + 2 of 16000 keys   134 / 171     16 + 1 of 4000 keys   68 / 60
+    //                             200 + 40              406 / 512      32 + 2                81.5 / 86       8 + 1 of 2000 keys   53 / 42
+    //                             64 + 1                146 / 177      24 + 1                  65 / 70       2 + 2                39 / 28
+    //   .. heads of 64            24 + 2                 51 / 73       .. 2 key heads  60 + 2  68 / 103
+    //   .. in 8 bits              16 + 1                 48 / 66       8 + 1, heads of 64      26 / 33      200 + 1 of 400 keys   56 / 67
+    //   1 to 64 rows              20 requests            58 / 42       100 requests          292 / 274
+    //   1 to 500 rows             30 requests            87 / 84       100 requests          352 / 329
+    //   trees of 1 to 22 rows behind up to 161 keys, 40 requests, heads of 64   16.6 / 10.7, in 8 bits 23 / 15
     const double bytes = (double)requests * most_keys * kv_heads * dim * 4;
     const int64_t tiles = (int64_t)requests * kv_heads;
     const bool little = (tiles <= 2 * kComputeUnits && most_keys <= 4 * (8192 / dim)) || (!bits8 && requests <= 32 && tiles <= kComputeUnits && bytes <= 300e6);

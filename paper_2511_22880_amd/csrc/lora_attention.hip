@@ -909,8 +909,10 @@ __global__ __launch_bounds__(64 * kFewWaves, C == 1 ? 2 : 1) void k_attend_few(A
 // 16000 keys, 961 GFLOP, 990 to 1040 us, 0.92 to 0.97 PFLOP/s (a large library product 1.23).  Of an earlier 1035 us the exponentials were 65, putting keys and values
 // into LDS 135 and asking for them 125, though they were near (the same keys over and over: level).  So addresses come from lanes that have them (by a few instructions
 // on one lane's value: trees 75.7 to 72.8), and eight wavefronts wait for each other every second step (with that 1065 to 1035; 131 KB of LDS, which one work group a
-// compute unit has to itself).  The order laid down in `take` took it from 1200.  Trees of 8 to 24 tokens, 289 MB: 64 us, 4.5 TB/s, by the 64 KB that a compute unit's
-// two work groups have on the way (registers are full: 64 keys more would spill).  64 columns a wavefront instead of 32, half as many reads of LDS a product: 2066 to
+// compute unit has to itself).  The order laid down in `take` took it from 1200.  Trees of 8 to 24 tokens, 289 MB: 63 to 66 us and 8 of join, on another card 83 in all
+// (3.9 to 4.5 TB/s), by the 64 KB that a compute unit's two work groups have on the way.  Registers are full with heads of 128, and some are spilled: 2 and 8 in bf16 (eight
+// and four wavefronts), 27 and 32 in 8 bits; with heads of 64 none.  In 8 bits with heads of 128 the trees take 81 us (bf16 72) for half the bytes, 8 prompts of 256 to
+// 2048 tokens 75 (59), the pieces 1100 (1000).  64 columns a wavefront instead of 32, half as many reads of LDS a product: 2066 to
 // 2700 against 1435 then, one wavefront a SIMD; loads past the caches 1202 against 1080.  32 keys at a time with the exponentials beside the next ones' products: 1033
 // against 1023, trees 76 against 73.6; the wavefronts that bring K doing so behind their products, those that bring V before: 1046 against 1030.
 // ------------------------------------------------------------------------------------------------

@@ -56,6 +56,24 @@ def test_wide_products_spill_nothing(kernel):
     assert hits[0][".vgpr_spill_count"] == 0 and hits[0][".private_segment_fixed_size"] == 0
 
 
+@pytest.mark.parametrize("kernel, registers, spilled", [
+    # two work groups of four wavefronts on a compute unit have 256 registers a wavefront; of those above, one
+    ("k_attend_fewILi64ELb0ELi1E", 128, 0), ("k_attend_fewILi64ELb1ELi1E", 256, 0), ("k_attend_fewILi128ELb0ELi1E", 256, 0), ("k_attend_fewILi128ELb1ELi1E", 256, 0),
+    ("k_attend_fewILi64ELb0ELi2E", 256, 0), ("k_attend_fewILi64ELb1ELi2E", 280, 0), ("k_attend_fewILi128ELb0ELi2E", 316, 0), ("k_attend_fewILi128ELb1ELi2E", 386, 0),
+    ("k_attend_wideILi64ELb0ELi4E", 256, 0), ("k_attend_wideILi64ELb0ELi8E", 256, 0), ("k_attend_wideILi64ELb1ELi4E", 256, 0), ("k_attend_wideILi64ELb1ELi8E", 256, 0),
+    # heads of 128 take all of them and a few more
+    ("k_attend_wideILi128ELb0ELi4E", 256, 8), ("k_attend_wideILi128ELb0ELi8E", 256, 2), ("k_attend_wideILi128ELb1ELi4E", 256, 32), ("k_attend_wideILi128ELb1ELi8E", 256, 27),
+    ("k_turnILi0E", 64, 0), ("k_turnILi1E", 64, 0), ("k_turnILi2E", 64, 0),
+])
+def test_registers_of_attention(kernel, registers, spilled):
+    """How many wavefronts a SIMD has, and what goes to memory and back in a step: no more than the comments at the kernels and their rules say."""
+    hits = [k for name, k in _kernels().items() if "4lora" in name and kernel in name]
+    assert len(hits) == 1
+    k = hits[0]
+    assert k[".vgpr_count"] <= registers and k[".vgpr_spill_count"] <= spilled, (k[".vgpr_count"], k[".vgpr_spill_count"])
+    assert spilled or k[".private_segment_fixed_size"] == 0
+
+
 def _dynamic_symbols():
     """(offset of the code object, its sections' headers, symbol's entry, name) of every dynamic symbol of the library's AMDGPU code."""
     data, at = open(build.LIB, "rb").read(), 0
