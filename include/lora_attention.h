@@ -94,7 +94,8 @@ lora_status_t lora_cache_append(const void *k, int64_t k_token, int64_t k_head, 
  *   tree NULL:  its own n keys up to i (a prompt, a piece of one, a single token);
  *   tree:       those of its own keys j for which bit j of tree[starts[r] + i] is set (a drafted token: its ancestors and itself); of a request's
  *               own keys only the first 64 can be seen.
- * A row that sees no key, or only keys whose score is -infinity, is zeros.  Keys that a row does not see have no part in it, whatever their slots hold.
+ * A row that sees no key, or only keys whose score is -infinity, is zeros.  Keys that a row does not see have no part in it, whatever their slots hold; an infinity or
+ * NaN among the values that it sees makes that dim of y an infinity or NaN, which of them is not said where its weight is too small for 32 bits.
  * Keys on pages outside 0 .. pages - 1 are seen by none; lengths behind page_table's width * page_size count as that; rows of q behind the last request's are
  * left as they are in y.  A request may have no rows, and lengths[r] may be less than n (key j of its own is then key lengths[r] - n + j, where there is one).
  * starts must not descend: the host counts tiles and work groups by that.  Where they do, requests share rows, the call still returns LORA_OK, and any row, also one of a request
@@ -109,6 +110,8 @@ lora_status_t lora_cache_append(const void *k, int64_t k_token, int64_t k_head, 
  * workspace: device, 16-byte aligned, of lora_attention_workspace_bytes() or more; its contents are of no account, and calls that may run at the same time need one each.
  * Products are bf16 x bf16 (E4M3 is exact there) with fp32 sums; scores, weights' sum and the running maximum are fp32.  Weights are relative to a maximum that may lag behind the true
  * one by 2^8, and a weight (in 8 bits times its value's scale) is rounded to bf16 for its product with v; in bf16 the weights' sum is of the rounded ones; y is rounded once.
+ * Sums are divided at the end, so finite values have to leave them room: 2^8 times the sum of a request's |v| in a dim is less than 2^128, or infinities come of it.  In 8 bits, v's scales
+ * below 2^-100 cost the weights bits.
  * scale: finite, and so are its multiple by log2 e and that times any score; a negative one is one of -q.  The same call gives the same bits. */
 lora_status_t lora_attention_workspace_bytes(int32_t tokens, int32_t q_heads, int32_t requests, int32_t width, const lora_cache_t *cache,
                                              size_t *bytes);

@@ -599,6 +599,20 @@ def test_scales_and_sharp_scores(scale):
     Batch([(1, 300), (20, 90), (150, 170)], 8, 2, 64, loud=4.0).check(scale=scale)
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("power", [105, -100])
+def test_large_and_small_values(power, bits):
+    """as large as sums of 300 weights of up to 2^8 leave room for, and as small as weights times their scales keep their bits"""
+    batch = Batch([(1, 300), (1, 17), (20, 90), (150, 170)], 8, 2, 64, bits=bits, loud=4.0, seed=12)
+    if bits == 8:
+        batch.tensors["v_scales"].copy_(torch.rand(batch.tensors["v_scales"].shape, generator=gen(13), device="cuda").clamp(min=0.25) * 2.0 ** power)
+    else:
+        batch.tensors["v"].mul_(2.0 ** power)
+    for most in (0, 1, 150):
+        batch.check(most)
+        assert torch.isfinite(batch.y).all() and batch.y.abs().sum(dtype=torch.float64) > 0
+
+
 def test_scores_of_minus_infinity_have_no_weight():
     batch = Batch([(1, 40), (20, 60), (100, 130)], 4, 2, 64)
     batch.q.fill_(1.0)
